@@ -346,6 +346,98 @@ int svg2_kmeans_pp_init(const void *X, int dtype, int H, int N, int d, int C,
                         void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
+ * svg2_rope -- from the rows of a projection to the layer's operands, for up to
+ * three tensors of one shape (Q, K and V of one layer) in one launch: RMS norm,
+ * rotary positions over several axes (time, height, width), token order ->
+ * head order.  For each tensor, token n and head h,
+ *   x' = x * w / sqrt(mean(x^2) + eps)     where norm_weight is given; the mean is over the head (SVG2_NORM_HEAD, w [d])
+ *                                          or over all heads of the token (SVG2_NORM_TOKEN, w [H,d])
+ *   y[i] = x'[i] cos(a) - x'[j] sin(a), y[j] = x'[i] sin(a) + x'[j] cos(a)     where rotate is set; a = pos[axis(p)] * freq[p]
+ *                                          for pair p = 0 .. d/2-1, (i,j) = (2p, 2p+1) (SVG2_ROPE_ADJACENT) or
+ *                                          (p, p + d/2) (SVG2_ROPE_HALVES)
+ * and y = x' otherwise (a tensor that is only moved is copied bit for bit).
+ * Axis k takes the next axis_pairs[k] pairs; a token at position 0 and a pair
+ * of frequency 0 are not rotated.  Angles are formed in double precision, norm
+ * and rotation in fp32, rounded once to dtype.
+ *   src, dst       [B,N,H,d] dtype each, element (b,n,h,i) at b*stride[0] + n*stride[1] + h*stride[2] + i (elements);
+ *                  16-byte aligned, strides multiples of 16 bytes.  The layer's [B*H,N,d] has strides (H*N*d, d, N*d).
+ *                  dst may be src with the same strides; any other overlap is undefined.  dst strides are positive
+ *                  wherever the dimension is larger than 1.
+ *   rotate         non-zero: the tensor is rotated
+ *   norm_weight    fp32, 16-byte aligned, or NULL: no norm
+ *   pos            [B,N,n_axes] int32, batch stride pos_stride_b (0: all batches share one), dense inside
+ *   freq           [d/2] fp64; both may be NULL where nothing is rotated
+ *   n_axes 1..4, axis_pairs >= 0 with sum d/2; eps > 0; d 64 or 128; B*N <= 2^26
+ * svg2_rope_backward: with dY (strides dst_stride, of any sign: it is only read) the gradients
+ *   dX[t] [B,N,H,d] with strides dx_stride (alignment as src; must not overlap an input), and
+ *   dW[t] (shape of norm_weight[t], fp32; ignored where that is NULL).
+ *   args as in the forward call; args->dst is ignored, args->src is read where norm_weight is given.
+ * The sums over tokens are formed in a fixed order: results are the same from
+ * run to run.
+ * ------------------------------------------------------------------------- */
+enum { SVG2_ROPE_ADJACENT = 0, SVG2_ROPE_HALVES = 1 };
+enum { SVG2_NORM_HEAD = 0, SVG2_NORM_TOKEN = 1 };
+
+typedef struct svg2_rope_args {
+    int n_tensors;                  /* 1..3 */
+    int dtype, B, N, H, d;
+    const void *src[3];
+    void *dst[3];
+    int rotate[3];
+    const float *norm_weight[3];
+    int64_t src_stride[3];
+    int64_t dst_stride[3];
+    const int32_t *pos;
+    int64_t pos_stride_b;
+    const double *freq;
+    int n_axes;
+    int axis_pairs[4];
+    int pairing;                    /* SVG2_ROPE_ADJACENT or SVG2_ROPE_HALVES */
+    int norm_scope;                 /* SVG2_NORM_HEAD or SVG2_NORM_TOKEN      */
+    float eps;
+} svg2_rope_args;
+
+int svg2_rope(const svg2_rope_args *args, void *stream);
+size_t svg2_rope_backward_workspace_size(const svg2_rope_args *args);
+int svg2_rope_backward(const svg2_rope_args *args, const void *const *dY, void *const *dX, const int64_t *dx_stride,
+                       float *const *dW, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Microscaled 4-bit floating point (OCP MXFP4) -- the projections in front of
+ * and behind the layer.  32 neighbouring values along the contracted axis share
+ * one power of two (E8M0: a byte, exponent + 127, 255 = NaN); a value is E2M1
+ * (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives).  The block's exponent is
+ * floor(log2(max |x|)) - 2, at least -127; x / 2^exponent is rounded to nearest,
+ * ties to even, and saturates at 6.  A block that holds an infinity or a NaN is
+ * all NaN.
+ * An operand of R rows and K columns is stored, with Kp = K rounded up to 128, as
+ *   codes  [R, Kp/2] bytes       element 2j in the low half of byte j, 2j+1 in the high half; 16-byte aligned
+ *   scales [Kp/128, R, 4] bytes  scale of columns 32b .. 32b+31 of row r at [b/4, r, b%4]; 16-byte aligned
+ * with zeros in the columns behind K.
+ *
+ * svg2_quantize_mxfp4: X [M,G,Kg] dtype, element (m,g,i) at m*stride_m + g*stride_g + i: M rows of K = G*Kg columns (G = 1 for
+ * an ordinary matrix; the layer's O [H,N,d] is M = N, G = H, Kg = d with strides (d, N*d)).
+ *   transposed = 0: operand of M rows, K columns; transposed != 0: operand of K rows, M columns (X^T, blocks along the rows of
+ *   X), which is what a gradient's product contracts.
+ * Any strides and alignment of X (16-byte aligned rows of a multiple of 8 columns are read fastest).
+ * svg2_dequantize_mxfp4: the values of an operand, exactly, into X [R,K] dtype with row stride ldx >= K.
+ *
+ * svg2_matmul_mxfp4: C [M,N] = A B^T + bias for operands A (M rows) and B (N rows) of K columns; out_dtype is the type of C,
+ * ldc >= N its row stride, bias [N] fp32 or NULL.  The matrix cores sum in fp32; one rounding at the end.  With A the quantised
+ * activations and B the quantised weights this is a linear layer; its gradients are the same product on dY and W^T (for dX),
+ * dY^T and X^T (for dW).
+ * C must not overlap an input.  Rows up to 2^26 each, K up to 2^26.
+ * ------------------------------------------------------------------------- */
+int svg2_quantize_mxfp4(const void *X, int dtype, int M, int G, int Kg, int64_t stride_m, int64_t stride_g,
+                        int transposed, void *codes, void *scales, void *stream);
+int svg2_dequantize_mxfp4(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx,
+                          void *stream);
+size_t svg2_matmul_mxfp4_workspace_size(int M, int N, int K);
+int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const void *B_scales, int M, int N, int K,
+                      const float *bias, int out_dtype, void *C, int64_t ldc, void *ws, size_t ws_bytes,
+                      void *stream);
+
+/* ---------------------------------------------------------------------------
  * Timing for benchmarks (HOST-side state, one per process).
  * svg2_profile_enable(1): every later svg2_forward* call records HIP events
  * around its stages on the caller's stream (events are created on first use;

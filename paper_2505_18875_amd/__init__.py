@@ -11,4 +11,6 @@ from .binding import (  # noqa: F401
     svg2_kmeans, svg2_permute, svg2_permute_noalloc, svg2_profile_enable, svg2_profile_read, svg2_profile_read_kernels, svg2_select_topp, svg2_sparse_attn,
     svg2_sparse_attn_gather_free, svg2_attention_recall, svg2_kmeans_pp_init,
     svg2_quantize_fp8, svg2_sparse_attn_fp8, svg2_forward_fp8,
+    svg2_grid_positions, svg2_rope_frequencies, svg2_rope, svg2_rope_backward,
+    svg2_quantize_mxfp4, svg2_dequantize_mxfp4, svg2_matmul_mxfp4,
 )

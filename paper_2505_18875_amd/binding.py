@@ -34,6 +34,8 @@ EXPORTS = (
     "svg2_forward_fp8_workspace_size", "svg2_forward_fp8",
     "svg2_attention_recall_workspace_size", "svg2_attention_recall",
     "svg2_kmeans_pp_init_workspace_size", "svg2_kmeans_pp_init",
+    "svg2_rope", "svg2_rope_backward_workspace_size", "svg2_rope_backward",
+    "svg2_quantize_mxfp4", "svg2_dequantize_mxfp4", "svg2_matmul_mxfp4_workspace_size", "svg2_matmul_mxfp4",
     "svg2_profile_enable", "svg2_profile_read", "svg2_profile_read_kernels",
 )
 STAGES = ("kmeans", "permute", "select", "attn_plan", "attn")
@@ -51,6 +53,19 @@ class _ForwardAux(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in (
         "labels_q", "labels_k", "counts_q", "counts_k", "offsets_q", "offsets_k",
         "perm_q", "perm_k", "row_ptr", "col_idx", "density", "lse")]
+
+
+ROPE_PAIRINGS = ("adjacent", "halves")
+NORM_SCOPES = ("head", "token")
+
+
+class _RopeArgs(ctypes.Structure):
+    _fields_ = [("n_tensors", ctypes.c_int), ("dtype", ctypes.c_int), ("B", ctypes.c_int), ("N", ctypes.c_int),
+                ("H", ctypes.c_int), ("d", ctypes.c_int), ("src", ctypes.c_void_p * 3), ("dst", ctypes.c_void_p * 3),
+                ("rotate", ctypes.c_int * 3), ("norm_weight", ctypes.c_void_p * 3), ("src_stride", ctypes.c_int64 * 3),
+                ("dst_stride", ctypes.c_int64 * 3), ("pos", ctypes.c_void_p), ("pos_stride_b", ctypes.c_int64),
+                ("freq", ctypes.c_void_p), ("n_axes", ctypes.c_int), ("axis_pairs", ctypes.c_int * 4),
+                ("pairing", ctypes.c_int), ("norm_scope", ctypes.c_int), ("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -96,6 +111,14 @@ def load_library() -> ctypes.CDLL:
         lib.svg2_attention_recall.argtypes = [vp, vp, i, i, vp, vp, vp, sz, vp]
         lib.svg2_kmeans_pp_init_workspace_size.argtypes = [i, i, i]
         lib.svg2_kmeans_pp_init.argtypes = [vp, i, i, i, i, i, vp, vp, vp, vp, sz, vp]
+        lib.svg2_rope.argtypes = [vp, vp]
+        lib.svg2_rope_backward_workspace_size.argtypes = [vp]
+        lib.svg2_rope_backward.argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
+        i64 = ctypes.c_int64
+        lib.svg2_quantize_mxfp4.argtypes = [vp, i, i, i, i, i64, i64, i, vp, vp, vp]
+        lib.svg2_dequantize_mxfp4.argtypes = [vp, vp, i, i, i, vp, i64, vp]
+        lib.svg2_matmul_mxfp4_workspace_size.argtypes = [i, i, i]
+        lib.svg2_matmul_mxfp4.argtypes = [vp, vp, vp, vp, i, i, i, vp, i, vp, i64, vp, sz, vp]
         lib.svg2_profile_enable.argtypes = [i]
         lib.svg2_profile_read.argtypes = [vp, vp]
         lib.svg2_profile_read_kernels.argtypes = [vp, vp]
@@ -388,6 +411,250 @@ def svg2_kmeans_pp_init(X, C, u, *, ws=None):
     _check(lib.svg2_kmeans_pp_init(_dev(X, name="X"), _dtype_code(X), H, N, d, C, _dev(u, torch.float64, "u"),
                                    _dev(centroids), _dev(picked), _dev(ws), ws.numel(), _stream()))
     return SimpleNamespace(centroids=centroids, picked=picked)
+
+
+def _strided(t: torch.Tensor, name: str, device=None, dtype=None) -> int:
+    """Address of a GPU tensor of any strides whose innermost dimension is contiguous."""
+    if not t.is_cuda:
+        raise ValueError("%s must live on the GPU" % name)
+    if device is not None and t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+    return t.data_ptr()
+
+
+def _dense(t: Optional[torch.Tensor], name: str, device, dtype, shape) -> Optional[int]:
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return _strided(t, name, device, dtype)
+
+
+def _outer_strides(t: torch.Tensor):
+    """Strides of all but the last dimension; 0 where the dimension has one entry (torch leaves anything there)."""
+    return [t.stride(k) if t.shape[k] > 1 else 0 for k in range(t.dim() - 1)]
+
+
+def _same_views(tensors, name, device, dtype, shape):
+    strides = _outer_strides(tensors[0])
+    for i, t in enumerate(tensors):
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError("%s[%d] must be %s, got %s" % (name, i, list(shape), list(t.shape)))
+        if _outer_strides(t) != strides:
+            raise ValueError("%s must share one set of strides" % name)
+        _strided(t, "%s[%d]" % (name, i), device, dtype)
+    return strides
+
+
+def svg2_grid_positions(grid, *, first=(0, 0, 0), extra=0, device="cuda"):
+    """Positions (time, height, width) of a video's tokens in raster order, int32 [T*Y*X + extra, 3], the grid starting at
+    `first`; `extra` tokens behind the video's (text) get position 0, which rotates nothing."""
+    axes = [torch.arange(n, dtype=torch.int32, device=device) + f for n, f in zip(grid, first)]
+    video = torch.stack([a.reshape(-1) for a in torch.meshgrid(*axes, indexing="ij")], 1)
+    return torch.cat([video, video.new_zeros((extra, len(axes)))]).contiguous()
+
+
+def svg2_rope_frequencies(axis_pairs, *, theta=10000.0, device="cuda"):
+    """Frequencies of the usual rotary positions, fp64 [sum(axis_pairs)]: pair i of an axis of n pairs has theta^(-i/n)."""
+    return torch.cat([torch.as_tensor(float(theta), dtype=torch.float64) ** (-torch.arange(n, dtype=torch.float64) / n)
+                      for n in axis_pairs if n > 0]).to(device)
+
+
+def _rope_args(views, shape, dtype, device, pos, freq, axis_pairs, rotate, norm_weights, norm_scope, eps, pairing):
+    n = len(views)
+    B, N, H, d = shape
+    if pairing not in ROPE_PAIRINGS:
+        raise ValueError("pairing must be one of %s" % (ROPE_PAIRINGS,))
+    if norm_scope not in NORM_SCOPES:
+        raise ValueError("norm_scope must be one of %s" % (NORM_SCOPES,))
+    rotate = [True] * n if rotate is None else [bool(r) for r in rotate]
+    norm_weights = [None] * n if norm_weights is None else list(norm_weights)
+    if len(rotate) != n or len(norm_weights) != n:
+        raise ValueError("rotate and norm_weights need one entry per tensor")
+    a = _RopeArgs()
+    a.n_tensors, a.dtype, a.B, a.N, a.H, a.d = n, dtype, B, N, H, d
+    a.rotate = (ctypes.c_int * 3)(*[int(r) for r in rotate])
+    wshape = (d,) if norm_scope == "head" else (H, d)
+    a.norm_weight = (ctypes.c_void_p * 3)(*[_dense(w, "norm_weights[%d]" % i, device, torch.float32, wshape)
+                                            for i, w in enumerate(norm_weights)])
+    if any(rotate):
+        axis_pairs = [int(x) for x in axis_pairs]
+        if not 1 <= len(axis_pairs) <= 4:
+            raise ValueError("axis_pairs must have 1 to 4 entries")
+        if pos.dim() == 2:
+            pos = pos[None]
+        if tuple(pos.shape) not in ((1, N, len(axis_pairs)), (B, N, len(axis_pairs))):
+            raise ValueError("pos must be [N,%d] or [B,N,%d], got %s" % (len(axis_pairs), len(axis_pairs), list(pos.shape)))
+        _strided(pos, "pos", device, torch.int32)
+        if not pos[0].is_contiguous():
+            raise ValueError("pos must be dense inside a batch")
+        a.pos = pos.data_ptr()
+        a.pos_stride_b = pos.stride(0) if pos.shape[0] > 1 else 0
+        a.freq = _dense(freq, "freq", device, torch.float64, (d // 2,))
+        a.n_axes = len(axis_pairs)
+        a.axis_pairs = (ctypes.c_int * 4)(*axis_pairs)
+    a.pairing, a.norm_scope, a.eps = ROPE_PAIRINGS.index(pairing), NORM_SCOPES.index(norm_scope), float(eps)
+    return a, norm_weights
+
+
+def _token_views(tensors, name):
+    """[N,H,d] or [B,N,H,d] tensors as [B,N,H,d] views."""
+    tensors = list(tensors)
+    if not 1 <= len(tensors) <= 3:
+        raise ValueError("%s: one to three tensors" % name)
+    out = [t[None] if t.dim() == 3 else t for t in tensors]
+    if any(t.dim() != 4 for t in out):
+        raise ValueError("%s must be [N,H,d] or [B,N,H,d]" % name)
+    return out
+
+
+def _head_order(t, B, N, H, d):
+    """[B*H,N,d] as a [B,N,H,d] view."""
+    if tuple(t.shape) != (B * H, N, d):
+        raise ValueError("expected [%d,%d,%d], got %s" % (B * H, N, d, list(t.shape)))
+    return t.unflatten(0, (B, H)).transpose(1, 2)
+
+
+def svg2_rope(tensors, pos=None, freq=None, *, axis_pairs=(), rotate=None, norm_weights=None, norm_scope="head", eps=1e-6,
+              pairing="adjacent", outs=None):
+    """RMS norm, rotary positions over several axes and the move to head order of up to three tensors (Q, K, V).
+
+    tensors: [N,H,d] or [B,N,H,d] views of one shape and set of strides (slices of a packed projection); pos int32
+    [N,axes] or [B,N,axes]; freq fp64 [d/2]; axis_pairs: pairs of each axis; rotate: per tensor, default all;
+    norm_weights: per tensor fp32 [d] (norm_scope "head") or [H,d] ("token"), or None.  Returns [B*H,N,d] tensors, or
+    `outs` ([B,N,H,d] views of any strides; `tensors` themselves for a call in place)."""
+    lib = load_library()
+    views = _token_views(tensors, "tensors")
+    B, N, H, d = shape = views[0].shape
+    dev = views[0].device
+    strides = _same_views(views, "tensors", dev, views[0].dtype, shape)
+    a, _ = _rope_args(views, shape, _dtype_code(views[0]), dev, pos, freq, axis_pairs, rotate, norm_weights, norm_scope, eps, pairing)
+    if outs is None:
+        result = [torch.empty((B * H, N, d), dtype=views[0].dtype, device=dev) for _ in views]
+        dst = [_head_order(t, B, N, H, d) for t in result]
+    else:
+        result = list(outs)
+        dst = _token_views(result, "outs")
+        if len(dst) != len(views):
+            raise ValueError("one output per tensor")
+    dst_strides = _same_views(dst, "outs", dev, views[0].dtype, shape)
+    a.src = (ctypes.c_void_p * 3)(*[t.data_ptr() for t in views])
+    a.dst = (ctypes.c_void_p * 3)(*[t.data_ptr() for t in dst])
+    a.src_stride, a.dst_stride = (ctypes.c_int64 * 3)(*strides), (ctypes.c_int64 * 3)(*dst_strides)
+    with torch.cuda.device(dev):
+        _check(lib.svg2_rope(ctypes.addressof(a), _stream()))
+    return result
+
+
+def svg2_rope_backward(grads, tensors, pos=None, freq=None, *, axis_pairs=(), rotate=None, norm_weights=None,
+                       norm_scope="head", eps=1e-6, pairing="adjacent", outs=None, ws=None):
+    """Gradients of svg2_rope: grads ([B*H,N,d], or [B,N,H,d] views of one set of strides) and the forward call's arguments
+    -> grads of `tensors` (dense [B,N,H,d], or `outs`, views of any strides) and of norm_weights (None where None)."""
+    lib = load_library()
+    views = _token_views(tensors, "tensors")
+    B, N, H, d = shape = views[0].shape
+    dev = views[0].device
+    strides = _same_views(views, "tensors", dev, views[0].dtype, shape)
+    a, weights = _rope_args(views, shape, _dtype_code(views[0]), dev, pos, freq, axis_pairs, rotate, norm_weights, norm_scope, eps,
+                            pairing)
+    grads = [_head_order(g, B, N, H, d) if g.dim() == 3 else g for g in grads]
+    if outs is None:
+        result = [torch.empty(shape, dtype=views[0].dtype, device=dev) for _ in views]
+        dx = result
+    else:
+        result = list(outs)
+        dx = _token_views(result, "outs")
+    if len(grads) != len(views) or len(dx) != len(views):
+        raise ValueError("one gradient and one output per tensor")
+    g_strides = _same_views(grads, "grads", dev, views[0].dtype, shape)
+    dx_strides = _same_views(dx, "outs", dev, views[0].dtype, shape)
+    dw = [None if w is None else torch.empty_like(w) for w in weights]
+    a.src = (ctypes.c_void_p * 3)(*[t.data_ptr() for t in views])
+    # a gradient may be an expanded view (it is only read); the C entry takes its layout as the forward's dst
+    a.src_stride, a.dst_stride = (ctypes.c_int64 * 3)(*strides), (ctypes.c_int64 * 3)(*g_strides)
+    ptrs = lambda ts: (ctypes.c_void_p * 3)(*[None if t is None else t.data_ptr() for t in ts])  # noqa: E731
+    with torch.cuda.device(dev):
+        ws = _workspace(lib.svg2_rope_backward_workspace_size(ctypes.addressof(a)), dev) if ws is None else ws
+        _check(lib.svg2_rope_backward(ctypes.addressof(a), ptrs(grads), ptrs(dx), (ctypes.c_int64 * 3)(*dx_strides), ptrs(dw),
+                                      _dev(ws), ws.numel(), _stream()))
+    return SimpleNamespace(grads=result, dweights=dw)
+
+
+def _mxfp4_empty(R, K, device):
+    nk = -(-K // 128)
+    return (torch.empty((R, nk * 64), dtype=torch.uint8, device=device),
+            torch.empty((nk, R, 4), dtype=torch.uint8, device=device))
+
+
+def _mxfp4_operand(codes, scales, name, device):
+    """Checks an operand's two tensors; rows and padded columns."""
+    if codes.dim() != 2 or codes.shape[1] % 64:
+        raise ValueError("%s: codes must be [R, Kp/2] with Kp a multiple of 128, got %s" % (name, list(codes.shape)))
+    R, Kp = codes.shape[0], 2 * codes.shape[1]
+    _dense(codes, name + " codes", device, torch.uint8, (R, Kp // 2))
+    _dense(scales, name + " scales", device, torch.uint8, (Kp // 128, R, 4))
+    return R, Kp
+
+
+def svg2_quantize_mxfp4(X, *, transposed=False):
+    """X [M,K], or [M,G,Kg] for K = G*Kg columns in groups of any stride (the layer's O as O.transpose(0, 1)) -> MXFP4
+    operand (codes [M,Kp/2], scales [Kp/128,M,4] uint8); transposed: of X^T, [K rows, M columns]."""
+    lib = load_library()
+    if X.dim() not in (2, 3):
+        raise ValueError("X must be [M,K] or [M,G,Kg]")
+    view = X[:, None] if X.dim() == 2 else X
+    M, G, Kg = view.shape
+    ptr = _strided(view, "X")
+    sm, sg = _outer_strides(view)
+    codes, scales = _mxfp4_empty(G * Kg, M, X.device) if transposed else _mxfp4_empty(M, G * Kg, X.device)
+    with torch.cuda.device(X.device):
+        _check(lib.svg2_quantize_mxfp4(ptr, _dtype_code(X), M, G, Kg, sm, sg, int(transposed), codes.data_ptr(),
+                                       scales.data_ptr(), _stream()))
+    return codes, scales
+
+
+def svg2_dequantize_mxfp4(codes, scales, K=None, *, dtype=torch.bfloat16, out=None):
+    """The values of an MXFP4 operand, [R,K] (K: all padded columns where None)."""
+    lib = load_library()
+    dev = codes.device
+    R, Kp = _mxfp4_operand(codes, scales, "operand", dev)
+    K = Kp if K is None else int(K)
+    if not Kp - 128 < K <= Kp:
+        raise ValueError("K = %d does not belong to %d padded columns" % (K, Kp))
+    out = torch.empty((R, K), dtype=dtype, device=dev) if out is None else out
+    if tuple(out.shape) != (R, K):
+        raise ValueError("out must be [%d,%d]" % (R, K))
+    ptr = _strided(out, "out", dev)
+    with torch.cuda.device(dev):
+        _check(lib.svg2_dequantize_mxfp4(codes.data_ptr(), scales.data_ptr(), R, K, _dtype_code(out), ptr,
+                                         out.stride(0) if R > 1 else K, _stream()))
+    return out
+
+
+def svg2_matmul_mxfp4(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bfloat16, out=None, ws=None):
+    """C [M,N] = A B^T + bias of two MXFP4 operands (M and N rows of the same columns); bias fp32 [N]."""
+    lib = load_library()
+    dev = A.device
+    M, Kp = _mxfp4_operand(A, A_scales, "A", dev)
+    N, Kb = _mxfp4_operand(B, B_scales, "B", dev)
+    if Kb != Kp:
+        raise ValueError("A has %d padded columns, B has %d" % (Kp, Kb))
+    C = torch.empty((M, N), dtype=out_dtype, device=dev) if out is None else out
+    if tuple(C.shape) != (M, N):
+        raise ValueError("out must be [%d,%d]" % (M, N))
+    ptr = _strided(C, "out", dev)
+    bias_ptr = _dense(bias, "bias", dev, torch.float32, (N,))
+    with torch.cuda.device(dev):
+        ws = _workspace(lib.svg2_matmul_mxfp4_workspace_size(M, N, Kp), dev) if ws is None else ws
+        _check(lib.svg2_matmul_mxfp4(A.data_ptr(), A_scales.data_ptr(), B.data_ptr(), B_scales.data_ptr(), M, N, Kp, bias_ptr,
+                                     _dtype_code(C), ptr, C.stride(0) if M > 1 else N, _dev(ws), ws.numel(), _stream()))
+    return C
 
 
 def svg2_profile_enable(level) -> None:

@@ -67,6 +67,74 @@ static int check_ws(const void *ws, size_t have, size_t need)
     return SVG2_OK;
 }
 
+static bool multiple_of(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// strides of a [B,N,H,d] tensor that svg2_rope* reads or writes
+static int check_rope_strides(const svg2_rope_args *a, const char *name, const int64_t *stride, bool written)
+{
+    const int sizes[3] = {a->B, a->N, a->H}, per16 = a->dtype == SVG2_BF16 ? 8 : 4;
+    for (int k = 0; k < 3; ++k) {
+        SVG2_REQUIRE(stride[k] % per16 == 0, SVG2_INVALID_ARG, "%s stride %d (%lld elements) is not a multiple of 16 bytes", name, k,
+                     (long long)stride[k]);
+        SVG2_REQUIRE(!written || sizes[k] == 1 || stride[k] > 0, SVG2_INVALID_ARG, "%s stride %d = %lld must be positive", name, k,
+                     (long long)stride[k]);
+    }
+    return SVG2_OK;
+}
+
+// dst_written: the tensors with args->dst_stride are results (forward); else they are gradients, which are only read
+static int check_rope(const svg2_rope_args *a, bool dst_written)
+{
+    SVG2_REQUIRE(a != nullptr, SVG2_INVALID_ARG, "args is null");
+    SVG2_REQUIRE(a->n_tensors >= 1 && a->n_tensors <= 3, SVG2_INVALID_ARG, "n_tensors = %d must be 1, 2 or 3", a->n_tensors);
+    SVG2_TRY(check_common(a->dtype, a->H, a->N, a->d));
+    SVG2_REQUIRE(a->B >= 1 && (double)a->B * a->N <= 67108864.0, SVG2_INVALID_ARG,
+                 "B = %d must be positive and B * N = %g at most 2^26", a->B, (double)a->B * a->N);
+    SVG2_REQUIRE((double)a->B * a->H * (double)a->N * a->d < 1099511627776.0, SVG2_INVALID_ARG, "B*H*N*d is 2^40 or more");
+    SVG2_REQUIRE(a->pairing == SVG2_ROPE_ADJACENT || a->pairing == SVG2_ROPE_HALVES, SVG2_INVALID_ARG,
+                 "pairing %d is not SVG2_ROPE_ADJACENT or SVG2_ROPE_HALVES", a->pairing);
+    SVG2_REQUIRE(a->norm_scope == SVG2_NORM_HEAD || a->norm_scope == SVG2_NORM_TOKEN, SVG2_INVALID_ARG,
+                 "norm_scope %d is not SVG2_NORM_HEAD or SVG2_NORM_TOKEN", a->norm_scope);
+    SVG2_TRY(check_rope_strides(a, "src", a->src_stride, false));
+    SVG2_TRY(check_rope_strides(a, "dst", a->dst_stride, dst_written));
+    bool rotated = false;
+    for (int t = 0; t < a->n_tensors; ++t) {
+        rotated |= a->rotate[t] != 0;
+        if (!a->norm_weight[t]) continue;
+        SVG2_REQUIRE(multiple_of(a->norm_weight[t], 16), SVG2_INVALID_ARG, "norm_weight[%d] is not 16-byte aligned", t);
+        SVG2_REQUIRE(a->eps > 0.f && a->eps < 1e30f, SVG2_INVALID_ARG, "eps = %g must be positive and finite", (double)a->eps);
+    }
+    if (rotated) {
+        SVG2_REQUIRE(a->n_axes >= 1 && a->n_axes <= 4, SVG2_INVALID_ARG, "n_axes = %d must be in 1..4", a->n_axes);
+        long long pairs = 0;
+        for (int k = 0; k < a->n_axes; ++k) {
+            SVG2_REQUIRE(a->axis_pairs[k] >= 0, SVG2_INVALID_ARG, "axis_pairs[%d] = %d is negative", k, a->axis_pairs[k]);
+            pairs += a->axis_pairs[k];
+        }
+        SVG2_REQUIRE(pairs == a->d / 2, SVG2_INVALID_ARG, "the axes have %lld pairs, a head of %d has %d", pairs, a->d, a->d / 2);
+        SVG2_REQUIRE(a->pos && a->freq, SVG2_INVALID_ARG, "pos and freq must be non-null where a tensor is rotated");
+        SVG2_REQUIRE(multiple_of(a->pos, 4) && multiple_of(a->freq, 8), SVG2_INVALID_ARG, "pos or freq is not aligned");
+        SVG2_REQUIRE(a->pos_stride_b >= 0, SVG2_INVALID_ARG, "pos_stride_b = %lld is negative", (long long)a->pos_stride_b);
+    }
+    return SVG2_OK;
+}
+
+// rows, columns and buffers of a microscaled operand
+static int check_mxfp4(const char *name, const void *codes, const void *scales, long long R, long long K)
+{
+    SVG2_REQUIRE(R >= 1 && K >= 1 && R <= 67108864 && K <= 67108864, SVG2_INVALID_ARG,
+                 "%s: %lld rows and %lld columns must be in 1..2^26", name, R, K);
+    SVG2_REQUIRE(codes && scales, SVG2_INVALID_ARG, "%s: codes and scales must be non-null", name);
+    SVG2_REQUIRE(multiple_of(codes, 16) && multiple_of(scales, 16), SVG2_INVALID_ARG, "%s: codes or scales are not 16-byte aligned", name);
+    return SVG2_OK;
+}
+
+static int check_dtype(int dtype)
+{
+    SVG2_REQUIRE(dtype == SVG2_F32 || dtype == SVG2_BF16, SVG2_UNSUPPORTED, "dtype %d is not SVG2_F32 or SVG2_BF16", dtype);
+    return SVG2_OK;
+}
+
 // (kernel, device) pairs whose dynamic-LDS limit has been raised, with the size it was raised to
 struct LdsAttr {
     const void *kernel;
@@ -567,6 +635,113 @@ int svg2_kmeans_pp_init(const void *X, int dtype, int H, int N, int d, int C, co
     SVG2_REQUIRE(X && u && centroids, SVG2_INVALID_ARG, "X, u and centroids must be non-null");
     SVG2_TRY(check_ws(ws, ws_bytes, kpp_ws_bytes(H, N, C)));
     return kpp_launch(X, dtype, H, N, d, C, u, centroids, picked, ws, static_cast<hipStream_t>(stream));
+}
+
+int svg2_rope(const svg2_rope_args *a, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_rope(a, true));
+    for (int t = 0; t < a->n_tensors; ++t) {
+        SVG2_REQUIRE(a->src[t] && a->dst[t], SVG2_INVALID_ARG, "src[%d] / dst[%d] is null", t, t);
+        SVG2_REQUIRE(multiple_of(a->src[t], 16) && multiple_of(a->dst[t], 16), SVG2_INVALID_ARG,
+                     "src[%d] or dst[%d] is not 16-byte aligned", t, t);
+        SVG2_REQUIRE(a->src[t] != a->dst[t] || memcmp(a->src_stride, a->dst_stride, sizeof(a->src_stride)) == 0, SVG2_INVALID_ARG,
+                     "dst[%d] is src[%d] with other strides", t, t);
+        for (int u = 0; u < a->n_tensors; ++u)
+            SVG2_REQUIRE(u == t || (a->dst[t] != a->src[u] && a->dst[t] != a->dst[u]), SVG2_INVALID_ARG,
+                         "dst[%d] must not alias another tensor's src or dst", t);
+    }
+    return rope_launch(a, static_cast<hipStream_t>(stream));
+}
+
+size_t svg2_rope_backward_workspace_size(const svg2_rope_args *a)
+{
+    if (check_rope(a, false) != SVG2_OK) return 256;
+    return rope_bwd_ws_bytes(a);
+}
+
+int svg2_rope_backward(const svg2_rope_args *a, const void *const *dY, void *const *dX, const int64_t *dx_stride,
+                       float *const *dW, void *ws, size_t ws_bytes, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_rope(a, false));
+    SVG2_REQUIRE(dY && dX && dx_stride, SVG2_INVALID_ARG, "dY, dX and dx_stride must be non-null");
+    SVG2_TRY(check_rope_strides(a, "dX", dx_stride, true));
+    for (int t = 0; t < a->n_tensors; ++t) {
+        SVG2_REQUIRE(dY[t] && dX[t], SVG2_INVALID_ARG, "dY[%d] / dX[%d] is null", t, t);
+        SVG2_REQUIRE(multiple_of(dY[t], 16) && multiple_of(dX[t], 16), SVG2_INVALID_ARG,
+                     "dY[%d] or dX[%d] is not 16-byte aligned", t, t);
+        if (a->norm_weight[t]) {
+            SVG2_REQUIRE(a->src[t] && multiple_of(a->src[t], 16), SVG2_INVALID_ARG, "src[%d] is null or not 16-byte aligned", t);
+            SVG2_REQUIRE(dW && dW[t], SVG2_INVALID_ARG, "dW[%d] is null, norm_weight[%d] is not", t, t);
+        }
+        for (int u = 0; u < a->n_tensors; ++u) {
+            SVG2_REQUIRE(dX[t] != dY[u] && (!a->norm_weight[u] || dX[t] != a->src[u]), SVG2_INVALID_ARG,
+                         "dX[%d] must not alias an input", t);
+            SVG2_REQUIRE(u == t || dX[t] != dX[u], SVG2_INVALID_ARG, "dX[%d] must not alias dX[%d]", t, u);
+            SVG2_REQUIRE(u == t || !a->norm_weight[t] || !a->norm_weight[u] || dW[t] != dW[u], SVG2_INVALID_ARG,
+                         "dW[%d] must not alias dW[%d]", t, u);
+        }
+    }
+    SVG2_TRY(check_ws(ws, ws_bytes, rope_bwd_ws_bytes(a)));
+    return rope_bwd_launch(a, dY, dX, dx_stride, dW, ws, static_cast<hipStream_t>(stream));
+}
+
+int svg2_quantize_mxfp4(const void *X, int dtype, int M, int G, int Kg, int64_t stride_m, int64_t stride_g, int transposed,
+                        void *codes, void *scales, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_dtype(dtype));
+    SVG2_REQUIRE(G >= 1 && Kg >= 1, SVG2_INVALID_ARG, "G = %d and Kg = %d must be positive", G, Kg);
+    const long long K = (long long)G * Kg;
+    SVG2_TRY(check_mxfp4("result", codes, scales, transposed ? K : M, transposed ? M : K));
+    SVG2_REQUIRE(X != nullptr, SVG2_INVALID_ARG, "X is null");
+    SVG2_REQUIRE(multiple_of(X, dtype == SVG2_BF16 ? 2 : 4), SVG2_INVALID_ARG, "X is not aligned to its elements");
+    SVG2_REQUIRE(X != codes && X != scales && codes != scales, SVG2_INVALID_ARG, "codes and scales must not alias X or each other");
+    return mxfp4_quant_launch(X, dtype, M, G, Kg, stride_m, stride_g, transposed != 0, codes, scales,
+                              static_cast<hipStream_t>(stream));
+}
+
+int svg2_dequantize_mxfp4(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_dtype(dtype));
+    SVG2_TRY(check_mxfp4("operand", codes, scales, R, K));
+    SVG2_REQUIRE(X != nullptr, SVG2_INVALID_ARG, "X is null");
+    SVG2_REQUIRE(multiple_of(X, dtype == SVG2_BF16 ? 2 : 4), SVG2_INVALID_ARG, "X is not aligned to its elements");
+    SVG2_REQUIRE(ldx >= K, SVG2_INVALID_ARG, "ldx = %lld is less than K = %d", (long long)ldx, K);
+    SVG2_REQUIRE(X != codes && X != scales, SVG2_INVALID_ARG, "X must not alias an input");
+    return mxfp4_values_launch(codes, scales, R, K, dtype, X, ldx, static_cast<hipStream_t>(stream));
+}
+
+// the product's tiles are numbered in one grid dimension
+static int check_product_size(int M, int N)
+{
+    SVG2_REQUIRE((double)cdiv(M, 128) * cdiv(N, 128) < 16777216.0, SVG2_INVALID_ARG, "C of %d x %d has 2^24 tiles or more", M, N);
+    return SVG2_OK;
+}
+
+size_t svg2_matmul_mxfp4_workspace_size(int M, int N, int K)
+{
+    if (M < 1 || N < 1 || K < 1 || M > 67108864 || N > 67108864 || K > 67108864 || check_product_size(M, N) != SVG2_OK) return 256;
+    return mxfp4_matmul_ws_bytes(M, N, K);
+}
+
+int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const void *B_scales, int M, int N, int K,
+                      const float *bias, int out_dtype, void *C, int64_t ldc, void *ws, size_t ws_bytes, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_dtype(out_dtype));
+    SVG2_TRY(check_mxfp4("A", A, A_scales, M, K));
+    SVG2_TRY(check_mxfp4("B", B, B_scales, N, K));
+    SVG2_TRY(check_product_size(M, N));
+    SVG2_REQUIRE(C != nullptr, SVG2_INVALID_ARG, "C is null");
+    SVG2_REQUIRE(multiple_of(C, out_dtype == SVG2_BF16 ? 2 : 4) && multiple_of(bias, 4), SVG2_INVALID_ARG,
+                 "C or bias is not aligned to its elements");
+    SVG2_REQUIRE(ldc >= N, SVG2_INVALID_ARG, "ldc = %lld is less than N = %d", (long long)ldc, N);
+    SVG2_REQUIRE(C != A && C != A_scales && C != B && C != B_scales && C != bias, SVG2_INVALID_ARG, "C must not alias an input");
+    SVG2_TRY(check_ws(ws, ws_bytes, mxfp4_matmul_ws_bytes(M, N, K)));
+    return mxfp4_matmul_launch(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc, ws, static_cast<hipStream_t>(stream));
 }
 
 int svg2_profile_enable(int level)

@@ -199,4 +199,18 @@ size_t kpp_ws_bytes(int H, int N, int C);
 int kpp_launch(const void *X, int dtype, int H, int N, int d, int C, const double *u, float *centroids,
                int32_t *picked, void *ws, hipStream_t st);
 
+// rotary positions, norm and order of Q, K, V (svg2_rope.hip)
+int rope_launch(const svg2_rope_args *a, hipStream_t st);
+size_t rope_bwd_ws_bytes(const svg2_rope_args *a);
+int rope_bwd_launch(const svg2_rope_args *a, const void *const *dY, void *const *dX, const int64_t *dx_stride,
+                    float *const *dW, void *ws, hipStream_t st);
+
+// microscaled 4-bit floating point (svg2_mxfp4.hip)
+int mxfp4_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t sm, int64_t sg, bool transposed, void *codes,
+                       void *scales, hipStream_t st);
+int mxfp4_values_launch(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx, hipStream_t st);
+size_t mxfp4_matmul_ws_bytes(int M, int N, int K);
+int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
+                        int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st);
+
 }  // namespace svg2

@@ -1,0 +1,553 @@
+// From a projection's rows to the layer's operands: RMS norm of Q and K, rotary positions over several axes, token order
+// -> head order, and the gradients of that.
+//
+//   n      = x * rsqrt(mean(x^2) + eps) * w         mean over the head, or over all heads of the token
+//   y[i,j] = (n[i] cos a - n[j] sin a,  n[i] sin a + n[j] cos a)     pair p = (i,j), a = pos[axis(p)] * freq[p]
+// backward, with g = dy turned by -a:
+//   dw = sum over tokens (and heads) of g n / w,   dx = r (g w - x r mean(g w x r)),   r = rsqrt(mean(x^2) + eps)
+//
+// Every element is read once and written once, some ten operations each: HBM bounds it, so the kernels are built around the
+// loads.  One wavefront per token and tensor; a lane holds four pairs (8 elements), 8 or 16 lanes a head, 8 or 4 heads a
+// step, and up to CH steps are loaded before the first is used.  A token of 40 heads of 128 thus stays in registers between
+// the sum of squares over all its heads and the result, and no lane needs an element of another's.  The angle of a lane's pairs
+// is the same for every head, so four cosines and sines per lane and token serve all of them: cheap enough to compute
+// in place, in 64 bits up to the quarter turn (positions of 10^6 times a frequency of 1 leave no fraction in 32), instead of
+// reading a table.
+#include "svg2_common.h"
+
+namespace svg2 {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+struct RopeArgs {
+    const void *src[3];             // forward: x; backward: x (null where the tensor has no norm)
+    const void *grad[3];            // backward: dy
+    void *dst[3];                   // forward: y; backward: dx
+    const float *weight[3];         // fp32 [d] or [H,d], null: no norm
+    long long ss[3], gs[3], ds[3];  // strides of src, grad, dst: batch, token, head
+    const int32_t *pos;
+    long long pos_b;
+    const double *freq;
+    int n_axes, end[4];             // pairs of axis k: end[k-1] .. end[k]
+    int rotate;                     // bit t: tensor t is rotated
+    int B, N, H, token_scope;
+    float eps;
+    float *rinv;                    // backward, long token rows: 1 / rms of every token, [3][B N]
+    float *partial;                 // backward: partial sums of dw, [3][P][cols]
+    float *dw[3];
+    int P, cols;
+};
+
+// ---- four pairs of a lane --------------------------------------------------
+template <typename T> struct Raw { uint4 q[sizeof(T) / 2]; };
+
+template <typename T, int D, bool ADJ> __device__ __forceinline__ Raw<T> load_pairs(const T *head, int c)
+{
+    Raw<T> r;
+    if constexpr (ADJ) {
+#pragma unroll
+        for (unsigned k = 0; k < sizeof(T) / 2; ++k) r.q[k] = reinterpret_cast<const uint4 *>(head + 8 * c)[k];
+    } else if constexpr (sizeof(T) == 4) {
+        r.q[0] = *reinterpret_cast<const uint4 *>(head + 4 * c);
+        r.q[1] = *reinterpret_cast<const uint4 *>(head + D / 2 + 4 * c);
+    } else {
+        const uint2 a = *reinterpret_cast<const uint2 *>(head + 4 * c), b = *reinterpret_cast<const uint2 *>(head + D / 2 + 4 * c);
+        r.q[0] = make_uint4(a.x, a.y, b.x, b.y);
+    }
+    return r;
+}
+
+template <typename T, int D, bool ADJ> __device__ __forceinline__ void store_pairs(T *head, int c, const Raw<T> &r)
+{
+    if constexpr (ADJ) {
+#pragma unroll
+        for (unsigned k = 0; k < sizeof(T) / 2; ++k) reinterpret_cast<uint4 *>(head + 8 * c)[k] = r.q[k];
+    } else if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<uint4 *>(head + 4 * c) = r.q[0];
+        *reinterpret_cast<uint4 *>(head + D / 2 + 4 * c) = r.q[1];
+    } else {
+        *reinterpret_cast<uint2 *>(head + 4 * c) = make_uint2(r.q[0].x, r.q[0].y);
+        *reinterpret_cast<uint2 *>(head + D / 2 + 4 * c) = make_uint2(r.q[0].z, r.q[0].w);
+    }
+}
+
+// the eight elements in the order they are stored in; element e of pair k is v[at(k, e)]
+template <bool ADJ> __device__ constexpr int at(int k, int e) { return ADJ ? 2 * k + e : 4 * e + k; }
+
+template <typename T> __device__ __forceinline__ void decode(const Raw<T> &r, float *v)
+{
+#pragma unroll
+    for (unsigned k = 0; k < sizeof(T) / 2; ++k) {
+        const unsigned w[4] = {r.q[k].x, r.q[k].y, r.q[k].z, r.q[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                v[4 * k + i] = __uint_as_float(w[i]);
+            } else {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+            }
+        }
+    }
+}
+
+// the one rounding of a bf16 result (to nearest even; NaN stays NaN)
+template <typename T> __device__ __forceinline__ Raw<T> encode(const float *v)
+{
+    Raw<T> r;
+    if constexpr (sizeof(T) == 4) {
+        r.q[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        r.q[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    } else {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x2 p = {v[2 * i], v[2 * i + 1]};
+            w[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(p, bf16x2));
+        }
+        r.q[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return r;
+}
+
+template <int D, bool ADJ> __device__ __forceinline__ void load_weight(const float *w, int c, float *v)
+{
+    const float4 a = *reinterpret_cast<const float4 *>(w + (ADJ ? 8 * c : 4 * c));
+    const float4 b = *reinterpret_cast<const float4 *>(w + (ADJ ? 8 * c + 4 : D / 2 + 4 * c));
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+
+// cosine and sine of the four angles of a lane.  The quarter turns are taken off in 64 bits (two-part pi / 2: the error is
+// that of the product pos * freq itself), what remains is at most pi / 4 and goes through the Taylor polynomials, whose next
+// terms there are 2e-9 (sine, x^11 / 11!) and 1e-10 (cosine, x^12 / 12!).
+__device__ __forceinline__ void angles(const RopeArgs &A, int b, int n, int c, float *cs, float *sn)
+{
+    const int32_t *pos = A.pos + (long long)b * A.pos_b + (long long)n * A.n_axes;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int p = 4 * c + k;
+        int axis = 0;
+#pragma unroll
+        for (int x = 0; x < 3; ++x) axis += (x + 1 < A.n_axes && p >= A.end[x]) ? 1 : 0;
+        const double t = (double)pos[axis] * A.freq[p];
+        const double q = rint(t * 0.63661977236758134);
+        const float r = (float)fma(-q, 6.123233995736766e-17, fma(-q, 1.5707963267948966, t));
+        const int quadrant = (int)(q - 4.0 * floor(q * 0.25));
+        const float z = r * r;
+        const float s = r + r * z * (-1.f / 6 + z * (1.f / 120 + z * (-1.f / 5040 + z * (1.f / 362880))));
+        const float co = 1.f + z * (-0.5f + z * (1.f / 24 + z * (-1.f / 720 + z * (1.f / 40320 - z * (1.f / 3628800)))));
+        const float u = (quadrant & 1) ? s : co, v = (quadrant & 1) ? co : s;
+        cs[k] = (quadrant == 1 || quadrant == 2) ? -u : u;
+        sn[k] = quadrant >= 2 ? -v : v;
+    }
+}
+
+template <bool ADJ> __device__ __forceinline__ void turn(float *v, const float *cs, const float *sn, float sense)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float a = v[at<ADJ>(k, 0)], b = v[at<ADJ>(k, 1)], s = sense * sn[k];
+        v[at<ADJ>(k, 0)] = a * cs[k] - b * s;
+        v[at<ADJ>(k, 1)] = a * s + b * cs[k];
+    }
+}
+
+// sum over groups of `width` lanes (8, 16: a head; 64: the wavefront)
+__device__ __forceinline__ float group_sum(float x, int width)
+{
+    for (int o = width >> 1; o > 0; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+// ---- forward ---------------------------------------------------------------
+// grid (ceil(B N / 4), tensors), block 256
+template <typename T, int D, bool ADJ> __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs A)
+{
+    constexpr int LPH = D / 8, HPS = 64 / LPH, CH = 10;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int token = blockIdx.x * 4 + wave, t = blockIdx.y;
+    if (token >= A.B * A.N) return;
+    const int b = token / A.N, n = token - b * A.N;
+    const int hl = lane / LPH, c = lane % LPH;
+    const T *src = static_cast<const T *>(A.src[t]) + b * A.ss[0] + n * A.ss[1];
+    T *dst = static_cast<T *>(A.dst[t]) + b * A.ds[0] + n * A.ds[1];
+    const float *weight = A.weight[t];
+    const bool rotate = (A.rotate >> t) & 1, whole = weight && A.token_scope;
+    const int steps = (A.H + HPS - 1) / HPS;
+
+    Raw<T> raw[CH];
+    auto load = [&](int s0) {
+#pragma unroll
+        for (int s = 0; s < CH; ++s) {
+            const int h = (s0 + s) * HPS + hl;
+            if (h < A.H) raw[s] = load_pairs<T, D, ADJ>(src + h * A.ss[2], c);
+        }
+    };
+    float cs[4], sn[4], w[8], rinv = 1.f;
+    if (whole) {
+        float sum = 0.f;
+        for (int s0 = 0; s0 < steps; s0 += CH) {
+            load(s0);
+#pragma unroll
+            for (int s = 0; s < CH; ++s) {
+                float v[8];
+                decode(raw[s], v);
+                if ((s0 + s) * HPS + hl < A.H)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
+            }
+        }
+        rinv = 1.f / sqrtf(group_sum(sum, 64) / ((float)A.H * D) + A.eps);
+    } else if (weight) {
+        load_weight<D, ADJ>(weight, c, w);
+    }
+    if (rotate) angles(A, b, n, c, cs, sn);
+    for (int s0 = 0; s0 < steps; s0 += CH) {
+        if (!whole || steps > CH) load(s0);
+#pragma unroll
+        for (int s = 0; s < CH; ++s) {
+            const int h = (s0 + s) * HPS + hl;
+            if ((s0 + s) * HPS >= A.H) continue;
+            if (weight || rotate) {
+                float v[8];
+                decode(raw[s], v);
+                if (weight) {
+                    if (whole) {
+                        if (h < A.H) load_weight<D, ADJ>(weight + h * D, c, w);
+                    } else {
+                        float sum = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
+                        rinv = 1.f / sqrtf(group_sum(sum, LPH) * (1.f / D) + A.eps);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = v[k] * rinv * w[k];
+                }
+                if (rotate) turn<ADJ>(v, cs, sn, 1.f);
+                raw[s] = encode<T>(v);
+            }
+            if (h < A.H) store_pairs<T, D, ADJ>(dst + h * A.ds[2], c, raw[s]);
+        }
+    }
+}
+
+// ---- backward --------------------------------------------------------------
+// How the weights' gradient is summed: per lane over the tokens of a wavefront, over the block's wavefronts in LDS, over the
+// blocks by rope_dw_kernel, each in a fixed order, so that it is the same from run to run.
+enum { DW_NONE = 0, DW_HEAD = 1, DW_TOKEN = 2, DW_LONG = 3 };
+//   DW_HEAD    [d] weights: 8 sums per lane
+//   DW_TOKEN   [H,d] weights of a token that fits CH steps: its sums stay in registers beside it
+//   DW_LONG    longer tokens: read twice here (sums, then results); 1 / rms is left for rope_dw_long_kernel
+
+template <typename T> constexpr int bwd_steps() { return sizeof(T) == 2 ? 10 : 5; }     // CH
+
+// adds the block's four wavefronts' sums in order into s[cols]
+template <int D, bool ADJ> __device__ __forceinline__ void add_to(float *s, int c, const float *v, bool first)
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int i = ADJ ? 8 * c + k : (k < 4 ? 4 * c + k : D / 2 + 4 * c + k - 4);
+        s[i] = first ? v[k] : s[i] + v[k];
+    }
+}
+
+// grid (blocks, tensors), block 256: wavefronts stride over the tokens
+template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256, 2) void rope_bwd_kernel(const RopeArgs A)
+{
+    constexpr int LPH = D / 8, HPS = 64 / LPH, CH = bwd_steps<T>();
+    constexpr int ACC = DW == DW_TOKEN ? CH : 1;
+    extern __shared__ float s_dw[];             // [cols] (DW_HEAD, DW_TOKEN)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = blockIdx.y;
+    const int hl = lane / LPH, c = lane % LPH, steps = (A.H + HPS - 1) / HPS, tokens = A.B * A.N;
+    const float *weight = DW == DW_NONE ? nullptr : A.weight[t];
+    const bool rotate = (A.rotate >> t) & 1;
+
+    float acc[ACC][8], w[8];
+#pragma unroll
+    for (int s = 0; s < ACC; ++s)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[s][k] = 0.f;
+    if (DW == DW_HEAD && weight) load_weight<D, ADJ>(weight, c, w);
+
+    for (int token = blockIdx.x * 4 + wave; token < tokens; token += gridDim.x * 4) {
+        const int b = token / A.N, n = token - b * A.N;
+        const T *x = static_cast<const T *>(A.src[t]) + b * A.ss[0] + n * A.ss[1];
+        const T *g = static_cast<const T *>(A.grad[t]) + b * A.gs[0] + n * A.gs[1];
+        T *dx = static_cast<T *>(A.dst[t]) + b * A.ds[0] + n * A.ds[1];
+        Raw<T> rg[CH], rx[CH];
+        auto load = [&](int s0) {
+#pragma unroll
+            for (int s = 0; s < CH; ++s) {
+                const int h = (s0 + s) * HPS + hl;
+                if (h >= A.H) continue;
+                rg[s] = load_pairs<T, D, ADJ>(g + h * A.gs[2], c);
+                if (DW != DW_NONE && weight) rx[s] = load_pairs<T, D, ADJ>(x + h * A.ss[2], c);
+            }
+        };
+        float cs[4], sn[4], rinv = 1.f, mean = 0.f;
+        if ((DW == DW_TOKEN || DW == DW_LONG) && weight) {
+            float xx = 0.f, gx = 0.f;
+            for (int s0 = 0; s0 < steps; s0 += CH) {
+                load(s0);
+                if (s0 == 0 && rotate) angles(A, b, n, c, cs, sn);
+#pragma unroll
+                for (int s = 0; s < CH; ++s) {
+                    const int h = (s0 + s) * HPS + hl;
+                    if (h >= A.H) continue;
+                    float vx[8], vg[8];
+                    decode(rx[s], vx);
+                    decode(rg[s], vg);
+                    if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+                    load_weight<D, ADJ>(weight + h * D, c, w);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        xx = fmaf(vx[k], vx[k], xx);
+                        gx = fmaf(vg[k] * w[k], vx[k], gx);
+                    }
+                }
+            }
+            const float count = (float)A.H * D;
+            rinv = 1.f / sqrtf(group_sum(xx, 64) / count + A.eps);
+            mean = group_sum(gx, 64) * rinv / count;
+            if (DW == DW_LONG && lane == 0) A.rinv[(size_t)t * tokens + token] = rinv;
+        } else if (rotate) {
+            angles(A, b, n, c, cs, sn);
+        }
+        for (int s0 = 0; s0 < steps; s0 += CH) {
+            if (!(DW == DW_TOKEN && weight)) load(s0);
+#pragma unroll
+            for (int s = 0; s < CH; ++s) {
+                const int h = (s0 + s) * HPS + hl;
+                if ((s0 + s) * HPS >= A.H) continue;
+                if (weight || rotate) {
+                    float vg[8];
+                    decode(rg[s], vg);
+                    if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+                    if (DW != DW_NONE && weight) {
+                        float vx[8];
+                        decode(rx[s], vx);
+                        if (DW == DW_HEAD) {
+                            float xx = 0.f, gx = 0.f;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                xx = fmaf(vx[k], vx[k], xx);
+                                gx = fmaf(vg[k] * w[k], vx[k], gx);
+                            }
+                            rinv = 1.f / sqrtf(group_sum(xx, LPH) * (1.f / D) + A.eps);
+                            mean = group_sum(gx, LPH) * rinv * (1.f / D);
+                        } else if (h < A.H) {
+                            load_weight<D, ADJ>(weight + h * D, c, w);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float xn = vx[k] * rinv;
+                            if (DW == DW_HEAD || DW == DW_TOKEN) {
+                                const float add = vg[k] * xn;
+                                float &to = acc[DW == DW_TOKEN ? s : 0][k];
+                                to = h < A.H ? to + add : to;
+                            }
+                            vg[k] = rinv * (vg[k] * w[k] - xn * mean);
+                        }
+                    }
+                    rg[s] = encode<T>(vg);
+                }
+                if (h < A.H) store_pairs<T, D, ADJ>(dx + h * A.ds[2], c, rg[s]);
+            }
+        }
+    }
+
+    if ((DW == DW_HEAD || DW == DW_TOKEN) && weight) {          // the same for the whole block
+        if (DW == DW_HEAD)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                for (int o = LPH; o < 64; o <<= 1) acc[0][k] += __shfl_xor(acc[0][k], o);
+        for (int turn_of = 0; turn_of < 4; ++turn_of) {
+            if (wave == turn_of) {
+                if (DW == DW_HEAD) {
+                    if (hl == 0) add_to<D, ADJ>(s_dw, c, acc[0], wave == 0);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < ACC; ++s)
+                        if (s * HPS + hl < A.H) add_to<D, ADJ>(s_dw + (s * HPS + hl) * D, c, acc[s], wave == 0);
+                }
+            }
+            __syncthreads();
+        }
+        float *out = A.partial + ((size_t)t * A.P + blockIdx.x) * A.cols;
+        for (int i = threadIdx.x; i < A.cols; i += 256) out[i] = s_dw[i];
+    }
+}
+
+// DW_LONG: grid (ceil(H / HPS), P, tensors), block 256: one step of heads, every P-th group of four tokens
+template <typename T, int D, bool ADJ> __global__ __launch_bounds__(256) void rope_dw_long_kernel(const RopeArgs A)
+{
+    constexpr int LPH = D / 8, HPS = 64 / LPH;
+    __shared__ float s_dw[512];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = blockIdx.z;
+    const int hl = lane / LPH, c = lane % LPH, h = blockIdx.x * HPS + hl, tokens = A.B * A.N;
+    if (!A.weight[t]) return;
+    const bool rotate = (A.rotate >> t) & 1;
+    float acc[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[k] = 0.f;
+    for (int token = blockIdx.y * 4 + wave; token < tokens; token += gridDim.y * 4) {
+        const int b = token / A.N, n = token - b * A.N;
+        float cs[4], sn[4];
+        if (rotate) angles(A, b, n, c, cs, sn);
+        const float rinv = A.rinv[(size_t)t * tokens + token];
+        if (h < A.H) {
+            float vx[8], vg[8];
+            decode(load_pairs<T, D, ADJ>(static_cast<const T *>(A.src[t]) + b * A.ss[0] + n * A.ss[1] + h * A.ss[2], c), vx);
+            decode(load_pairs<T, D, ADJ>(static_cast<const T *>(A.grad[t]) + b * A.gs[0] + n * A.gs[1] + h * A.gs[2], c), vg);
+            if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) acc[k] += vg[k] * (vx[k] * rinv);
+        }
+    }
+    for (int turn_of = 0; turn_of < 4; ++turn_of) {
+        if (wave == turn_of) add_to<D, ADJ>(s_dw + hl * D, c, acc, wave == 0);
+        __syncthreads();
+    }
+    float *out = A.partial + ((size_t)t * A.P + blockIdx.y) * A.cols + (size_t)blockIdx.x * 512;
+    for (int i = threadIdx.x; i < 512; i += 256)
+        if ((size_t)blockIdx.x * 512 + i < (size_t)A.cols) out[i] = s_dw[i];
+}
+
+// grid (ceil(cols / 64), tensors), block 256: dw = sum of the P partial sums, 64 bits
+__global__ __launch_bounds__(256) void rope_dw_kernel(const RopeArgs A)
+{
+    __shared__ double s[4][64];
+    const int t = blockIdx.y, j = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + j;
+    if (!A.weight[t]) return;
+    double sum = 0.0;
+    if (i < A.cols)
+        for (int p = wave; p < A.P; p += 4) sum += A.partial[((size_t)t * A.P + p) * A.cols + i];
+    s[wave][j] = sum;
+    __syncthreads();
+    if (wave == 0 && i < A.cols) A.dw[t][i] = (float)((s[0][j] + s[1][j]) + (s[2][j] + s[3][j]));
+}
+
+// ---- launchers -------------------------------------------------------------
+static RopeArgs device_args(const svg2_rope_args *a)
+{
+    RopeArgs A = {};
+    for (int t = 0; t < a->n_tensors; ++t) {
+        A.src[t] = a->src[t];
+        A.dst[t] = a->dst[t];
+        A.weight[t] = a->norm_weight[t];
+        A.rotate |= a->rotate[t] ? 1 << t : 0;
+    }
+    for (int k = 0; k < 3; ++k) {
+        A.ss[k] = a->src_stride[k];
+        A.ds[k] = a->dst_stride[k];
+    }
+    A.pos = a->pos;
+    A.pos_b = a->pos_stride_b;
+    A.freq = a->freq;
+    A.n_axes = a->n_axes;
+    for (int k = 0, e = 0; k < a->n_axes; ++k) A.end[k] = e += a->axis_pairs[k];
+    A.B = a->B;
+    A.N = a->N;
+    A.H = a->H;
+    A.token_scope = a->norm_scope == SVG2_NORM_TOKEN;
+    A.eps = a->eps;
+    return A;
+}
+
+template <typename F> static int with_types(const svg2_rope_args *a, F f)
+{
+    const bool adj = a->pairing == SVG2_ROPE_ADJACENT;
+    if (a->dtype == SVG2_BF16) {
+        if (a->d == 128) return adj ? f((bf16_t *)0, std::integral_constant<int, 128>(), std::true_type()) : f((bf16_t *)0, std::integral_constant<int, 128>(), std::false_type());
+        return adj ? f((bf16_t *)0, std::integral_constant<int, 64>(), std::true_type()) : f((bf16_t *)0, std::integral_constant<int, 64>(), std::false_type());
+    }
+    if (a->d == 128) return adj ? f((float *)0, std::integral_constant<int, 128>(), std::true_type()) : f((float *)0, std::integral_constant<int, 128>(), std::false_type());
+    return adj ? f((float *)0, std::integral_constant<int, 64>(), std::true_type()) : f((float *)0, std::integral_constant<int, 64>(), std::false_type());
+}
+
+int rope_launch(const svg2_rope_args *a, hipStream_t st)
+{
+    const RopeArgs A = device_args(a);
+    return with_types(a, [&](auto *tp, auto dim, auto adj) -> int {
+        using T = std::remove_pointer_t<decltype(tp)>;
+        const dim3 grid(cdiv(A.B * A.N, 4), a->n_tensors);
+        rope_kernel<T, decltype(dim)::value, decltype(adj)::value><<<grid, 256, 0, st>>>(A);
+        SVG2_HIP_CHECK(hipGetLastError());
+        return SVG2_OK;
+    });
+}
+
+struct RopeBwdPlan {
+    int dw, P, blocks, cols;
+    size_t rinv_bytes, total;
+};
+
+static RopeBwdPlan bwd_plan(const svg2_rope_args *a)
+{
+    RopeBwdPlan p = {};
+    const int tokens = a->B * a->N, steps = cdiv(a->H, 64 / (a->d / 8));
+    bool normed = false;
+    for (int t = 0; t < a->n_tensors; ++t) normed |= a->norm_weight[t] != nullptr;
+    if (!normed) p.dw = DW_NONE;
+    else if (a->norm_scope == SVG2_NORM_HEAD) p.dw = DW_HEAD;
+    else p.dw = steps <= (a->dtype == SVG2_BF16 ? bwd_steps<bf16_t>() : bwd_steps<float>()) ? DW_TOKEN : DW_LONG;
+    p.cols = p.dw == DW_HEAD ? a->d : a->H * a->d;
+    p.blocks = cdiv(tokens, 4);
+    if (p.dw == DW_HEAD || p.dw == DW_TOKEN) {          // one partial sum per block: two blocks per CU
+        if (p.blocks > 512) p.blocks = 512;
+        p.P = p.blocks;
+    } else if (p.dw == DW_LONG) {                       // 64 slices of the tokens, fewer where a partial sum is long
+        const int most = 1 + (1 << 23) / p.cols;
+        p.P = p.blocks < 64 ? p.blocks : 64;
+        if (p.P > most) p.P = most;
+        p.rinv_bytes = align256(3 * (size_t)tokens * sizeof(float));
+    }
+    p.total = p.rinv_bytes + 3 * (size_t)p.P * p.cols * sizeof(float);
+    if (p.total < 256) p.total = 256;
+    return p;
+}
+
+size_t rope_bwd_ws_bytes(const svg2_rope_args *a) { return bwd_plan(a).total; }
+
+int rope_bwd_launch(const svg2_rope_args *a, const void *const *dY, void *const *dX, const int64_t *dx_stride,
+                    float *const *dW, void *ws, hipStream_t st)
+{
+    RopeArgs A = device_args(a);
+    const RopeBwdPlan p = bwd_plan(a);
+    for (int t = 0; t < a->n_tensors; ++t) {
+        A.grad[t] = dY[t];
+        A.dst[t] = dX[t];
+        A.dw[t] = A.weight[t] ? dW[t] : nullptr;
+    }
+    for (int k = 0; k < 3; ++k) {
+        A.gs[k] = a->dst_stride[k];
+        A.ds[k] = dx_stride[k];
+    }
+    A.rinv = static_cast<float *>(ws);
+    A.partial = reinterpret_cast<float *>(static_cast<char *>(ws) + p.rinv_bytes);
+    A.P = p.P;
+    A.cols = p.cols;
+    return with_types(a, [&](auto *tp, auto dim, auto adj) -> int {
+        using T = std::remove_pointer_t<decltype(tp)>;
+        constexpr int D = decltype(dim)::value;
+        constexpr bool ADJ = decltype(adj)::value;
+        const dim3 grid(p.blocks, a->n_tensors);
+        if (p.dw == DW_NONE) rope_bwd_kernel<T, D, ADJ, DW_NONE><<<grid, 256, 0, st>>>(A);
+        else if (p.dw == DW_HEAD) rope_bwd_kernel<T, D, ADJ, DW_HEAD><<<grid, 256, D * sizeof(float), st>>>(A);
+        else if (p.dw == DW_TOKEN) rope_bwd_kernel<T, D, ADJ, DW_TOKEN><<<grid, 256, (size_t)p.cols * sizeof(float), st>>>(A);
+        else rope_bwd_kernel<T, D, ADJ, DW_LONG><<<grid, 256, 0, st>>>(A);
+        SVG2_HIP_CHECK(hipGetLastError());
+        if (p.dw == DW_LONG) {
+            rope_dw_long_kernel<T, D, ADJ><<<dim3(cdiv(p.cols, 512), p.P, a->n_tensors), 256, 0, st>>>(A);
+            SVG2_HIP_CHECK(hipGetLastError());
+        }
+        if (p.dw != DW_NONE) {
+            rope_dw_kernel<<<dim3(cdiv(p.cols, 64), a->n_tensors), 256, 0, st>>>(A);
+            SVG2_HIP_CHECK(hipGetLastError());
+        }
+        return SVG2_OK;
+    });
+}
+
+}  // namespace svg2
