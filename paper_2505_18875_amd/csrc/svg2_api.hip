@@ -714,16 +714,17 @@ int svg2_dequantize_mxfp4(const void *codes, const void *scales, int R, int K, i
     return mxfp4_values_launch(codes, scales, R, K, dtype, X, ldx, static_cast<hipStream_t>(stream));
 }
 
-// the product's tiles are numbered in one grid dimension
-static int check_product_size(int M, int N)
+// the product's tiles are numbered in one grid dimension, and a tile's rows are addressed by 32-bit byte offsets
+static int check_product_size(int M, int N, int K)
 {
-    SVG2_REQUIRE((double)cdiv(M, 128) * cdiv(N, 128) < 16777216.0, SVG2_INVALID_ARG, "C of %d x %d has 2^24 tiles or more", M, N);
+    SVG2_REQUIRE(K <= 16777216, SVG2_INVALID_ARG, "K = %d exceeds 2^24", K);
+    SVG2_REQUIRE((double)cdiv(M, 128) * cdiv(N, 128) < 8388608.0, SVG2_INVALID_ARG, "C of %d x %d has 2^23 tiles of 128 x 128 or more", M, N);
     return SVG2_OK;
 }
 
 size_t svg2_matmul_mxfp4_workspace_size(int M, int N, int K)
 {
-    if (M < 1 || N < 1 || K < 1 || M > 67108864 || N > 67108864 || K > 67108864 || check_product_size(M, N) != SVG2_OK) return 256;
+    if (M < 1 || N < 1 || K < 1 || M > 67108864 || N > 67108864 || K > 67108864 || check_product_size(M, N, K) != SVG2_OK) return 256;
     return mxfp4_matmul_ws_bytes(M, N, K);
 }
 
@@ -734,13 +735,14 @@ int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const 
     SVG2_TRY(check_dtype(out_dtype));
     SVG2_TRY(check_mxfp4("A", A, A_scales, M, K));
     SVG2_TRY(check_mxfp4("B", B, B_scales, N, K));
-    SVG2_TRY(check_product_size(M, N));
+    SVG2_TRY(check_product_size(M, N, K));
     SVG2_REQUIRE(C != nullptr, SVG2_INVALID_ARG, "C is null");
     SVG2_REQUIRE(multiple_of(C, out_dtype == SVG2_BF16 ? 2 : 4) && multiple_of(bias, 4), SVG2_INVALID_ARG,
                  "C or bias is not aligned to its elements");
     SVG2_REQUIRE(ldc >= N, SVG2_INVALID_ARG, "ldc = %lld is less than N = %d", (long long)ldc, N);
     SVG2_REQUIRE(C != A && C != A_scales && C != B && C != B_scales && C != bias, SVG2_INVALID_ARG, "C must not alias an input");
     SVG2_TRY(check_ws(ws, ws_bytes, mxfp4_matmul_ws_bytes(M, N, K)));
+    SVG2_TRY(mxfp4_matmul_prepare());
     return mxfp4_matmul_launch(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc, ws, static_cast<hipStream_t>(stream));
 }
 

@@ -223,80 +223,239 @@ struct ProductArgs {
     int tiles_n;
 };
 
-template <typename T> __device__ __forceinline__ void store4(T *c, const float *v, int left, bool vec)
+// 4 bytes per lane into LDS (see load_to_lds_16)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_to_lds_4(const char *base, unsigned byte_off, const unsigned char *dst)
 {
-    if constexpr (sizeof(T) == 4) {
-        if (vec && left >= 4) { *reinterpret_cast<float4 *>(c) = make_float4(v[0], v[1], v[2], v[3]); return; }
-    } else {
-        if (vec && left >= 4) { *reinterpret_cast<uint2 *>(c) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); return; }
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < left) {
-            if constexpr (sizeof(T) == 4) c[i] = v[i];
-            else c[i] = (bf16_t)pack_bf16(v[i], 0.f);
-        }
+    const unsigned lds_addr = (unsigned)(size_t)(const lds_u8 *)dst;
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+                 :
+                 : "v"(byte_off), "s"(base), "s"(lds_addr)
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
-// v_mfma_scale_f32_32x32x64_f8f6f4 on E2M1 operands: lane l gives 32 values of row l % 32 (16 bytes), columns 32 (l / 32) ..,
-// and their scale.  The rows of B go in first: a lane's results are then neighbours in a row of C.
-// grid (tiles), block 256 = 2 x 2 wavefronts of 64 x 64 results; rows behind the last are read as the last and not stored.
-template <typename T> __global__ __launch_bounds__(256) void mxfp4_product_kernel(const ProductArgs P, bool vec)
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+__device__ __forceinline__ i32x8 fragment(const uint4 &u) { return i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0}; }
+
+// The tiled product.  v_mfma_scale_f32_32x32x64_f8f6f4 on E2M1 operands: lane l gives 32 values of row l % 32 (16 bytes), columns
+// 32 (l / 32) .., and their scale.  The rows of B go in first: a lane's results are then neighbours in a row of C.
+//
+// Workgroup: 2 x 2 wavefronts of 32 WT x 32 WT results.  A stage is 128 columns of the 64 WT rows of either side with their
+// scales; four stages are in LDS, three of them on their way while one is used, straight from memory (global_load_lds).  Within a
+// stage the two halves of 64 columns alternate between two register sets: the next half is read from LDS while the matrix
+// instructions of this one run.  The one barrier of a stage stands in its middle.
+// WT = 4, one wavefront a SIMD: 32 instructions of 32 cycles a stage, in which LDS gives 64 KB to the registers (512 cycles) and
+// takes 34 KB (272).
+// In LDS row r has 64 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.
+// Rows behind the last are read as the last and not stored.
+constexpr int PR_STAGES = 4;
+template <int WT> constexpr int pr_stage_bytes() { return 2 * 64 * WT * 64 + 2 * 64 * WT * 4; }
+
+__device__ __forceinline__ int spread(int r) { return ((r >> 1) & 3) ^ ((r >> 3) & 1); }
+
+template <int WT, typename T> __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void mxfp4_product_kernel(const ProductArgs P, bool vec)
 {
+    constexpr int BT = 64 * WT, SIDE = BT * 64, STAGE = pr_stage_bytes<WT>();
+    constexpr int NS = WT < 2 ? 1 : WT / 2, LOADS = 2 * WT + NS;    // loads of a wavefront and stage: scales, all
+    extern __shared__ __attribute__((aligned(256))) unsigned char s_tile[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 31, half = lane >> 5;
-    const int m0 = (blockIdx.x / P.tiles_n) * 128 + (wave >> 1) * 64, n0 = (blockIdx.x % P.tiles_n) * 128 + (wave & 1) * 64;
-    f32x16 acc[2][2] = {};
-    const uint8_t *a[2], *b[2];
-    const unsigned *sa[2], *sb[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int m = min(m0 + 32 * i + row, P.M - 1), n = min(n0 + 32 * i + row, P.N - 1);
-        a[i] = P.A + (long long)m * P.nk * 64 + half * 16;
-        b[i] = P.B + (long long)n * P.nk * 64 + half * 16;
-        sa[i] = reinterpret_cast<const unsigned *>(P.SA) + m;
-        sb[i] = reinterpret_cast<const unsigned *>(P.SB) + n;
+
+    // which tile: the XCDs (every eighth workgroup) get contiguous parts of an order that goes down 8 tiles of C, then right, so
+    // that what an XCD works on at a time is a compact patch and shares its rows in that XCD's L2
+    int tm, tn;
+    {
+        const int tiles_m = (P.M + BT - 1) / BT, total = tiles_m * P.tiles_n;
+        const int xcd = blockIdx.x & 7, part = total >> 3, rest = total & 7;
+        const int t = xcd * part + min(xcd, rest) + (blockIdx.x >> 3);
+        const int group = t / (8 * P.tiles_n), in = t - group * 8 * P.tiles_n, high = min(8, tiles_m - group * 8);
+        tm = group * 8 + in % high;
+        tn = in / high;
     }
-    for (int kc = 0; kc < P.nk; ++kc) {
-        int xa[2], xb[2];
+    const int m0 = tm * BT, n0 = tn * BT;
+    const long long row_bytes = (long long)P.nk * 64;
+    const char *ga = reinterpret_cast<const char *>(P.A) + m0 * row_bytes, *gb = reinterpret_cast<const char *>(P.B) + n0 * row_bytes;
+    const char *gsa = reinterpret_cast<const char *>(P.SA) + m0 * 4LL, *gsb = reinterpret_cast<const char *>(P.SB) + n0 * 4LL;
+
+    // this lane's part of the loads: 16 rows x 64 bytes each
+    unsigned off_a[WT], off_b[WT], off_s[NS];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            xa[i] = (int)(sa[i][(long long)kc * P.M] >> (8 * half));        // bytes 0 and 2: this half's blocks
-            xb[i] = (int)(sb[i][(long long)kc * P.N] >> (8 * half));
+    for (int i = 0; i < WT; ++i) {
+        const int r = (wave * WT + i) * 16 + (lane >> 2), piece = (lane & 3) ^ spread(r);
+        off_a[i] = (unsigned)min(r, P.M - 1 - m0) * (unsigned)row_bytes + piece * 16;
+        off_b[i] = (unsigned)min(r, P.N - 1 - n0) * (unsigned)row_bytes + piece * 16;
+    }
+    // scales: 2 BT words, A's then B's, 64 a load (WT = 1: two wavefronts load the same)
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        const int at = (wave * NS + i) * 64 % (2 * BT), r = at % BT + lane;
+        off_s[i] = 4u * (unsigned)(at < BT ? min(r, P.M - 1 - m0) : min(r, P.N - 1 - n0));
+    }
+    // piece g of a stage's loads: WT of A, WT of B, NS of scales
+    auto load_piece = [&](int kc, int g) {
+        unsigned char *to = s_tile + (kc % PR_STAGES) * STAGE;
+        if (g < WT) {
+            load_to_lds_16(ga + kc * 64LL, off_a[g], to + (wave * WT + g) * 1024);
+        } else if (g < 2 * WT) {
+            load_to_lds_16(gb + kc * 64LL, off_b[g - WT], to + SIDE + (wave * WT + g - WT) * 1024);
+        } else {
+            const int at = (wave * NS + g - 2 * WT) * 64 % (2 * BT);
+            load_to_lds_4(at < BT ? gsa + kc * 4LL * P.M : gsb + kc * 4LL * P.N, off_s[g - 2 * WT], to + 2 * SIDE + at * 4);
+        }
+    };
+    auto load_stage = [&](int kc) {
+#pragma unroll
+        for (int g = 0; g < LOADS; ++g) load_piece(kc, g);
+    };
+
+    f32x16 acc[WT][WT];
+#pragma unroll
+    for (int i = 0; i < WT; ++i)
+#pragma unroll
+        for (int j = 0; j < WT; ++j)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
+
+    const int ra = (wave >> 1) * 32 * WT, rb = (wave & 1) * 32 * WT;
+    const int at = row * 64 + ((half ^ spread(row)) << 4);          // first half of a stage; the second: piece ^ 2
+    struct Set { uint4 a[WT], b[WT]; };
+    // fragment g of a half: b 0, a 0, b 1 .., a 1 ..: in the order in which the products need them
+    auto read_piece = [&](int kc, int k, int g, Set &f) {
+        const unsigned char *s = s_tile + (kc % PR_STAGES) * STAGE + (at ^ (k * 32));
+        const bool is_a = g == 1 || g > WT;
+        const int i = g < 2 ? 0 : g <= WT ? g - 1 : g - WT;
+        if (is_a) f.a[i] = *reinterpret_cast<const uint4 *>(s + (ra + 32 * i) * 64);
+        else f.b[i] = *reinterpret_cast<const uint4 *>(s + SIDE + (rb + 32 * i) * 64);
+    };
+    struct Scales { unsigned a[WT], b[WT]; };
+    auto read_scales = [&](int kc, Scales &x) {
+        const unsigned *s = reinterpret_cast<const unsigned *>(s_tile + (kc % PR_STAGES) * STAGE + 2 * SIDE);
+#pragma unroll
+        for (int i = 0; i < WT; ++i) {
+            x.b[i] = s[BT + rb + 32 * i + row];
+            x.a[i] = s[ra + 32 * i + row];
+        }
+    };
+    auto take_scales = [&](const Scales &x, Scales &y) {            // bytes 0 and 2: this lane's blocks of the two halves
+#pragma unroll
+        for (int i = 0; i < WT; ++i) {
+            y.a[i] = x.a[i] >> (8 * half);
+            y.b[i] = x.b[i] >> (8 * half);
+        }
+    };
+    auto multiply = [&](const Set &f, const Scales &x, int e, auto second) {
+        constexpr int SEL = decltype(second)::value ? 2 : 0;
+        const int i = e / WT, j = e % WT;
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fragment(f.b[j]), fragment(f.a[i]), acc[i][j], 4, 4, SEL,
+                                                                    (int)x.b[j], SEL, (int)x.a[i]);
+    };
+
+    Set f0, f1;
+    Scales x, next;
+    // One stage.  NEXT: there is a stage behind it; LOAD: and one three behind it; PENDING: loads that may still be on their way when
+    // stage kc + 1 is needed.  The groups (two fragments' worth of LDS reads or loads, then matrix instructions) keep the written
+    // order: left to itself the compiler puts all reads in front and the matrix cores wait for them.
+    auto step = [&](int kc, auto load, auto has_next, auto pending) {
+        constexpr bool LOAD = decltype(load)::value, NEXT = decltype(has_next)::value;
+        constexpr int GROUPS = 2 * WT, EACH = (LOADS + GROUPS - 1) / GROUPS;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            read_piece(kc, 1, g, f1);
+#pragma unroll
+            for (int e = g * WT * WT / GROUPS; e < (g + 1) * WT * WT / GROUPS; ++e) multiply(f0, x, e, std::false_type());
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (NEXT) {
+            // stage kc + 1 has arrived for every wavefront; every wavefront is done with stage kc - 1, whose place is free
+            wait_loads<decltype(pending)::value>();
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            read_scales(kc + 1, next);
         }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            i32x8 fa[2], fb[2];
+        for (int g = 0; g < GROUPS; ++g) {
+            if (LOAD)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int4 u = *reinterpret_cast<const int4 *>(a[i] + kc * 64LL + k * 32), w = *reinterpret_cast<const int4 *>(b[i] + kc * 64LL + k * 32);
-                fa[i] = i32x8{u.x, u.y, u.z, u.w, 0, 0, 0, 0};
-                fb[i] = i32x8{w.x, w.y, w.z, w.w, 0, 0, 0, 0};
-            }
+                for (int e = g * EACH; e < (g + 1) * EACH && e < LOADS; ++e) load_piece(kc + 3, e);
+            if (NEXT) read_piece(kc + 1, 0, g, f0);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[i][j] = k == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], 4, 4, 0, xb[j], 0, xa[i])
-                                       : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], 4, 4, 2, xb[j], 2, xa[i]);
+            for (int e = g * WT * WT / GROUPS; e < (g + 1) * WT * WT / GROUPS; ++e) multiply(f1, x, e, std::true_type());
+            if (NEXT && g == GROUPS - 1) take_scales(next, x);
+            __builtin_amdgcn_sched_barrier(0);
         }
-    }
-    // results: lane holds row m0 + 32 i + l % 32 of C, columns n0 + 32 j + 8 q + 4 (l / 32) .. + 3 in registers 4 q .. 4 q + 3
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    using Most = std::integral_constant<int, LOADS>;
+    using None = std::integral_constant<int, 0>;
+
+    const int nk = P.nk;
+    load_stage(0);
+    if (nk > 1) load_stage(1);
+    if (nk > 2) load_stage(2);
+    if (nk > 2) wait_loads<2 * LOADS>();
+    else if (nk > 1) wait_loads<LOADS>();
+    else wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_scales(0, next);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int m = m0 + 32 * i + row;
-        if (m >= P.M) continue;
+    for (int g = 0; g < 2 * WT; ++g) read_piece(0, 0, g, f0);
+    take_scales(next, x);
+    for (int kc = 0; kc + 3 < nk; ++kc) step(kc, Yes(), Yes(), Most());
+    if (nk >= 3) step(nk - 3, No(), Yes(), Most());
+    if (nk >= 2) step(nk - 2, No(), Yes(), None());
+    step(nk - 1, No(), No(), None());
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");     // the last results are read by vector instructions from here on
+
+    // Results: lane holds row m0 + ra + 32 i + l % 32 of C, columns n0 + rb + 32 j + 8 q + 4 (l / 32) .. + 3 in registers 4 q ..
+    // 4 q + 3.  Stored from there, an instruction would write 32 pieces of 16 bytes; 32 rows at a time go through LDS instead (a part
+    // of its own for each wavefront, where the stages were) and out in whole rows of the wavefront's columns.
+    constexpr int COLS = 32 * WT, ROW = COLS * (int)sizeof(T) + 16, PER16 = 16 / (int)sizeof(T);
+    static_assert(4 * 32 * ROW <= PR_STAGES * STAGE, "the stages' place holds 32 rows of every wavefront");
+    __builtin_amdgcn_s_barrier();                                  // every wavefront has read its last stage
+    asm volatile("" ::: "memory");
+    unsigned char *s = s_tile + wave * 32 * ROW;
+    const int n_first = n0 + rb, n_left = P.N - n_first;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+    for (int i = 0; i < WT; ++i) {
+#pragma unroll
+        for (int j = 0; j < WT; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int n = n0 + 32 * j + 8 * q + 4 * half;
-                if (n >= P.N) continue;
+                const int n = 32 * j + 8 * q + 4 * half;
                 float v[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r] + (P.bias && n + r < P.N ? P.bias[n + r] : 0.f);
-                store4(static_cast<T *>(P.C) + (long long)m * P.ldc + n, v, P.N - n, vec);
+                for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r] + (P.bias ? P.bias[min(n_first + n + r, P.N - 1)] : 0.f);
+                unsigned char *to = s + row * ROW + n * (int)sizeof(T);
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+                else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
             }
+        const int m_first = m0 + ra + 32 * i;
+        if (vec) {
+            constexpr int LANES = COLS / PER16, AT_ONCE = 64 / LANES;       // lanes a row, rows an instruction
+            const int c = lane % LANES, first = c * PER16;
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
+                const int r = r0 + lane / LANES;
+                const unsigned char *from = s + r * ROW + c * 16;
+                T *to = static_cast<T *>(P.C) + (long long)(m_first + r) * P.ldc + n_first + first;
+                if (m_first + r < P.M) {
+                    if (first + PER16 <= n_left) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
+                    else
+                        for (int e = 0; e < PER16 && first + e < n_left; ++e) to[e] = reinterpret_cast<const T *>(from)[e];
+                }
+            }
+        } else {
+            for (int e = lane; e < 32 * COLS; e += 64) {
+                const int r = e / COLS, c = e % COLS;
+                if (m_first + r < P.M && c < n_left)
+                    static_cast<T *>(P.C)[(long long)(m_first + r) * P.ldc + n_first + c] = reinterpret_cast<const T *>(s + r * ROW)[c];
+            }
+        }
     }
 }
 
@@ -360,18 +519,37 @@ int mxfp4_values_launch(const void *codes, const void *scales, int M, int K, int
 
 size_t mxfp4_matmul_ws_bytes(int M, int N, int K) { (void)M; (void)N; (void)K; return 256; }
 
+int mxfp4_matmul_prepare()
+{
+    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<4, bf16_t>), PR_STAGES * pr_stage_bytes<4>()));
+    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<4, float>), PR_STAGES * pr_stage_bytes<4>()));
+    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<2, bf16_t>), PR_STAGES * pr_stage_bytes<2>()));
+    return set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<2, float>), PR_STAGES * pr_stage_bytes<2>());
+}
+
+template <int WT> static int product_tiles(ProductArgs P, int out_dtype, bool vec, hipStream_t st)
+{
+    P.tiles_n = cdiv(P.N, 64 * WT);
+    const int tiles = cdiv(P.M, 64 * WT) * P.tiles_n;
+    const size_t lds = PR_STAGES * pr_stage_bytes<WT>();
+    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<WT, bf16_t><<<tiles, 256, lds, st>>>(P, vec);
+    else mxfp4_product_kernel<WT, float><<<tiles, 256, lds, st>>>(P, vec);
+    SVG2_HIP_CHECK(hipGetLastError());
+    return SVG2_OK;
+}
+
 int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
                         int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st)
 {
     (void)ws;
-    ProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
-                     static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, cdiv(N, 128)};
-    const bool vec = aligned(C, out_dtype == SVG2_BF16 ? 8 : 16) && ldc % 4 == 0;
-    const int tiles = cdiv(M, 128) * P.tiles_n;
-    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<bf16_t><<<tiles, 256, 0, st>>>(P, vec);
-    else mxfp4_product_kernel<float><<<tiles, 256, 0, st>>>(P, vec);
-    SVG2_HIP_CHECK(hipGetLastError());
-    return SVG2_OK;
+    const ProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
+                           static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0};
+    const bool vec = aligned(C, 16) && ldc % (out_dtype == SVG2_BF16 ? 8 : 4) == 0;
+    // the largest tile that leaves every CU one
+    auto tiles = [&](int wt) { return (long long)cdiv(M, 64 * wt) * cdiv(N, 64 * wt); };
+    if (tiles(4) >= 256) return product_tiles<4>(P, out_dtype, vec, st);
+    if (tiles(2) >= 256) return product_tiles<2>(P, out_dtype, vec, st);
+    return product_tiles<1>(P, out_dtype, vec, st);
 }
 
 }  // namespace svg2
