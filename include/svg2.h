@@ -426,6 +426,7 @@ int svg2_rope_backward(const svg2_rope_args *args, const void *const *dY, void *
  * ldc >= N its row stride, bias [N] fp32 or NULL.  The matrix cores sum in fp32; one rounding at the end.  With A the quantised
  * activations and B the quantised weights this is a linear layer; its gradients are the same product on dY and W^T (for dX),
  * dY^T and X^T (for dW).
+ * Where svg2_matmul_mxfp4_workspace_size returns 256 no scratch is needed and ws may be NULL.
  * C must not overlap an input.  Rows and columns up to 2^26 (the product: K up to 2^24, C up to 2^23 tiles of 128 x 128).
  * ------------------------------------------------------------------------- */
 int svg2_quantize_mxfp4(const void *X, int dtype, int M, int G, int Kg, int64_t stride_m, int64_t stride_g,

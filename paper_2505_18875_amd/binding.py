@@ -8,6 +8,7 @@ exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from types import SimpleNamespace
@@ -67,6 +68,8 @@ class _RopeArgs(ctypes.Structure):
                 ("freq", ctypes.c_void_p), ("n_axes", ctypes.c_int), ("axis_pairs", ctypes.c_int * 4),
                 ("pairing", ctypes.c_int), ("norm_scope", ctypes.c_int), ("eps", ctypes.c_float)]
 
+
+_P3, _I3 = ctypes.c_void_p * 3, ctypes.c_int64 * 3
 
 _lib = None
 
@@ -413,13 +416,28 @@ def svg2_kmeans_pp_init(X, C, u, *, ws=None):
     return SimpleNamespace(centroids=centroids, picked=picked)
 
 
+# The calls below are short on the GPU where there are few tokens, so their checks are written to cost little: every attribute
+# of a tensor is asked for once.
+
+def _raw_stream(device: torch.device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _on(device: torch.device):
+    """Context in which `device` is the current one."""
+    return _HERE_ALREADY if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
+
+
+_HERE_ALREADY = contextlib.nullcontext()
+
+
 def _strided(t: torch.Tensor, name: str, device=None, dtype=None) -> int:
     """Address of a GPU tensor of any strides whose innermost dimension is contiguous."""
     if not t.is_cuda:
         raise ValueError("%s must live on the GPU" % name)
     if device is not None and t.device != device:
         raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
@@ -429,27 +447,54 @@ def _strided(t: torch.Tensor, name: str, device=None, dtype=None) -> int:
 def _dense(t: Optional[torch.Tensor], name: str, device, dtype, shape) -> Optional[int]:
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
     return _strided(t, name, device, dtype)
 
 
-def _outer_strides(t: torch.Tensor):
+def _outer_strides(shape, stride):
     """Strides of all but the last dimension; 0 where the dimension has one entry (torch leaves anything there)."""
-    return [t.stride(k) if t.shape[k] > 1 else 0 for k in range(t.dim() - 1)]
+    return [s if n > 1 else 0 for n, s in zip(shape[:-1], stride[:-1])]
 
 
-def _same_views(tensors, name, device, dtype, shape):
-    strides = _outer_strides(tensors[0])
+def _three(xs):
+    return tuple(xs) + (None,) * (3 - len(xs))
+
+
+def _token_views(tensors, name, device, dtype, shape=None):
+    """One to three [N,H,d] or [B,N,H,d] tensors of one shape and one set of strides -> (B,N,H,d), the three outer strides,
+    addresses."""
+    if not 1 <= len(tensors) <= 3:
+        raise ValueError("%s: one to three tensors" % name)
+    own, stride = tensors[0].shape, tensors[0].stride()
+    if len(own) == 4:
+        full, outer = tuple(own), _outer_strides(own, stride)
+    elif len(own) == 3:
+        full, outer = (1,) + tuple(own), [0] + _outer_strides(own, stride)
+    else:
+        raise ValueError("%s must be [N,H,d] or [B,N,H,d]" % name)
+    if shape is not None and full != shape:
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(own)))
     for i, t in enumerate(tensors):
-        if tuple(t.shape) != tuple(shape):
-            raise ValueError("%s[%d] must be %s, got %s" % (name, i, list(shape), list(t.shape)))
-        if _outer_strides(t) != strides:
-            raise ValueError("%s must share one set of strides" % name)
-        _strided(t, "%s[%d]" % (name, i), device, dtype)
-    return strides
+        if i and (t.shape != own or (t.stride() != stride and _outer_strides(own, t.stride()) != _outer_strides(own, stride))):
+            raise ValueError("%s must share one shape and one set of strides" % name)
+    return full, outer, [_strided(t, name, device, dtype) for t in tensors]
+
+
+def _head_order(tensors, name, device, dtype, shape):
+    """As _token_views for [B*H,N,d] tensors that stand for [B,N,H,d]; [B,N,H,d] tensors themselves are taken too."""
+    B, N, H, d = shape
+    own = tensors[0].shape
+    if len(own) != 3:
+        return _token_views(tensors, name, device, dtype, shape)[1:]
+    stride = tensors[0].stride()
+    for t in tensors:
+        if t.shape != (B * H, N, d) or t.stride() != stride:
+            raise ValueError("%s must all be [%d,%d,%d] with one set of strides" % (name, B * H, N, d))
+    s = _outer_strides(own, stride)
+    return [H * s[0] if B > 1 else 0, s[1], s[0] if H > 1 else 0], [_strided(t, name, device, dtype) for t in tensors]
 
 
 def svg2_grid_positions(grid, *, first=(0, 0, 0), extra=0, device="cuda"):
@@ -466,59 +511,38 @@ def svg2_rope_frequencies(axis_pairs, *, theta=10000.0, device="cuda"):
                       for n in axis_pairs if n > 0]).to(device)
 
 
-def _rope_args(views, shape, dtype, device, pos, freq, axis_pairs, rotate, norm_weights, norm_scope, eps, pairing):
-    n = len(views)
+def _rope_args(n, dtype, device, shape, src, src_stride, dst, dst_stride, pos, freq, axis_pairs, rotate, norm_weights, norm_scope,
+               eps, pairing):
+    """The C struct, with every check that needs the tensors themselves."""
     B, N, H, d = shape
     if pairing not in ROPE_PAIRINGS:
         raise ValueError("pairing must be one of %s" % (ROPE_PAIRINGS,))
     if norm_scope not in NORM_SCOPES:
         raise ValueError("norm_scope must be one of %s" % (NORM_SCOPES,))
-    rotate = [True] * n if rotate is None else [bool(r) for r in rotate]
-    norm_weights = [None] * n if norm_weights is None else list(norm_weights)
-    if len(rotate) != n or len(norm_weights) != n:
+    rotate = (True,) * n if rotate is None else tuple(rotate)
+    weights = (None,) * n if norm_weights is None else tuple(norm_weights)
+    if len(rotate) != n or len(weights) != n:
         raise ValueError("rotate and norm_weights need one entry per tensor")
-    a = _RopeArgs()
-    a.n_tensors, a.dtype, a.B, a.N, a.H, a.d = n, dtype, B, N, H, d
-    a.rotate = (ctypes.c_int * 3)(*[int(r) for r in rotate])
     wshape = (d,) if norm_scope == "head" else (H, d)
-    a.norm_weight = (ctypes.c_void_p * 3)(*[_dense(w, "norm_weights[%d]" % i, device, torch.float32, wshape)
-                                            for i, w in enumerate(norm_weights)])
+    w = [None if x is None else _dense(x, "norm_weights", device, torch.float32, wshape) for x in weights]
+    pos_ptr = freq_ptr = None
+    pos_stride, axes = 0, ()
     if any(rotate):
-        axis_pairs = [int(x) for x in axis_pairs]
-        if not 1 <= len(axis_pairs) <= 4:
+        axes = tuple(int(x) for x in axis_pairs)
+        if not 1 <= len(axes) <= 4:
             raise ValueError("axis_pairs must have 1 to 4 entries")
-        if pos.dim() == 2:
-            pos = pos[None]
-        if tuple(pos.shape) not in ((1, N, len(axis_pairs)), (B, N, len(axis_pairs))):
-            raise ValueError("pos must be [N,%d] or [B,N,%d], got %s" % (len(axis_pairs), len(axis_pairs), list(pos.shape)))
-        _strided(pos, "pos", device, torch.int32)
-        if not pos[0].is_contiguous():
+        k = len(axes)
+        have = tuple(pos.shape)
+        if have != (N, k) and have != (B, N, k) and have != (1, N, k):
+            raise ValueError("pos must be [N,%d] or [B,N,%d], got %s" % (k, k, list(have)))
+        if not (pos.is_contiguous() or (len(have) == 3 and pos[0].is_contiguous())):
             raise ValueError("pos must be dense inside a batch")
-        a.pos = pos.data_ptr()
-        a.pos_stride_b = pos.stride(0) if pos.shape[0] > 1 else 0
-        a.freq = _dense(freq, "freq", device, torch.float64, (d // 2,))
-        a.n_axes = len(axis_pairs)
-        a.axis_pairs = (ctypes.c_int * 4)(*axis_pairs)
-    a.pairing, a.norm_scope, a.eps = ROPE_PAIRINGS.index(pairing), NORM_SCOPES.index(norm_scope), float(eps)
-    return a, norm_weights
-
-
-def _token_views(tensors, name):
-    """[N,H,d] or [B,N,H,d] tensors as [B,N,H,d] views."""
-    tensors = list(tensors)
-    if not 1 <= len(tensors) <= 3:
-        raise ValueError("%s: one to three tensors" % name)
-    out = [t[None] if t.dim() == 3 else t for t in tensors]
-    if any(t.dim() != 4 for t in out):
-        raise ValueError("%s must be [N,H,d] or [B,N,H,d]" % name)
-    return out
-
-
-def _head_order(t, B, N, H, d):
-    """[B*H,N,d] as a [B,N,H,d] view."""
-    if tuple(t.shape) != (B * H, N, d):
-        raise ValueError("expected [%d,%d,%d], got %s" % (B * H, N, d, list(t.shape)))
-    return t.unflatten(0, (B, H)).transpose(1, 2)
+        pos_ptr = _strided(pos, "pos", device, torch.int32)
+        pos_stride = pos.stride(0) if len(have) == 3 and have[0] > 1 else 0
+        freq_ptr = _dense(freq, "freq", device, torch.float64, (d // 2,))
+    return _RopeArgs(n, dtype, B, N, H, d, _three(src), _three(dst), tuple([1 if r else 0 for r in rotate]), _three(w),
+                     tuple(src_stride), tuple(dst_stride), pos_ptr, pos_stride, freq_ptr, len(axes), axes,
+                     ROPE_PAIRINGS.index(pairing), NORM_SCOPES.index(norm_scope), eps), weights
 
 
 def svg2_rope(tensors, pos=None, freq=None, *, axis_pairs=(), rotate=None, norm_weights=None, norm_scope="head", eps=1e-6,
@@ -528,28 +552,24 @@ def svg2_rope(tensors, pos=None, freq=None, *, axis_pairs=(), rotate=None, norm_
     tensors: [N,H,d] or [B,N,H,d] views of one shape and set of strides (slices of a packed projection); pos int32
     [N,axes] or [B,N,axes]; freq fp64 [d/2]; axis_pairs: pairs of each axis; rotate: per tensor, default all;
     norm_weights: per tensor fp32 [d] (norm_scope "head") or [H,d] ("token"), or None.  Returns [B*H,N,d] tensors, or
-    `outs` ([B,N,H,d] views of any strides; `tensors` themselves for a call in place)."""
+    `outs` ([N,H,d] or [B,N,H,d] views of any strides; `tensors` themselves for a call in place)."""
     lib = load_library()
-    views = _token_views(tensors, "tensors")
-    B, N, H, d = shape = views[0].shape
-    dev = views[0].device
-    strides = _same_views(views, "tensors", dev, views[0].dtype, shape)
-    a, _ = _rope_args(views, shape, _dtype_code(views[0]), dev, pos, freq, axis_pairs, rotate, norm_weights, norm_scope, eps, pairing)
+    n, first = len(tensors), tensors[0]
+    dtype, dev = first.dtype, first.device
+    shape, src_stride, src = _token_views(tensors, "tensors", dev, dtype)
+    B, N, H, d = shape
     if outs is None:
-        result = [torch.empty((B * H, N, d), dtype=views[0].dtype, device=dev) for _ in views]
-        dst = [_head_order(t, B, N, H, d) for t in result]
+        outs = [torch.empty((B * H, N, d), dtype=dtype, device=dev) for _ in range(n)]
+        dst_stride, dst = (H * N * d, d, N * d), [t.data_ptr() for t in outs]
     else:
-        result = list(outs)
-        dst = _token_views(result, "outs")
-        if len(dst) != len(views):
+        if len(outs) != n:
             raise ValueError("one output per tensor")
-    dst_strides = _same_views(dst, "outs", dev, views[0].dtype, shape)
-    a.src = (ctypes.c_void_p * 3)(*[t.data_ptr() for t in views])
-    a.dst = (ctypes.c_void_p * 3)(*[t.data_ptr() for t in dst])
-    a.src_stride, a.dst_stride = (ctypes.c_int64 * 3)(*strides), (ctypes.c_int64 * 3)(*dst_strides)
-    with torch.cuda.device(dev):
-        _check(lib.svg2_rope(ctypes.addressof(a), _stream()))
-    return result
+        _, dst_stride, dst = _token_views(outs, "outs", dev, dtype, shape)
+    a, _ = _rope_args(n, _dtype_code(first), dev, shape, src, src_stride, dst, dst_stride, pos, freq, axis_pairs, rotate, norm_weights,
+                      norm_scope, eps, pairing)
+    with _on(dev):
+        _check(lib.svg2_rope(ctypes.byref(a), _raw_stream(dev)))
+    return outs
 
 
 def svg2_rope_backward(grads, tensors, pos=None, freq=None, *, axis_pairs=(), rotate=None, norm_weights=None,
@@ -557,33 +577,24 @@ def svg2_rope_backward(grads, tensors, pos=None, freq=None, *, axis_pairs=(), ro
     """Gradients of svg2_rope: grads ([B*H,N,d], or [B,N,H,d] views of one set of strides) and the forward call's arguments
     -> grads of `tensors` (dense [B,N,H,d], or `outs`, views of any strides) and of norm_weights (None where None)."""
     lib = load_library()
-    views = _token_views(tensors, "tensors")
-    B, N, H, d = shape = views[0].shape
-    dev = views[0].device
-    strides = _same_views(views, "tensors", dev, views[0].dtype, shape)
-    a, weights = _rope_args(views, shape, _dtype_code(views[0]), dev, pos, freq, axis_pairs, rotate, norm_weights, norm_scope, eps,
-                            pairing)
-    grads = [_head_order(g, B, N, H, d) if g.dim() == 3 else g for g in grads]
+    n, first = len(tensors), tensors[0]
+    dtype, dev = first.dtype, first.device
+    shape, src_stride, src = _token_views(tensors, "tensors", dev, dtype)
     if outs is None:
-        result = [torch.empty(shape, dtype=views[0].dtype, device=dev) for _ in views]
-        dx = result
-    else:
-        result = list(outs)
-        dx = _token_views(result, "outs")
-    if len(grads) != len(views) or len(dx) != len(views):
+        outs = [torch.empty(shape, dtype=dtype, device=dev) for _ in range(n)]
+    if len(grads) != n or len(outs) != n:
         raise ValueError("one gradient and one output per tensor")
-    g_strides = _same_views(grads, "grads", dev, views[0].dtype, shape)
-    dx_strides = _same_views(dx, "outs", dev, views[0].dtype, shape)
+    g_stride, g = _head_order(grads, "grads", dev, dtype, shape)
+    _, dx_stride, dx = _token_views(outs, "outs", dev, dtype, shape)
+    # the C entry takes the gradients' layout as that of the forward's results; they are only read
+    a, weights = _rope_args(n, _dtype_code(first), dev, shape, src, src_stride, (), g_stride, pos, freq, axis_pairs, rotate,
+                            norm_weights, norm_scope, eps, pairing)
     dw = [None if w is None else torch.empty_like(w) for w in weights]
-    a.src = (ctypes.c_void_p * 3)(*[t.data_ptr() for t in views])
-    # a gradient may be an expanded view (it is only read); the C entry takes its layout as the forward's dst
-    a.src_stride, a.dst_stride = (ctypes.c_int64 * 3)(*strides), (ctypes.c_int64 * 3)(*g_strides)
-    ptrs = lambda ts: (ctypes.c_void_p * 3)(*[None if t is None else t.data_ptr() for t in ts])  # noqa: E731
-    with torch.cuda.device(dev):
-        ws = _workspace(lib.svg2_rope_backward_workspace_size(ctypes.addressof(a)), dev) if ws is None else ws
-        _check(lib.svg2_rope_backward(ctypes.addressof(a), ptrs(grads), ptrs(dx), (ctypes.c_int64 * 3)(*dx_strides), ptrs(dw),
-                                      _dev(ws), ws.numel(), _stream()))
-    return SimpleNamespace(grads=result, dweights=dw)
+    with _on(dev):
+        ws = _workspace(lib.svg2_rope_backward_workspace_size(ctypes.byref(a)), dev) if ws is None else ws
+        _check(lib.svg2_rope_backward(ctypes.byref(a), _P3(*g), _P3(*dx), _I3(*dx_stride),
+                                      _P3(*[None if t is None else t.data_ptr() for t in dw]), _dev(ws), ws.numel(), _raw_stream(dev)))
+    return SimpleNamespace(grads=outs, dweights=dw)
 
 
 def _mxfp4_empty(R, K, device):
@@ -594,12 +605,13 @@ def _mxfp4_empty(R, K, device):
 
 def _mxfp4_operand(codes, scales, name, device):
     """Checks an operand's two tensors; rows and padded columns."""
-    if codes.dim() != 2 or codes.shape[1] % 64:
-        raise ValueError("%s: codes must be [R, Kp/2] with Kp a multiple of 128, got %s" % (name, list(codes.shape)))
-    R, Kp = codes.shape[0], 2 * codes.shape[1]
-    _dense(codes, name + " codes", device, torch.uint8, (R, Kp // 2))
-    _dense(scales, name + " scales", device, torch.uint8, (Kp // 128, R, 4))
-    return R, Kp
+    shape = codes.shape
+    if len(shape) != 2 or shape[1] % 64:
+        raise ValueError("%s: codes must be [R, Kp/2] with Kp a multiple of 128, got %s" % (name, list(shape)))
+    R, half = shape
+    _dense(codes, name, device, torch.uint8, shape)
+    _dense(scales, name, device, torch.uint8, (half // 64, R, 4))
+    return R, 2 * half
 
 
 def svg2_quantize_mxfp4(X, *, transposed=False):
@@ -608,14 +620,17 @@ def svg2_quantize_mxfp4(X, *, transposed=False):
     lib = load_library()
     if X.dim() not in (2, 3):
         raise ValueError("X must be [M,K] or [M,G,Kg]")
-    view = X[:, None] if X.dim() == 2 else X
-    M, G, Kg = view.shape
-    ptr = _strided(view, "X")
-    sm, sg = _outer_strides(view)
-    codes, scales = _mxfp4_empty(G * Kg, M, X.device) if transposed else _mxfp4_empty(M, G * Kg, X.device)
-    with torch.cuda.device(X.device):
-        _check(lib.svg2_quantize_mxfp4(ptr, _dtype_code(X), M, G, Kg, sm, sg, int(transposed), codes.data_ptr(),
-                                       scales.data_ptr(), _stream()))
+    ptr, dev, shape = _strided(X, "X"), X.device, X.shape
+    if len(shape) == 2:
+        (M, Kg), G = shape, 1
+        sm, sg = _outer_strides(shape, X.stride())[0], 0
+    else:
+        M, G, Kg = shape
+        sm, sg = _outer_strides(shape, X.stride())
+    codes, scales = _mxfp4_empty(G * Kg, M, dev) if transposed else _mxfp4_empty(M, G * Kg, dev)
+    with _on(dev):
+        _check(lib.svg2_quantize_mxfp4(ptr, _dtype_code(X), M, G, Kg, sm, sg, 1 if transposed else 0, codes.data_ptr(),
+                                       scales.data_ptr(), _raw_stream(dev)))
     return codes, scales
 
 
@@ -628,12 +643,12 @@ def svg2_dequantize_mxfp4(codes, scales, K=None, *, dtype=torch.bfloat16, out=No
     if not Kp - 128 < K <= Kp:
         raise ValueError("K = %d does not belong to %d padded columns" % (K, Kp))
     out = torch.empty((R, K), dtype=dtype, device=dev) if out is None else out
-    if tuple(out.shape) != (R, K):
+    if out.shape != (R, K):
         raise ValueError("out must be [%d,%d]" % (R, K))
     ptr = _strided(out, "out", dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         _check(lib.svg2_dequantize_mxfp4(codes.data_ptr(), scales.data_ptr(), R, K, _dtype_code(out), ptr,
-                                         out.stride(0) if R > 1 else K, _stream()))
+                                         out.stride(0) if R > 1 else K, _raw_stream(dev)))
     return out
 
 
@@ -646,14 +661,17 @@ def svg2_matmul_mxfp4(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bf
     if Kb != Kp:
         raise ValueError("A has %d padded columns, B has %d" % (Kp, Kb))
     C = torch.empty((M, N), dtype=out_dtype, device=dev) if out is None else out
-    if tuple(C.shape) != (M, N):
+    if C.shape != (M, N):
         raise ValueError("out must be [%d,%d]" % (M, N))
     ptr = _strided(C, "out", dev)
     bias_ptr = _dense(bias, "bias", dev, torch.float32, (N,))
-    with torch.cuda.device(dev):
-        ws = _workspace(lib.svg2_matmul_mxfp4_workspace_size(M, N, Kp), dev) if ws is None else ws
+    with _on(dev):
+        need = lib.svg2_matmul_mxfp4_workspace_size(M, N, Kp) if ws is None else 0
+        if need > 256:                  # at 256 the product needs none
+            ws = _workspace(need, dev)
         _check(lib.svg2_matmul_mxfp4(A.data_ptr(), A_scales.data_ptr(), B.data_ptr(), B_scales.data_ptr(), M, N, Kp, bias_ptr,
-                                     _dtype_code(C), ptr, C.stride(0) if M > 1 else N, _dev(ws), ws.numel(), _stream()))
+                                     _dtype_code(C), ptr, C.stride(0) if M > 1 else N, _dev(ws), 0 if ws is None else ws.numel(),
+                                     _raw_stream(dev)))
     return C
 
 

@@ -741,7 +741,8 @@ int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const 
                  "C or bias is not aligned to its elements");
     SVG2_REQUIRE(ldc >= N, SVG2_INVALID_ARG, "ldc = %lld is less than N = %d", (long long)ldc, N);
     SVG2_REQUIRE(C != A && C != A_scales && C != B && C != B_scales && C != bias, SVG2_INVALID_ARG, "C must not alias an input");
-    SVG2_TRY(check_ws(ws, ws_bytes, mxfp4_matmul_ws_bytes(M, N, K)));
+    const size_t need = mxfp4_matmul_ws_bytes(M, N, K);         // 256: none is used
+    if (need > 256 || ws) SVG2_TRY(check_ws(ws, ws_bytes, need));
     SVG2_TRY(mxfp4_matmul_prepare());
     return mxfp4_matmul_launch(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc, ws, static_cast<hipStream_t>(stream));
 }

@@ -131,7 +131,7 @@ def test_matmul_mxfp4_refuses(lib):
     ok = (1 << 20, 2 << 20, 3 << 20, 4 << 20, 128, 256, 512, None, 1, 5 << 20, 256, 256, 1 << 40, None)
     for at, v, code, word in ((0, None, 1, b"A:"), (1, None, 1, b"A:"), (2, 8, 1, b"B:"), (3, None, 1, b"B:"), (4, 0, 1, b"rows"), (5, -3, 1, b"rows"),
                               (6, 0, 1, b"columns"), (7, 2, 1, b"aligned"), (8, 9, 2, b"dtype"), (9, None, 1, b"null"), (9, (5 << 20) + 1, 1, b"aligned"),
-                              (10, 255, 1, b"ldc"), (9, 1 << 20, 1, b"alias"), (11, None, 1, b"workspace"), (11, 8, 1, b"aligned"), (12, 16, 3, b"workspace")):
+                              (10, 255, 1, b"ldc"), (9, 1 << 20, 1, b"alias"), (11, 8, 1, b"aligned"), (12, 16, 3, b"workspace")):
         args = list(ok)
         args[at] = v
         assert lib.svg2_matmul_mxfp4(*args) == code, (at, v)
