@@ -118,29 +118,35 @@ template <int D, bool ADJ> __device__ __forceinline__ void load_weight(const flo
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
 
-// cosine and sine of the four angles of a lane.  The quarter turns are taken off in 64 bits (two-part pi / 2: the error is
+// cosine and sine of the angle of pair p; of the four of a lane.  The quarter turns are taken off in 64 bits (two-part pi / 2: the error is
 // that of the product pos * freq itself), what remains is at most pi / 4 and goes through the Taylor polynomials, whose next
 // terms there are 2e-9 (sine, x^11 / 11!) and 1e-10 (cosine, x^12 / 12!).
+__device__ __forceinline__ void angle(const RopeArgs &A, const int32_t *pos, int p, float &cs, float &sn)
+{
+    int axis = 0;
+#pragma unroll
+    for (int x = 0; x < 3; ++x) axis += (x + 1 < A.n_axes && p >= A.end[x]) ? 1 : 0;
+    const double t = (double)pos[axis] * A.freq[p];
+    const double q = rint(t * 0.63661977236758134);
+    const float r = (float)fma(-q, 6.123233995736766e-17, fma(-q, 1.5707963267948966, t));
+    const int quadrant = (int)(q - 4.0 * floor(q * 0.25));
+    const float z = r * r;
+    const float s = r + r * z * (-1.f / 6 + z * (1.f / 120 + z * (-1.f / 5040 + z * (1.f / 362880))));
+    const float co = 1.f + z * (-0.5f + z * (1.f / 24 + z * (-1.f / 720 + z * (1.f / 40320 - z * (1.f / 3628800)))));
+    const float u = (quadrant & 1) ? s : co, v = (quadrant & 1) ? co : s;
+    cs = (quadrant == 1 || quadrant == 2) ? -u : u;
+    sn = quadrant >= 2 ? -v : v;
+}
+
+__device__ __forceinline__ const int32_t *position(const RopeArgs &A, int b, int n)
+{
+    return A.pos + (long long)b * A.pos_b + (long long)n * A.n_axes;
+}
+
 __device__ __forceinline__ void angles(const RopeArgs &A, int b, int n, int c, float *cs, float *sn)
 {
-    const int32_t *pos = A.pos + (long long)b * A.pos_b + (long long)n * A.n_axes;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int p = 4 * c + k;
-        int axis = 0;
-#pragma unroll
-        for (int x = 0; x < 3; ++x) axis += (x + 1 < A.n_axes && p >= A.end[x]) ? 1 : 0;
-        const double t = (double)pos[axis] * A.freq[p];
-        const double q = rint(t * 0.63661977236758134);
-        const float r = (float)fma(-q, 6.123233995736766e-17, fma(-q, 1.5707963267948966, t));
-        const int quadrant = (int)(q - 4.0 * floor(q * 0.25));
-        const float z = r * r;
-        const float s = r + r * z * (-1.f / 6 + z * (1.f / 120 + z * (-1.f / 5040 + z * (1.f / 362880))));
-        const float co = 1.f + z * (-0.5f + z * (1.f / 24 + z * (-1.f / 720 + z * (1.f / 40320 - z * (1.f / 3628800)))));
-        const float u = (quadrant & 1) ? s : co, v = (quadrant & 1) ? co : s;
-        cs[k] = (quadrant == 1 || quadrant == 2) ? -u : u;
-        sn[k] = quadrant >= 2 ? -v : v;
-    }
+    for (int k = 0; k < 4; ++k) angle(A, position(A, b, n), 4 * c + k, cs[k], sn[k]);
 }
 
 template <bool ADJ> __device__ __forceinline__ void turn(float *v, const float *cs, const float *sn, float sense)
@@ -233,41 +239,65 @@ template <typename T, int D, bool ADJ> __global__ __launch_bounds__(256) void ro
 }
 
 // ---- backward --------------------------------------------------------------
-// How the weights' gradient is summed: per lane over the tokens of a wavefront, over the block's wavefronts in LDS, over the
-// blocks by rope_dw_kernel, each in a fixed order, so that it is the same from run to run.
-enum { DW_NONE = 0, DW_HEAD = 1, DW_TOKEN = 2, DW_LONG = 3 };
-//   DW_HEAD    [d] weights: 8 sums per lane
-//   DW_TOKEN   [H,d] weights of a token that fits CH steps: its sums stay in registers beside it
+// How the weights' gradient is summed: per lane over the tokens that pass through it, over the block's wavefronts in LDS where
+// they hold the same columns, over the blocks by rope_dw_kernel, each in a fixed order, so that it is the same from run to run.
+enum { DW_NONE = 0, DW_HEAD = 1, DW_ROW = 2, DW_LONG = 3 };
+//   DW_HEAD    [d] weights: 8 sums per lane (rope_bwd_kernel)
+//   DW_ROW     [H,d] weights, up to 8192: a wavefront (up to 2048) or a workgroup holds a token, its weights and its sums
+//              (rope_bwd_row_kernel).  One wavefront does not hold a token of 5120 values and their sums: 1032 us for Q, K and V of
+//              16,384 tokens, most of it spilled registers
 //   DW_LONG    longer tokens: read twice here (sums, then results); 1 / rms is left for rope_dw_long_kernel
+constexpr int ROW_STEPS = 4;        // most steps of 8 values a thread that are held
 
-template <typename T> constexpr int bwd_steps() { return sizeof(T) == 2 ? 10 : 5; }     // CH
+template <int D, bool ADJ> __device__ __forceinline__ int column(int c, int k)     // where value k of lane c is in its head
+{
+    return ADJ ? 8 * c + k : (k < 4 ? 4 * c + k : D / 2 + 4 * c + k - 4);
+}
 
 // adds the block's four wavefronts' sums in order into s[cols]
 template <int D, bool ADJ> __device__ __forceinline__ void add_to(float *s, int c, const float *v, bool first)
 {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const int i = ADJ ? 8 * c + k : (k < 4 ? 4 * c + k : D / 2 + 4 * c + k - 4);
+        const int i = column<D, ADJ>(c, k);
         s[i] = first ? v[k] : s[i] + v[k];
+    }
+}
+
+// sums of a lane's share: x^2 and g w x
+__device__ __forceinline__ void add_sums(const float *vx, const float *vg, const float *w, float &xx, float &gx)
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        xx = fmaf(vx[k], vx[k], xx);
+        gx = fmaf(vg[k] * w[k], vx[k], gx);
+    }
+}
+
+// vg: g on entry, dx on return; acc += g xn (add: this lane has a head)
+__device__ __forceinline__ void norm_gradient(const float *vx, float *vg, const float *w, float rinv, float mean, float *acc, bool add)
+{
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float xn = vx[k] * rinv;
+        if (add) acc[k] += vg[k] * xn;
+        vg[k] = rinv * (vg[k] * w[k] - xn * mean);
     }
 }
 
 // grid (blocks, tensors), block 256: wavefronts stride over the tokens
 template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256, 2) void rope_bwd_kernel(const RopeArgs A)
 {
-    constexpr int LPH = D / 8, HPS = 64 / LPH, CH = bwd_steps<T>();
-    constexpr int ACC = DW == DW_TOKEN ? CH : 1;
-    extern __shared__ float s_dw[];             // [cols] (DW_HEAD, DW_TOKEN)
+    constexpr int LPH = D / 8, HPS = 64 / LPH, CH = DW == DW_LONG ? 2 : 4;
+    __shared__ float s_dw[D];                   // DW_HEAD
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = blockIdx.y;
     const int hl = lane / LPH, c = lane % LPH, steps = (A.H + HPS - 1) / HPS, tokens = A.B * A.N;
     const float *weight = DW == DW_NONE ? nullptr : A.weight[t];
     const bool rotate = (A.rotate >> t) & 1;
 
-    float acc[ACC][8], w[8];
+    float acc[8], w[8];
 #pragma unroll
-    for (int s = 0; s < ACC; ++s)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) acc[s][k] = 0.f;
+    for (int k = 0; k < 8; ++k) acc[k] = 0.f;
     if (DW == DW_HEAD && weight) load_weight<D, ADJ>(weight, c, w);
 
     for (int token = blockIdx.x * 4 + wave; token < tokens; token += gridDim.x * 4) {
@@ -286,7 +316,7 @@ template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256,
             }
         };
         float cs[4], sn[4], rinv = 1.f, mean = 0.f;
-        if ((DW == DW_TOKEN || DW == DW_LONG) && weight) {
+        if (DW == DW_LONG && weight) {
             float xx = 0.f, gx = 0.f;
             for (int s0 = 0; s0 < steps; s0 += CH) {
                 load(s0);
@@ -300,22 +330,18 @@ template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256,
                     decode(rg[s], vg);
                     if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
                     load_weight<D, ADJ>(weight + h * D, c, w);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        xx = fmaf(vx[k], vx[k], xx);
-                        gx = fmaf(vg[k] * w[k], vx[k], gx);
-                    }
+                    add_sums(vx, vg, w, xx, gx);
                 }
             }
             const float count = (float)A.H * D;
             rinv = 1.f / sqrtf(group_sum(xx, 64) / count + A.eps);
             mean = group_sum(gx, 64) * rinv / count;
-            if (DW == DW_LONG && lane == 0) A.rinv[(size_t)t * tokens + token] = rinv;
+            if (lane == 0) A.rinv[(size_t)t * tokens + token] = rinv;
         } else if (rotate) {
             angles(A, b, n, c, cs, sn);
         }
         for (int s0 = 0; s0 < steps; s0 += CH) {
-            if (!(DW == DW_TOKEN && weight)) load(s0);
+            load(s0);
 #pragma unroll
             for (int s = 0; s < CH; ++s) {
                 const int h = (s0 + s) * HPS + hl;
@@ -329,26 +355,13 @@ template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256,
                         decode(rx[s], vx);
                         if (DW == DW_HEAD) {
                             float xx = 0.f, gx = 0.f;
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                xx = fmaf(vx[k], vx[k], xx);
-                                gx = fmaf(vg[k] * w[k], vx[k], gx);
-                            }
+                            add_sums(vx, vg, w, xx, gx);
                             rinv = 1.f / sqrtf(group_sum(xx, LPH) * (1.f / D) + A.eps);
                             mean = group_sum(gx, LPH) * rinv * (1.f / D);
                         } else if (h < A.H) {
                             load_weight<D, ADJ>(weight + h * D, c, w);
                         }
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float xn = vx[k] * rinv;
-                            if (DW == DW_HEAD || DW == DW_TOKEN) {
-                                const float add = vg[k] * xn;
-                                float &to = acc[DW == DW_TOKEN ? s : 0][k];
-                                to = h < A.H ? to + add : to;
-                            }
-                            vg[k] = rinv * (vg[k] * w[k] - xn * mean);
-                        }
+                        norm_gradient(vx, vg, w, rinv, mean, acc, DW == DW_HEAD && h < A.H);
                     }
                     rg[s] = encode<T>(vg);
                 }
@@ -357,25 +370,116 @@ template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256,
         }
     }
 
-    if ((DW == DW_HEAD || DW == DW_TOKEN) && weight) {          // the same for the whole block
-        if (DW == DW_HEAD)
+    if (DW == DW_HEAD && weight) {              // the same for the whole block
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                for (int o = LPH; o < 64; o <<= 1) acc[0][k] += __shfl_xor(acc[0][k], o);
+        for (int k = 0; k < 8; ++k)
+            for (int o = LPH; o < 64; o <<= 1) acc[k] += __shfl_xor(acc[k], o);
         for (int turn_of = 0; turn_of < 4; ++turn_of) {
-            if (wave == turn_of) {
-                if (DW == DW_HEAD) {
-                    if (hl == 0) add_to<D, ADJ>(s_dw, c, acc[0], wave == 0);
-                } else {
-#pragma unroll
-                    for (int s = 0; s < ACC; ++s)
-                        if (s * HPS + hl < A.H) add_to<D, ADJ>(s_dw + (s * HPS + hl) * D, c, acc[s], wave == 0);
-                }
-            }
+            if (wave == turn_of && hl == 0) add_to<D, ADJ>(s_dw, c, acc, wave == 0);
             __syncthreads();
         }
         float *out = A.partial + ((size_t)t * A.P + blockIdx.x) * A.cols;
-        for (int i = threadIdx.x; i < A.cols; i += 256) out[i] = s_dw[i];
+        for (int i = threadIdx.x; i < D; i += 256) out[i] = s_dw[i];
+    }
+}
+
+// DW_ROW: grid (P, tensors), block G = 64 or 256: workgroups stride over the tokens, S steps of 8 G values hold one.  The angles of a
+// token are formed by its first d/2 threads, one each, and go round through LDS.  Two copies of what goes through LDS, used in turn:
+// a copy is written again only behind a barrier that every thread reaches after it has read it.
+template <typename T, int D, bool ADJ, int G, int S> __global__ __launch_bounds__(G) void rope_bwd_row_kernel(const RopeArgs A)
+{
+    constexpr int LPH = D / 8, HPS = G / LPH, WAVES = G / 64;
+    __shared__ __attribute__((aligned(16))) float s_cs[2][D / 2], s_sn[2][D / 2];
+    __shared__ float s_sum[2][WAVES][2];
+    const int tid = threadIdx.x, wave = tid >> 6, t = blockIdx.y, hl = tid / LPH, c = tid % LPH, tokens = A.B * A.N;
+    const float *weight = A.weight[t];
+    const bool rotate = (A.rotate >> t) & 1;
+    float acc[S][8], w[S][8];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[s][k] = w[s][k] = 0.f;
+        if (weight && s * HPS + hl < A.H) load_weight<D, ADJ>(weight + (s * HPS + hl) * D, c, w[s]);
+    }
+    int copy = 0;
+    for (int token = blockIdx.x; token < tokens; token += gridDim.x, copy ^= 1) {
+        const int b = token / A.N, n = token - b * A.N;
+        const T *x = static_cast<const T *>(A.src[t]) + b * A.ss[0] + n * A.ss[1];
+        const T *g = static_cast<const T *>(A.grad[t]) + b * A.gs[0] + n * A.gs[1];
+        T *dx = static_cast<T *>(A.dst[t]) + b * A.ds[0] + n * A.ds[1];
+        Raw<T> rg[S], rx[S];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int h = s * HPS + hl;
+            if (h >= A.H) continue;
+            rg[s] = load_pairs<T, D, ADJ>(g + h * A.gs[2], c);
+            if (weight) rx[s] = load_pairs<T, D, ADJ>(x + h * A.ss[2], c);
+        }
+        float cs[4], sn[4], rinv = 1.f, mean = 0.f;
+        if (rotate) {
+            if (tid < D / 2) angle(A, position(A, b, n), tid, s_cs[copy][tid], s_sn[copy][tid]);
+            __syncthreads();
+            const float4 u = *reinterpret_cast<const float4 *>(&s_cs[copy][4 * c]), v = *reinterpret_cast<const float4 *>(&s_sn[copy][4 * c]);
+            cs[0] = u.x; cs[1] = u.y; cs[2] = u.z; cs[3] = u.w;
+            sn[0] = v.x; sn[1] = v.y; sn[2] = v.z; sn[3] = v.w;
+        }
+        if (weight) {
+            float xx = 0.f, gx = 0.f;
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                if (s * HPS + hl >= A.H) continue;
+                float vx[8], vg[8];
+                decode(rx[s], vx);
+                decode(rg[s], vg);
+                if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+                add_sums(vx, vg, w[s], xx, gx);
+            }
+            xx = group_sum(xx, 64);
+            gx = group_sum(gx, 64);
+            if (WAVES > 1) {
+                if ((tid & 63) == 0) {
+                    s_sum[copy][wave][0] = xx;
+                    s_sum[copy][wave][1] = gx;
+                }
+                __syncthreads();
+                xx = gx = 0.f;
+#pragma unroll
+                for (int k = 0; k < WAVES; ++k) {
+                    xx += s_sum[copy][k][0];
+                    gx += s_sum[copy][k][1];
+                }
+            }
+            const float count = (float)A.H * D;
+            rinv = 1.f / sqrtf(xx / count + A.eps);
+            mean = gx * rinv / count;
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int h = s * HPS + hl;
+            if (h >= A.H) continue;
+            if (weight || rotate) {
+                float vg[8];
+                decode(rg[s], vg);
+                if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+                if (weight) {
+                    float vx[8];
+                    decode(rx[s], vx);
+                    norm_gradient(vx, vg, w[s], rinv, mean, acc[s], true);
+                }
+                rg[s] = encode<T>(vg);
+            }
+            store_pairs<T, D, ADJ>(dx + h * A.ds[2], c, rg[s]);
+        }
+    }
+    if (weight) {
+        float *out = A.partial + ((size_t)t * A.P + blockIdx.x) * A.cols;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const int h = s * HPS + hl;
+            if (h >= A.H) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) out[h * D + column<D, ADJ>(c, k)] = acc[s][k];
+        }
     }
 }
 
@@ -414,18 +518,24 @@ template <typename T, int D, bool ADJ> __global__ __launch_bounds__(256) void ro
         if ((size_t)blockIdx.x * 512 + i < (size_t)A.cols) out[i] = s_dw[i];
 }
 
-// grid (ceil(cols / 64), tensors), block 256: dw = sum of the P partial sums, 64 bits
-__global__ __launch_bounds__(256) void rope_dw_kernel(const RopeArgs A)
+// grid (ceil(cols / 64), tensors), block 1024: dw = sum of the P partial sums, 64 bits; 16 wavefronts take every 16th
+__global__ __launch_bounds__(1024) void rope_dw_kernel(const RopeArgs A)
 {
-    __shared__ double s[4][64];
+    __shared__ double s[16][64];
     const int t = blockIdx.y, j = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + j;
     if (!A.weight[t]) return;
     double sum = 0.0;
-    if (i < A.cols)
-        for (int p = wave; p < A.P; p += 4) sum += A.partial[((size_t)t * A.P + p) * A.cols + i];
+    if (i < A.cols) {
+        const float *p = A.partial + ((size_t)t * A.P + wave) * A.cols + i;
+#pragma unroll 8
+        for (int k = wave; k < A.P; k += 16, p += 16 * (size_t)A.cols) sum += *p;
+    }
     s[wave][j] = sum;
     __syncthreads();
-    if (wave == 0 && i < A.cols) A.dw[t][i] = (float)((s[0][j] + s[1][j]) + (s[2][j] + s[3][j]));
+    if (wave == 0 && i < A.cols) {
+        for (int k = 1; k < 16; ++k) sum += s[k][j];
+        A.dw[t][i] = (float)sum;
+    }
 }
 
 // ---- launchers -------------------------------------------------------------
@@ -486,16 +596,17 @@ struct RopeBwdPlan {
 static RopeBwdPlan bwd_plan(const svg2_rope_args *a)
 {
     RopeBwdPlan p = {};
-    const int tokens = a->B * a->N, steps = cdiv(a->H, 64 / (a->d / 8));
+    const int tokens = a->B * a->N;
     bool normed = false;
     for (int t = 0; t < a->n_tensors; ++t) normed |= a->norm_weight[t] != nullptr;
     if (!normed) p.dw = DW_NONE;
     else if (a->norm_scope == SVG2_NORM_HEAD) p.dw = DW_HEAD;
-    else p.dw = steps <= (a->dtype == SVG2_BF16 ? bwd_steps<bf16_t>() : bwd_steps<float>()) ? DW_TOKEN : DW_LONG;
+    else p.dw = a->H * a->d <= ROW_STEPS * 2048 ? DW_ROW : DW_LONG;
     p.cols = p.dw == DW_HEAD ? a->d : a->H * a->d;
-    p.blocks = cdiv(tokens, 4);
-    if (p.dw == DW_HEAD || p.dw == DW_TOKEN) {          // one partial sum per block: two blocks per CU
-        if (p.blocks > 512) p.blocks = 512;
+    p.blocks = p.dw == DW_ROW ? tokens : cdiv(tokens, 4);
+    if (p.dw == DW_HEAD || p.dw == DW_ROW) {            // one partial sum per block: two blocks of 256 per CU and tensor
+        const int most = p.dw == DW_ROW && p.cols <= ROW_STEPS * 512 ? 2048 : 512;
+        if (p.blocks > most) p.blocks = most;
         p.P = p.blocks;
     } else if (p.dw == DW_LONG) {                       // 64 slices of the tokens, fewer where a partial sum is long
         const int most = 1 + (1 << 23) / p.cols;
@@ -534,16 +645,21 @@ int rope_bwd_launch(const svg2_rope_args *a, const void *const *dY, void *const 
         constexpr bool ADJ = decltype(adj)::value;
         const dim3 grid(p.blocks, a->n_tensors);
         if (p.dw == DW_NONE) rope_bwd_kernel<T, D, ADJ, DW_NONE><<<grid, 256, 0, st>>>(A);
-        else if (p.dw == DW_HEAD) rope_bwd_kernel<T, D, ADJ, DW_HEAD><<<grid, 256, D * sizeof(float), st>>>(A);
-        else if (p.dw == DW_TOKEN) rope_bwd_kernel<T, D, ADJ, DW_TOKEN><<<grid, 256, (size_t)p.cols * sizeof(float), st>>>(A);
-        else rope_bwd_kernel<T, D, ADJ, DW_LONG><<<grid, 256, 0, st>>>(A);
+        else if (p.dw == DW_HEAD) rope_bwd_kernel<T, D, ADJ, DW_HEAD><<<grid, 256, 0, st>>>(A);
+        else if (p.dw == DW_LONG) rope_bwd_kernel<T, D, ADJ, DW_LONG><<<grid, 256, 0, st>>>(A);
+        else if (p.cols <= 512) rope_bwd_row_kernel<T, D, ADJ, 64, 1><<<grid, 64, 0, st>>>(A);
+        else if (p.cols <= 1024) rope_bwd_row_kernel<T, D, ADJ, 64, 2><<<grid, 64, 0, st>>>(A);
+        else if (p.cols <= 2048) rope_bwd_row_kernel<T, D, ADJ, 64, 4><<<grid, 64, 0, st>>>(A);
+        else if (p.cols <= 4096) rope_bwd_row_kernel<T, D, ADJ, 256, 2><<<grid, 256, 0, st>>>(A);
+        else if (p.cols <= 6144) rope_bwd_row_kernel<T, D, ADJ, 256, 3><<<grid, 256, 0, st>>>(A);
+        else rope_bwd_row_kernel<T, D, ADJ, 256, 4><<<grid, 256, 0, st>>>(A);
         SVG2_HIP_CHECK(hipGetLastError());
         if (p.dw == DW_LONG) {
             rope_dw_long_kernel<T, D, ADJ><<<dim3(cdiv(p.cols, 512), p.P, a->n_tensors), 256, 0, st>>>(A);
             SVG2_HIP_CHECK(hipGetLastError());
         }
         if (p.dw != DW_NONE) {
-            rope_dw_kernel<<<dim3(cdiv(p.cols, 64), a->n_tensors), 256, 0, st>>>(A);
+            rope_dw_kernel<<<dim3(cdiv(p.cols, 64), a->n_tensors), 1024, 0, st>>>(A);
             SVG2_HIP_CHECK(hipGetLastError());
         }
         return SVG2_OK;

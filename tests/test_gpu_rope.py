@@ -139,15 +139,19 @@ def test_rope_position_zero_zero_rows_and_special_values(svg2):
 BACKWARD = [
     (torch.float32, 1, 1, 1, 64, "token", "adjacent"),
     (torch.float32, 2, 19, 7, 64, "head", "halves"),
-    (torch.float32, 1, 13, 20, 128, "token", "halves"),         # the longest fp32 token that is read once
-    (torch.float32, 1, 14, 21, 128, "token", "adjacent"),       # one head more: read twice
+    (torch.float32, 1, 13, 16, 128, "token", "halves"),         # the longest token that a wavefront holds
+    (torch.float32, 1, 14, 17, 128, "token", "adjacent"),       # one head more: a workgroup holds it
+    (torch.bfloat16, 1, 21, 128, 64, "token", "halves"),        # the longest that a workgroup holds, and the next
+    (torch.float32, 2, 11, 64, 128, "token", "adjacent"),
+    (torch.float32, 1, 10, 65, 128, "token", "halves"),
+    (torch.bfloat16, 1, 1031, 40, 128, "token", "adjacent"),    # more tokens than workgroups
     (torch.bfloat16, 1, 9, 40, 128, "token", "adjacent"),
     (torch.bfloat16, 1, 10, 41, 128, "token", "halves"),
     (torch.bfloat16, 3, 31, 5, 128, "head", "adjacent"),
     (torch.bfloat16, 1, 17, 12, 64, "none", "halves"),
     (torch.bfloat16, 1, 2309, 3, 64, "token", "adjacent"),      # more groups of tokens than workgroups
     (torch.float32, 1, 2111, 2, 64, "head", "adjacent"),
-    (torch.float32, 1, 301, 45, 64, "token", "adjacent"),       # long tokens, more groups of them than slices
+    (torch.float32, 1, 301, 131, 64, "token", "adjacent"),      # long tokens, more groups of them than slices
 ]
 
 
