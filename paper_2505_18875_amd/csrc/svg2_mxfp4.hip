@@ -243,60 +243,72 @@ __device__ __forceinline__ i32x8 fragment(const uint4 &u) { return i32x8{(int)u.
 // The tiled product.  v_mfma_scale_f32_32x32x64_f8f6f4 on E2M1 operands: lane l gives 32 values of row l % 32 (16 bytes), columns
 // 32 (l / 32) .., and their scale.  The rows of B go in first: a lane's results are then neighbours in a row of C.
 //
-// Workgroup: 2 x 2 wavefronts of 32 WT x 32 WT results.  A stage is 128 columns of the 64 WT rows of either side with their
-// scales; four stages are in LDS, three of them on their way while one is used, straight from memory (global_load_lds).  Within a
-// stage the two halves of 64 columns alternate between two register sets: the next half is read from LDS while the matrix
-// instructions of this one run.  The one barrier of a stage stands in its middle.
+// Workgroup: 2 x 2 wavefronts of 32 WT x 32 WT results, one tile of C after another.  A stage is 128 columns of the 64 WT rows of
+// either side with their scales; NB stages are in LDS, all but one of them on their way while one is used, straight from memory
+// (global_load_lds).  Within a stage the two halves of 64 columns alternate between two register sets: the next half is read from
+// LDS while the matrix instructions of this one run.  The one barrier of a stage stands in its middle.
 // WT = 4, one wavefront a SIMD: 32 instructions of 32 cycles a stage, in which LDS gives 64 KB to the registers (512 cycles) and
 // takes 34 KB (272).
 // In LDS row r has 64 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.
 // Rows behind the last are read as the last and not stored.
-constexpr int PR_STAGES = 4;
-template <int WT> constexpr int pr_stage_bytes() { return 2 * 64 * WT * 64 + 2 * 64 * WT * 4; }
+template <int WT> struct Tile {
+    static constexpr int BT = 64 * WT, SIDE = BT * 64, STAGE = 2 * SIDE + 2 * BT * 4;
+    static constexpr int NB = WT == 4 ? 4 : 3;                              // stages in LDS
+    static constexpr int NS = WT < 2 ? 1 : WT / 2, LOADS = 2 * WT + NS;     // loads of a wavefront and stage: scales, all
+    // results on their way out: 32 rows of 128 bytes (WT = 1, bf16: 64) for each wavefront
+    template <typename T> static constexpr int out_cols() { return 32 * WT * (int)sizeof(T) < 128 ? 32 * WT : 128 / (int)sizeof(T); }
+    template <typename T> static constexpr int out_row() { return out_cols<T>() * (int)sizeof(T) + 16; }
+    static constexpr int BIAS = NB * STAGE, OUT = BIAS + 2 * BT * 4;
+    template <typename T> static constexpr int lds() { return OUT + 4 * 32 * out_row<T>(); }
+};
 
 __device__ __forceinline__ int spread(int r) { return ((r >> 1) & 3) ^ ((r >> 3) & 1); }
 
 template <int WT, typename T> __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void mxfp4_product_kernel(const ProductArgs P, bool vec)
 {
-    constexpr int BT = 64 * WT, SIDE = BT * 64, STAGE = pr_stage_bytes<WT>();
-    constexpr int NS = WT < 2 ? 1 : WT / 2, LOADS = 2 * WT + NS;    // loads of a wavefront and stage: scales, all
+    using L = Tile<WT>;
+    constexpr int BT = L::BT, SIDE = L::SIDE, STAGE = L::STAGE, NB = L::NB, NS = L::NS, LOADS = L::LOADS, MULS = WT * WT;
     extern __shared__ __attribute__((aligned(256))) unsigned char s_tile[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 31, half = lane >> 5;
-
-    // which tile: the XCDs (every eighth workgroup) get contiguous parts of an order that goes down 8 tiles of C, then right, so
-    // that what an XCD works on at a time is a compact patch and shares its rows in that XCD's L2
-    int tm, tn;
-    {
-        const int tiles_m = (P.M + BT - 1) / BT, total = tiles_m * P.tiles_n;
-        const int xcd = blockIdx.x & 7, part = total >> 3, rest = total & 7;
-        const int t = xcd * part + min(xcd, rest) + (blockIdx.x >> 3);
-        const int group = t / (8 * P.tiles_n), in = t - group * 8 * P.tiles_n, high = min(8, tiles_m - group * 8);
-        tm = group * 8 + in % high;
-        tn = in / high;
-    }
-    const int m0 = tm * BT, n0 = tn * BT;
     const long long row_bytes = (long long)P.nk * 64;
-    const char *ga = reinterpret_cast<const char *>(P.A) + m0 * row_bytes, *gb = reinterpret_cast<const char *>(P.B) + n0 * row_bytes;
-    const char *gsa = reinterpret_cast<const char *>(P.SA) + m0 * 4LL, *gsb = reinterpret_cast<const char *>(P.SB) + n0 * 4LL;
+    const int nk = P.nk;
 
-    // this lane's part of the loads: 16 rows x 64 bytes each
-    unsigned off_a[WT], off_b[WT], off_s[NS];
+    // Which tiles: the XCDs (every eighth workgroup) get contiguous parts of an order that goes down 8 tiles of C, then right, and
+    // their workgroups take turns, so that what an XCD works on at a time is a compact patch and shares its rows in that XCD's L2.
+    const int tiles_m = (P.M + BT - 1) / BT, total = tiles_m * P.tiles_n;
+    const int xcd = blockIdx.x & 7, part = total >> 3, rest = total & 7, first = xcd * part + min(xcd, rest);
+    const int mine = part + (xcd < rest), slots = (gridDim.x + 7 - xcd) >> 3;
+
+    int m0, n0;
+    const char *ga, *gb, *gsa, *gsb;
+    unsigned off_a[WT], off_b[WT], off_s[NS];           // this lane's part of the loads: 16 rows x 64 bytes each
+    auto set_tile = [&](int k) {
+        const int t = first + k, group = t / (8 * P.tiles_n), in = t - group * 8 * P.tiles_n, high = min(8, tiles_m - group * 8);
+        m0 = (group * 8 + in % high) * BT;
+        n0 = (in / high) * BT;
+        ga = reinterpret_cast<const char *>(P.A) + m0 * row_bytes;
+        gb = reinterpret_cast<const char *>(P.B) + n0 * row_bytes;
+        gsa = reinterpret_cast<const char *>(P.SA) + m0 * 4LL;
+        gsb = reinterpret_cast<const char *>(P.SB) + n0 * 4LL;
+        int l = lane;
+        asm("" : "+v"(l));
 #pragma unroll
-    for (int i = 0; i < WT; ++i) {
-        const int r = (wave * WT + i) * 16 + (lane >> 2), piece = (lane & 3) ^ spread(r);
-        off_a[i] = (unsigned)min(r, P.M - 1 - m0) * (unsigned)row_bytes + piece * 16;
-        off_b[i] = (unsigned)min(r, P.N - 1 - n0) * (unsigned)row_bytes + piece * 16;
-    }
-    // scales: 2 BT words, A's then B's, 64 a load (WT = 1: two wavefronts load the same)
+        for (int i = 0; i < WT; ++i) {
+            const int r = (wave * WT + i) * 16 + (l >> 2), piece = (l & 3) ^ spread(r);
+            off_a[i] = (unsigned)min(r, P.M - 1 - m0) * (unsigned)row_bytes + piece * 16;
+            off_b[i] = (unsigned)min(r, P.N - 1 - n0) * (unsigned)row_bytes + piece * 16;
+        }
+        // scales: 2 BT words, A's then B's, 64 a load (WT = 1: two wavefronts load the same)
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        const int at = (wave * NS + i) * 64 % (2 * BT), r = at % BT + lane;
-        off_s[i] = 4u * (unsigned)(at < BT ? min(r, P.M - 1 - m0) : min(r, P.N - 1 - n0));
-    }
+        for (int i = 0; i < NS; ++i) {
+            const int at = (wave * NS + i) * 64 % (2 * BT), r = at % BT + l;
+            off_s[i] = 4u * (unsigned)(at < BT ? min(r, P.M - 1 - m0) : min(r, P.N - 1 - n0));
+        }
+    };
     // piece g of a stage's loads: WT of A, WT of B, NS of scales
     auto load_piece = [&](int kc, int g) {
-        unsigned char *to = s_tile + (kc % PR_STAGES) * STAGE;
+        unsigned char *to = s_tile + (kc % NB) * STAGE;
         if (g < WT) {
             load_to_lds_16(ga + kc * 64LL, off_a[g], to + (wave * WT + g) * 1024);
         } else if (g < 2 * WT) {
@@ -306,25 +318,25 @@ template <int WT, typename T> __global__ __launch_bounds__(256, WT == 4 ? 1 : 2)
             load_to_lds_4(at < BT ? gsa + kc * 4LL * P.M : gsb + kc * 4LL * P.N, off_s[g - 2 * WT], to + 2 * SIDE + at * 4);
         }
     };
-    auto load_stage = [&](int kc) {
+    // what a tile's first NB - 1 stages need, its bias in front (WT < 4: some wavefronts load the same part)
+    auto load_first = [&](int copy) {
+        if (P.bias)
+            load_to_lds_4(reinterpret_cast<const char *>(P.bias + n0), 4u * (unsigned)min(wave * 64 % BT + lane, P.N - 1 - n0),
+                          s_tile + L::BIAS + copy * BT * 4 + wave * 64 % BT * 4);
 #pragma unroll
-        for (int g = 0; g < LOADS; ++g) load_piece(kc, g);
+        for (int kc = 0; kc < NB - 1; ++kc)
+            if (kc < nk)
+#pragma unroll
+                for (int g = 0; g < LOADS; ++g) load_piece(kc, g);
     };
 
     f32x16 acc[WT][WT];
-#pragma unroll
-    for (int i = 0; i < WT; ++i)
-#pragma unroll
-        for (int j = 0; j < WT; ++j)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
-
     const int ra = (wave >> 1) * 32 * WT, rb = (wave & 1) * 32 * WT;
     const int at = row * 64 + ((half ^ spread(row)) << 4);          // first half of a stage; the second: piece ^ 2
     struct Set { uint4 a[WT], b[WT]; };
     // fragment g of a half: b 0, a 0, b 1 .., a 1 ..: in the order in which the products need them
     auto read_piece = [&](int kc, int k, int g, Set &f) {
-        const unsigned char *s = s_tile + (kc % PR_STAGES) * STAGE + (at ^ (k * 32));
+        const unsigned char *s = s_tile + (kc % NB) * STAGE + (at ^ (k * 32));
         const bool is_a = g == 1 || g > WT;
         const int i = g < 2 ? 0 : g <= WT ? g - 1 : g - WT;
         if (is_a) f.a[i] = *reinterpret_cast<const uint4 *>(s + (ra + 32 * i) * 64);
@@ -332,7 +344,7 @@ template <int WT, typename T> __global__ __launch_bounds__(256, WT == 4 ? 1 : 2)
     };
     struct Scales { unsigned a[WT], b[WT]; };
     auto read_scales = [&](int kc, Scales &x) {
-        const unsigned *s = reinterpret_cast<const unsigned *>(s_tile + (kc % PR_STAGES) * STAGE + 2 * SIDE);
+        const unsigned *s = reinterpret_cast<const unsigned *>(s_tile + (kc % NB) * STAGE + 2 * SIDE);
 #pragma unroll
         for (int i = 0; i < WT; ++i) {
             x.b[i] = s[BT + rb + 32 * i + row];
@@ -353,109 +365,139 @@ template <int WT, typename T> __global__ __launch_bounds__(256, WT == 4 ? 1 : 2)
                                                                     (int)x.b[j], SEL, (int)x.a[i]);
     };
 
+    // Loads and stores come back in the order in which they were issued.  The last tile's stores lie between the loads of this
+    // tile's first NB - 1 stages and all later ones, and the first waits of a tile let them pass (`after`: that many were issued).
+    constexpr int STORES = WT * WT * 32 * 32 * (int)sizeof(T) / 1024;
+    bool after = false;
+    auto wait_but = [&](auto loads, bool stores) {
+        constexpr int N = decltype(loads)::value;
+        if (stores) wait_loads<(N + STORES < 63 ? N + STORES : 63)>();
+        else wait_loads<N>();
+    };
+
     Set f0, f1;
     Scales x, next;
-    // One stage.  NEXT: there is a stage behind it; LOAD: and one three behind it; PENDING: loads that may still be on their way when
-    // stage kc + 1 is needed.  The groups (two fragments' worth of LDS reads or loads, then matrix instructions) keep the written
-    // order: left to itself the compiler puts all reads in front and the matrix cores wait for them.
+    // One stage.  NEXT: there is a stage behind it; LOAD: and one NB - 1 behind it; PENDING: loads that may still be on their way when
+    // stage kc + 1 is needed.  Between the fences the written order is kept, LDS reads and loads spread over the matrix instructions:
+    // left to itself the compiler puts all reads in front and the matrix cores wait for them.
     auto step = [&](int kc, auto load, auto has_next, auto pending) {
         constexpr bool LOAD = decltype(load)::value, NEXT = decltype(has_next)::value;
-        constexpr int GROUPS = 2 * WT, EACH = (LOADS + GROUPS - 1) / GROUPS;
+        constexpr int READS = 2 * WT, LOADS_FROM = MULS > LOADS ? MULS - LOADS : 0;
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            read_piece(kc, 1, g, f1);
-#pragma unroll
-            for (int e = g * WT * WT / GROUPS; e < (g + 1) * WT * WT / GROUPS; ++e) multiply(f0, x, e, std::false_type());
+        for (int e = 0; e < (MULS > READS ? MULS : READS); ++e) {
+            if (e < READS) read_piece(kc, 1, e, f1);
+            if (e < MULS) multiply(f0, x, e, std::false_type());
             __builtin_amdgcn_sched_barrier(0);
         }
         if (NEXT) {
             // stage kc + 1 has arrived for every wavefront; every wavefront is done with stage kc - 1, whose place is free
-            wait_loads<decltype(pending)::value>();
+            wait_but(pending, after && kc < NB - 2);
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             read_scales(kc + 1, next);
         }
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            if (LOAD)
+        for (int e = 0; e < (MULS > READS ? MULS : READS); ++e) {
+            if (NEXT && e < READS) read_piece(kc + 1, 0, e, f0);
+            if (LOAD) {
+                if (MULS > LOADS) {
+                    if (e >= LOADS_FROM) load_piece(kc + NB - 1, e - LOADS_FROM);
+                } else {
 #pragma unroll
-                for (int e = g * EACH; e < (g + 1) * EACH && e < LOADS; ++e) load_piece(kc + 3, e);
-            if (NEXT) read_piece(kc + 1, 0, g, f0);
-#pragma unroll
-            for (int e = g * WT * WT / GROUPS; e < (g + 1) * WT * WT / GROUPS; ++e) multiply(f1, x, e, std::true_type());
-            if (NEXT && g == GROUPS - 1) take_scales(next, x);
+                    for (int g = 0; g < LOADS; ++g)
+                        if (g * READS / LOADS == e) load_piece(kc + NB - 1, g);
+                }
+            }
+            if (e < MULS) multiply(f1, x, e, std::true_type());
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (NEXT) take_scales(next, x);
     };
     using Yes = std::true_type;
     using No = std::false_type;
-    using Most = std::integral_constant<int, LOADS>;
+    using Most = std::integral_constant<int, (NB - 3) * LOADS>;
     using None = std::integral_constant<int, 0>;
 
-    const int nk = P.nk;
-    load_stage(0);
-    if (nk > 1) load_stage(1);
-    if (nk > 2) load_stage(2);
-    if (nk > 2) wait_loads<2 * LOADS>();
-    else if (nk > 1) wait_loads<LOADS>();
-    else wait_loads<0>();
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    read_scales(0, next);
+    int k = blockIdx.x >> 3, copy = 0;
+    if (k >= mine) return;
+    set_tile(k);
+    load_first(copy);
+    for (; k < mine; k += slots, copy ^= 1) {
 #pragma unroll
-    for (int g = 0; g < 2 * WT; ++g) read_piece(0, 0, g, f0);
-    take_scales(next, x);
-    for (int kc = 0; kc + 3 < nk; ++kc) step(kc, Yes(), Yes(), Most());
-    if (nk >= 3) step(nk - 3, No(), Yes(), Most());
-    if (nk >= 2) step(nk - 2, No(), Yes(), None());
-    step(nk - 1, No(), No(), None());
-    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");     // the last results are read by vector instructions from here on
+        for (int i = 0; i < WT; ++i)
+#pragma unroll
+            for (int j = 0; j < WT; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        if (nk >= NB - 1) wait_but(std::integral_constant<int, (NB - 2) * LOADS>(), after);
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read_scales(0, next);
+#pragma unroll
+        for (int g = 0; g < 2 * WT; ++g) read_piece(0, 0, g, f0);
+        take_scales(next, x);
+        int kc = 0;
+        for (; kc + NB - 1 < nk; ++kc) step(kc, Yes(), Yes(), Most());
+        if (NB > 3 && kc + 2 < nk) step(kc++, No(), Yes(), Most());
+        for (; kc + 1 < nk; ++kc) step(kc, No(), Yes(), None());
+        step(kc, No(), No(), None());
+        __builtin_amdgcn_s_barrier();                               // every wavefront has read its last stage
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");         // the last results are read by vector instructions from here on
 
-    // Results: lane holds row m0 + ra + 32 i + l % 32 of C, columns n0 + rb + 32 j + 8 q + 4 (l / 32) .. + 3 in registers 4 q ..
-    // 4 q + 3.  Stored from there, an instruction would write 32 pieces of 16 bytes; 32 rows at a time go through LDS instead (a part
-    // of its own for each wavefront, where the stages were) and out in whole rows of the wavefront's columns.
-    constexpr int COLS = 32 * WT, ROW = COLS * (int)sizeof(T) + 16, PER16 = 16 / (int)sizeof(T);
-    static_assert(4 * 32 * ROW <= PR_STAGES * STAGE, "the stages' place holds 32 rows of every wavefront");
-    __builtin_amdgcn_s_barrier();                                  // every wavefront has read its last stage
-    asm volatile("" ::: "memory");
-    unsigned char *s = s_tile + wave * 32 * ROW;
-    const int n_first = n0 + rb, n_left = P.N - n_first;
-#pragma unroll
-    for (int i = 0; i < WT; ++i) {
-#pragma unroll
-        for (int j = 0; j < WT; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = 32 * j + 8 * q + 4 * half;
-                float v[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r] + (P.bias ? P.bias[min(n_first + n + r, P.N - 1)] : 0.f);
-                unsigned char *to = s + row * ROW + n * (int)sizeof(T);
-                if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
-                else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-            }
-        const int m_first = m0 + ra + 32 * i;
-        if (vec) {
-            constexpr int LANES = COLS / PER16, AT_ONCE = 64 / LANES;       // lanes a row, rows an instruction
-            const int c = lane % LANES, first = c * PER16;
-#pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
-                const int r = r0 + lane / LANES;
-                const unsigned char *from = s + r * ROW + c * 16;
-                T *to = static_cast<T *>(P.C) + (long long)(m_first + r) * P.ldc + n_first + first;
-                if (m_first + r < P.M) {
-                    if (first + PER16 <= n_left) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
-                    else
-                        for (int e = 0; e < PER16 && first + e < n_left; ++e) to[e] = reinterpret_cast<const T *>(from)[e];
-                }
-            }
-        } else {
-            for (int e = lane; e < 32 * COLS; e += 64) {
-                const int r = e / COLS, c = e % COLS;
-                if (m_first + r < P.M && c < n_left)
-                    static_cast<T *>(P.C)[(long long)(m_first + r) * P.ldc + n_first + c] = reinterpret_cast<const T *>(s + r * ROW)[c];
-            }
+        const int m_first = m0 + ra, n_first = n0 + rb, n_left = P.N - n_first;
+        const bool full = vec && m0 + BT <= P.M && n0 + BT <= P.N;
+        if (k + slots < mine) {                                     // the next tile's first stages come while this one goes out
+            set_tile(k + slots);
+            load_first(copy ^ 1);
         }
+        after = full;
+
+        // Results: lane holds row m_first + 32 i + l % 32 of C, columns n_first + 32 j + 8 q + 4 (l / 32) .. + 3 in registers 4 q ..
+        // 4 q + 3.  Stored from there, an instruction would write 32 pieces of 16 bytes; 32 rows of 128 bytes at a time go through LDS
+        // instead (a part of its own for each wavefront).
+        constexpr int COLS = L::template out_cols<T>(), ROW = L::template out_row<T>(), PER16 = 16 / (int)sizeof(T), JS = COLS / 32;
+        int l = lane;
+        asm("" : "+v"(l));         // addresses below are formed here, not kept in registers through the loop over the stages
+        unsigned char *s = s_tile + L::OUT + wave * 32 * ROW;
+        const float *bias = reinterpret_cast<const float *>(s_tile + L::BIAS) + copy * BT + rb;
+#pragma unroll
+        for (int i = 0; i < WT; ++i)
+#pragma unroll
+            for (int j0 = 0; j0 < WT; j0 += JS) {
+#pragma unroll
+                for (int j = j0; j < j0 + JS; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int n = 32 * j + 8 * q + 4 * (l >> 5);
+                        float v[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
+                        if (P.bias) {
+                            const float4 add = *reinterpret_cast<const float4 *>(bias + n);
+                            v[0] += add.x; v[1] += add.y; v[2] += add.z; v[3] += add.w;
+                        }
+                        unsigned char *to = s + (l & 31) * ROW + (n - 32 * j0) * (int)sizeof(T);
+                        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+                        else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                    }
+                constexpr int LANES = COLS / PER16, AT_ONCE = 64 / LANES;       // lanes a row, rows an instruction
+                T *C = static_cast<T *>(P.C) + (long long)(m_first + 32 * i) * P.ldc + n_first + 32 * j0;
+                const int rows = P.M - m_first - 32 * i, cols = n_left - 32 * j0;
+                if (full) {
+#pragma unroll
+                    for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
+                        const int r = r0 + l / LANES, c = l % LANES;
+                        *reinterpret_cast<uint4 *>(C + (long long)r * P.ldc + c * PER16) = *reinterpret_cast<const uint4 *>(s + r * ROW + c * 16);
+                    }
+                } else {
+                    for (int e = l; e < 32 * COLS; e += 64) {
+                        const int r = e / COLS, c = e % COLS;
+                        if (r < rows && c < cols) C[(long long)r * P.ldc + c] = reinterpret_cast<const T *>(s + r * ROW)[c];
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);      // else all results leave the accumulators first, for want of registers to memory
+            }
     }
 }
 
@@ -519,21 +561,26 @@ int mxfp4_values_launch(const void *codes, const void *scales, int M, int K, int
 
 size_t mxfp4_matmul_ws_bytes(int M, int N, int K) { (void)M; (void)N; (void)K; return 256; }
 
+template <int WT> static int prepare_tiles()
+{
+    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<WT, bf16_t>), Tile<WT>::template lds<bf16_t>()));
+    return set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<WT, float>), Tile<WT>::template lds<float>());
+}
+
 int mxfp4_matmul_prepare()
 {
-    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<4, bf16_t>), PR_STAGES * pr_stage_bytes<4>()));
-    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<4, float>), PR_STAGES * pr_stage_bytes<4>()));
-    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<2, bf16_t>), PR_STAGES * pr_stage_bytes<2>()));
-    return set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<2, float>), PR_STAGES * pr_stage_bytes<2>());
+    SVG2_TRY(prepare_tiles<4>());
+    SVG2_TRY(prepare_tiles<2>());
+    return prepare_tiles<1>();
 }
 
 template <int WT> static int product_tiles(ProductArgs P, int out_dtype, bool vec, hipStream_t st)
 {
     P.tiles_n = cdiv(P.N, 64 * WT);
-    const int tiles = cdiv(P.M, 64 * WT) * P.tiles_n;
-    const size_t lds = PR_STAGES * pr_stage_bytes<WT>();
-    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<WT, bf16_t><<<tiles, 256, lds, st>>>(P, vec);
-    else mxfp4_product_kernel<WT, float><<<tiles, 256, lds, st>>>(P, vec);
+    const int tiles = cdiv(P.M, 64 * WT) * P.tiles_n, resident = 256 * (WT == 4 ? 1 : WT == 2 ? 2 : 4);
+    const int grid = tiles < resident ? tiles : resident;
+    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<WT, bf16_t><<<grid, 256, Tile<WT>::template lds<bf16_t>(), st>>>(P, vec);
+    else mxfp4_product_kernel<WT, float><<<grid, 256, Tile<WT>::template lds<float>(), st>>>(P, vec);
     SVG2_HIP_CHECK(hipGetLastError());
     return SVG2_OK;
 }
