@@ -14,6 +14,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(bf16_t x) { return bf16_to_f32(x); }
@@ -228,7 +229,7 @@ struct ProductArgs {
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds_4(const char *base, unsigned byte_off, const unsigned char *dst)
 {
-    const unsigned lds_addr = (unsigned)(size_t)(const lds_u8 *)dst;
+    const unsigned lds_addr = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8 *)dst);
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
                  :
                  : "v"(byte_off), "s"(base), "s"(lds_addr)
@@ -243,211 +244,218 @@ __device__ __forceinline__ i32x8 fragment(const uint4 &u) { return i32x8{(int)u.
 // The tiled product.  v_mfma_scale_f32_32x32x64_f8f6f4 on E2M1 operands: lane l gives 32 values of row l % 32 (16 bytes), columns
 // 32 (l / 32) .., and their scale.  The rows of B go in first: a lane's results are then neighbours in a row of C.
 //
-// Workgroup: 2 x 2 wavefronts of 32 WT x 32 WT results, one tile of C after another.  A stage is 128 columns of the 64 WT rows of
-// either side with their scales; NB stages are in LDS, all but one of them on their way while one is used, straight from memory
-// (global_load_lds).  Within a stage the two halves of 64 columns alternate between two register sets: the next half is read from
-// LDS while the matrix instructions of this one run.  The one barrier of a stage stands in its middle.
-// WT = 4, one wavefront a SIMD: 32 instructions of 32 cycles a stage, in which LDS gives 64 KB to the registers (512 cycles) and
-// takes 34 KB (272).
-// In LDS row r has 64 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.
+// Workgroup: WM x WN wavefronts of 32 WI x 32 WJ results, one tile of C after another.  A stage is 256 columns of the tile's rows of
+// either side with their scales: 128 bytes of a row, a cache line.  Two stages are in LDS, one on its way while the other is used,
+// straight from memory (global_load_lds).  A stage is used in four quarters of 64 columns, which alternate between two register
+// sets: the next quarter is read from LDS while the matrix instructions of this one run.  The one barrier of a stage stands before
+// its last quarter: the next stage has arrived by then, and this one's place is free as soon as its last quarter is in registers.
+// In LDS row r has 128 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.
 // Rows behind the last are read as the last and not stored.
-template <int WT> struct Tile {
-    static constexpr int BT = 64 * WT, SIDE = BT * 64, STAGE = 2 * SIDE + 2 * BT * 4;
-    static constexpr int NB = WT == 4 ? 4 : 3;                              // stages in LDS
-    static constexpr int NS = WT < 2 ? 1 : WT / 2, LOADS = 2 * WT + NS;     // loads of a wavefront and stage: scales, all
-    // results on their way out: 32 rows of 128 bytes (WT = 1, bf16: 64) for each wavefront
-    template <typename T> static constexpr int out_cols() { return 32 * WT * (int)sizeof(T) < 128 ? 32 * WT : 128 / (int)sizeof(T); }
+template <int WM_, int WN_, int WI_, int WJ_> struct Tile {
+    static constexpr int WM = WM_, WN = WN_, WI = WI_, WJ = WJ_, WAVES = WM * WN, BM = 32 * WI * WM, BN = 32 * WJ * WN;
+    static constexpr int SA = (BM + BN) * 128, STAGE = SA + 2 * (BM + BN) * 4;          // rows; two words of scales each
+    static constexpr int LA = BM / 8 / WAVES, LB = BN / 8 / WAVES;                      // loads of a wavefront and stage: 8 rows each
+    static constexpr int NS = 2 * (BM + BN) / 64 < WAVES ? 1 : 2 * (BM + BN) / 64 / WAVES, LOADS = LA + LB + NS;     // scales, all
+    // results on their way out: 32 rows of 128 bytes (less where a wavefront has fewer) for each wavefront, in the stage that is free
+    template <typename T> static constexpr int out_cols() { return 32 * WJ * (int)sizeof(T) < 128 ? 32 * WJ : 128 / (int)sizeof(T); }
     template <typename T> static constexpr int out_row() { return out_cols<T>() * (int)sizeof(T) + 16; }
-    static constexpr int BIAS = NB * STAGE, OUT = BIAS + 2 * BT * 4;
-    template <typename T> static constexpr int lds() { return OUT + 4 * 32 * out_row<T>(); }
+    static constexpr int OUT = WAVES * 32 * (128 + 16), BIAS = 2 * BN * 4;               // the bias of this tile and of the next
+    static constexpr int LDS = BIAS + STAGE + (OUT > STAGE ? OUT : STAGE);
+    static_assert(LA >= 1 && LB >= 1, "");
 };
 
-__device__ __forceinline__ int spread(int r) { return ((r >> 1) & 3) ^ ((r >> 3) & 1); }
+__device__ __forceinline__ int spread(int r) { return ((r >> 1) & 7) ^ ((r & 1) << 2); }
 
-template <int WT, typename T> __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void mxfp4_product_kernel(const ProductArgs P, bool vec)
+template <typename L, typename T> __global__ __launch_bounds__(64 * L::WAVES, L::BM == 256 ? L::WAVES / 4 : 2)
+void mxfp4_product_kernel(const ProductArgs P, bool vec)
 {
-    using L = Tile<WT>;
-    constexpr int BT = L::BT, SIDE = L::SIDE, STAGE = L::STAGE, NB = L::NB, NS = L::NS, LOADS = L::LOADS, MULS = WT * WT;
+    constexpr int WI = L::WI, WJ = L::WJ, BM = L::BM, BN = L::BN, STAGE = L::STAGE, LA = L::LA, LB = L::LB, NS = L::NS;
+    constexpr int LOADS = L::LOADS, MULS = WI * WJ, READS = WI + WJ, SLOTS = MULS > READS ? MULS : READS;
     extern __shared__ __attribute__((aligned(256))) unsigned char s_tile[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 31, half = lane >> 5;
     const long long row_bytes = (long long)P.nk * 64;
-    const int nk = P.nk;
+    const int stages = (P.nk + 1) >> 1;
+    const bool odd = P.nk & 1;                          // the last stage has 128 columns only
 
     // Which tiles: the XCDs (every eighth workgroup) get contiguous parts of an order that goes down 8 tiles of C, then right, and
     // their workgroups take turns, so that what an XCD works on at a time is a compact patch and shares its rows in that XCD's L2.
-    const int tiles_m = (P.M + BT - 1) / BT, total = tiles_m * P.tiles_n;
+    const int tiles_m = (P.M + BM - 1) / BM, total = tiles_m * P.tiles_n;
     const int xcd = blockIdx.x & 7, part = total >> 3, rest = total & 7, first = xcd * part + min(xcd, rest);
     const int mine = part + (xcd < rest), slots = (gridDim.x + 7 - xcd) >> 3;
 
     int m0, n0;
     const char *ga, *gb, *gsa, *gsb;
-    unsigned off_a[WT], off_b[WT], off_s[NS];           // this lane's part of the loads: 16 rows x 64 bytes each
+    unsigned off_a[LA], off_b[LB], off_s[NS];           // this lane's part of the loads: 8 rows x 128 bytes each
     auto set_tile = [&](int k) {
         const int t = first + k, group = t / (8 * P.tiles_n), in = t - group * 8 * P.tiles_n, high = min(8, tiles_m - group * 8);
-        m0 = (group * 8 + in % high) * BT;
-        n0 = (in / high) * BT;
+        m0 = __builtin_amdgcn_readfirstlane((group * 8 + in % high) * BM);
+        n0 = __builtin_amdgcn_readfirstlane((in / high) * BN);
         ga = reinterpret_cast<const char *>(P.A) + m0 * row_bytes;
         gb = reinterpret_cast<const char *>(P.B) + n0 * row_bytes;
         gsa = reinterpret_cast<const char *>(P.SA) + m0 * 4LL;
         gsb = reinterpret_cast<const char *>(P.SB) + n0 * 4LL;
         int l = lane;
-        asm("" : "+v"(l));
+        asm("" : "+v"(l));          // formed here, not kept in registers through the loop over the stages
 #pragma unroll
-        for (int i = 0; i < WT; ++i) {
-            const int r = (wave * WT + i) * 16 + (l >> 2), piece = (l & 3) ^ spread(r);
-            off_a[i] = (unsigned)min(r, P.M - 1 - m0) * (unsigned)row_bytes + piece * 16;
-            off_b[i] = (unsigned)min(r, P.N - 1 - n0) * (unsigned)row_bytes + piece * 16;
+        for (int i = 0; i < LA; ++i) {
+            const int r = (wave * LA + i) * 8 + (l >> 3);
+            off_a[i] = (unsigned)min(r, P.M - 1 - m0) * (unsigned)row_bytes + ((l & 7) ^ spread(r)) * 16;
         }
-        // scales: 2 BT words, A's then B's, 64 a load (WT = 1: two wavefronts load the same)
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            const int r = (wave * LB + i) * 8 + (l >> 3);
+            off_b[i] = (unsigned)min(r, P.N - 1 - n0) * (unsigned)row_bytes + ((l & 7) ^ spread(r)) * 16;
+        }
+        // scales: BM + BN words, A's then B's, twice; 64 a load (small tiles: some wavefronts load the same)
 #pragma unroll
         for (int i = 0; i < NS; ++i) {
-            const int at = (wave * NS + i) * 64 % (2 * BT), r = at % BT + l;
-            off_s[i] = 4u * (unsigned)(at < BT ? min(r, P.M - 1 - m0) : min(r, P.N - 1 - n0));
+            const int at = (wave * NS + i) * 64 % (2 * (BM + BN)) % (BM + BN);
+            off_s[i] = 4u * (unsigned)(at < BM ? min(at + l, P.M - 1 - m0) : min(at - BM + l, P.N - 1 - n0));
         }
     };
-    // piece g of a stage's loads: WT of A, WT of B, NS of scales
-    auto load_piece = [&](int kc, int g) {
-        unsigned char *to = s_tile + (kc % NB) * STAGE;
-        if (g < WT) {
-            load_to_lds_16(ga + kc * 64LL, off_a[g], to + (wave * WT + g) * 1024);
-        } else if (g < 2 * WT) {
-            load_to_lds_16(gb + kc * 64LL, off_b[g - WT], to + SIDE + (wave * WT + g - WT) * 1024);
+    const unsigned upper = (((lane >> 2) ^ (lane >> 3)) & 1) << 6;
+    // piece g of a stage's loads: LA of A, LB of B, NS of scales.  half_row: the stage has only 64 bytes of a row; the lanes of the
+    // other 64 load the first again.
+    auto load_piece = [&](int st, int g, bool half_row) {
+        unsigned char *to = s_tile + L::BIAS + (st & 1) * STAGE;
+        if (g < LA + LB) {
+            const bool is_a = g < LA;
+            const int i = is_a ? g : g - LA;
+            const unsigned off = is_a ? off_a[i] : off_b[i];
+            // bit 2 of the lane's piece, (l & 7) ^ spread(row)
+            const unsigned behind = (upper ^ (((wave * (is_a ? LA : LB) + i) & 1) << 6)) & (half_row ? 64u : 0u);
+            load_to_lds_16((is_a ? ga : gb) + st * 128LL, off - behind,
+                           to + (is_a ? 0 : BM * 128) + (wave * (is_a ? LA : LB) + i) * 1024);
         } else {
-            const int at = (wave * NS + g - 2 * WT) * 64 % (2 * BT);
-            load_to_lds_4(at < BT ? gsa + kc * 4LL * P.M : gsb + kc * 4LL * P.N, off_s[g - 2 * WT], to + 2 * SIDE + at * 4);
+            const int word = (wave * NS + g - LA - LB) * 64 % (2 * (BM + BN)), second = word >= BM + BN, at = word - second * (BM + BN);
+            const long long kc = half_row ? 2 * st : 2 * st + second;
+            load_to_lds_4(at < BM ? gsa + kc * 4 * P.M : gsb + kc * 4 * P.N, off_s[g - LA - LB], to + L::SA + word * 4);
         }
     };
-    // what a tile's first NB - 1 stages need, its bias in front (WT < 4: some wavefronts load the same part)
+    // a tile's first stage, its bias in front (some wavefronts may load the same part)
     auto load_first = [&](int copy) {
         if (P.bias)
-            load_to_lds_4(reinterpret_cast<const char *>(P.bias + n0), 4u * (unsigned)min(wave * 64 % BT + lane, P.N - 1 - n0),
-                          s_tile + L::BIAS + copy * BT * 4 + wave * 64 % BT * 4);
+            load_to_lds_4(reinterpret_cast<const char *>(P.bias + n0), 4u * (unsigned)min(wave * 64 % BN + lane, P.N - 1 - n0),
+                          s_tile + copy * BN * 4 + wave * 64 % BN * 4);
 #pragma unroll
-        for (int kc = 0; kc < NB - 1; ++kc)
-            if (kc < nk)
-#pragma unroll
-                for (int g = 0; g < LOADS; ++g) load_piece(kc, g);
+        for (int g = 0; g < LOADS; ++g) load_piece(0, g, odd && stages == 1);
     };
 
-    f32x16 acc[WT][WT];
-    const int ra = (wave >> 1) * 32 * WT, rb = (wave & 1) * 32 * WT;
-    const int at = row * 64 + ((half ^ spread(row)) << 4);          // first half of a stage; the second: piece ^ 2
-    struct Set { uint4 a[WT], b[WT]; };
-    // fragment g of a half: b 0, a 0, b 1 .., a 1 ..: in the order in which the products need them
-    auto read_piece = [&](int kc, int k, int g, Set &f) {
-        const unsigned char *s = s_tile + (kc % NB) * STAGE + (at ^ (k * 32));
-        const bool is_a = g == 1 || g > WT;
-        const int i = g < 2 ? 0 : g <= WT ? g - 1 : g - WT;
-        if (is_a) f.a[i] = *reinterpret_cast<const uint4 *>(s + (ra + 32 * i) * 64);
-        else f.b[i] = *reinterpret_cast<const uint4 *>(s + SIDE + (rb + 32 * i) * 64);
-    };
-    struct Scales { unsigned a[WT], b[WT]; };
-    auto read_scales = [&](int kc, Scales &x) {
-        const unsigned *s = reinterpret_cast<const unsigned *>(s_tile + (kc % NB) * STAGE + 2 * SIDE);
-#pragma unroll
-        for (int i = 0; i < WT; ++i) {
-            x.b[i] = s[BT + rb + 32 * i + row];
-            x.a[i] = s[ra + 32 * i + row];
+    f32x16 acc[WI][WJ];
+    const int ra = (wave / L::WN) * 32 * WI, rb = (wave % L::WN) * 32 * WJ;
+    const int at = row * 128 + ((half ^ spread(row)) << 4);         // quarter 0; quarter q: piece ^ 2 q
+    struct Set { uint4 a[WI], b[WJ]; };
+    // fragment g of a quarter, in the order in which the products need them: b 0, a 0, b 1 .., a 1 ..
+    auto read_piece = [&](int st, int q, int g, Set &f) {
+        const unsigned char *s = s_tile + L::BIAS + (st & 1) * STAGE + (at ^ (q * 32));
+        if (g == 1 || g > WJ) {
+            const int i = g == 1 ? 0 : g - WJ;
+            f.a[i] = *reinterpret_cast<const uint4 *>(s + (ra + 32 * i) * 128);
+        } else {
+            const int i = g == 0 ? 0 : g - 1;
+            f.b[i] = *reinterpret_cast<const uint4 *>(s + (BM + rb + 32 * i) * 128);
         }
     };
-    auto take_scales = [&](const Scales &x, Scales &y) {            // bytes 0 and 2: this lane's blocks of the two halves
+    struct Scales { unsigned a[WI], b[WJ]; };
+    auto read_scales = [&](int st, int word, Scales &x) {           // word 0: quarters 0 and 1, word 1: 2 and 3
+        const unsigned *s = reinterpret_cast<const unsigned *>(s_tile + L::BIAS + (st & 1) * STAGE + L::SA) + word * (BM + BN) + row;
 #pragma unroll
-        for (int i = 0; i < WT; ++i) {
-            y.a[i] = x.a[i] >> (8 * half);
-            y.b[i] = x.b[i] >> (8 * half);
-        }
+        for (int j = 0; j < WJ; ++j) x.b[j] = s[BM + rb + 32 * j];
+#pragma unroll
+        for (int i = 0; i < WI; ++i) x.a[i] = s[ra + 32 * i];
+    };
+    auto take_scales = [&](const Scales &x, Scales &y) {            // bytes 0 and 2: this lane's blocks of an even and an odd quarter
+#pragma unroll
+        for (int i = 0; i < WI; ++i) y.a[i] = x.a[i] >> (8 * half);
+#pragma unroll
+        for (int j = 0; j < WJ; ++j) y.b[j] = x.b[j] >> (8 * half);
     };
     auto multiply = [&](const Set &f, const Scales &x, int e, auto second) {
         constexpr int SEL = decltype(second)::value ? 2 : 0;
-        const int i = e / WT, j = e % WT;
+        const int i = e / WJ, j = e % WJ;
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fragment(f.b[j]), fragment(f.a[i]), acc[i][j], 4, 4, SEL,
                                                                     (int)x.b[j], SEL, (int)x.a[i]);
     };
 
-    // Loads and stores come back in the order in which they were issued.  The last tile's stores lie between the loads of this
-    // tile's first NB - 1 stages and all later ones, and the first waits of a tile let them pass (`after`: that many were issued).
-    constexpr int STORES = WT * WT * 32 * 32 * (int)sizeof(T) / 1024;
-    bool after = false;
-    auto wait_but = [&](auto loads, bool stores) {
-        constexpr int N = decltype(loads)::value;
-        if (stores) wait_loads<(N + STORES < 63 ? N + STORES : 63)>();
-        else wait_loads<N>();
-    };
-
     Set f0, f1;
     Scales x, next;
-    // One stage.  NEXT: there is a stage behind it; LOAD: and one NB - 1 behind it; PENDING: loads that may still be on their way when
-    // stage kc + 1 is needed.  Between the fences the written order is kept, LDS reads and loads spread over the matrix instructions:
-    // left to itself the compiler puts all reads in front and the matrix cores wait for them.
-    auto step = [&](int kc, auto load, auto has_next, auto pending) {
-        constexpr bool LOAD = decltype(load)::value, NEXT = decltype(has_next)::value;
-        constexpr int READS = 2 * WT, LOADS_FROM = MULS > LOADS ? MULS - LOADS : 0;
-#pragma unroll
-        for (int e = 0; e < (MULS > READS ? MULS : READS); ++e) {
-            if (e < READS) read_piece(kc, 1, e, f1);
-            if (e < MULS) multiply(f0, x, e, std::false_type());
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (NEXT) {
-            // stage kc + 1 has arrived for every wavefront; every wavefront is done with stage kc - 1, whose place is free
-            wait_but(pending, after && kc < NB - 2);
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            read_scales(kc + 1, next);
-        }
-#pragma unroll
-        for (int e = 0; e < (MULS > READS ? MULS : READS); ++e) {
-            if (NEXT && e < READS) read_piece(kc + 1, 0, e, f0);
-            if (LOAD) {
-                if (MULS > LOADS) {
-                    if (e >= LOADS_FROM) load_piece(kc + NB - 1, e - LOADS_FROM);
-                } else {
-#pragma unroll
-                    for (int g = 0; g < LOADS; ++g)
-                        if (g * READS / LOADS == e) load_piece(kc + NB - 1, g);
-                }
-            }
-            if (e < MULS) multiply(f1, x, e, std::true_type());
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (NEXT) take_scales(next, x);
-    };
     using Yes = std::true_type;
     using No = std::false_type;
-    using Most = std::integral_constant<int, (NB - 3) * LOADS>;
-    using None = std::integral_constant<int, 0>;
+    // One quarter: the products of f, while fragment e of (st, q) goes to g and a part of a stage's loads is issued (all in the first
+    // quarter that may: they have most time then).  Between the fences the written order is kept: left to itself the compiler puts all
+    // reads in front and the matrix cores wait for them.
+    auto quarter = [&](const Set &f, auto second, Set &g, int st, int q, auto read, auto load, int load_st, bool half_row) {
+#pragma unroll
+        for (int e = 0; e < SLOTS; ++e) {
+            if (decltype(read)::value && e < READS) read_piece(st, q, e, g);
+            if (decltype(load)::value)
+#pragma unroll
+                for (int p = 0; p < LOADS; ++p)
+                    if (p * SLOTS / LOADS == e) load_piece(load_st, p, half_row);
+            if (e < MULS) multiply(f, x, e, second);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
 
+    constexpr int STORES = WI * WJ * 32 * 32 * (int)sizeof(T) / 1024;       // of a wavefront and tile, if nothing of it is cut off
+    bool after = false;                                 // that many were issued behind the loads of this tile's first stage
     int k = blockIdx.x >> 3, copy = 0;
     if (k >= mine) return;
     set_tile(k);
     load_first(copy);
     for (; k < mine; k += slots, copy ^= 1) {
 #pragma unroll
-        for (int i = 0; i < WT; ++i)
+        for (int i = 0; i < WI; ++i)
 #pragma unroll
-            for (int j = 0; j < WT; ++j)
+            for (int j = 0; j < WJ; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-        if (nk >= NB - 1) wait_but(std::integral_constant<int, (NB - 2) * LOADS>(), after);
+        // loads and stores come back in the order in which they were issued: the last tile's stores may still be on their way
+        if (after) wait_loads<(STORES < 63 ? STORES : 63)>();
         else wait_loads<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        read_scales(0, next);
+        read_scales(0, 0, next);
 #pragma unroll
-        for (int g = 0; g < 2 * WT; ++g) read_piece(0, 0, g, f0);
+        for (int g = 0; g < READS; ++g) read_piece(0, 0, g, f0);
+        if (stages > 1)
+#pragma unroll
+            for (int g = 0; g < LOADS; ++g) load_piece(1, g, odd && stages == 2);
         take_scales(next, x);
-        int kc = 0;
-        for (; kc + NB - 1 < nk; ++kc) step(kc, Yes(), Yes(), Most());
-        if (NB > 3 && kc + 2 < nk) step(kc++, No(), Yes(), Most());
-        for (; kc + 1 < nk; ++kc) step(kc, No(), Yes(), None());
-        step(kc, No(), No(), None());
+        // (the products stand in one straight line for each of the three: in two branches, they would leave the accumulators in
+        // different registers, to be copied where the branches meet)
+        auto stage = [&](int st, auto load) {
+            read_scales(st, 1, next);
+            quarter(f0, No(), f1, st, 1, Yes(), No(), 0, false);
+            quarter(f1, Yes(), f0, st, 2, Yes(), No(), 0, false);
+            take_scales(next, x);
+            quarter(f0, No(), f1, st, 3, Yes(), No(), 0, false);
+            // the next stage has arrived for every wavefront, and every wavefront has the last quarter of this one
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            read_scales(st + 1, 0, next);
+            quarter(f1, Yes(), f0, st + 1, 0, Yes(), load, st + 2, odd && st + 3 == stages);
+            take_scales(next, x);
+        };
+        int st = 0;
+        for (; st + 2 < stages; ++st) stage(st, Yes());
+        if (st + 1 < stages) stage(st++, No());
+        quarter(f0, No(), f1, st, 1, Yes(), No(), 0, false);
+        if (!odd) {
+            read_scales(st, 1, next);
+            quarter(f1, Yes(), f0, st, 2, Yes(), No(), 0, false);
+            take_scales(next, x);
+            quarter(f0, No(), f1, st, 3, Yes(), No(), 0, false);
+        }
+        quarter(f1, Yes(), f0, st, 0, No(), No(), 0, false);
         __builtin_amdgcn_s_barrier();                               // every wavefront has read its last stage
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");         // the last results are read by vector instructions from here on
 
         const int m_first = m0 + ra, n_first = n0 + rb, n_left = P.N - n_first;
-        const bool full = vec && m0 + BT <= P.M && n0 + BT <= P.N;
-        if (k + slots < mine) {                                     // the next tile's first stages come while this one goes out
+        const bool full = vec && m0 + BM <= P.M && n0 + BN <= P.N;
+        if (k + slots < mine) {                                     // the next tile's first stage comes while this one goes out
             set_tile(k + slots);
             load_first(copy ^ 1);
         }
@@ -455,16 +463,16 @@ template <int WT, typename T> __global__ __launch_bounds__(256, WT == 4 ? 1 : 2)
 
         // Results: lane holds row m_first + 32 i + l % 32 of C, columns n_first + 32 j + 8 q + 4 (l / 32) .. + 3 in registers 4 q ..
         // 4 q + 3.  Stored from there, an instruction would write 32 pieces of 16 bytes; 32 rows of 128 bytes at a time go through LDS
-        // instead (a part of its own for each wavefront).
+        // instead (the second stage's place, a part of its own for each wavefront).
         constexpr int COLS = L::template out_cols<T>(), ROW = L::template out_row<T>(), PER16 = 16 / (int)sizeof(T), JS = COLS / 32;
         int l = lane;
-        asm("" : "+v"(l));         // addresses below are formed here, not kept in registers through the loop over the stages
-        unsigned char *s = s_tile + L::OUT + wave * 32 * ROW;
-        const float *bias = reinterpret_cast<const float *>(s_tile + L::BIAS) + copy * BT + rb;
+        asm("" : "+v"(l));
+        unsigned char *s = s_tile + L::BIAS + STAGE + wave * 32 * ROW;
+        const float *bias = reinterpret_cast<const float *>(s_tile) + copy * BN + rb;
 #pragma unroll
-        for (int i = 0; i < WT; ++i)
+        for (int i = 0; i < WI; ++i)
 #pragma unroll
-            for (int j0 = 0; j0 < WT; j0 += JS) {
+            for (int j0 = 0; j0 < WJ; j0 += JS) {
 #pragma unroll
                 for (int j = j0; j < j0 + JS; ++j)
 #pragma unroll
@@ -499,6 +507,55 @@ template <int WT, typename T> __global__ __launch_bounds__(256, WT == 4 ? 1 : 2)
                 __builtin_amdgcn_sched_barrier(0);      // else all results leave the accumulators first, for want of registers to memory
             }
     }
+}
+
+// Few rows (M up to 16): the rows of B are read once, and how fast they come is what counts, so nothing goes through LDS and the
+// contraction is split over the wavefronts of a workgroup.  v_mfma_scale_f32_16x16x128_f8f6f4: lane l gives 32 values of row l % 16,
+// columns 32 (l / 16) ..: 64 neighbouring bytes of a row, two instructions a cache line.  16 rows of B a workgroup, the rows of A
+// behind the last as the last; every wavefront has FEW_PAIRS lines of its rows on their way before it uses the first.  The
+// wavefronts' sums meet in LDS and are added in order.
+// One token, 15,360 x 5120 weights (42 MB with their scales): 13 us a call, through 64 x 64 tiles 15.
+constexpr int FEW_ROWS = 16, FEW_PAIRS = 4, FEW_WAVES = 16;
+
+template <typename T> __global__ __launch_bounds__(64 * FEW_WAVES) void mxfp4_few_kernel(const ProductArgs P)
+{
+    __shared__ __attribute__((aligned(16))) float s_sum[FEW_WAVES * 256];          // [wavefront][row of A][row of B]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int r = lane & 15, g = lane >> 4, n0 = blockIdx.x * 16, pairs = (P.nk + 1) >> 1;
+    const int n = min(n0 + r, P.N - 1), m = min(r, P.M - 1);
+    const uint8_t *b = P.B + (long long)n * P.nk * 64 + g * 16, *a = P.A + (long long)m * P.nk * 64 + g * 16;
+    const unsigned *sb = reinterpret_cast<const unsigned *>(P.SB) + n, *sa = reinterpret_cast<const unsigned *>(P.SA) + m;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = wave; p0 < pairs; p0 += waves * FEW_PAIRS) {
+        constexpr int U = 2 * FEW_PAIRS;
+        uint4 vb[U], va[U];
+        unsigned xb[U], xa[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int kc = 2 * (p0 + (u >> 1) * waves) + (u & 1);
+            const bool there = kc < P.nk;                           // zeros behind the end: they add nothing
+            vb[u] = there ? *reinterpret_cast<const uint4 *>(b + kc * 64LL) : make_uint4(0, 0, 0, 0);
+            xb[u] = there ? sb[(long long)kc * P.N] : 0u;
+            va[u] = there ? *reinterpret_cast<const uint4 *>(a + kc * 64LL) : make_uint4(0, 0, 0, 0);
+            xa[u] = there ? sa[(long long)kc * P.M] : 0u;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(vb[u]), fragment(va[u]), acc, 4, 4, 0, (int)(xb[u] >> (8 * g)), 0,
+                                                                   (int)(xa[u] >> (8 * g)));
+    }
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    // lane holds row l % 16 of A, rows 4 (l / 16) .. + 3 of B
+    *reinterpret_cast<float4 *>(s_sum + (wave * 16 + r) * 16 + 4 * g) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    __syncthreads();
+    const int i = threadIdx.x, row = i >> 4, col = n0 + (i & 15);
+    if (i >= 256 || row >= P.M || col >= P.N) return;
+    float v = 0.f;
+    for (int k = 0; k < waves; ++k) v += s_sum[k * 256 + i];
+    if (P.bias) v += P.bias[col];
+    T *to = static_cast<T *>(P.C) + (long long)row * P.ldc + col;
+    if constexpr (sizeof(T) == 4) *to = v;
+    else *to = (bf16_t)pack_bf16(v, 0.f);
 }
 
 // ---- launchers -------------------------------------------------------------
@@ -561,26 +618,58 @@ int mxfp4_values_launch(const void *codes, const void *scales, int M, int K, int
 
 size_t mxfp4_matmul_ws_bytes(int M, int N, int K) { (void)M; (void)N; (void)K; return 256; }
 
-template <int WT> static int prepare_tiles()
+using Large = Tile<2, 4, 4, 2>;
+using Medium = Tile<2, 2, 2, 2>;
+using Small = Tile<2, 2, 1, 1>;
+
+template <typename L> static int prepare_tiles()
 {
-    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<WT, bf16_t>), Tile<WT>::template lds<bf16_t>()));
-    return set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<WT, float>), Tile<WT>::template lds<float>());
+    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<L, bf16_t>), L::LDS));
+    return set_dynamic_lds(reinterpret_cast<const void *>(&mxfp4_product_kernel<L, float>), L::LDS);
 }
 
 int mxfp4_matmul_prepare()
 {
-    SVG2_TRY(prepare_tiles<4>());
-    SVG2_TRY(prepare_tiles<2>());
-    return prepare_tiles<1>();
+    SVG2_TRY(prepare_tiles<Large>());
+    SVG2_TRY(prepare_tiles<Medium>());
+    return prepare_tiles<Small>();
 }
 
-template <int WT> static int product_tiles(ProductArgs P, int out_dtype, bool vec, hipStream_t st)
+// Microseconds that the product takes with these tiles, by what was measured: `start` a tile, and for each stage of 256 columns
+// alone[..] with one workgroup a CU up to full[..] with as many as fit (Large 1, Medium 2, Small 4).  Large tiles do most with
+// what they load, small ones leave fewer CUs idle: measured, large / medium / small,
+//   8192 x 8192 x 8192    249 / 302 / 459 us        4096 x 5120 x 5120    78 / 65 / 102 us       512 x 5120 x 5120   33 / 17 / 17 us
+//   4096 x 4096 x 4096     40 /  45 /  65 us        2048 x 2048 x 2048    18 / 11 /  12 us       300 x 5120 x 5120   40 / 21 / 14 us
+template <typename L> static double tile_time(int M, int N, int K)
 {
-    P.tiles_n = cdiv(P.N, 64 * WT);
-    const int tiles = cdiv(P.M, 64 * WT) * P.tiles_n, resident = 256 * (WT == 4 ? 1 : WT == 2 ? 2 : 4);
+    constexpr int R = L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4;
+    constexpr double start = R == 1 ? 7.0 : R == 2 ? 3.5 : 2.0, alone = R == 1 ? 1.6 : R == 2 ? 0.62 : 0.38, full = R == 1 ? 1.78 : R == 2 ? 1.09 : 0.86;
+    const long long tiles = (long long)cdiv(M, L::BM) * cdiv(N, L::BN), rounds = tiles / (256 * R), rest = (tiles - rounds * 256 * R + 255) / 256;
+    const double stages = cdiv(K, 256);
+    const double last = rest == 0 ? 0.0 : start + stages * (R == 1 ? alone : alone + (full - alone) * (double)(rest - 1) / (R > 1 ? R - 1 : 1));
+    return (double)rounds * (start + stages * full) + last;
+}
+
+template <typename L> static int product_tiles(ProductArgs P, int out_dtype, bool vec, hipStream_t st)
+{
+    P.tiles_n = cdiv(P.N, L::BN);
+    const int tiles = cdiv(P.M, L::BM) * P.tiles_n, resident = 256 * (L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4);
     const int grid = tiles < resident ? tiles : resident;
-    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<WT, bf16_t><<<grid, 256, Tile<WT>::template lds<bf16_t>(), st>>>(P, vec);
-    else mxfp4_product_kernel<WT, float><<<grid, 256, Tile<WT>::template lds<float>(), st>>>(P, vec);
+    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<L, bf16_t><<<grid, 64 * L::WAVES, L::LDS, st>>>(P, vec);
+    else mxfp4_product_kernel<L, float><<<grid, 64 * L::WAVES, L::LDS, st>>>(P, vec);
+    SVG2_HIP_CHECK(hipGetLastError());
+    return SVG2_OK;
+}
+
+static int product_few(const ProductArgs &P, int out_dtype, hipStream_t st)
+{
+    // 4 wavefronts, 8 or 16: enough of them for the whole card and for every line of a row to be on its way at once, not more than
+    // there are lines in a row
+    const int blocks = cdiv(P.N, 16), pairs = cdiv(P.nk, 2);
+    int waves = 4;
+    while (waves < FEW_WAVES && waves < pairs && ((long long)blocks * waves < 4096 || waves * FEW_PAIRS < pairs)) waves *= 2;
+    if (out_dtype == SVG2_BF16) mxfp4_few_kernel<bf16_t><<<blocks, 64 * waves, 0, st>>>(P);
+    else mxfp4_few_kernel<float><<<blocks, 64 * waves, 0, st>>>(P);
     SVG2_HIP_CHECK(hipGetLastError());
     return SVG2_OK;
 }
@@ -592,11 +681,11 @@ int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void
     const ProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
                            static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0};
     const bool vec = aligned(C, 16) && ldc % (out_dtype == SVG2_BF16 ? 8 : 4) == 0;
-    // the largest tile that leaves every CU one
-    auto tiles = [&](int wt) { return (long long)cdiv(M, 64 * wt) * cdiv(N, 64 * wt); };
-    if (tiles(4) >= 256) return product_tiles<4>(P, out_dtype, vec, st);
-    if (tiles(2) >= 256) return product_tiles<2>(P, out_dtype, vec, st);
-    return product_tiles<1>(P, out_dtype, vec, st);
+    if (M <= FEW_ROWS) return product_few(P, out_dtype, st);
+    const double large = tile_time<Large>(M, N, K), medium = tile_time<Medium>(M, N, K), small = tile_time<Small>(M, N, K);
+    if (large <= medium && large <= small) return product_tiles<Large>(P, out_dtype, vec, st);
+    if (medium <= small) return product_tiles<Medium>(P, out_dtype, vec, st);
+    return product_tiles<Small>(P, out_dtype, vec, st);
 }
 
 }  // namespace svg2

@@ -111,12 +111,13 @@ def _operand(R, K, seed, exps=(-6, 7)):
     return c, s, torch.from_numpy(c).cuda(), torch.from_numpy(s).cuda()
 
 
-# rows of a few tokens, of half a tile and across tiles; columns of one block of 128 up to a long sum
-PRODUCTS = [(1, 1, 1), (1, 64, 128), (1, 513, 640), (2, 96, 300), (7, 1000, 1000), (16, 130, 4224), (17, 255, 256), (33, 65, 129),
-            (64, 512, 2048), (65, 127, 384), (128, 128, 128), (129, 257, 512), (255, 300, 1280), (256, 256, 256), (300, 1023, 777),
-            (513, 640, 1000), (1000, 77, 64),
-            # enough results for tiles of 128 x 128 and of 256 x 256, ragged; one to five stages of the loop
-            (2049, 2177, 100), (2000, 2100, 513), (4129, 4225, 128), (4100, 4200, 200), (4200, 4099, 300), (4097, 4101, 640)]
+# rows of a few tokens, of half a tile and across tiles; columns of one block of 128 up to a long sum (even and odd numbers of them:
+# a stage is two)
+PRODUCTS = [(1, 1, 1), (1, 64, 128), (1, 513, 640), (2, 96, 300), (7, 1000, 1000), (16, 130, 4224), (15, 33, 17000), (17, 255, 256),
+            (33, 65, 129), (64, 512, 2048), (65, 127, 384), (128, 128, 128), (129, 257, 512), (255, 300, 1280), (256, 256, 256),
+            (300, 1023, 777), (513, 640, 1000), (1000, 77, 64),
+            # more tiles of 64 x 64 than fit at once, and more than one of 128 x 128 or 256 x 256 for a workgroup; one to five stages
+            (2049, 2177, 100), (2000, 2100, 513), (4129, 4225, 300), (4095, 4090, 513), (8190, 4093, 300), (4090, 8100, 1100)]
 
 
 @pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
