@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 from types import SimpleNamespace
 from typing import Optional
 
@@ -36,7 +37,7 @@ EXPORTS = (
     "svg2_attention_recall_workspace_size", "svg2_attention_recall",
     "svg2_kmeans_pp_init_workspace_size", "svg2_kmeans_pp_init",
     "svg2_rope", "svg2_rope_backward_workspace_size", "svg2_rope_backward",
-    "svg2_quantize_mxfp4", "svg2_dequantize_mxfp4", "svg2_matmul_mxfp4_workspace_size", "svg2_matmul_mxfp4",
+    "svg2_quantize_mxfp4", "svg2_dequantize_mxfp4", "svg2_matmul_mxfp4",
     "svg2_profile_enable", "svg2_profile_read", "svg2_profile_read_kernels",
 )
 STAGES = ("kmeans", "permute", "select", "attn_plan", "attn")
@@ -60,13 +61,8 @@ ROPE_PAIRINGS = ("adjacent", "halves")
 NORM_SCOPES = ("head", "token")
 
 
-class _RopeArgs(ctypes.Structure):
-    _fields_ = [("n_tensors", ctypes.c_int), ("dtype", ctypes.c_int), ("B", ctypes.c_int), ("N", ctypes.c_int),
-                ("H", ctypes.c_int), ("d", ctypes.c_int), ("src", ctypes.c_void_p * 3), ("dst", ctypes.c_void_p * 3),
-                ("rotate", ctypes.c_int * 3), ("norm_weight", ctypes.c_void_p * 3), ("src_stride", ctypes.c_int64 * 3),
-                ("dst_stride", ctypes.c_int64 * 3), ("pos", ctypes.c_void_p), ("pos_stride_b", ctypes.c_int64),
-                ("freq", ctypes.c_void_p), ("n_axes", ctypes.c_int), ("axis_pairs", ctypes.c_int * 4),
-                ("pairing", ctypes.c_int), ("norm_scope", ctypes.c_int), ("eps", ctypes.c_float)]
+# svg2_rope_args, packed as the C compiler lays it out (a ctypes structure takes twice as long to fill)
+_ROPE_ARGS = struct.Struct("@6i3P3P3i3P3q3qPqPi4iiif0q")
 
 
 _P3, _I3 = ctypes.c_void_p * 3, ctypes.c_int64 * 3
@@ -120,8 +116,7 @@ def load_library() -> ctypes.CDLL:
         i64 = ctypes.c_int64
         lib.svg2_quantize_mxfp4.argtypes = [vp, i, i, i, i, i64, i64, i, vp, vp, vp]
         lib.svg2_dequantize_mxfp4.argtypes = [vp, vp, i, i, i, vp, i64, vp]
-        lib.svg2_matmul_mxfp4_workspace_size.argtypes = [i, i, i]
-        lib.svg2_matmul_mxfp4.argtypes = [vp, vp, vp, vp, i, i, i, vp, i, vp, i64, vp, sz, vp]
+        lib.svg2_matmul_mxfp4.argtypes = [vp, vp, vp, vp, i, i, i, vp, i, vp, i64, vp]
         lib.svg2_profile_enable.argtypes = [i]
         lib.svg2_profile_read.argtypes = [vp, vp]
         lib.svg2_profile_read_kernels.argtypes = [vp, vp]
@@ -416,8 +411,8 @@ def svg2_kmeans_pp_init(X, C, u, *, ws=None):
     return SimpleNamespace(centroids=centroids, picked=picked)
 
 
-# The calls below are short on the GPU where there are few tokens, so their checks are written to cost little: every attribute
-# of a tensor is asked for once.
+# The calls below are short on the GPU where there are few tokens, so their checks are written to cost little: one condition per
+# tensor, and what exactly is wrong is found out only then.
 
 def _raw_stream(device: torch.device) -> int:
     return torch._C._cuda_getCurrentRawStream(device.index)
@@ -431,70 +426,78 @@ def _on(device: torch.device):
 _HERE_ALREADY = contextlib.nullcontext()
 
 
-def _strided(t: torch.Tensor, name: str, device=None, dtype=None) -> int:
-    """Address of a GPU tensor of any strides whose innermost dimension is contiguous."""
+def _gpu(t: torch.Tensor, name: str) -> torch.device:
     if not t.is_cuda:
         raise ValueError("%s must live on the GPU" % name)
-    if device is not None and t.device != device:
+    return t.device
+
+
+def _refuse(t: torch.Tensor, name: str, device, dtype, shape):
+    if t.device != device:
         raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-    if dtype is not None and t.dtype is not dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError("%s must be contiguous in its last dimension" % name)
+    if t.shape != shape:
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+    raise ValueError("%s must be contiguous" % name)
+
+
+def _dense(t: Optional[torch.Tensor], name: str, device, dtype, shape) -> int:
+    """Address of a dense tensor; 0 for None."""
+    if t is None:
+        return 0
+    if t.shape != shape or t.dtype is not dtype or t.device != device or not t.is_contiguous():
+        _refuse(t, name, device, dtype, shape)
     return t.data_ptr()
 
 
-def _dense(t: Optional[torch.Tensor], name: str, device, dtype, shape) -> Optional[int]:
-    if t is None:
-        return None
-    if t.shape != shape:
-        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
-    return _strided(t, name, device, dtype)
-
-
 def _outer_strides(shape, stride):
-    """Strides of all but the last dimension; 0 where the dimension has one entry (torch leaves anything there)."""
+    """Strides of all but the last dimension, which has to be contiguous; 0 where a dimension has one entry (torch leaves anything
+    there)."""
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError("a tensor's last dimension must be contiguous")
     return [s if n > 1 else 0 for n, s in zip(shape[:-1], stride[:-1])]
 
 
 def _three(xs):
-    return tuple(xs) + (None,) * (3 - len(xs))
+    return xs if len(xs) == 3 else (*xs, 0, 0, 0)[:3]
+
+
+def _views(tensors, name, device, dtype, own):
+    """One to three tensors of shape `own` and one set of strides -> outer strides, addresses."""
+    stride = tensors[0].stride()
+    outer = _outer_strides(own, stride)
+    ptrs = []
+    for t in tensors:
+        if t.shape != own or t.dtype is not dtype or t.device != device or (
+                t.stride() != stride and _outer_strides(own, t.stride()) != outer):
+            if t.shape == own and t.dtype is dtype and t.device == device:
+                raise ValueError("%s must share one set of strides" % name)
+            _refuse(t, name, device, dtype, own)
+        ptrs.append(t.data_ptr())
+    return outer, ptrs
 
 
 def _token_views(tensors, name, device, dtype, shape=None):
     """One to three [N,H,d] or [B,N,H,d] tensors of one shape and one set of strides -> (B,N,H,d), the three outer strides,
     addresses."""
-    if not 1 <= len(tensors) <= 3:
-        raise ValueError("%s: one to three tensors" % name)
-    own, stride = tensors[0].shape, tensors[0].stride()
-    if len(own) == 4:
-        full, outer = tuple(own), _outer_strides(own, stride)
-    elif len(own) == 3:
-        full, outer = (1,) + tuple(own), [0] + _outer_strides(own, stride)
-    else:
+    own = tensors[0].shape
+    full = tuple(own) if len(own) == 4 else (1, *own)
+    if len(full) != 4:
         raise ValueError("%s must be [N,H,d] or [B,N,H,d]" % name)
     if shape is not None and full != shape:
         raise ValueError("%s must be %s, got %s" % (name, list(shape), list(own)))
-    for i, t in enumerate(tensors):
-        if i and (t.shape != own or (t.stride() != stride and _outer_strides(own, t.stride()) != _outer_strides(own, stride))):
-            raise ValueError("%s must share one shape and one set of strides" % name)
-    return full, outer, [_strided(t, name, device, dtype) for t in tensors]
+    outer, ptrs = _views(tensors, name, device, dtype, own)
+    return full, outer if len(own) == 4 else [0] + outer, ptrs
 
 
 def _head_order(tensors, name, device, dtype, shape):
     """As _token_views for [B*H,N,d] tensors that stand for [B,N,H,d]; [B,N,H,d] tensors themselves are taken too."""
     B, N, H, d = shape
-    own = tensors[0].shape
-    if len(own) != 3:
+    if tensors[0].dim() != 3:
         return _token_views(tensors, name, device, dtype, shape)[1:]
-    stride = tensors[0].stride()
-    for t in tensors:
-        if t.shape != (B * H, N, d) or t.stride() != stride:
-            raise ValueError("%s must all be [%d,%d,%d] with one set of strides" % (name, B * H, N, d))
-    s = _outer_strides(own, stride)
-    return [H * s[0] if B > 1 else 0, s[1], s[0] if H > 1 else 0], [_strided(t, name, device, dtype) for t in tensors]
+    s, ptrs = _views(tensors, name, device, dtype, (B * H, N, d))
+    return [H * s[0] if B > 1 else 0, s[1], s[0] if H > 1 else 0], ptrs
 
 
 def svg2_grid_positions(grid, *, first=(0, 0, 0), extra=0, device="cuda"):
@@ -513,36 +516,41 @@ def svg2_rope_frequencies(axis_pairs, *, theta=10000.0, device="cuda"):
 
 def _rope_args(n, dtype, device, shape, src, src_stride, dst, dst_stride, pos, freq, axis_pairs, rotate, norm_weights, norm_scope,
                eps, pairing):
-    """The C struct, with every check that needs the tensors themselves."""
+    """svg2_rope_args, with every check that needs the tensors themselves; the norms' weights."""
     B, N, H, d = shape
     if pairing not in ROPE_PAIRINGS:
         raise ValueError("pairing must be one of %s" % (ROPE_PAIRINGS,))
     if norm_scope not in NORM_SCOPES:
         raise ValueError("norm_scope must be one of %s" % (NORM_SCOPES,))
-    rotate = (True,) * n if rotate is None else tuple(rotate)
-    weights = (None,) * n if norm_weights is None else tuple(norm_weights)
+    rotate = (True,) * n if rotate is None else rotate
+    weights = (None,) * n if norm_weights is None else norm_weights
     if len(rotate) != n or len(weights) != n:
         raise ValueError("rotate and norm_weights need one entry per tensor")
     wshape = (d,) if norm_scope == "head" else (H, d)
-    w = [None if x is None else _dense(x, "norm_weights", device, torch.float32, wshape) for x in weights]
-    pos_ptr = freq_ptr = None
-    pos_stride, axes = 0, ()
+    w = [0 if x is None else _dense(x, "norm_weights", device, torch.float32, wshape) for x in weights]
+    pos_ptr = freq_ptr = pos_stride = 0
+    axes = ()
     if any(rotate):
-        axes = tuple(int(x) for x in axis_pairs)
-        if not 1 <= len(axes) <= 4:
-            raise ValueError("axis_pairs must have 1 to 4 entries")
+        if pos is None or freq is None:
+            raise ValueError("pos and freq are needed where a tensor is rotated")
+        axes = axis_pairs
         k = len(axes)
-        have = tuple(pos.shape)
-        if have != (N, k) and have != (B, N, k) and have != (1, N, k):
+        if not 1 <= k <= 4:
+            raise ValueError("axis_pairs must have 1 to 4 entries")
+        have = pos.shape
+        if have == (N, k):
+            pos_ptr = _dense(pos, "pos", device, torch.int32, have)
+        elif have == (B, N, k) or have == (1, N, k):
+            pos_ptr = pos.data_ptr()
+            _dense(pos[0], "pos", device, torch.int32, (N, k))
+            pos_stride = pos.stride(0) if have[0] > 1 else 0
+        else:
             raise ValueError("pos must be [N,%d] or [B,N,%d], got %s" % (k, k, list(have)))
-        if not (pos.is_contiguous() or (len(have) == 3 and pos[0].is_contiguous())):
-            raise ValueError("pos must be dense inside a batch")
-        pos_ptr = _strided(pos, "pos", device, torch.int32)
-        pos_stride = pos.stride(0) if len(have) == 3 and have[0] > 1 else 0
         freq_ptr = _dense(freq, "freq", device, torch.float64, (d // 2,))
-    return _RopeArgs(n, dtype, B, N, H, d, _three(src), _three(dst), tuple([1 if r else 0 for r in rotate]), _three(w),
-                     tuple(src_stride), tuple(dst_stride), pos_ptr, pos_stride, freq_ptr, len(axes), axes,
-                     ROPE_PAIRINGS.index(pairing), NORM_SCOPES.index(norm_scope), eps), weights
+    r = [1 if x else 0 for x in rotate]
+    return _ROPE_ARGS.pack(n, dtype, B, N, H, d, *_three(src), *_three(dst), *_three(r), *_three(w), *src_stride, *dst_stride, pos_ptr,
+                           pos_stride, freq_ptr, len(axes), *(*axes, 0, 0, 0, 0)[:4], ROPE_PAIRINGS.index(pairing),
+                           NORM_SCOPES.index(norm_scope), eps), weights
 
 
 def svg2_rope(tensors, pos=None, freq=None, *, axis_pairs=(), rotate=None, norm_weights=None, norm_scope="head", eps=1e-6,
@@ -554,12 +562,15 @@ def svg2_rope(tensors, pos=None, freq=None, *, axis_pairs=(), rotate=None, norm_
     norm_weights: per tensor fp32 [d] (norm_scope "head") or [H,d] ("token"), or None.  Returns [B*H,N,d] tensors, or
     `outs` ([N,H,d] or [B,N,H,d] views of any strides; `tensors` themselves for a call in place)."""
     lib = load_library()
-    n, first = len(tensors), tensors[0]
-    dtype, dev = first.dtype, first.device
+    n = len(tensors)
+    if not 1 <= n <= 3:
+        raise ValueError("one to three tensors")
+    first = tensors[0]
+    dtype, dev = first.dtype, _gpu(first, "tensors")
     shape, src_stride, src = _token_views(tensors, "tensors", dev, dtype)
     B, N, H, d = shape
     if outs is None:
-        outs = [torch.empty((B * H, N, d), dtype=dtype, device=dev) for _ in range(n)]
+        outs = [first.new_empty((B * H, N, d)) for _ in range(n)]
         dst_stride, dst = (H * N * d, d, N * d), [t.data_ptr() for t in outs]
     else:
         if len(outs) != n:
@@ -568,7 +579,7 @@ def svg2_rope(tensors, pos=None, freq=None, *, axis_pairs=(), rotate=None, norm_
     a, _ = _rope_args(n, _dtype_code(first), dev, shape, src, src_stride, dst, dst_stride, pos, freq, axis_pairs, rotate, norm_weights,
                       norm_scope, eps, pairing)
     with _on(dev):
-        _check(lib.svg2_rope(ctypes.byref(a), _raw_stream(dev)))
+        _check(lib.svg2_rope(a, _raw_stream(dev)))
     return outs
 
 
@@ -577,11 +588,14 @@ def svg2_rope_backward(grads, tensors, pos=None, freq=None, *, axis_pairs=(), ro
     """Gradients of svg2_rope: grads ([B*H,N,d], or [B,N,H,d] views of one set of strides) and the forward call's arguments
     -> grads of `tensors` (dense [B,N,H,d], or `outs`, views of any strides) and of norm_weights (None where None)."""
     lib = load_library()
-    n, first = len(tensors), tensors[0]
-    dtype, dev = first.dtype, first.device
+    n = len(tensors)
+    if not 1 <= n <= 3:
+        raise ValueError("one to three tensors")
+    first = tensors[0]
+    dtype, dev = first.dtype, _gpu(first, "tensors")
     shape, src_stride, src = _token_views(tensors, "tensors", dev, dtype)
     if outs is None:
-        outs = [torch.empty(shape, dtype=dtype, device=dev) for _ in range(n)]
+        outs = [first.new_empty(shape) for _ in range(n)]
     if len(grads) != n or len(outs) != n:
         raise ValueError("one gradient and one output per tensor")
     g_stride, g = _head_order(grads, "grads", dev, dtype, shape)
@@ -591,16 +605,10 @@ def svg2_rope_backward(grads, tensors, pos=None, freq=None, *, axis_pairs=(), ro
                             norm_weights, norm_scope, eps, pairing)
     dw = [None if w is None else torch.empty_like(w) for w in weights]
     with _on(dev):
-        ws = _workspace(lib.svg2_rope_backward_workspace_size(ctypes.byref(a)), dev) if ws is None else ws
-        _check(lib.svg2_rope_backward(ctypes.byref(a), _P3(*g), _P3(*dx), _I3(*dx_stride),
+        ws = _workspace(lib.svg2_rope_backward_workspace_size(a), dev) if ws is None else ws
+        _check(lib.svg2_rope_backward(a, _P3(*g), _P3(*dx), _I3(*dx_stride),
                                       _P3(*[None if t is None else t.data_ptr() for t in dw]), _dev(ws), ws.numel(), _raw_stream(dev)))
     return SimpleNamespace(grads=outs, dweights=dw)
-
-
-def _mxfp4_empty(R, K, device):
-    nk = -(-K // 128)
-    return (torch.empty((R, nk * 64), dtype=torch.uint8, device=device),
-            torch.empty((nk, R, 4), dtype=torch.uint8, device=device))
 
 
 def _mxfp4_operand(codes, scales, name, device):
@@ -609,27 +617,38 @@ def _mxfp4_operand(codes, scales, name, device):
     if len(shape) != 2 or shape[1] % 64:
         raise ValueError("%s: codes must be [R, Kp/2] with Kp a multiple of 128, got %s" % (name, list(shape)))
     R, half = shape
-    _dense(codes, name, device, torch.uint8, shape)
-    _dense(scales, name, device, torch.uint8, (half // 64, R, 4))
-    return R, 2 * half
+    return R, 2 * half, _dense(codes, name, device, torch.uint8, shape), _dense(scales, name, device, torch.uint8, (half // 64, R, 4))
+
+
+def _rows(t, name, device, shape):
+    """Address and row stride of a matrix whose rows are contiguous."""
+    if t.shape != shape or t.device != device:
+        _refuse(t, name, device, t.dtype, shape)
+    stride = t.stride()
+    if stride[1] != 1 and shape[1] > 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+    return t.data_ptr(), stride[0] if shape[0] > 1 else shape[1]
 
 
 def svg2_quantize_mxfp4(X, *, transposed=False):
     """X [M,K], or [M,G,Kg] for K = G*Kg columns in groups of any stride (the layer's O as O.transpose(0, 1)) -> MXFP4
     operand (codes [M,Kp/2], scales [Kp/128,M,4] uint8); transposed: of X^T, [K rows, M columns]."""
     lib = load_library()
-    if X.dim() not in (2, 3):
-        raise ValueError("X must be [M,K] or [M,G,Kg]")
-    ptr, dev, shape = _strided(X, "X"), X.device, X.shape
+    dev, shape = _gpu(X, "X"), X.shape
+    strides = _outer_strides(shape, X.stride())
     if len(shape) == 2:
-        (M, Kg), G = shape, 1
-        sm, sg = _outer_strides(shape, X.stride())[0], 0
+        (M, K), G, (sm,), sg = shape, 1, strides, 0
+        Kg = K
+    elif len(shape) == 3:
+        (M, G, Kg), (sm, sg) = shape, strides
+        K = G * Kg
     else:
-        M, G, Kg = shape
-        sm, sg = _outer_strides(shape, X.stride())
-    codes, scales = _mxfp4_empty(G * Kg, M, dev) if transposed else _mxfp4_empty(M, G * Kg, dev)
+        raise ValueError("X must be [M,K] or [M,G,Kg]")
+    R, nk = (K, -(-M // 128)) if transposed else (M, -(-K // 128))
+    codes = torch.empty((R, nk * 64), dtype=torch.uint8, device=dev)
+    scales = codes.new_empty((nk, R, 4))
     with _on(dev):
-        _check(lib.svg2_quantize_mxfp4(ptr, _dtype_code(X), M, G, Kg, sm, sg, 1 if transposed else 0, codes.data_ptr(),
+        _check(lib.svg2_quantize_mxfp4(X.data_ptr(), _dtype_code(X), M, G, Kg, sm, sg, 1 if transposed else 0, codes.data_ptr(),
                                        scales.data_ptr(), _raw_stream(dev)))
     return codes, scales
 
@@ -637,40 +656,30 @@ def svg2_quantize_mxfp4(X, *, transposed=False):
 def svg2_dequantize_mxfp4(codes, scales, K=None, *, dtype=torch.bfloat16, out=None):
     """The values of an MXFP4 operand, [R,K] (K: all padded columns where None)."""
     lib = load_library()
-    dev = codes.device
-    R, Kp = _mxfp4_operand(codes, scales, "operand", dev)
-    K = Kp if K is None else int(K)
+    dev = _gpu(codes, "codes")
+    R, Kp, c, s = _mxfp4_operand(codes, scales, "operand", dev)
+    K = Kp if K is None else K
     if not Kp - 128 < K <= Kp:
         raise ValueError("K = %d does not belong to %d padded columns" % (K, Kp))
     out = torch.empty((R, K), dtype=dtype, device=dev) if out is None else out
-    if out.shape != (R, K):
-        raise ValueError("out must be [%d,%d]" % (R, K))
-    ptr = _strided(out, "out", dev)
+    ptr, ld = _rows(out, "out", dev, (R, K))
     with _on(dev):
-        _check(lib.svg2_dequantize_mxfp4(codes.data_ptr(), scales.data_ptr(), R, K, _dtype_code(out), ptr,
-                                         out.stride(0) if R > 1 else K, _raw_stream(dev)))
+        _check(lib.svg2_dequantize_mxfp4(c, s, R, K, _dtype_code(out), ptr, ld, _raw_stream(dev)))
     return out
 
 
-def svg2_matmul_mxfp4(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bfloat16, out=None, ws=None):
+def svg2_matmul_mxfp4(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bfloat16, out=None):
     """C [M,N] = A B^T + bias of two MXFP4 operands (M and N rows of the same columns); bias fp32 [N]."""
     lib = load_library()
-    dev = A.device
-    M, Kp = _mxfp4_operand(A, A_scales, "A", dev)
-    N, Kb = _mxfp4_operand(B, B_scales, "B", dev)
+    dev = _gpu(A, "A")
+    M, Kp, a, sa = _mxfp4_operand(A, A_scales, "A", dev)
+    N, Kb, b, sb = _mxfp4_operand(B, B_scales, "B", dev)
     if Kb != Kp:
         raise ValueError("A has %d padded columns, B has %d" % (Kp, Kb))
     C = torch.empty((M, N), dtype=out_dtype, device=dev) if out is None else out
-    if C.shape != (M, N):
-        raise ValueError("out must be [%d,%d]" % (M, N))
-    ptr = _strided(C, "out", dev)
-    bias_ptr = _dense(bias, "bias", dev, torch.float32, (N,))
+    ptr, ld = _rows(C, "out", dev, (M, N))
     with _on(dev):
-        need = lib.svg2_matmul_mxfp4_workspace_size(M, N, Kp) if ws is None else 0
-        if need > 256:                  # at 256 the product needs none
-            ws = _workspace(need, dev)
-        _check(lib.svg2_matmul_mxfp4(A.data_ptr(), A_scales.data_ptr(), B.data_ptr(), B_scales.data_ptr(), M, N, Kp, bias_ptr,
-                                     _dtype_code(C), ptr, C.stride(0) if M > 1 else N, _dev(ws), 0 if ws is None else ws.numel(),
+        _check(lib.svg2_matmul_mxfp4(a, sa, b, sb, M, N, Kp, _dense(bias, "bias", dev, torch.float32, (N,)), _dtype_code(C), ptr, ld,
                                      _raw_stream(dev)))
     return C
 

@@ -209,9 +209,8 @@ int rope_bwd_launch(const svg2_rope_args *a, const void *const *dY, void *const 
 int mxfp4_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t sm, int64_t sg, bool transposed, void *codes,
                        void *scales, hipStream_t st);
 int mxfp4_values_launch(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx, hipStream_t st);
-size_t mxfp4_matmul_ws_bytes(int M, int N, int K);
 int mxfp4_matmul_prepare();
 int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
-                        int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st);
+                        int out_dtype, void *C, int64_t ldc, hipStream_t st);
 
 }  // namespace svg2

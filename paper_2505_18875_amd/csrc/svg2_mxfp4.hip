@@ -616,8 +616,6 @@ int mxfp4_values_launch(const void *codes, const void *scales, int M, int K, int
     return SVG2_OK;
 }
 
-size_t mxfp4_matmul_ws_bytes(int M, int N, int K) { (void)M; (void)N; (void)K; return 256; }
-
 using Large = Tile<2, 4, 4, 2>;
 using Medium = Tile<2, 2, 2, 2>;
 using Small = Tile<2, 2, 1, 1>;
@@ -675,9 +673,8 @@ static int product_few(const ProductArgs &P, int out_dtype, hipStream_t st)
 }
 
 int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
-                        int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st)
+                        int out_dtype, void *C, int64_t ldc, hipStream_t st)
 {
-    (void)ws;
     const ProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
                            static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0};
     const bool vec = aligned(C, 16) && ldc % (out_dtype == SVG2_BF16 ? 8 : 4) == 0;

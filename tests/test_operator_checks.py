@@ -17,8 +17,30 @@ def lib():
     return binding.load_library()
 
 
+class _RopeArgs(ctypes.Structure):
+    """svg2_rope_args of include/svg2.h"""
+    _fields_ = [("n_tensors", ctypes.c_int), ("dtype", ctypes.c_int), ("B", ctypes.c_int), ("N", ctypes.c_int),
+                ("H", ctypes.c_int), ("d", ctypes.c_int), ("src", ctypes.c_void_p * 3), ("dst", ctypes.c_void_p * 3),
+                ("rotate", ctypes.c_int * 3), ("norm_weight", ctypes.c_void_p * 3), ("src_stride", ctypes.c_int64 * 3),
+                ("dst_stride", ctypes.c_int64 * 3), ("pos", ctypes.c_void_p), ("pos_stride_b", ctypes.c_int64),
+                ("freq", ctypes.c_void_p), ("n_axes", ctypes.c_int), ("axis_pairs", ctypes.c_int * 4),
+                ("pairing", ctypes.c_int), ("norm_scope", ctypes.c_int), ("eps", ctypes.c_float)]
+
+
+def test_the_binding_packs_the_struct_as_c_does():
+    from paper_2505_18875_amd.binding import _ROPE_ARGS
+    values = list(range(1, 36))
+    packed = _ROPE_ARGS.pack(*values[:-1], 0.5)
+    assert len(packed) == ctypes.sizeof(_RopeArgs)
+    a = _RopeArgs.from_buffer_copy(packed)
+    flat = []
+    for name, _ in _RopeArgs._fields_:
+        v = getattr(a, name)
+        flat += list(v) if hasattr(v, "__len__") else [v]
+    assert flat[:-1] == values[:-1] and flat[-1] == 0.5
+
+
 def _args(**change):
-    from paper_2505_18875_amd.binding import _RopeArgs
     a = _RopeArgs()
     a.n_tensors, a.dtype, a.B, a.N, a.H, a.d = 2, 1, 2, 8, 4, 64
     a.src = (ctypes.c_void_p * 3)(1 << 20, 2 << 20, 3 << 20)
@@ -128,18 +150,16 @@ def test_dequantize_mxfp4_refuses(lib):
 
 
 def test_matmul_mxfp4_refuses(lib):
-    ok = (1 << 20, 2 << 20, 3 << 20, 4 << 20, 128, 256, 512, None, 1, 5 << 20, 256, 256, 1 << 40, None)
+    ok = (1 << 20, 2 << 20, 3 << 20, 4 << 20, 128, 256, 512, None, 1, 5 << 20, 256, None)
     for at, v, code, word in ((0, None, 1, b"A:"), (1, None, 1, b"A:"), (2, 8, 1, b"B:"), (3, None, 1, b"B:"), (4, 0, 1, b"rows"), (5, -3, 1, b"rows"),
-                              (6, 0, 1, b"columns"), (7, 2, 1, b"aligned"), (8, 9, 2, b"dtype"), (9, None, 1, b"null"), (9, (5 << 20) + 1, 1, b"aligned"),
-                              (10, 255, 1, b"ldc"), (9, 1 << 20, 1, b"alias"), (11, 8, 1, b"aligned"), (12, 16, 3, b"workspace")):
+                              (6, 0, 1, b"columns"), (6, (1 << 24) + 1, 1, b"2^24"), (7, 2, 1, b"aligned"), (8, 9, 2, b"dtype"), (9, None, 1, b"null"),
+                              (9, (5 << 20) + 1, 1, b"aligned"), (10, 255, 1, b"ldc"), (9, 1 << 20, 1, b"alias")):
         args = list(ok)
         args[at] = v
         assert lib.svg2_matmul_mxfp4(*args) == code, (at, v)
         assert word in lib.svg2_last_error(), (at, v, lib.svg2_last_error())
-    assert lib.svg2_matmul_mxfp4(1 << 20, 2 << 20, 3 << 20, 4 << 20, 1 << 21, 1 << 21, 512, None, 1, 5 << 20, 1 << 21, 256, 1 << 40, None) == 1
+    assert lib.svg2_matmul_mxfp4(1 << 20, 2 << 20, 3 << 20, 4 << 20, 1 << 21, 1 << 21, 512, None, 1, 5 << 20, 1 << 21, None) == 1
     assert b"tiles" in lib.svg2_last_error()
-    assert lib.svg2_matmul_mxfp4_workspace_size(0, 4, 4) == 256
-    assert lib.svg2_matmul_mxfp4_workspace_size(75600, 5120, 5120) >= 256
 
 
 def test_bindings_refuse(lib):
