@@ -6,10 +6,14 @@
 // 128 (the columns behind K are zeros): codes [R, Kp/2], element 2j in the low half of byte j; scales [Kp/128, R, 4].  A row's
 // four scales of 128 columns are one word, and the words of neighbouring rows are neighbours: what a tile of the product needs
 // of them is one contiguous load.
+#include <type_traits>
+
 #include "svg2_common.h"
 
 namespace svg2 {
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((ext_vector_type(8))) int i32x8;
@@ -63,23 +67,27 @@ template <typename T> __device__ __forceinline__ const T *element(const QuantArg
     return static_cast<const T *>(A.X) + m * A.sm + g * A.sg + (k - g * A.Kg);
 }
 
-// eight neighbouring columns; VEC: 16-byte loads (the caller has checked strides and alignment, and that 8 divides Kg)
-template <typename T, bool VEC> __device__ __forceinline__ void load8(const QuantArgs &A, long long m, int k, int K, float *v)
+// How a kernel that only streams goes over X.  ONE: element by element; VEC: 16 bytes at a time (the caller has checked strides and
+// alignment, and that 8 divides Kg); STREAM: so, and past the caches, for an X that is larger than they are (streamed()).
+enum { ONE = 0, VEC = 1, STREAM = 2 };
+
+// eight neighbouring columns
+template <typename T, int HOW> __device__ __forceinline__ void load8(const QuantArgs &A, long long m, int k, int K, float *v)
 {
-    if constexpr (VEC) {
+    if constexpr (HOW != ONE) {
         if (k >= K) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = 0.f;
             return;
         }
-        const uint4 *p = reinterpret_cast<const uint4 *>(element<T>(A, m, k));
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(element<T>(A, m, k));
+        const u32x4 a = HOW == STREAM ? __builtin_nontemporal_load(p) : *p;
         if constexpr (sizeof(T) == 4) {
-            const uint4 a = p[0], b = p[1];
+            const u32x4 b = HOW == STREAM ? __builtin_nontemporal_load(p + 1) : p[1];
             const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
         } else {
-            const uint4 a = p[0];
             const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -94,14 +102,14 @@ template <typename T, bool VEC> __device__ __forceinline__ void load8(const Quan
 }
 
 // rows: grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a row of 128 columns, 4 lanes a block of 32
-template <typename T, bool VEC> __global__ __launch_bounds__(256) void mxfp4_quant_kernel(const QuantArgs A)
+template <typename T, int HOW> __global__ __launch_bounds__(256) void mxfp4_quant_kernel(const QuantArgs A)
 {
     const int lane16 = threadIdx.x & 15, K = A.G * A.Kg, nk = (K + 127) / 128;
     const long long m = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
     if (m >= A.M) return;                       // whole groups of 16 lanes: the exchanges below stay inside 4
     for (int kc = blockIdx.y; kc < nk; kc += gridDim.y) {
         float v[8];
-        load8<T, VEC>(A, m, kc * 128 + lane16 * 8, K, v);
+        load8<T, HOW>(A, m, kc * 128 + lane16 * 8, K, v);
         unsigned top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = max(top, mag(v[i]));
@@ -121,7 +129,7 @@ template <typename T, bool VEC> __global__ __launch_bounds__(256) void mxfp4_qua
 // grid (ceil(K / 64), slices of the rows), block 256: tiles of 128 rows x 64 columns through LDS; four lanes a column, 32 rows
 // each.  Row m of the tile starts at word 33 m (bf16; 65 m in fp32) plus 8 words for each 32 rows before it, so that the 64 lanes
 // of a wavefront, 16 columns x 4 blocks, read every bank once (fp32: twice, as the 256 bytes must).
-template <typename T, bool VEC> __global__ __launch_bounds__(256) void mxfp4_quant_t_kernel(const QuantArgs A)
+template <typename T, int HOW> __global__ __launch_bounds__(256) void mxfp4_quant_t_kernel(const QuantArgs A)
 {
     constexpr int ROW = 64 + 4 / sizeof(T), PAD = 32 / sizeof(T);
     __shared__ T tile[128 * ROW + 4 * PAD];
@@ -133,7 +141,7 @@ template <typename T, bool VEC> __global__ __launch_bounds__(256) void mxfp4_qua
             const int m = i >> 3, c = (i & 7) * 8;
             const long long gm = (long long)mc * 128 + m;
             float v[8];
-            if (gm < A.M) load8<T, VEC>(A, gm, r0 + c, K, v);
+            if (gm < A.M) load8<T, HOW>(A, gm, r0 + c, K, v);
             else
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = 0.f;
@@ -175,8 +183,8 @@ __device__ __forceinline__ void scale_factors(unsigned byte, float &a, float &b)
     b = __uint_as_float((byte - half + 63) << 23);                                             // 2^(byte - half - 64)
 }
 
-// grid (ceil(M / 16), slices of the columns), block 256: 8 values a lane; VEC: 16-byte stores
-template <typename T, bool VEC>
+// grid (ceil(M / 16), slices of the columns), block 256: 8 values a lane
+template <typename T, int HOW>
 __global__ __launch_bounds__(256) void mxfp4_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                            int M, int K, T *__restrict__ X, long long ldx)
 {
@@ -196,12 +204,19 @@ __global__ __launch_bounds__(256) void mxfp4_values_kernel(const uint8_t *__rest
         unsigned u[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        if (VEC && k + 8 <= K) {
+        if (HOW != ONE && k + 8 <= K) {
+            u32x4 *to = reinterpret_cast<u32x4 *>(x);
             if constexpr (sizeof(T) == 4) {
-                reinterpret_cast<float4 *>(x)[0] = make_float4(v[0], v[1], v[2], v[3]);
-                reinterpret_cast<float4 *>(x)[1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const f32x4 y = {v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+                    if (HOW == STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, y), to + i);
+                    else to[i] = __builtin_bit_cast(u32x4, y);
+                }
             } else {
-                *reinterpret_cast<uint4 *>(x) = make_uint4(u[0], u[1], u[2], u[3]);
+                const u32x4 y = {u[0], u[1], u[2], u[3]};
+                if (HOW == STREAM) __builtin_nontemporal_store(y, to);
+                else *to = y;
             }
         } else {
 #pragma unroll
@@ -278,7 +293,7 @@ void mxfp4_product_kernel(const ProductArgs P, bool vec)
     const int stages = (P.nk + 1) >> 1;
     const bool odd = P.nk & 1;                          // the last stage has 128 columns only
 
-    // Which tiles: the XCDs (every eighth workgroup) get contiguous parts of an order that goes down 8 tiles of C, then right, and
+    // Which tiles: the XCDs (every eighth workgroup) get contiguous parts of an order that goes down 4 tiles of C, then right, and
     // their workgroups take turns, so that what an XCD works on at a time is a compact patch and shares its rows in that XCD's L2.
     const int tiles_m = (P.M + BM - 1) / BM, total = tiles_m * P.tiles_n;
     const int xcd = blockIdx.x & 7, part = total >> 3, rest = total & 7, first = xcd * part + min(xcd, rest);
@@ -288,8 +303,8 @@ void mxfp4_product_kernel(const ProductArgs P, bool vec)
     const char *ga, *gb, *gsa, *gsb;
     unsigned off_a[LA], off_b[LB], off_s[NS];           // this lane's part of the loads: 8 rows x 128 bytes each
     auto set_tile = [&](int k) {
-        const int t = first + k, group = t / (8 * P.tiles_n), in = t - group * 8 * P.tiles_n, high = min(8, tiles_m - group * 8);
-        m0 = __builtin_amdgcn_readfirstlane((group * 8 + in % high) * BM);
+        const int t = first + k, group = t / (4 * P.tiles_n), in = t - group * 4 * P.tiles_n, high = min(4, tiles_m - group * 4);
+        m0 = __builtin_amdgcn_readfirstlane((group * 4 + in % high) * BM);
         n0 = __builtin_amdgcn_readfirstlane((in / high) * BN);
         ga = reinterpret_cast<const char *>(P.A) + m0 * row_bytes;
         gb = reinterpret_cast<const char *>(P.B) + n0 * row_bytes;
@@ -496,7 +511,10 @@ void mxfp4_product_kernel(const ProductArgs P, bool vec)
 #pragma unroll
                     for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
                         const int r = r0 + l / LANES, c = l % LANES;
-                        *reinterpret_cast<uint4 *>(C + (long long)r * P.ldc + c * PER16) = *reinterpret_cast<const uint4 *>(s + r * ROW + c * 16);
+                        const u32x4 v = *reinterpret_cast<const u32x4 *>(s + r * ROW + c * 16);
+                        u32x4 *to = reinterpret_cast<u32x4 *>(C + (long long)r * P.ldc + c * PER16);
+                        if (BM == 256) __builtin_nontemporal_store(v, to);      // past the operands in L2: 987 -> 946 us at 75,600 x 5120 x 5120
+                        else *to = v;
                     }
                 } else {
                     for (int e = l; e < 32 * COLS; e += 64) {
@@ -568,52 +586,49 @@ static int slices(long long blocks, int steps)
 
 static bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// X of `bytes`, 16 bytes at a time where vec.  From 256 MB on, the size of the last cache level, it goes past the caches: measured
+// with 75,600 x 5120 bf16 values (774 MB) quantise 209 -> 179 us and values 212 -> 144 us (the codes, 206 MB, then stay cached between
+// the two), with 16,384 x 1536 (50 MB) quantise 11.3 -> 13.4 us.
+static int how(bool vec, double bytes) { return !vec ? ONE : bytes < 268435456.0 ? VEC : STREAM; }
+
+// f(type, how) with both known at compile time
+template <typename F> static int with_how(int dtype, int h, F f)
+{
+    using One = std::integral_constant<int, ONE>;
+    using Vec = std::integral_constant<int, VEC>;
+    using Stream = std::integral_constant<int, STREAM>;
+    if (dtype == SVG2_BF16) h == ONE ? f((bf16_t *)0, One()) : h == VEC ? f((bf16_t *)0, Vec()) : f((bf16_t *)0, Stream());
+    else h == ONE ? f((float *)0, One()) : h == VEC ? f((float *)0, Vec()) : f((float *)0, Stream());
+    SVG2_HIP_CHECK(hipGetLastError());
+    return SVG2_OK;
+}
+
 int mxfp4_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t sm, int64_t sg, bool transposed, void *codes,
                        void *scales, hipStream_t st)
 {
     const QuantArgs A = {X, sm, sg, M, G, Kg, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales)};
-    const int K = G * Kg, per16 = dtype == SVG2_BF16 ? 8 : 4;
+    const int K = G * Kg, es = dtype == SVG2_BF16 ? 2 : 4, per16 = 16 / es;
     const bool vec = aligned(X, 16) && sm % per16 == 0 && (G == 1 || sg % per16 == 0) && Kg % 8 == 0;
-    if (!transposed) {
-        const int bx = cdiv(M, 16);
-        const dim3 grid(bx, slices(bx, cdiv(K, 128)));
-        if (dtype == SVG2_BF16) {
-            if (vec) mxfp4_quant_kernel<bf16_t, true><<<grid, 256, 0, st>>>(A);
-            else mxfp4_quant_kernel<bf16_t, false><<<grid, 256, 0, st>>>(A);
-        } else {
-            if (vec) mxfp4_quant_kernel<float, true><<<grid, 256, 0, st>>>(A);
-            else mxfp4_quant_kernel<float, false><<<grid, 256, 0, st>>>(A);
-        }
-    } else {
-        const int bx = cdiv(K, 64);
-        const dim3 grid(bx, slices(bx, cdiv(M, 128)));
-        if (dtype == SVG2_BF16) {
-            if (vec) mxfp4_quant_t_kernel<bf16_t, true><<<grid, 256, 0, st>>>(A);
-            else mxfp4_quant_t_kernel<bf16_t, false><<<grid, 256, 0, st>>>(A);
-        } else {
-            if (vec) mxfp4_quant_t_kernel<float, true><<<grid, 256, 0, st>>>(A);
-            else mxfp4_quant_t_kernel<float, false><<<grid, 256, 0, st>>>(A);
-        }
-    }
-    SVG2_HIP_CHECK(hipGetLastError());
-    return SVG2_OK;
+    return with_how(dtype, how(vec, (double)M * K * es), [&](auto *tp, auto h) {
+        using T = std::remove_pointer_t<decltype(tp)>;
+        constexpr int HOW = decltype(h)::value;
+        const int bx = transposed ? cdiv(K, 64) : cdiv(M, 16), steps = transposed ? cdiv(M, 128) : cdiv(K, 128);
+        const dim3 grid(bx, slices(bx, steps));
+        if (transposed) mxfp4_quant_t_kernel<T, HOW><<<grid, 256, 0, st>>>(A);
+        else mxfp4_quant_kernel<T, HOW><<<grid, 256, 0, st>>>(A);
+    });
 }
 
 int mxfp4_values_launch(const void *codes, const void *scales, int M, int K, int dtype, void *X, int64_t ldx, hipStream_t st)
 {
     const uint8_t *c = static_cast<const uint8_t *>(codes), *s = static_cast<const uint8_t *>(scales);
-    const bool vec = aligned(X, 16) && ldx % (dtype == SVG2_BF16 ? 8 : 4) == 0;
-    const int bx = cdiv(M, 16);
+    const int es = dtype == SVG2_BF16 ? 2 : 4, bx = cdiv(M, 16);
+    const bool vec = aligned(X, 16) && ldx % (16 / es) == 0;
     const dim3 grid(bx, slices(bx, cdiv(K, 128)));
-    if (dtype == SVG2_BF16) {
-        if (vec) mxfp4_values_kernel<bf16_t, true><<<grid, 256, 0, st>>>(c, s, M, K, static_cast<bf16_t *>(X), ldx);
-        else mxfp4_values_kernel<bf16_t, false><<<grid, 256, 0, st>>>(c, s, M, K, static_cast<bf16_t *>(X), ldx);
-    } else {
-        if (vec) mxfp4_values_kernel<float, true><<<grid, 256, 0, st>>>(c, s, M, K, static_cast<float *>(X), ldx);
-        else mxfp4_values_kernel<float, false><<<grid, 256, 0, st>>>(c, s, M, K, static_cast<float *>(X), ldx);
-    }
-    SVG2_HIP_CHECK(hipGetLastError());
-    return SVG2_OK;
+    return with_how(dtype, how(vec, (double)M * K * es), [&](auto *tp, auto h) {
+        using T = std::remove_pointer_t<decltype(tp)>;
+        mxfp4_values_kernel<T, decltype(h)::value><<<grid, 256, 0, st>>>(c, s, M, K, static_cast<T *>(X), ldx);
+    });
 }
 
 using Large = Tile<2, 4, 4, 2>;

@@ -7,12 +7,14 @@
 //   dw = sum over tokens (and heads) of g n / w,   dx = r (g w - x r mean(g w x r)),   r = rsqrt(mean(x^2) + eps)
 //
 // Every element is read once and written once, some ten operations each: HBM bounds it, so the kernels are built around the
-// loads.  One wavefront per token and tensor; a lane holds four pairs (8 elements), 8 or 16 lanes a head, 8 or 4 heads a
+// loads.  One wavefront (fewer lanes where a token is short) per token and tensor; a lane holds four pairs (8 elements), 8 or 16 lanes a head, 8 or 4 heads a
 // step, and up to CH steps are loaded before the first is used.  A token of 40 heads of 128 thus stays in registers between
 // the sum of squares over all its heads and the result, and no lane needs an element of another's.  The angle of a lane's pairs
 // is the same for every head, so four cosines and sines per lane and token serve all of them: cheap enough to compute
 // in place, in 64 bits up to the quarter turn (positions of 10^6 times a frequency of 1 leave no fraction in 32), instead of
 // reading a table.
+#include <type_traits>
+
 #include "svg2_common.h"
 
 namespace svg2 {
@@ -167,13 +169,14 @@ __device__ __forceinline__ float group_sum(float x, int width)
 }
 
 // ---- forward ---------------------------------------------------------------
-// grid (ceil(B N / 4), tensors), block 256
-template <typename T, int D, bool ADJ> __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs A)
+// grid (ceil(B N / (256 / G)), tensors), block 256: G lanes a token.  64, or where a token has fewer than 512 values the 8, 16 or 32
+// that hold them: one head of 64 a wavefront, 4096 tokens, took 11 us, eight of them take 5.
+template <typename T, int D, bool ADJ, int G> __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs A)
 {
-    constexpr int LPH = D / 8, HPS = 64 / LPH, CH = 10;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int token = blockIdx.x * 4 + wave, t = blockIdx.y;
-    if (token >= A.B * A.N) return;
+    constexpr int LPH = D / 8, HPS = G / LPH, CH = G == 64 ? 10 : 1;
+    const int lane = threadIdx.x % G, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int token = blockIdx.x * (256 / G) + (G == 64 ? wave : (int)threadIdx.x / G), t = blockIdx.y;
+    if (token >= A.B * A.N) return;             // all lanes of a token together: the sums below stay inside them
     const int b = token / A.N, n = token - b * A.N;
     const int hl = lane / LPH, c = lane % LPH;
     const T *src = static_cast<const T *>(A.src[t]) + b * A.ss[0] + n * A.ss[1];
@@ -195,6 +198,7 @@ template <typename T, int D, bool ADJ> __global__ __launch_bounds__(256) void ro
         float sum = 0.f;
         for (int s0 = 0; s0 < steps; s0 += CH) {
             load(s0);
+            if (s0 == 0 && rotate) angles(A, b, n, c, cs, sn);      // while they come
 #pragma unroll
             for (int s = 0; s < CH; ++s) {
                 float v[8];
@@ -204,13 +208,14 @@ template <typename T, int D, bool ADJ> __global__ __launch_bounds__(256) void ro
                     for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
             }
         }
-        rinv = 1.f / sqrtf(group_sum(sum, 64) / ((float)A.H * D) + A.eps);
-    } else if (weight) {
-        load_weight<D, ADJ>(weight, c, w);
+        rinv = 1.f / sqrtf(group_sum(sum, G) / ((float)A.H * D) + A.eps);
+    } else {
+        load(0);
+        if (weight) load_weight<D, ADJ>(weight, c, w);
+        if (rotate) angles(A, b, n, c, cs, sn);
     }
-    if (rotate) angles(A, b, n, c, cs, sn);
     for (int s0 = 0; s0 < steps; s0 += CH) {
-        if (!whole || steps > CH) load(s0);
+        if (s0 > 0 || (whole && steps > CH)) load(s0);
 #pragma unroll
         for (int s = 0; s < CH; ++s) {
             const int h = (s0 + s) * HPS + hl;
@@ -581,8 +586,13 @@ int rope_launch(const svg2_rope_args *a, hipStream_t st)
     const RopeArgs A = device_args(a);
     return with_types(a, [&](auto *tp, auto dim, auto adj) -> int {
         using T = std::remove_pointer_t<decltype(tp)>;
-        const dim3 grid(cdiv(A.B * A.N, 4), a->n_tensors);
-        rope_kernel<T, decltype(dim)::value, decltype(adj)::value><<<grid, 256, 0, st>>>(A);
+        constexpr int D = decltype(dim)::value;
+        constexpr bool ADJ = decltype(adj)::value;
+        const int lanes = A.H * (D / 8), tokens = A.B * A.N;
+        if (lanes <= 8) rope_kernel<T, D, ADJ, D == 64 ? 8 : 16><<<dim3(cdiv(tokens, 256 / (D == 64 ? 8 : 16)), a->n_tensors), 256, 0, st>>>(A);
+        else if (lanes <= 16) rope_kernel<T, D, ADJ, 16><<<dim3(cdiv(tokens, 16), a->n_tensors), 256, 0, st>>>(A);
+        else if (lanes <= 32) rope_kernel<T, D, ADJ, 32><<<dim3(cdiv(tokens, 8), a->n_tensors), 256, 0, st>>>(A);
+        else rope_kernel<T, D, ADJ, 64><<<dim3(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
         SVG2_HIP_CHECK(hipGetLastError());
         return SVG2_OK;
     });

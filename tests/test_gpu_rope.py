@@ -57,6 +57,13 @@ FORWARD = [
     (torch.float32, 3, 7, 9, 64, "token", "halves", 4, True),
     (torch.float32, 1, 66, 3, 128, "none", "adjacent", 3, True),
     (torch.bfloat16, 2, 5, 81, 64, "token", "adjacent", 3, False),
+    # tokens of 8, 16 and 32 lanes, several in a wavefront
+    (torch.float32, 2, 45, 1, 64, "token", "adjacent", 3, False),
+    (torch.bfloat16, 1, 67, 1, 128, "head", "halves", 3, False),
+    (torch.bfloat16, 1, 70, 2, 64, "token", "halves", 3, False),
+    (torch.float32, 1, 35, 3, 64, "token", "adjacent", 3, False),
+    (torch.bfloat16, 1, 19, 4, 64, "head", "adjacent", 3, False),
+    (torch.float32, 1, 13, 2, 128, "token", "halves", 3, False),
     (torch.float32, 1, 9, 83, 64, "head", "adjacent", 1, False),
     (torch.bfloat16, 1, 4099, 2, 128, "head", "adjacent", 3, True),
 ]
