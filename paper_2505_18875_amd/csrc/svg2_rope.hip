@@ -171,9 +171,9 @@ __device__ __forceinline__ float group_sum(float x, int width)
 // ---- forward ---------------------------------------------------------------
 // grid (ceil(B N / (256 / G)), tensors), block 256: G lanes a token.  64, or where a token has fewer than 512 values the 8, 16 or 32
 // that hold them: one head of 64 a wavefront, 4096 tokens, took 11 us, eight of them take 5.
-template <typename T, int D, bool ADJ, int G> __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs A)
+template <typename T, int D, bool ADJ, int G, int CH> __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs A)
 {
-    constexpr int LPH = D / 8, HPS = G / LPH, CH = G == 64 ? 10 : 1;
+    constexpr int LPH = D / 8, HPS = G / LPH;
     const int lane = threadIdx.x % G, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int token = blockIdx.x * (256 / G) + (G == 64 ? wave : (int)threadIdx.x / G), t = blockIdx.y;
     if (token >= A.B * A.N) return;             // all lanes of a token together: the sums below stay inside them
@@ -240,6 +240,75 @@ template <typename T, int D, bool ADJ, int G> __global__ __launch_bounds__(256) 
             }
             if (h < A.H) store_pairs<T, D, ADJ>(dst + h * A.ds[2], c, raw[s]);
         }
+    }
+}
+
+// Long tokens, not too many: grid (B N, tensors), block 256.  A workgroup takes a token, S steps of 2048 values, so that everything it reads is
+// asked for at once; its angles, one a thread, and the sum of squares go round through LDS.
+// Measured, us for Q, K and V of 40 heads of 128, this kernel / rope_kernel: 1 token 3.8 / 7.5, 256: 5.2 / 8.9, 1024: 11.5 / 15.2,
+// 4096: 38 / 43, 16,384: 205 / 202, 75,600: 938 / 862; 32 heads, 8192 tokens: 77 / 84.
+template <typename T, int D, bool ADJ, int S> __global__ __launch_bounds__(256) void rope_row_kernel(const RopeArgs A)
+{
+    constexpr int LPH = D / 8, HPS = 256 / LPH;
+    __shared__ __attribute__((aligned(16))) float s_cs[D / 2], s_sn[D / 2];
+    __shared__ float s_sum[4];
+    const int tid = threadIdx.x, token = blockIdx.x, t = blockIdx.y, hl = tid / LPH, c = tid % LPH;
+    const int b = token / A.N, n = token - b * A.N;
+    const T *src = static_cast<const T *>(A.src[t]) + b * A.ss[0] + n * A.ss[1];
+    T *dst = static_cast<T *>(A.dst[t]) + b * A.ds[0] + n * A.ds[1];
+    const float *weight = A.weight[t];
+    const bool rotate = (A.rotate >> t) & 1;
+    Raw<T> raw[S];
+    float w[S][8], sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int h = s * HPS + hl;
+        if (h >= A.H) continue;
+        raw[s] = load_pairs<T, D, ADJ>(src + h * A.ss[2], c);
+        if (weight) load_weight<D, ADJ>(weight + (A.token_scope ? h * D : 0), c, w[s]);
+    }
+    if (rotate && tid < D / 2) angle(A, position(A, b, n), tid, s_cs[tid], s_sn[tid]);
+    if (weight && A.token_scope) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            float v[8];
+            decode(raw[s], v);
+            if (s * HPS + hl < A.H)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum = fmaf(v[k], v[k], sum);
+        }
+        sum = group_sum(sum, 64);
+        if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
+    }
+    __syncthreads();
+    float cs[4], sn[4], rinv = 1.f;
+    if (weight && A.token_scope) rinv = 1.f / sqrtf(((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])) / ((float)A.H * D) + A.eps);
+    if (rotate) {
+        const float4 u = *reinterpret_cast<const float4 *>(&s_cs[4 * c]), v = *reinterpret_cast<const float4 *>(&s_sn[4 * c]);
+        cs[0] = u.x; cs[1] = u.y; cs[2] = u.z; cs[3] = u.w;
+        sn[0] = v.x; sn[1] = v.y; sn[2] = v.z; sn[3] = v.w;
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        const int h = s * HPS + hl;
+        if (h >= A.H) continue;                 // whole heads: the sum below stays inside one
+        if (weight || rotate) {
+            float v[8];
+            decode(raw[s], v);
+            if (weight) {
+                if (!A.token_scope) {
+                    float x2 = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x2 = fmaf(v[k], v[k], x2);
+                    rinv = 1.f / sqrtf(group_sum(x2, LPH) * (1.f / D) + A.eps);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = v[k] * rinv * w[s][k];
+            }
+            if (rotate) turn<ADJ>(v, cs, sn, 1.f);
+            raw[s] = encode<T>(v);
+        }
+        store_pairs<T, D, ADJ>(dst + h * A.ds[2], c, raw[s]);
     }
 }
 
@@ -589,10 +658,14 @@ int rope_launch(const svg2_rope_args *a, hipStream_t st)
         constexpr int D = decltype(dim)::value;
         constexpr bool ADJ = decltype(adj)::value;
         const int lanes = A.H * (D / 8), tokens = A.B * A.N;
-        if (lanes <= 8) rope_kernel<T, D, ADJ, D == 64 ? 8 : 16><<<dim3(cdiv(tokens, 256 / (D == 64 ? 8 : 16)), a->n_tensors), 256, 0, st>>>(A);
-        else if (lanes <= 16) rope_kernel<T, D, ADJ, 16><<<dim3(cdiv(tokens, 16), a->n_tensors), 256, 0, st>>>(A);
-        else if (lanes <= 32) rope_kernel<T, D, ADJ, 32><<<dim3(cdiv(tokens, 8), a->n_tensors), 256, 0, st>>>(A);
-        else rope_kernel<T, D, ADJ, 64><<<dim3(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
+        if (lanes <= 8) rope_kernel<T, D, ADJ, D == 64 ? 8 : 16, 1><<<dim3(cdiv(tokens, 256 / (D == 64 ? 8 : 16)), a->n_tensors), 256, 0, st>>>(A);
+        else if (lanes <= 16) rope_kernel<T, D, ADJ, 16, 1><<<dim3(cdiv(tokens, 16), a->n_tensors), 256, 0, st>>>(A);
+        else if (lanes <= 32) rope_kernel<T, D, ADJ, 32, 1><<<dim3(cdiv(tokens, 8), a->n_tensors), 256, 0, st>>>(A);
+        else if (lanes <= 128) rope_kernel<T, D, ADJ, 64, 2><<<dim3(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
+        // more than two steps of a wavefront: a workgroup a token, up to where both are bound by memory
+        else if (tokens <= 8192 && lanes <= 256) rope_row_kernel<T, D, ADJ, 1><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
+        else if (tokens <= 8192 && lanes <= 768) rope_row_kernel<T, D, ADJ, 3><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
+        else rope_kernel<T, D, ADJ, 64, 10><<<dim3(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
         SVG2_HIP_CHECK(hipGetLastError());
         return SVG2_OK;
     });

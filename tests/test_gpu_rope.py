@@ -54,9 +54,20 @@ FORWARD = [
     (torch.bfloat16, 2, 37, 5, 64, "head", "halves", 3, False),
     (torch.bfloat16, 1, 33, 40, 128, "token", "adjacent", 3, False),
     (torch.bfloat16, 1, 18, 41, 128, "token", "halves", 2, False),
+    (torch.bfloat16, 1, 8201, 17, 64, "token", "adjacent", 3, False),       # many tokens of more than two steps, a wavefront each
+    (torch.float32, 1, 8195, 9, 128, "head", "halves", 3, False),
     (torch.float32, 3, 7, 9, 64, "token", "halves", 4, True),
     (torch.float32, 1, 66, 3, 128, "none", "adjacent", 3, True),
     (torch.bfloat16, 2, 5, 81, 64, "token", "adjacent", 3, False),
+    (torch.bfloat16, 2, 7, 97, 64, "token", "halves", 3, False),            # a token that takes two rounds of a wavefront
+    (torch.float32, 1, 6, 131, 128, "head", "adjacent", 3, False),
+    # long tokens, a workgroup each
+    (torch.bfloat16, 1, 1, 40, 128, "token", "adjacent", 3, True),
+    (torch.float32, 2, 3, 17, 64, "token", "halves", 3, False),
+    (torch.bfloat16, 2, 128, 32, 64, "head", "adjacent", 3, False),
+    (torch.bfloat16, 1, 257, 33, 64, "head", "halves", 3, False),
+    (torch.float32, 1, 5, 48, 128, "none", "halves", 2, False),
+    (torch.bfloat16, 1, 3, 49, 128, "token", "adjacent", 3, False),
     # tokens of 8, 16 and 32 lanes, several in a wavefront
     (torch.float32, 2, 45, 1, 64, "token", "adjacent", 3, False),
     (torch.bfloat16, 1, 67, 1, 128, "head", "halves", 3, False),
