@@ -419,7 +419,7 @@ int svg2_rope_backward(const svg2_rope_args *args, const void *const *dY, void *
  * an ordinary matrix; the layer's O [H,N,d] is M = N, G = H, Kg = d with strides (d, N*d)).
  *   transposed = 0: operand of M rows, K columns; transposed != 0: operand of K rows, M columns (X^T, blocks along the rows of
  *   X), which is what a gradient's product contracts.
- * Any strides and alignment of X (16-byte aligned rows of a multiple of 8 columns are read fastest).
+ * Any strides of X, any address that its elements may have.
  * svg2_dequantize_mxfp4: the values of an operand, exactly, into X [R,K] dtype with row stride ldx >= K.
  *
  * svg2_matmul_mxfp4: C [M,N] = A B^T + bias for operands A (M rows) and B (N rows) of K columns; out_dtype is the type of C,

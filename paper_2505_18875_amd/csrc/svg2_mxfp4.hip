@@ -13,7 +13,7 @@
 namespace svg2 {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));     // 16 bytes at any element's address: one load or store all the same
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((ext_vector_type(8))) int i32x8;
@@ -67,23 +67,15 @@ template <typename T> __device__ __forceinline__ const T *element(const QuantArg
     return static_cast<const T *>(A.X) + m * A.sm + g * A.sg + (k - g * A.Kg);
 }
 
-// How a kernel that only streams goes over X.  ONE: element by element; VEC: 16 bytes at a time (the caller has checked strides and
-// alignment, and that 8 divides Kg); STREAM: so, and past the caches, for an X that is larger than they are (streamed()).
-enum { ONE = 0, VEC = 1, STREAM = 2 };
-
-// eight neighbouring columns
-template <typename T, int HOW> __device__ __forceinline__ void load8(const QuantArgs &A, long long m, int k, int K, float *v)
+// eight neighbouring columns: one load where they are all there and in one group, whatever their address; STREAM: past the caches,
+// for an X that is larger than they are (streamed())
+template <typename T, bool STREAM> __device__ __forceinline__ void load8(const QuantArgs &A, long long m, int k, int K, float *v)
 {
-    if constexpr (HOW != ONE) {
-        if (k >= K) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
-            return;
-        }
-        const u32x4 *p = reinterpret_cast<const u32x4 *>(element<T>(A, m, k));
-        const u32x4 a = HOW == STREAM ? __builtin_nontemporal_load(p) : *p;
+    if (k + 8 <= K && (A.G == 1 || k % A.Kg + 8 <= A.Kg)) {
+        const u32x4_any *p = reinterpret_cast<const u32x4_any *>(element<T>(A, m, k));
+        const u32x4 a = STREAM ? __builtin_nontemporal_load(p) : *p;
         if constexpr (sizeof(T) == 4) {
-            const u32x4 b = HOW == STREAM ? __builtin_nontemporal_load(p + 1) : p[1];
+            const u32x4 b = STREAM ? __builtin_nontemporal_load(p + 1) : p[1];
             const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
@@ -102,14 +94,14 @@ template <typename T, int HOW> __device__ __forceinline__ void load8(const Quant
 }
 
 // rows: grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a row of 128 columns, 4 lanes a block of 32
-template <typename T, int HOW> __global__ __launch_bounds__(256) void mxfp4_quant_kernel(const QuantArgs A)
+template <typename T, bool STREAM> __global__ __launch_bounds__(256) void mxfp4_quant_kernel(const QuantArgs A)
 {
     const int lane16 = threadIdx.x & 15, K = A.G * A.Kg, nk = (K + 127) / 128;
     const long long m = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
     if (m >= A.M) return;                       // whole groups of 16 lanes: the exchanges below stay inside 4
     for (int kc = blockIdx.y; kc < nk; kc += gridDim.y) {
         float v[8];
-        load8<T, HOW>(A, m, kc * 128 + lane16 * 8, K, v);
+        load8<T, STREAM>(A, m, kc * 128 + lane16 * 8, K, v);
         unsigned top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = max(top, mag(v[i]));
@@ -126,49 +118,55 @@ template <typename T, int HOW> __global__ __launch_bounds__(256) void mxfp4_quan
 }
 
 // transposed: the rows of the result are the columns of X, blocks run along the rows of X.
-// grid (ceil(K / 64), slices of the rows), block 256: tiles of 128 rows x 64 columns through LDS; four lanes a column, 32 rows
-// each.  Row m of the tile starts at word 33 m (bf16; 65 m in fp32) plus 8 words for each 32 rows before it, so that the 64 lanes
-// of a wavefront, 16 columns x 4 blocks, read every bank once (fp32: twice, as the 256 bytes must).
-template <typename T, int HOW> __global__ __launch_bounds__(256) void mxfp4_quant_t_kernel(const QuantArgs A)
+// grid (ceil(K / 64) rounded up to 8, slices of the rows), block 256: tiles of 128 rows x 64 columns through LDS; four lanes a column,
+// 32 rows each.  A slice is `per` neighbouring tiles, an even number: two of them fill a cache line of codes.  Neighbouring columns go to
+// the same XCD (every eighth workgroup): where rows are not whole lines they share some.
+// In LDS a row takes 33 words in bf16 (65 in fp32), and 8 words more for each 32 rows before it, so that the 64 lanes of a wavefront,
+// 16 columns x 4 blocks, read every bank once (fp32: twice, as the 256 bytes must).
+template <typename T> __global__ __launch_bounds__(256) void mxfp4_quant_t_kernel(const QuantArgs A, int per)
 {
-    constexpr int ROW = 64 + 4 / sizeof(T), PAD = 32 / sizeof(T);
-    __shared__ T tile[128 * ROW + 4 * PAD];
-    const int K = A.G * A.Kg, nm = (A.M + 127) / 128, r0 = blockIdx.x * 64;
-    const int rr = threadIdx.x >> 2, mb = threadIdx.x & 3;          // phase 2: column, block of 32 rows
-    for (int mc = blockIdx.y; mc < nm; mc += gridDim.y) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < 128 * 8; i += 256) {
-            const int m = i >> 3, c = (i & 7) * 8;
-            const long long gm = (long long)mc * 128 + m;
-            float v[8];
-            if (gm < A.M) load8<T, HOW>(A, gm, r0 + c, K, v);
+    constexpr int WORDS = 16 * (int)sizeof(T) + 1, PAD = 8;
+    __shared__ unsigned tile[128 * WORDS + 4 * PAD];
+    const int K = A.G * A.Kg, nm = (A.M + 127) / 128, r0 = ((blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3)) * 64;
+    const int from = blockIdx.y * per, end = r0 < K ? min(nm, from + per) : from;
+    const int rr = threadIdx.x >> 2, mb = threadIdx.x & 3;          // column and block of 32 rows
+    for (int mc = from; mc < end; ++mc) {
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const long long m = (long long)mc * 128 + i * 32 + (threadIdx.x >> 3);
+            if (m < A.M) load8<T, false>(A, m, r0 + (threadIdx.x & 7) * 8, K, v[i]);
             else
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = 0.f;
-            T *row = tile + m * ROW + (m >> 5) * PAD + c;
+                for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+        }
+        __syncthreads();                        // the last tile has been read
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            unsigned *w = tile + (i * 32 + (threadIdx.x >> 3)) * WORDS + i * PAD + (threadIdx.x & 7) * 2 * (int)sizeof(T);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if constexpr (sizeof(T) == 4) row[e] = v[e];
-                else row[e] = (bf16_t)(__float_as_uint(v[e]) >> 16);
+                if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(v[i][e]);
+                else if (e & 1) w[e >> 1] = (__float_as_uint(v[i][e]) & 0xFFFF0000u) | (__float_as_uint(v[i][e - 1]) >> 16);
             }
         }
         __syncthreads();
-        float v[32];
+        float x[32];
         unsigned top = 0;
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
-            v[e] = to_f32(tile[(mb * 32 + e) * ROW + mb * PAD + rr]);
-            top = max(top, mag(v[e]));
+            x[e] = to_f32(reinterpret_cast<const T *>(tile + (mb * 32 + e) * WORDS + mb * PAD)[rr]);
+            top = max(top, mag(x[e]));
         }
         float inv;
         const unsigned byte = block_scale(top, inv);
         if (byte == 255)
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] = 0.f;
-        if (r0 + rr < K) {
-            const long long r = r0 + rr;
+            for (int e = 0; e < 32; ++e) x[e] = 0.f;
+        const long long r = r0 + rr;
+        if (r < K) {
             *reinterpret_cast<uint4 *>(A.codes + r * (nm * 64LL) + mc * 64 + mb * 16) =
-                make_uint4(codes8(v, inv), codes8(v + 8, inv), codes8(v + 16, inv), codes8(v + 24, inv));
+                make_uint4(codes8(x, inv), codes8(x + 8, inv), codes8(x + 16, inv), codes8(x + 24, inv));
             A.scales[((long long)mc * K + r) * 4 + mb] = (uint8_t)byte;
         }
     }
@@ -183,44 +181,46 @@ __device__ __forceinline__ void scale_factors(unsigned byte, float &a, float &b)
     b = __uint_as_float((byte - half + 63) << 23);                                             // 2^(byte - half - 64)
 }
 
-// grid (ceil(M / 16), slices of the columns), block 256: 8 values a lane
-template <typename T, int HOW>
+// grid (row groups, slices of the columns), block 256: a lane writes 16 bytes, 8 or 4 values
+template <typename T> constexpr int values_rows() { return 256 / (128 * (int)sizeof(T) / 16); }     // rows of a workgroup: 16 bf16, 8 fp32
+
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void mxfp4_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                            int M, int K, T *__restrict__ X, long long ldx)
 {
-    const int lane16 = threadIdx.x & 15, nk = (K + 127) / 128;
-    const long long m = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+    constexpr int PER = 16 / (int)sizeof(T), LANES = 128 / PER;
+    const int lane = threadIdx.x % LANES, nk = (K + 127) / 128;
+    const long long m = (long long)blockIdx.x * values_rows<T>() + threadIdx.x / LANES;
     if (m >= M) return;
     for (int kc = blockIdx.y; kc < nk; kc += gridDim.y) {
-        const unsigned w = reinterpret_cast<const unsigned *>(codes + m * (nk * 64LL) + kc * 64)[lane16];
-        float a, b, v[8];
-        scale_factors(scales[((long long)kc * M + m) * 4 + (lane16 >> 2)], a, b);
-        const f32x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1),
-                            __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3)};
+        const uint8_t *from = codes + m * (nk * 64LL) + kc * 64 + lane * (PER / 2);
+        const unsigned w = PER == 8 ? *reinterpret_cast<const unsigned *>(from) : *reinterpret_cast<const unsigned short *>(from);
+        float a, b, v[PER];
+        scale_factors(scales[((long long)kc * M + m) * 4 + lane / (32 / PER)], a, b);
+        f32x2 p[4];
+        p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
+        p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+        if (PER == 8) {
+            p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
+            p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+        }
+        unsigned u[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p[i >> 1][i & 1] * a * b;
-        const int k = kc * 128 + lane16 * 8;
+        for (int i = 0; i < PER; ++i) v[i] = p[i >> 1][i & 1] * a * b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) u[i] = __float_as_uint(v[i]);
+            else u[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+        }
+        const int k = kc * 128 + lane * PER;
         T *x = X + m * ldx + k;
-        unsigned u[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        if (HOW != ONE && k + 8 <= K) {
-            u32x4 *to = reinterpret_cast<u32x4 *>(x);
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const f32x4 y = {v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
-                    if (HOW == STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, y), to + i);
-                    else to[i] = __builtin_bit_cast(u32x4, y);
-                }
-            } else {
-                const u32x4 y = {u[0], u[1], u[2], u[3]};
-                if (HOW == STREAM) __builtin_nontemporal_store(y, to);
-                else *to = y;
-            }
+        if (k + PER <= K) {
+            const u32x4 y = {u[0], u[1], u[2], u[3]};
+            if (STREAM) __builtin_nontemporal_store(y, reinterpret_cast<u32x4_any *>(x));
+            else *reinterpret_cast<u32x4_any *>(x) = y;
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int i = 0; i < PER; ++i)
                 if (k + i < K) {
                     if constexpr (sizeof(T) == 4) x[i] = v[i];
                     else x[i] = (bf16_t)(u[i >> 1] >> (16 * (i & 1)));
@@ -282,7 +282,7 @@ template <int WM_, int WN_, int WI_, int WJ_> struct Tile {
 __device__ __forceinline__ int spread(int r) { return ((r >> 1) & 7) ^ ((r & 1) << 2); }
 
 template <typename L, typename T> __global__ __launch_bounds__(64 * L::WAVES, L::BM == 256 ? L::WAVES / 4 : 2)
-void mxfp4_product_kernel(const ProductArgs P, bool vec)
+void mxfp4_product_kernel(const ProductArgs P)
 {
     constexpr int WI = L::WI, WJ = L::WJ, BM = L::BM, BN = L::BN, STAGE = L::STAGE, LA = L::LA, LB = L::LB, NS = L::NS;
     constexpr int LOADS = L::LOADS, MULS = WI * WJ, READS = WI + WJ, SLOTS = MULS > READS ? MULS : READS;
@@ -469,7 +469,7 @@ void mxfp4_product_kernel(const ProductArgs P, bool vec)
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");         // the last results are read by vector instructions from here on
 
         const int m_first = m0 + ra, n_first = n0 + rb, n_left = P.N - n_first;
-        const bool full = vec && m0 + BM <= P.M && n0 + BN <= P.N;
+        const bool full = m0 + BM <= P.M && n0 + BN <= P.N;
         if (k + slots < mine) {                                     // the next tile's first stage comes while this one goes out
             set_tile(k + slots);
             load_first(copy ^ 1);
@@ -512,14 +512,18 @@ void mxfp4_product_kernel(const ProductArgs P, bool vec)
                     for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
                         const int r = r0 + l / LANES, c = l % LANES;
                         const u32x4 v = *reinterpret_cast<const u32x4 *>(s + r * ROW + c * 16);
-                        u32x4 *to = reinterpret_cast<u32x4 *>(C + (long long)r * P.ldc + c * PER16);
+                        u32x4_any *to = reinterpret_cast<u32x4_any *>(C + (long long)r * P.ldc + c * PER16);
                         if (BM == 256) __builtin_nontemporal_store(v, to);      // past the operands in L2: 987 -> 946 us at 75,600 x 5120 x 5120
                         else *to = v;
                     }
                 } else {
-                    for (int e = l; e < 32 * COLS; e += 64) {
-                        const int r = e / COLS, c = e % COLS;
-                        if (r < rows && c < cols) C[(long long)r * P.ldc + c] = reinterpret_cast<const T *>(s + r * ROW)[c];
+                    const int c = l % LANES * PER16;
+                    for (int r = l / LANES; r < 32 && r < rows; r += AT_ONCE) {
+                        const unsigned char *from = s + r * ROW + c * (int)sizeof(T);
+                        T *to = C + (long long)r * P.ldc + c;
+                        if (c + PER16 <= cols) *reinterpret_cast<u32x4_any *>(to) = *reinterpret_cast<const u32x4 *>(from);
+                        else
+                            for (int e = 0; e < PER16 && c + e < cols; ++e) to[e] = reinterpret_cast<const T *>(from)[e];
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);      // else all results leave the accumulators first, for want of registers to memory
@@ -584,21 +588,18 @@ static int slices(long long blocks, int steps)
     return (int)(want < 1 ? 1 : want > steps ? steps : want);
 }
 
-static bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+// From 256 MB on, the size of the last cache level, X goes past the caches: measured with 75,600 x 5120 bf16 values (774 MB) quantise
+// 209 -> 179 us and values 212 -> 144 us (the codes, 206 MB, then stay cached between the two), with 16,384 x 1536 (50 MB) quantise
+// 11.3 -> 13.4 us.
+// (A store past the caches that covers no whole lines is slow: 75,599 x 5119 values 419 us so, 210 through them.)
+static bool streamed(int M, int K, int es) { return (double)M * K * es >= 268435456.0; }
+static bool whole_lines(const void *p, int64_t ld, int es) { return (reinterpret_cast<uintptr_t>(p) & 127) == 0 && ld * es % 128 == 0; }
 
-// X of `bytes`, 16 bytes at a time where vec.  From 256 MB on, the size of the last cache level, it goes past the caches: measured
-// with 75,600 x 5120 bf16 values (774 MB) quantise 209 -> 179 us and values 212 -> 144 us (the codes, 206 MB, then stay cached between
-// the two), with 16,384 x 1536 (50 MB) quantise 11.3 -> 13.4 us.
-static int how(bool vec, double bytes) { return !vec ? ONE : bytes < 268435456.0 ? VEC : STREAM; }
-
-// f(type, how) with both known at compile time
-template <typename F> static int with_how(int dtype, int h, F f)
+// f(type, STREAM) with both known at compile time
+template <typename F> static int with_types(int dtype, bool stream, F f)
 {
-    using One = std::integral_constant<int, ONE>;
-    using Vec = std::integral_constant<int, VEC>;
-    using Stream = std::integral_constant<int, STREAM>;
-    if (dtype == SVG2_BF16) h == ONE ? f((bf16_t *)0, One()) : h == VEC ? f((bf16_t *)0, Vec()) : f((bf16_t *)0, Stream());
-    else h == ONE ? f((float *)0, One()) : h == VEC ? f((float *)0, Vec()) : f((float *)0, Stream());
+    if (dtype == SVG2_BF16) stream ? f((bf16_t *)0, std::true_type()) : f((bf16_t *)0, std::false_type());
+    else stream ? f((float *)0, std::true_type()) : f((float *)0, std::false_type());
     SVG2_HIP_CHECK(hipGetLastError());
     return SVG2_OK;
 }
@@ -607,27 +608,28 @@ int mxfp4_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t s
                        void *scales, hipStream_t st)
 {
     const QuantArgs A = {X, sm, sg, M, G, Kg, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales)};
-    const int K = G * Kg, es = dtype == SVG2_BF16 ? 2 : 4, per16 = 16 / es;
-    const bool vec = aligned(X, 16) && sm % per16 == 0 && (G == 1 || sg % per16 == 0) && Kg % 8 == 0;
-    return with_how(dtype, how(vec, (double)M * K * es), [&](auto *tp, auto h) {
+    const int K = G * Kg, es = dtype == SVG2_BF16 ? 2 : 4;
+    return with_types(dtype, streamed(M, K, es), [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
-        constexpr int HOW = decltype(h)::value;
-        const int bx = transposed ? cdiv(K, 64) : cdiv(M, 16), steps = transposed ? cdiv(M, 128) : cdiv(K, 128);
-        const dim3 grid(bx, slices(bx, steps));
-        if (transposed) mxfp4_quant_t_kernel<T, HOW><<<grid, 256, 0, st>>>(A);
-        else mxfp4_quant_kernel<T, HOW><<<grid, 256, 0, st>>>(A);
+        if (transposed) {
+            const int bx = cdiv(cdiv(K, 64), 8) * 8, pairs = cdiv(M, 256), share = (int)((long long)pairs * bx / 2048);
+            const int per = 2 * (share < 1 ? 1 : share);
+            mxfp4_quant_t_kernel<T><<<dim3(bx, cdiv(cdiv(M, 128), per)), 256, 0, st>>>(A, per);
+        } else {
+            const int bx = cdiv(M, 16);
+            mxfp4_quant_kernel<T, decltype(stream)::value><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(A);
+        }
     });
 }
 
 int mxfp4_values_launch(const void *codes, const void *scales, int M, int K, int dtype, void *X, int64_t ldx, hipStream_t st)
 {
     const uint8_t *c = static_cast<const uint8_t *>(codes), *s = static_cast<const uint8_t *>(scales);
-    const int es = dtype == SVG2_BF16 ? 2 : 4, bx = cdiv(M, 16);
-    const bool vec = aligned(X, 16) && ldx % (16 / es) == 0;
-    const dim3 grid(bx, slices(bx, cdiv(K, 128)));
-    return with_how(dtype, how(vec, (double)M * K * es), [&](auto *tp, auto h) {
+    const int es = dtype == SVG2_BF16 ? 2 : 4;
+    return with_types(dtype, streamed(M, K, es) && whole_lines(X, ldx, es), [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
-        mxfp4_values_kernel<T, decltype(h)::value><<<grid, 256, 0, st>>>(c, s, M, K, static_cast<T *>(X), ldx);
+        const int bx = cdiv(M, values_rows<T>());
+        mxfp4_values_kernel<T, decltype(stream)::value><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(c, s, M, K, static_cast<T *>(X), ldx);
     });
 }
 
@@ -663,13 +665,13 @@ template <typename L> static double tile_time(int M, int N, int K)
     return (double)rounds * (start + stages * full) + last;
 }
 
-template <typename L> static int product_tiles(ProductArgs P, int out_dtype, bool vec, hipStream_t st)
+template <typename L> static int product_tiles(ProductArgs P, int out_dtype, hipStream_t st)
 {
     P.tiles_n = cdiv(P.N, L::BN);
     const int tiles = cdiv(P.M, L::BM) * P.tiles_n, resident = 256 * (L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4);
     const int grid = tiles < resident ? tiles : resident;
-    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<L, bf16_t><<<grid, 64 * L::WAVES, L::LDS, st>>>(P, vec);
-    else mxfp4_product_kernel<L, float><<<grid, 64 * L::WAVES, L::LDS, st>>>(P, vec);
+    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<L, bf16_t><<<grid, 64 * L::WAVES, L::LDS, st>>>(P);
+    else mxfp4_product_kernel<L, float><<<grid, 64 * L::WAVES, L::LDS, st>>>(P);
     SVG2_HIP_CHECK(hipGetLastError());
     return SVG2_OK;
 }
@@ -692,12 +694,11 @@ int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void
 {
     const ProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
                            static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0};
-    const bool vec = aligned(C, 16) && ldc % (out_dtype == SVG2_BF16 ? 8 : 4) == 0;
     if (M <= FEW_ROWS) return product_few(P, out_dtype, st);
     const double large = tile_time<Large>(M, N, K), medium = tile_time<Medium>(M, N, K), small = tile_time<Small>(M, N, K);
-    if (large <= medium && large <= small) return product_tiles<Large>(P, out_dtype, vec, st);
-    if (medium <= small) return product_tiles<Medium>(P, out_dtype, vec, st);
-    return product_tiles<Small>(P, out_dtype, vec, st);
+    if (large <= medium && large <= small) return product_tiles<Large>(P, out_dtype, st);
+    if (medium <= small) return product_tiles<Medium>(P, out_dtype, st);
+    return product_tiles<Small>(P, out_dtype, st);
 }
 
 }  // namespace svg2
