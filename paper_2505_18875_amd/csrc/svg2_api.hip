@@ -673,7 +673,7 @@ int svg2_rope_backward(const svg2_rope_args *a, const void *const *dY, void *con
                      "dY[%d] or dX[%d] is not 16-byte aligned", t, t);
         if (a->norm_weight[t]) {
             SVG2_REQUIRE(a->src[t] && multiple_of(a->src[t], 16), SVG2_INVALID_ARG, "src[%d] is null or not 16-byte aligned", t);
-            SVG2_REQUIRE(dW && dW[t], SVG2_INVALID_ARG, "dW[%d] is null, norm_weight[%d] is not", t, t);
+            SVG2_REQUIRE(dW && dW[t] && multiple_of(dW[t], 4), SVG2_INVALID_ARG, "dW[%d] is null or not aligned, norm_weight[%d] is given", t, t);
         }
         for (int u = 0; u < a->n_tensors; ++u) {
             SVG2_REQUIRE(dX[t] != dY[u] && (!a->norm_weight[u] || dX[t] != a->src[u]), SVG2_INVALID_ARG,

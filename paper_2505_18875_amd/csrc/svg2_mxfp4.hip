@@ -256,6 +256,19 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 
 __device__ __forceinline__ i32x8 fragment(const uint4 &u) { return i32x8{(int)u.x, (int)u.y, (int)u.z, (int)u.w, 0, 0, 0, 0}; }
 
+// Wait states between the last matrix instructions and the vector instructions that read their results, more than either the compiler
+// or the hardware asks for (they are not agreed for these instructions).  The results are operands of the statement, all of them of
+// one: it stands behind every instruction that writes them and before every one that reads them, which an s_nop by itself does not.
+template <int I, int J> __device__ __forceinline__ void settle(f32x16 (&a)[I][J])
+{
+    static_assert(I * J == 8 || I * J == 4 || I * J == 1, "");
+    if constexpr (I * J == 8)
+        asm volatile("s_nop 15\n\ts_nop 15" : "+v"(a[0][0]), "+v"(a[0][1]), "+v"(a[1][0]), "+v"(a[1][1]), "+v"(a[2][0]), "+v"(a[2][1]),
+                     "+v"(a[3][0]), "+v"(a[3][1]));
+    else if constexpr (I * J == 4) asm volatile("s_nop 15\n\ts_nop 15" : "+v"(a[0][0]), "+v"(a[0][1]), "+v"(a[1][0]), "+v"(a[1][1]));
+    else asm volatile("s_nop 15\n\ts_nop 15" : "+v"(a[0][0]));
+}
+
 // The tiled product.  v_mfma_scale_f32_32x32x64_f8f6f4 on E2M1 operands: lane l gives 32 values of row l % 32 (16 bytes), columns
 // 32 (l / 32) .., and their scale.  The rows of B go in first: a lane's results are then neighbours in a row of C.
 //
@@ -465,8 +478,10 @@ void mxfp4_product_kernel(const ProductArgs P)
             quarter(f0, No(), f1, st, 3, Yes(), No(), 0, false);
         }
         quarter(f1, Yes(), f0, st, 0, No(), No(), 0, false);
-        __builtin_amdgcn_s_barrier();                               // every wavefront has read its last stage
-        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");         // the last results are read by vector instructions from here on
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();                               // every wavefront has the last of its last stage in registers
+        asm volatile("" ::: "memory");
+        settle(acc);
 
         const int m_first = m0 + ra, n_first = n0 + rb, n_left = P.N - n_first;
         const bool full = m0 + BM <= P.M && n0 + BN <= P.N;
@@ -566,7 +581,7 @@ template <typename T> __global__ __launch_bounds__(64 * FEW_WAVES) void mxfp4_fe
             acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(vb[u]), fragment(va[u]), acc, 4, 4, 0, (int)(xb[u] >> (8 * g)), 0,
                                                                    (int)(xa[u] >> (8 * g)));
     }
-    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    asm volatile("s_nop 15\n\ts_nop 15" : "+v"(acc));              // (see settle)
     // lane holds row l % 16 of A, rows 4 (l / 16) .. + 3 of B
     *reinterpret_cast<float4 *>(s_sum + (wave * 16 + r) * 16 + 4 * g) = make_float4(acc[0], acc[1], acc[2], acc[3]);
     __syncthreads();
