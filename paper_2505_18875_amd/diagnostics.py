@@ -11,8 +11,12 @@ figures; every number comes from the library's kernels through the C ABI):
   sequence   a denoising sequence: 10 steps, Q and K drifting by 0.05 N(0,1) per step, k-means warm-started
              from the previous step's centroids with 2 iterations, C_k in {500, 1000}, top-p from 0.5 to
              0.99: per-step layer time, density and attention recall      (Section 4.3, centroid cache)
+  block      the attention block of a video transformer around the layer, from hidden states to hidden states:
+             projection to Q, K, V, RMS norm + rotary positions + head order, svg2_forward, projection of O; with
+             the projections on MXFP4 operands and in bf16, time by stage, and output error of both against fp32
+             projections                                               (Section 5.1, "Models")
 
-Usage: python -m paper_2505_18875_amd.diagnostics {recall,clusters,seeding,fp8,sequence} [--workload wan_like] [--heads 8]
+Usage: python -m paper_2505_18875_amd.diagnostics {recall,clusters,seeding,fp8,sequence,block} [--workload wan_like] [--heads 8]
 """
 from __future__ import annotations
 
@@ -274,9 +278,71 @@ def sequence(args):
             del lse_all, res, one
 
 
+def block(args):
+    import torch
+    import paper_2505_18875_amd as svg2
+    w = wl.WORKLOADS[args.workload]
+    if w.dtype != "bf16":
+        raise SystemExit("the block runs in bf16")
+    H, d, N, bf16 = args.heads, w.d, w.N, torch.bfloat16
+    D = H * d
+    # hidden states with the workload's components: centre of the token's component plus unit noise; random weights, so that a
+    # projected channel has the hidden states' variance
+    g = torch.Generator(device="cuda")
+    g.manual_seed(w.seed)
+    comp = torch.from_numpy(wl.component_map(w, 0).astype(np.int64)).cuda()
+    centres = w.centre_scale * torch.randn((w.n_components, D), generator=g, device="cuda")
+    hidden = (centres[comp] + torch.randn((N, D), generator=g, device="cuda")).to(bf16)
+    w_qkv, w_out = [(torch.randn((n * D, D), generator=g, device="cuda") / D ** 0.5).to(bf16) for n in (3, 1)]
+    b_qkv, b_out = [0.1 * torch.randn((n * D,), generator=g, device="cuda") for n in (3, 1)]
+    norms = [1.0 + 0.1 * torch.randn((H, d), generator=g, device="cuda") for _ in range(2)] + [None]
+    side = 2 * (d // 6)                         # height and width get a third of a head each, rounded down to pairs
+    pairs = ((d - 2 * side) // 2, side // 2, side // 2)
+    pos, freq = svg2.svg2_grid_positions(w.grid), svg2.svg2_rope_frequencies(pairs)
+    q_qkv, q_out = svg2.svg2_quantize_mxfp4(w_qkv), svg2.svg2_quantize_mxfp4(w_out)
+    cent = {}
+
+    def project(kind, x, weight, quantised, bias):
+        """x [N,D] or O in head order [H,N,d] -> [N, rows of weight]"""
+        if kind == "mxfp4":
+            return svg2.svg2_matmul_mxfp4(*svg2.svg2_quantize_mxfp4(x.transpose(0, 1) if x.dim() == 3 else x), *quantised, bias=bias)
+        x = x.transpose(0, 1).reshape(N, D) if x.dim() == 3 else x
+        if kind == "fp32":
+            return (x.float() @ weight.float().t() + bias).to(bf16)
+        return torch.addmm(bias.to(bf16), x, weight.t())
+
+    def rope(qkv):
+        p = qkv.view(N, 3, H, d)
+        return svg2.svg2_rope([p[:, i] for i in range(3)], pos, freq, axis_pairs=pairs, rotate=(True, True, False),
+                              norm_weights=norms, norm_scope="token")
+
+    def layer(q, k, v):
+        if not cent:                            # the same initial centroids for every kind
+            cent["q"], cent["k"] = [t[:, torch.linspace(0, N - 1, C, device="cuda").long()].float().contiguous()
+                                    for t, C in ((q, w.Cq), (k, w.Ck))]
+        return svg2.svg2_forward(q, k, v, cent["q"].clone(), cent["k"].clone(), w.top_p, w.iters).O
+
+    def rel(a, b):
+        return ((a.double() - b.double()).pow(2).sum() / b.double().pow(2).sum()).sqrt().item()
+
+    ref = {}
+    print("Attention block of %d tokens and %d channels (%d heads of %d): %s" % (N, D, H, d, w.name))
+    print("\n| projections | to Q, K, V ms | norm + rotary + head order ms | svg2_forward ms | of O ms | block ms | "
+          "rel. rms err of Q, K, V | of O | of the block |\n|---|---|---|---|---|---|---|---|---|")
+    for kind in ("fp32", "bf16", "mxfp4"):
+        t1, qkv = _timed(lambda: project(kind, hidden, w_qkv, q_qkv, b_qkv))
+        t2, (q, k, v) = _timed(lambda: rope(qkv))
+        t3, O = _timed(lambda: layer(q, k, v))
+        t4, out = _timed(lambda: project(kind, O, w_out, q_out, b_out))
+        if kind == "fp32":
+            ref = dict(qkv=qkv, O=O, out=out)
+        print("| %s | %.3f | %.3f | %.3f | %.3f | %.3f | %.4f | %.4f | %.4f |" %
+              (kind, t1, t2, t3, t4, t1 + t2 + t3 + t4, rel(qkv, ref["qkv"]), rel(O, ref["O"]), rel(out, ref["out"])))
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("what", choices=("recall", "clusters", "seeding", "fp8", "sequence"))
+    ap.add_argument("what", choices=("recall", "clusters", "seeding", "fp8", "sequence", "block"))
     ap.add_argument("--workload", default="wan_like", choices=sorted(wl.WORKLOADS))
     ap.add_argument("--heads", type=int, default=8)
     args = ap.parse_args()
@@ -285,7 +351,7 @@ def main():
     svg2.load_library()
     if not torch.cuda.is_available():
         raise RuntimeError("diagnostics need a GPU")
-    {"recall": recall, "clusters": clusters, "seeding": seeding, "fp8": fp8, "sequence": sequence}[args.what](args)
+    {"recall": recall, "clusters": clusters, "seeding": seeding, "fp8": fp8, "sequence": sequence, "block": block}[args.what](args)
 
 
 if __name__ == "__main__":

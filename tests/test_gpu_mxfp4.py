@@ -284,3 +284,11 @@ def test_block_from_hidden_states_to_hidden_states(svg2):
     assert (np.abs(_np(Q)) @ np.abs(_np(K)).transpose(0, 2, 1)).max() / d ** 0.5 < 2 ** 6
     assert_within(O, p @ _np(V), (2.0 ** -8 + 2.0 ** -12) * (1 + 2.0 ** -7) * (p @ np.abs(_np(V))), torch.bfloat16, "attention")
     assert_within(out, *ops.product(val(_np(O).transpose(1, 0, 2).reshape(N, D)), val(_np(w_out)), _np(b_out)), torch.bfloat16, "out")
+
+
+def test_the_block_diagnostic_runs(svg2, capsys):
+    from types import SimpleNamespace
+    from paper_2505_18875_amd import diagnostics
+    diagnostics.block(SimpleNamespace(workload="small", heads=2))
+    rows = [l for l in capsys.readouterr().out.splitlines() if l.startswith(("| fp32", "| bf16", "| mxfp4"))]
+    assert len(rows) == 3 and all("nan" not in r for r in rows)
