@@ -551,8 +551,11 @@ void mxfp4_product_kernel(const ProductArgs P)
 // columns 32 (l / 16) ..: 64 neighbouring bytes of a row, two instructions a cache line.  16 rows of B a workgroup, the rows of A
 // behind the last as the last; every wavefront has FEW_PAIRS lines of its rows on their way before it uses the first.  The
 // wavefronts' sums meet in LDS and are added in order.
-// One token, 15,360 x 5120 weights (42 MB with their scales): 13 us a call, through 64 x 64 tiles 15.
+// Measured, this kernel / 64 x 64 tiles, us: one row and 15,360 x 5120 weights (42 MB with their scales) 10.7 / 13.5, 5120 x 5120
+// 7.2 / 10.4, 64 x 8192 4.7 / 13.2; from some 40 MB on the tiles' loads, which do not wait for registers, win: 16 rows, 20,480 x 5120
+// 15.9 / 13.6, 20,480 x 8192 24.4 / 19.4.
 constexpr int FEW_ROWS = 16, FEW_PAIRS = 4, FEW_WAVES = 16;
+static bool few(int M, int N, int K) { return M <= FEW_ROWS && (long long)N * K <= 5 << 24; }
 
 template <typename T> __global__ __launch_bounds__(64 * FEW_WAVES) void mxfp4_few_kernel(const ProductArgs P)
 {
@@ -606,7 +609,7 @@ static int slices(long long blocks, int steps)
 // From 256 MB on, the size of the last cache level, X goes past the caches: measured with 75,600 x 5120 bf16 values (774 MB) quantise
 // 209 -> 179 us and values 212 -> 144 us (the codes, 206 MB, then stay cached between the two), with 16,384 x 1536 (50 MB) quantise
 // 11.3 -> 13.4 us.
-// (A store past the caches that covers no whole lines is slow: 75,599 x 5119 values 419 us so, 210 through them.)
+// (A store past the caches that covers no whole lines is slow: 75,599 x 5119 values 419 us so, 312 through them.)
 static bool streamed(int M, int K, int es) { return (double)M * K * es >= 268435456.0; }
 static bool whole_lines(const void *p, int64_t ld, int es) { return (reinterpret_cast<uintptr_t>(p) & 127) == 0 && ld * es % 128 == 0; }
 
@@ -668,8 +671,8 @@ int mxfp4_matmul_prepare()
 // Microseconds that the product takes with these tiles, by what was measured: `start` a tile, and for each stage of 256 columns
 // alone[..] with one workgroup a CU up to full[..] with as many as fit (Large 1, Medium 2, Small 4).  Large tiles do most with
 // what they load, small ones leave fewer CUs idle: measured, large / medium / small,
-//   8192 x 8192 x 8192    249 / 302 / 459 us        4096 x 5120 x 5120    78 / 65 / 102 us       512 x 5120 x 5120   33 / 17 / 17 us
-//   4096 x 4096 x 4096     40 /  45 /  65 us        2048 x 2048 x 2048    18 / 11 /  12 us       300 x 5120 x 5120   40 / 21 / 14 us
+//   8192 x 8192 x 8192    264 / 302 / 459 us        4096 x 5120 x 5120    78 / 65 / 102 us       512 x 5120 x 5120   33 / 17 / 17 us
+//   4096 x 4096 x 4096     38 /  45 /  65 us        2048 x 2048 x 2048    18 / 11 /  12 us       300 x 5120 x 5120   40 / 21 / 14 us
 template <typename L> static double tile_time(int M, int N, int K)
 {
     constexpr int R = L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4;
@@ -709,7 +712,7 @@ int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void
 {
     const ProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
                            static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0};
-    if (M <= FEW_ROWS) return product_few(P, out_dtype, st);
+    if (few(M, N, K)) return product_few(P, out_dtype, st);
     const double large = tile_time<Large>(M, N, K), medium = tile_time<Medium>(M, N, K), small = tile_time<Small>(M, N, K);
     if (large <= medium && large <= small) return product_tiles<Large>(P, out_dtype, st);
     if (medium <= small) return product_tiles<Medium>(P, out_dtype, st);

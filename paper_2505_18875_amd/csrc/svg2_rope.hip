@@ -7,12 +7,13 @@
 //   dw = sum over tokens (and heads) of g n / w,   dx = r (g w - x r mean(g w x r)),   r = rsqrt(mean(x^2) + eps)
 //
 // Every element is read once and written once, some ten operations each: HBM bounds it, so the kernels are built around the
-// loads.  One wavefront (fewer lanes where a token is short) per token and tensor; a lane holds four pairs (8 elements), 8 or 16 lanes a head, 8 or 4 heads a
-// step, and up to CH steps are loaded before the first is used.  A token of 40 heads of 128 thus stays in registers between
-// the sum of squares over all its heads and the result, and no lane needs an element of another's.  The angle of a lane's pairs
-// is the same for every head, so four cosines and sines per lane and token serve all of them: cheap enough to compute
-// in place, in 64 bits up to the quarter turn (positions of 10^6 times a frequency of 1 leave no fraction in 32), instead of
-// reading a table.
+// loads.  One wavefront (fewer lanes where a token is short, a workgroup where it is long) per token and tensor; a lane holds
+// four pairs (8 elements), 8 or 16 lanes a head, 8 or 4 heads a step, and up to CH steps are loaded before the first is used.  A
+// token of 40 heads of 128 thus stays in registers between the sum of squares over all its heads and the result, and no lane
+// needs an element of another's.  The angle of a lane's pairs is the same for every head, so four cosines and sines per lane and
+// token serve all of them: cheap enough to compute in place, in 64 bits up to the quarter turn (positions of 10^6 times a
+// frequency of 1 leave no fraction in 32), instead of reading a table.
+// Q, K and V of 75,600 tokens of 40 heads of 128 in bf16 (4.6 GB in and out): 881 us, 5.3 TB/s; a large copy reaches 5.0.
 #include <type_traits>
 
 #include "svg2_common.h"
@@ -34,7 +35,7 @@ struct RopeArgs {
     int n_axes, end[4];             // pairs of axis k: end[k-1] .. end[k]
     int rotate;                     // bit t: tensor t is rotated
     int B, N, H, token_scope;
-    float eps;
+    float eps, sense;               // sense: 1, or -1 to turn back
     float *rinv;                    // backward, long token rows: 1 / rms of every token, [3][B N]
     float *partial;                 // backward: partial sums of dw, [3][P][cols]
     float *dw[3];
@@ -235,7 +236,7 @@ template <typename T, int D, bool ADJ, int G, int CH> __global__ __launch_bounds
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = v[k] * rinv * w[k];
                 }
-                if (rotate) turn<ADJ>(v, cs, sn, 1.f);
+                if (rotate) turn<ADJ>(v, cs, sn, A.sense);
                 raw[s] = encode<T>(v);
             }
             if (h < A.H) store_pairs<T, D, ADJ>(dst + h * A.ds[2], c, raw[s]);
@@ -243,8 +244,8 @@ template <typename T, int D, bool ADJ, int G, int CH> __global__ __launch_bounds
     }
 }
 
-// Long tokens, not too many: grid (B N, tensors), block 256.  A workgroup takes a token, S steps of 2048 values, so that everything it reads is
-// asked for at once; its angles, one a thread, and the sum of squares go round through LDS.
+// Long tokens, not too many: grid (B N, tensors), block 256.  A workgroup takes a token, S steps of 2048 values, so that everything
+// it reads is asked for at once; its angles, one a thread, and the sum of squares go round through LDS.
 // Measured, us for Q, K and V of 40 heads of 128, this kernel / rope_kernel: 1 token 3.8 / 7.5, 256: 5.2 / 8.9, 1024: 11.5 / 15.2,
 // 4096: 38 / 43, 16,384: 205 / 202, 75,600: 938 / 862; 32 heads, 8192 tokens: 77 / 84.
 template <typename T, int D, bool ADJ, int S> __global__ __launch_bounds__(256) void rope_row_kernel(const RopeArgs A)
@@ -305,7 +306,7 @@ template <typename T, int D, bool ADJ, int S> __global__ __launch_bounds__(256) 
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] = v[k] * rinv * w[s][k];
             }
-            if (rotate) turn<ADJ>(v, cs, sn, 1.f);
+            if (rotate) turn<ADJ>(v, cs, sn, A.sense);
             raw[s] = encode<T>(v);
         }
         store_pairs<T, D, ADJ>(dst + h * A.ds[2], c, raw[s]);
@@ -315,12 +316,13 @@ template <typename T, int D, bool ADJ, int S> __global__ __launch_bounds__(256) 
 // ---- backward --------------------------------------------------------------
 // How the weights' gradient is summed: per lane over the tokens that pass through it, over the block's wavefronts in LDS where
 // they hold the same columns, over the blocks by rope_dw_kernel, each in a fixed order, so that it is the same from run to run.
-enum { DW_NONE = 0, DW_HEAD = 1, DW_ROW = 2, DW_LONG = 3 };
-//   DW_HEAD    [d] weights: 8 sums per lane (rope_bwd_kernel)
-//   DW_ROW     [H,d] weights, up to 8192: a wavefront (up to 2048) or a workgroup holds a token, its weights and its sums
+enum { DW_NONE, DW_STEP, DW_ROW, DW_LONG };
+//   DW_NONE    no norm: the forward's kernels, turning back
+//   DW_STEP    [d] weights, or [H,d] of a token that is one step of a wavefront: 8 sums per lane (rope_bwd_kernel)
+//   DW_ROW     longer tokens, up to 8192 [H,d] weights: a wavefront (up to 2048) or a workgroup holds a token, its weights and its sums
 //              (rope_bwd_row_kernel).  One wavefront does not hold a token of 5120 values and their sums: 1032 us for Q, K and V of
-//              16,384 tokens, most of it spilled registers
-//   DW_LONG    longer tokens: read twice here (sums, then results); 1 / rms is left for rope_dw_long_kernel
+//              16,384 tokens, most of it spilled registers; the workgroup 294
+//   DW_LONG    tokens longer than that: read twice here (sums, then results); 1 / rms is left for rope_dw_long_kernel
 constexpr int ROW_STEPS = 4;        // most steps of 8 values a thread that are held
 
 template <int D, bool ADJ> __device__ __forceinline__ int column(int c, int k)     // where value k of lane c is in its head
@@ -359,22 +361,22 @@ __device__ __forceinline__ void norm_gradient(const float *vx, float *vg, const 
     }
 }
 
-// grid (blocks, tensors), block 256: wavefronts stride over the tokens
-template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256, 2) void rope_bwd_kernel(const RopeArgs A)
+// grid (blocks, tensors), block 256: G lanes a token (64, or the 8, 16 or 32 that hold it), wavefronts stride over the tokens
+template <typename T, int D, bool ADJ, int DW, int G> __global__ __launch_bounds__(256, 2) void rope_bwd_kernel(const RopeArgs A)
 {
-    constexpr int LPH = D / 8, HPS = 64 / LPH, CH = DW == DW_LONG ? 2 : 4;
-    __shared__ float s_dw[D];                   // DW_HEAD
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = blockIdx.y;
+    constexpr int LPH = D / 8, HPS = G / LPH, CH = G < 64 ? 1 : DW == DW_LONG ? 2 : 4;
+    __shared__ float s_dw[512];                 // DW_STEP
+    const int lane = threadIdx.x % G, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = blockIdx.y;
     const int hl = lane / LPH, c = lane % LPH, steps = (A.H + HPS - 1) / HPS, tokens = A.B * A.N;
-    const float *weight = DW == DW_NONE ? nullptr : A.weight[t];
-    const bool rotate = (A.rotate >> t) & 1;
+    const float *weight = A.weight[t];
+    const bool rotate = (A.rotate >> t) & 1, whole = A.token_scope;         // DW_STEP, whole: one step
 
     float acc[8], w[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) acc[k] = 0.f;
-    if (DW == DW_HEAD && weight) load_weight<D, ADJ>(weight, c, w);
+    if (DW == DW_STEP && weight && (!whole || hl < A.H)) load_weight<D, ADJ>(weight + (whole ? hl * D : 0), c, w);
 
-    for (int token = blockIdx.x * 4 + wave; token < tokens; token += gridDim.x * 4) {
+    for (int token = blockIdx.x * (256 / G) + (G == 64 ? wave : (int)threadIdx.x / G); token < tokens; token += gridDim.x * (256 / G)) {
         const int b = token / A.N, n = token - b * A.N;
         const T *x = static_cast<const T *>(A.src[t]) + b * A.ss[0] + n * A.ss[1];
         const T *g = static_cast<const T *>(A.grad[t]) + b * A.gs[0] + n * A.gs[1];
@@ -386,7 +388,7 @@ template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256,
                 const int h = (s0 + s) * HPS + hl;
                 if (h >= A.H) continue;
                 rg[s] = load_pairs<T, D, ADJ>(g + h * A.gs[2], c);
-                if (DW != DW_NONE && weight) rx[s] = load_pairs<T, D, ADJ>(x + h * A.ss[2], c);
+                if (weight) rx[s] = load_pairs<T, D, ADJ>(x + h * A.ss[2], c);
             }
         };
         float cs[4], sn[4], rinv = 1.f, mean = 0.f;
@@ -402,7 +404,7 @@ template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256,
                     float vx[8], vg[8];
                     decode(rx[s], vx);
                     decode(rg[s], vg);
-                    if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+                    if (rotate) turn<ADJ>(vg, cs, sn, A.sense);
                     load_weight<D, ADJ>(weight + h * D, c, w);
                     add_sums(vx, vg, w, xx, gx);
                 }
@@ -423,19 +425,27 @@ template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256,
                 if (weight || rotate) {
                     float vg[8];
                     decode(rg[s], vg);
-                    if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
-                    if (DW != DW_NONE && weight) {
+                    if (rotate) turn<ADJ>(vg, cs, sn, A.sense);
+                    if (weight) {
                         float vx[8];
                         decode(rx[s], vx);
-                        if (DW == DW_HEAD) {
+                        if (DW == DW_STEP) {
                             float xx = 0.f, gx = 0.f;
-                            add_sums(vx, vg, w, xx, gx);
-                            rinv = 1.f / sqrtf(group_sum(xx, LPH) * (1.f / D) + A.eps);
-                            mean = group_sum(gx, LPH) * rinv * (1.f / D);
+                            if (h < A.H) add_sums(vx, vg, w, xx, gx);
+                            const float count = whole ? (float)A.H * D : (float)D;
+                            if (whole) {
+                                xx = group_sum(xx, G);
+                                gx = group_sum(gx, G);
+                            } else {
+                                xx = group_sum(xx, LPH);
+                                gx = group_sum(gx, LPH);
+                            }
+                            rinv = 1.f / sqrtf(xx / count + A.eps);
+                            mean = gx * rinv / count;
                         } else if (h < A.H) {
                             load_weight<D, ADJ>(weight + h * D, c, w);
                         }
-                        norm_gradient(vx, vg, w, rinv, mean, acc, DW == DW_HEAD && h < A.H);
+                        norm_gradient(vx, vg, w, rinv, mean, acc, DW == DW_STEP && h < A.H);
                     }
                     rg[s] = encode<T>(vg);
                 }
@@ -444,16 +454,18 @@ template <typename T, int D, bool ADJ, int DW> __global__ __launch_bounds__(256,
         }
     }
 
-    if (DW == DW_HEAD && weight) {              // the same for the whole block
+    if (DW == DW_STEP && weight) {              // the same for the whole block
+        // lanes of one column: all heads and tokens of the wavefront, or (whole) its tokens
+        const int from = whole ? G : LPH, slot = (threadIdx.x & 63) / LPH;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            for (int o = LPH; o < 64; o <<= 1) acc[k] += __shfl_xor(acc[k], o);
+            for (int o = from; o < 64; o <<= 1) acc[k] += __shfl_xor(acc[k], o);
         for (int turn_of = 0; turn_of < 4; ++turn_of) {
-            if (wave == turn_of && hl == 0) add_to<D, ADJ>(s_dw, c, acc, wave == 0);
+            if (wave == turn_of && (whole ? slot < HPS && slot < A.H : slot == 0)) add_to<D, ADJ>(s_dw + (whole ? slot * D : 0), c, acc, wave == 0);
             __syncthreads();
         }
         float *out = A.partial + ((size_t)t * A.P + blockIdx.x) * A.cols;
-        for (int i = threadIdx.x; i < D; i += 256) out[i] = s_dw[i];
+        for (int i = threadIdx.x; i < A.cols; i += 256) out[i] = s_dw[i];
     }
 }
 
@@ -505,7 +517,7 @@ template <typename T, int D, bool ADJ, int G, int S> __global__ __launch_bounds_
                 float vx[8], vg[8];
                 decode(rx[s], vx);
                 decode(rg[s], vg);
-                if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+                if (rotate) turn<ADJ>(vg, cs, sn, A.sense);
                 add_sums(vx, vg, w[s], xx, gx);
             }
             xx = group_sum(xx, 64);
@@ -534,7 +546,7 @@ template <typename T, int D, bool ADJ, int G, int S> __global__ __launch_bounds_
             if (weight || rotate) {
                 float vg[8];
                 decode(rg[s], vg);
-                if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+                if (rotate) turn<ADJ>(vg, cs, sn, A.sense);
                 if (weight) {
                     float vx[8];
                     decode(rx[s], vx);
@@ -578,7 +590,7 @@ template <typename T, int D, bool ADJ> __global__ __launch_bounds__(256) void ro
             float vx[8], vg[8];
             decode(load_pairs<T, D, ADJ>(static_cast<const T *>(A.src[t]) + b * A.ss[0] + n * A.ss[1] + h * A.ss[2], c), vx);
             decode(load_pairs<T, D, ADJ>(static_cast<const T *>(A.grad[t]) + b * A.gs[0] + n * A.gs[1] + h * A.gs[2], c), vg);
-            if (rotate) turn<ADJ>(vg, cs, sn, -1.f);
+            if (rotate) turn<ADJ>(vg, cs, sn, A.sense);
 #pragma unroll
             for (int k = 0; k < 8; ++k) acc[k] += vg[k] * (vx[k] * rinv);
         }
@@ -636,6 +648,7 @@ static RopeArgs device_args(const svg2_rope_args *a)
     A.H = a->H;
     A.token_scope = a->norm_scope == SVG2_NORM_TOKEN;
     A.eps = a->eps;
+    A.sense = 1.f;
     return A;
 }
 
@@ -650,29 +663,40 @@ template <typename F> static int with_types(const svg2_rope_args *a, F f)
     return adj ? f((float *)0, std::integral_constant<int, 64>(), std::true_type()) : f((float *)0, std::integral_constant<int, 64>(), std::false_type());
 }
 
-int rope_launch(const svg2_rope_args *a, hipStream_t st)
+// f(lanes) with the lanes that take a token of one step, H heads of D: 8 (D = 64), 16, 32 or 64
+template <int D, typename F> static void with_lanes(int H, F f)
 {
-    const RopeArgs A = device_args(a);
+    const int lanes = H * (D / 8);
+    if (D == 64 && lanes <= 8) f(std::integral_constant<int, D == 64 ? 8 : 16>());
+    else if (lanes <= 16) f(std::integral_constant<int, 16>());
+    else if (lanes <= 32) f(std::integral_constant<int, 32>());
+    else f(std::integral_constant<int, 64>());
+}
+
+static int forward(const svg2_rope_args *a, const RopeArgs &A, hipStream_t st)
+{
     return with_types(a, [&](auto *tp, auto dim, auto adj) -> int {
         using T = std::remove_pointer_t<decltype(tp)>;
         constexpr int D = decltype(dim)::value;
         constexpr bool ADJ = decltype(adj)::value;
         const int lanes = A.H * (D / 8), tokens = A.B * A.N;
-        if (lanes <= 8) rope_kernel<T, D, ADJ, D == 64 ? 8 : 16, 1><<<dim3(cdiv(tokens, 256 / (D == 64 ? 8 : 16)), a->n_tensors), 256, 0, st>>>(A);
-        else if (lanes <= 16) rope_kernel<T, D, ADJ, 16, 1><<<dim3(cdiv(tokens, 16), a->n_tensors), 256, 0, st>>>(A);
-        else if (lanes <= 32) rope_kernel<T, D, ADJ, 32, 1><<<dim3(cdiv(tokens, 8), a->n_tensors), 256, 0, st>>>(A);
-        else if (lanes <= 128) rope_kernel<T, D, ADJ, 64, 2><<<dim3(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
         // more than two steps of a wavefront: a workgroup a token, up to where both are bound by memory
-        else if (tokens <= 8192 && lanes <= 256) rope_row_kernel<T, D, ADJ, 1><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
-        else if (tokens <= 8192 && lanes <= 768) rope_row_kernel<T, D, ADJ, 3><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
-        else rope_kernel<T, D, ADJ, 64, 10><<<dim3(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
+        if (lanes > 128 && tokens <= 8192 && lanes <= 256) rope_row_kernel<T, D, ADJ, 1><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
+        else if (lanes > 128 && tokens <= 8192 && lanes <= 768) rope_row_kernel<T, D, ADJ, 3><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
+        else if (lanes > 128) rope_kernel<T, D, ADJ, 64, 10><<<dim3(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
+        else with_lanes<D>(A.H, [&](auto g) {
+            constexpr int G = decltype(g)::value;
+            rope_kernel<T, D, ADJ, G, G == 64 ? 2 : 1><<<dim3(cdiv(tokens, 256 / G), a->n_tensors), 256, 0, st>>>(A);
+        });
         SVG2_HIP_CHECK(hipGetLastError());
         return SVG2_OK;
     });
 }
 
+int rope_launch(const svg2_rope_args *a, hipStream_t st) { return forward(a, device_args(a), st); }
+
 struct RopeBwdPlan {
-    int dw, P, blocks, cols;
+    int dw, P, blocks, cols, lanes;
     size_t rinv_bytes, total;
 };
 
@@ -683,11 +707,12 @@ static RopeBwdPlan bwd_plan(const svg2_rope_args *a)
     bool normed = false;
     for (int t = 0; t < a->n_tensors; ++t) normed |= a->norm_weight[t] != nullptr;
     if (!normed) p.dw = DW_NONE;
-    else if (a->norm_scope == SVG2_NORM_HEAD) p.dw = DW_HEAD;
+    else if (a->norm_scope == SVG2_NORM_HEAD || a->H * a->d <= 512) p.dw = DW_STEP;
     else p.dw = a->H * a->d <= ROW_STEPS * 2048 ? DW_ROW : DW_LONG;
-    p.cols = p.dw == DW_HEAD ? a->d : a->H * a->d;
-    p.blocks = p.dw == DW_ROW ? tokens : cdiv(tokens, 4);
-    if (p.dw == DW_HEAD || p.dw == DW_ROW) {            // one partial sum per block: two blocks of 256 per CU and tensor
+    p.cols = a->norm_scope == SVG2_NORM_HEAD ? a->d : a->H * a->d;
+    p.lanes = a->H * (a->d / 8) <= 8 ? 8 : a->H * (a->d / 8) <= 16 ? 16 : a->H * (a->d / 8) <= 32 ? 32 : 64;
+    p.blocks = p.dw == DW_ROW ? tokens : cdiv(tokens, p.dw == DW_STEP ? 256 / p.lanes : 4);
+    if (p.dw == DW_STEP || p.dw == DW_ROW) {            // one partial sum per block: two blocks of 256 per CU and tensor
         const int most = p.dw == DW_ROW && p.cols <= ROW_STEPS * 512 ? 2048 : 512;
         if (p.blocks > most) p.blocks = most;
         p.P = p.blocks;
@@ -718,6 +743,12 @@ int rope_bwd_launch(const svg2_rope_args *a, const void *const *dY, void *const 
         A.gs[k] = a->dst_stride[k];
         A.ds[k] = dx_stride[k];
     }
+    A.sense = -1.f;
+    if (p.dw == DW_NONE) {
+        for (int t = 0; t < a->n_tensors; ++t) A.src[t] = dY[t];
+        for (int k = 0; k < 3; ++k) A.ss[k] = a->dst_stride[k];
+        return forward(a, A, st);
+    }
     A.rinv = static_cast<float *>(ws);
     A.partial = reinterpret_cast<float *>(static_cast<char *>(ws) + p.rinv_bytes);
     A.P = p.P;
@@ -727,10 +758,8 @@ int rope_bwd_launch(const svg2_rope_args *a, const void *const *dY, void *const 
         constexpr int D = decltype(dim)::value;
         constexpr bool ADJ = decltype(adj)::value;
         const dim3 grid(p.blocks, a->n_tensors);
-        if (p.dw == DW_NONE) rope_bwd_kernel<T, D, ADJ, DW_NONE><<<grid, 256, 0, st>>>(A);
-        else if (p.dw == DW_HEAD) rope_bwd_kernel<T, D, ADJ, DW_HEAD><<<grid, 256, 0, st>>>(A);
-        else if (p.dw == DW_LONG) rope_bwd_kernel<T, D, ADJ, DW_LONG><<<grid, 256, 0, st>>>(A);
-        else if (p.cols <= 512) rope_bwd_row_kernel<T, D, ADJ, 64, 1><<<grid, 64, 0, st>>>(A);
+        if (p.dw == DW_STEP) with_lanes<D>(A.H, [&](auto g) { rope_bwd_kernel<T, D, ADJ, DW_STEP, decltype(g)::value><<<grid, 256, 0, st>>>(A); });
+        else if (p.dw == DW_LONG) rope_bwd_kernel<T, D, ADJ, DW_LONG, 64><<<grid, 256, 0, st>>>(A);
         else if (p.cols <= 1024) rope_bwd_row_kernel<T, D, ADJ, 64, 2><<<grid, 64, 0, st>>>(A);
         else if (p.cols <= 2048) rope_bwd_row_kernel<T, D, ADJ, 64, 4><<<grid, 64, 0, st>>>(A);
         else if (p.cols <= 4096) rope_bwd_row_kernel<T, D, ADJ, 256, 2><<<grid, 256, 0, st>>>(A);
@@ -741,10 +770,8 @@ int rope_bwd_launch(const svg2_rope_args *a, const void *const *dY, void *const 
             rope_dw_long_kernel<T, D, ADJ><<<dim3(cdiv(p.cols, 512), p.P, a->n_tensors), 256, 0, st>>>(A);
             SVG2_HIP_CHECK(hipGetLastError());
         }
-        if (p.dw != DW_NONE) {
-            rope_dw_kernel<<<dim3(cdiv(p.cols, 64), a->n_tensors), 1024, 0, st>>>(A);
-            SVG2_HIP_CHECK(hipGetLastError());
-        }
+        rope_dw_kernel<<<dim3(cdiv(p.cols, 64), a->n_tensors), 1024, 0, st>>>(A);
+        SVG2_HIP_CHECK(hipGetLastError());
         return SVG2_OK;
     });
 }

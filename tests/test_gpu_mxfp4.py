@@ -169,6 +169,22 @@ def test_product_of_small_integers_is_exact(svg2, M, N, K):
     assert np.array_equal(_np(got), ops.values(ac, as_) @ ops.values(bc, bs).T)
 
 
+def test_product_of_few_rows_and_many_columns(svg2):
+    """Five rows times 20,992 x 4096 codes go through tiles, half of them through the kernel for few rows: sums of multiples of 1/4 of
+    size 10^3, exact in fp32, so the same bits."""
+    M, N, K = 5, 20992, 4096
+    g = torch.Generator(device="cuda").manual_seed(4)
+    a, b = (torch.randint(0, 256, (R, K // 2), dtype=torch.uint8, device="cuda", generator=g) for R in (M, N))
+    one = lambda R: torch.full((K // 128, R, 4), 127, dtype=torch.uint8, device="cuda")     # noqa: E731
+    whole = svg2.svg2_matmul_mxfp4(a, one(M), b, one(N), out_dtype=torch.float32)
+    for h in (0, 1):
+        part = svg2.svg2_matmul_mxfp4(a, one(M), b[h * N // 2:(h + 1) * N // 2], one(N // 2), out_dtype=torch.float32)
+        assert torch.equal(whole[:, h * N // 2:(h + 1) * N // 2], part)
+    ref = torch.matmul(svg2.svg2_dequantize_mxfp4(a, one(M), dtype=torch.float32).double(),
+                       svg2.svg2_dequantize_mxfp4(b, one(N), dtype=torch.float32).double().t())
+    assert torch.equal(whole.double(), ref)
+
+
 @pytest.mark.parametrize("M,N", [(5, 70), (200, 300)])
 def test_product_keeps_nan_blocks_and_far_scales_apart(svg2, M, N):
     K = 512

@@ -167,8 +167,19 @@ BACKWARD = [
     (torch.bfloat16, 1, 10, 41, 128, "token", "halves"),
     (torch.bfloat16, 3, 31, 5, 128, "head", "adjacent"),
     (torch.bfloat16, 1, 17, 12, 64, "none", "halves"),
-    (torch.bfloat16, 1, 2309, 3, 64, "token", "adjacent"),      # more groups of tokens than workgroups
+    (torch.bfloat16, 1, 5309, 3, 64, "token", "adjacent"),      # more groups of tokens than workgroups
     (torch.float32, 1, 2111, 2, 64, "head", "adjacent"),
+    # several tokens in a wavefront; token and head norms of one step
+    (torch.bfloat16, 2, 41, 1, 64, "token", "halves"),
+    (torch.float32, 1, 47, 1, 128, "head", "adjacent"),
+    (torch.float32, 1, 39, 2, 64, "token", "adjacent"),
+    (torch.bfloat16, 1, 43, 3, 64, "token", "halves"),
+    (torch.float32, 1, 37, 4, 64, "head", "halves"),
+    (torch.bfloat16, 1, 29, 4, 128, "token", "adjacent"),
+    (torch.float32, 1, 31, 7, 64, "token", "adjacent"),
+    (torch.bfloat16, 1, 33, 9, 64, "token", "adjacent"),
+    (torch.bfloat16, 1, 35, 1, 64, "none", "adjacent"),
+    (torch.float32, 1, 27, 20, 128, "none", "halves"),
     (torch.float32, 1, 301, 131, 64, "token", "adjacent"),      # long tokens, more groups of them than slices
 ]
 
