@@ -68,7 +68,7 @@ template <typename T> __device__ __forceinline__ const T *element(const QuantArg
 }
 
 // eight neighbouring columns: one load where they are all there and in one group, whatever their address; STREAM: past the caches,
-// for an X that is larger than they are (streamed())
+// for an X that is larger than they are (see streamed)
 template <typename T, bool STREAM> __device__ __forceinline__ void load8(const QuantArgs &A, long long m, int k, int K, float *v)
 {
     if (k + 8 <= K && (A.G == 1 || k % A.Kg + 8 <= A.Kg)) {
@@ -606,12 +606,14 @@ static int slices(long long blocks, int steps)
     return (int)(want < 1 ? 1 : want > steps ? steps : want);
 }
 
-// From 256 MB on, the size of the last cache level, X goes past the caches: measured with 75,600 x 5120 bf16 values (774 MB) quantise
-// 209 -> 179 us and values 212 -> 144 us (the codes, 206 MB, then stay cached between the two), with 16,384 x 1536 (50 MB) quantise
-// 11.3 -> 13.4 us.
-// (A store past the caches that covers no whole lines is slow: 75,599 x 5119 values 419 us so, 312 through them.)
-static bool streamed(int M, int K, int es) { return (double)M * K * es >= 268435456.0; }
-static bool whole_lines(const void *p, int64_t ld, int es) { return (reinterpret_cast<uintptr_t>(p) & 127) == 0 && ld * es % 128 == 0; }
+// X goes past the caches from 256 MB on, the size of the last cache level, where its rows are whole lines.  Measured with 75,600 x
+// 5120 bf16 values (774 MB) quantise 213 -> 192 us and values 212 -> 145 us (the codes, 206 MB, then stay cached between the two).
+// A smaller X is better left in the caches: 16,384 x 1536 (50 MB), quantise 11.3 us, past them 13.4.  So are rows that share lines:
+// 75,599 x 5119, quantise 236 us, past them 262; values 312, past them 419.
+static bool streamed(const void *X, int M, int K, int64_t ld, int es)
+{
+    return (double)M * K * es >= 268435456.0 && (reinterpret_cast<uintptr_t>(X) & 127) == 0 && ld * es % 128 == 0;
+}
 
 // f(type, STREAM) with both known at compile time
 template <typename F> static int with_types(int dtype, bool stream, F f)
@@ -627,7 +629,8 @@ int mxfp4_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t s
 {
     const QuantArgs A = {X, sm, sg, M, G, Kg, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales)};
     const int K = G * Kg, es = dtype == SVG2_BF16 ? 2 : 4;
-    return with_types(dtype, streamed(M, K, es), [&](auto *tp, auto stream) {
+    const bool lines = G == 1 || (sg * es % 128 == 0 && Kg * es % 128 == 0);
+    return with_types(dtype, lines && streamed(X, M, K, sm, es), [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
         if (transposed) {
             const int bx = cdiv(cdiv(K, 64), 8) * 8, pairs = cdiv(M, 256), share = (int)((long long)pairs * bx / 2048);
@@ -644,7 +647,7 @@ int mxfp4_values_launch(const void *codes, const void *scales, int M, int K, int
 {
     const uint8_t *c = static_cast<const uint8_t *>(codes), *s = static_cast<const uint8_t *>(scales);
     const int es = dtype == SVG2_BF16 ? 2 : 4;
-    return with_types(dtype, streamed(M, K, es) && whole_lines(X, ldx, es), [&](auto *tp, auto stream) {
+    return with_types(dtype, streamed(X, M, K, ldx, es), [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
         const int bx = cdiv(M, values_rows<T>());
         mxfp4_values_kernel<T, decltype(stream)::value><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(c, s, M, K, static_cast<T *>(X), ldx);
