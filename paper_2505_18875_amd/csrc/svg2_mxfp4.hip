@@ -123,7 +123,7 @@ template <typename T, bool STREAM> __global__ __launch_bounds__(256) void mxfp4_
 // the same XCD (every eighth workgroup): where rows are not whole lines they share some.
 // In LDS a row takes 33 words in bf16 (65 in fp32), and 8 words more for each 32 rows before it, so that the 64 lanes of a wavefront,
 // 16 columns x 4 blocks, read every bank once (fp32: twice, as the 256 bytes must).
-template <typename T> __global__ __launch_bounds__(256) void mxfp4_quant_t_kernel(const QuantArgs A, int per)
+template <typename T, bool STREAM> __global__ __launch_bounds__(256) void mxfp4_quant_t_kernel(const QuantArgs A, int per)
 {
     constexpr int WORDS = 16 * (int)sizeof(T) + 1, PAD = 8;
     __shared__ unsigned tile[128 * WORDS + 4 * PAD];
@@ -135,7 +135,7 @@ template <typename T> __global__ __launch_bounds__(256) void mxfp4_quant_t_kerne
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const long long m = (long long)mc * 128 + i * 32 + (threadIdx.x >> 3);
-            if (m < A.M) load8<T, false>(A, m, r0 + (threadIdx.x & 7) * 8, K, v[i]);
+            if (m < A.M) load8<T, STREAM>(A, m, r0 + (threadIdx.x & 7) * 8, K, v[i]);
             else
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
@@ -607,7 +607,7 @@ static int slices(long long blocks, int steps)
 }
 
 // X goes past the caches from 256 MB on, the size of the last cache level, where its rows are whole lines.  Measured with 75,600 x
-// 5120 bf16 values (774 MB) quantise 213 -> 192 us and values 212 -> 145 us (the codes, 206 MB, then stay cached between the two).
+// 5120 bf16 values (774 MB) quantise 213 -> 192 us, transposed 291 -> 240, values 212 -> 145 (the codes, 206 MB, then stay cached).
 // A smaller X is better left in the caches: 16,384 x 1536 (50 MB), quantise 11.3 us, past them 13.4.  So are rows that share lines:
 // 75,599 x 5119, quantise 236 us, past them 262; values 312, past them 419.
 static bool streamed(const void *X, int M, int K, int64_t ld, int es)
@@ -635,7 +635,7 @@ int mxfp4_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t s
         if (transposed) {
             const int bx = cdiv(cdiv(K, 64), 8) * 8, pairs = cdiv(M, 256), share = (int)((long long)pairs * bx / 2048);
             const int per = 2 * (share < 1 ? 1 : share);
-            mxfp4_quant_t_kernel<T><<<dim3(bx, cdiv(cdiv(M, 128), per)), 256, 0, st>>>(A, per);
+            mxfp4_quant_t_kernel<T, decltype(stream)::value><<<dim3(bx, cdiv(cdiv(M, 128), per)), 256, 0, st>>>(A, per);
         } else {
             const int bx = cdiv(M, 16);
             mxfp4_quant_kernel<T, decltype(stream)::value><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(A);
