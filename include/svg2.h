@@ -426,15 +426,18 @@ int svg2_rope_backward(const svg2_rope_args *args, const void *const *dY, void *
  * ldc >= N its row stride, bias [N] fp32 or NULL.  The matrix cores sum in fp32; one rounding at the end.  With A the quantised
  * activations and B the quantised weights this is a linear layer; its gradients are the same product on dY and W^T (for dX),
  * dY^T and X^T (for dW).
- * None of the three needs a workspace.
+ * A product of few tiles and a long contraction is formed in parts, in the workspace.  Where svg2_matmul_mxfp4_workspace_size
+ * returns 256 none is used and ws may be NULL; the other two calls never need one.
  * C must not overlap an input.  Rows and columns up to 2^26 (the product: K up to 2^24, C up to 2^23 tiles of 128 x 128).
  * ------------------------------------------------------------------------- */
 int svg2_quantize_mxfp4(const void *X, int dtype, int M, int G, int Kg, int64_t stride_m, int64_t stride_g,
                         int transposed, void *codes, void *scales, void *stream);
 int svg2_dequantize_mxfp4(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx,
                           void *stream);
+size_t svg2_matmul_mxfp4_workspace_size(int M, int N, int K);
 int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const void *B_scales, int M, int N, int K,
-                      const float *bias, int out_dtype, void *C, int64_t ldc, void *stream);
+                      const float *bias, int out_dtype, void *C, int64_t ldc, void *ws, size_t ws_bytes,
+                      void *stream);
 
 /* ---------------------------------------------------------------------------
  * Timing for benchmarks (HOST-side state, one per process).

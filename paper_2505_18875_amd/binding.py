@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 import struct
 from types import SimpleNamespace
@@ -37,7 +38,7 @@ EXPORTS = (
     "svg2_attention_recall_workspace_size", "svg2_attention_recall",
     "svg2_kmeans_pp_init_workspace_size", "svg2_kmeans_pp_init",
     "svg2_rope", "svg2_rope_backward_workspace_size", "svg2_rope_backward",
-    "svg2_quantize_mxfp4", "svg2_dequantize_mxfp4", "svg2_matmul_mxfp4",
+    "svg2_quantize_mxfp4", "svg2_dequantize_mxfp4", "svg2_matmul_mxfp4_workspace_size", "svg2_matmul_mxfp4",
     "svg2_profile_enable", "svg2_profile_read", "svg2_profile_read_kernels",
 )
 STAGES = ("kmeans", "permute", "select", "attn_plan", "attn")
@@ -116,7 +117,8 @@ def load_library() -> ctypes.CDLL:
         i64 = ctypes.c_int64
         lib.svg2_quantize_mxfp4.argtypes = [vp, i, i, i, i, i64, i64, i, vp, vp, vp]
         lib.svg2_dequantize_mxfp4.argtypes = [vp, vp, i, i, i, vp, i64, vp]
-        lib.svg2_matmul_mxfp4.argtypes = [vp, vp, vp, vp, i, i, i, vp, i, vp, i64, vp]
+        lib.svg2_matmul_mxfp4_workspace_size.argtypes = [i, i, i]
+        lib.svg2_matmul_mxfp4.argtypes = [vp, vp, vp, vp, i, i, i, vp, i, vp, i64, vp, sz, vp]
         lib.svg2_profile_enable.argtypes = [i]
         lib.svg2_profile_read.argtypes = [vp, vp]
         lib.svg2_profile_read_kernels.argtypes = [vp, vp]
@@ -668,7 +670,12 @@ def svg2_dequantize_mxfp4(codes, scales, K=None, *, dtype=torch.bfloat16, out=No
     return out
 
 
-def svg2_matmul_mxfp4(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bfloat16, out=None):
+@functools.lru_cache(maxsize=4096)
+def _matmul_workspace_size(M, N, K):
+    return load_library().svg2_matmul_mxfp4_workspace_size(M, N, K)
+
+
+def svg2_matmul_mxfp4(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bfloat16, out=None, ws=None):
     """C [M,N] = A B^T + bias of two MXFP4 operands (M and N rows of the same columns); bias fp32 [N]."""
     lib = load_library()
     dev = _gpu(A, "A")
@@ -678,9 +685,13 @@ def svg2_matmul_mxfp4(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bf
         raise ValueError("A has %d padded columns, B has %d" % (Kp, Kb))
     C = torch.empty((M, N), dtype=out_dtype, device=dev) if out is None else out
     ptr, ld = _rows(C, "out", dev, (M, N))
+    if ws is None:
+        need = _matmul_workspace_size(M, N, Kp)
+        if need > 256:                  # at 256 the product uses none
+            ws = _workspace(need, dev)
     with _on(dev):
         _check(lib.svg2_matmul_mxfp4(a, sa, b, sb, M, N, Kp, _dense(bias, "bias", dev, torch.float32, (N,)), _dtype_code(C), ptr, ld,
-                                     _raw_stream(dev)))
+                                     _dev(ws), 0 if ws is None else ws.numel(), _raw_stream(dev)))
     return C
 
 

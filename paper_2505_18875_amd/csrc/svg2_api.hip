@@ -722,8 +722,14 @@ static int check_product_size(int M, int N, int K)
     return SVG2_OK;
 }
 
+size_t svg2_matmul_mxfp4_workspace_size(int M, int N, int K)
+{
+    if (M < 1 || N < 1 || K < 1 || M > 67108864 || N > 67108864 || check_product_size(M, N, K) != SVG2_OK) return 256;
+    return mxfp4_matmul_ws_bytes(M, N, K);
+}
+
 int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const void *B_scales, int M, int N, int K,
-                      const float *bias, int out_dtype, void *C, int64_t ldc, void *stream)
+                      const float *bias, int out_dtype, void *C, int64_t ldc, void *ws, size_t ws_bytes, void *stream)
 {
     clear_error();
     SVG2_TRY(check_dtype(out_dtype));
@@ -735,8 +741,11 @@ int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const 
                  "C or bias is not aligned to its elements");
     SVG2_REQUIRE(ldc >= N, SVG2_INVALID_ARG, "ldc = %lld is less than N = %d", (long long)ldc, N);
     SVG2_REQUIRE(C != A && C != A_scales && C != B && C != B_scales && C != bias, SVG2_INVALID_ARG, "C must not alias an input");
+    const size_t need = mxfp4_matmul_ws_bytes(M, N, K);         // 256: none is used
+    if (need > 256 || ws) SVG2_TRY(check_ws(ws, ws_bytes, need));
+    SVG2_REQUIRE(need == 256 || (ws != A && ws != B && ws != C), SVG2_INVALID_ARG, "the workspace must not alias an operand");
     SVG2_TRY(mxfp4_matmul_prepare());
-    return mxfp4_matmul_launch(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc, static_cast<hipStream_t>(stream));
+    return mxfp4_matmul_launch(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc, ws, static_cast<hipStream_t>(stream));
 }
 
 int svg2_profile_enable(int level)

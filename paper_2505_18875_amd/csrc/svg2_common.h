@@ -210,7 +210,8 @@ int mxfp4_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t s
                        void *scales, hipStream_t st);
 int mxfp4_values_launch(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx, hipStream_t st);
 int mxfp4_matmul_prepare();
+size_t mxfp4_matmul_ws_bytes(int M, int N, int K);
 int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
-                        int out_dtype, void *C, int64_t ldc, hipStream_t st);
+                        int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st);
 
 }  // namespace svg2

@@ -237,6 +237,7 @@ struct ProductArgs {
     void *C;
     long long ldc;
     int tiles_n;
+    int split, per;                 // the contraction in `split` parts of `per` stages, each with a C of its own, one behind the other
 };
 
 // 4 bytes per lane into LDS (see load_to_lds_16)
@@ -277,6 +278,7 @@ template <int I, int J> __device__ __forceinline__ void settle(f32x16 (&a)[I][J]
 // straight from memory (global_load_lds).  A stage is used in four quarters of 64 columns, which alternate between two register
 // sets: the next quarter is read from LDS while the matrix instructions of this one run.  The one barrier of a stage stands before
 // its last quarter: the next stage has arrived by then, and this one's place is free as soon as its last quarter is in registers.
+// Where there are few tiles and many stages, a part of the stages is a tile of its own (split), and mxfp4_join_kernel adds them up.
 // In LDS row r has 128 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.
 // Rows behind the last are read as the last and not stored.
 template <int WM_, int WN_, int WI_, int WJ_> struct Tile {
@@ -303,26 +305,34 @@ void mxfp4_product_kernel(const ProductArgs P)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 31, half = lane >> 5;
     const long long row_bytes = (long long)P.nk * 64;
-    const int stages = (P.nk + 1) >> 1;
-    const bool odd = P.nk & 1;                          // the last stage has 128 columns only
 
     // Which tiles: the XCDs (every eighth workgroup) get contiguous parts of an order that goes down 4 tiles of C, then right, and
     // their workgroups take turns, so that what an XCD works on at a time is a compact patch and shares its rows in that XCD's L2.
-    const int tiles_m = (P.M + BM - 1) / BM, total = tiles_m * P.tiles_n;
+    const int tiles_m = (P.M + BM - 1) / BM, tiles = tiles_m * P.tiles_n, total = tiles * P.split;
     const int xcd = blockIdx.x & 7, part = total >> 3, rest = total & 7, first = xcd * part + min(xcd, rest);
     const int mine = part + (xcd < rest), slots = (gridDim.x + 7 - xcd) >> 3;
 
-    int m0, n0;
+    int m0, n0, slice = 0, stages = P.per;
+    bool odd = P.nk & 1;                                // the last stage has 128 columns only
     const char *ga, *gb, *gsa, *gsb;
     unsigned off_a[LA], off_b[LB], off_s[NS];           // this lane's part of the loads: 8 rows x 128 bytes each
     auto set_tile = [&](int k) {
-        const int t = first + k, group = t / (4 * P.tiles_n), in = t - group * 4 * P.tiles_n, high = min(4, tiles_m - group * 4);
+        int t = first + k, first_stage = 0;
+        if (P.split > 1) {
+            slice = __builtin_amdgcn_readfirstlane(t / tiles);
+            t -= slice * tiles;
+            const int all = (P.nk + 1) >> 1;
+            first_stage = slice * P.per;
+            stages = min(P.per, all - first_stage);
+            odd = (P.nk & 1) && first_stage + stages == all;
+        }
+        const int group = t / (4 * P.tiles_n), in = t - group * 4 * P.tiles_n, high = min(4, tiles_m - group * 4);
         m0 = __builtin_amdgcn_readfirstlane((group * 4 + in % high) * BM);
         n0 = __builtin_amdgcn_readfirstlane((in / high) * BN);
-        ga = reinterpret_cast<const char *>(P.A) + m0 * row_bytes;
-        gb = reinterpret_cast<const char *>(P.B) + n0 * row_bytes;
-        gsa = reinterpret_cast<const char *>(P.SA) + m0 * 4LL;
-        gsb = reinterpret_cast<const char *>(P.SB) + n0 * 4LL;
+        ga = reinterpret_cast<const char *>(P.A) + m0 * row_bytes + first_stage * 128LL;
+        gb = reinterpret_cast<const char *>(P.B) + n0 * row_bytes + first_stage * 128LL;
+        gsa = reinterpret_cast<const char *>(P.SA) + m0 * 4LL + first_stage * 8LL * P.M;
+        gsb = reinterpret_cast<const char *>(P.SB) + n0 * 4LL + first_stage * 8LL * P.N;
         int l = lane;
         asm("" : "+v"(l));          // formed here, not kept in registers through the loop over the stages
 #pragma unroll
@@ -485,6 +495,7 @@ void mxfp4_product_kernel(const ProductArgs P)
 
         const int m_first = m0 + ra, n_first = n0 + rb, n_left = P.N - n_first;
         const bool full = m0 + BM <= P.M && n0 + BN <= P.N;
+        T *C_first = static_cast<T *>(P.C) + ((long long)slice * P.M + m_first) * P.ldc + n_first;
         if (k + slots < mine) {                                     // the next tile's first stage comes while this one goes out
             set_tile(k + slots);
             load_first(copy ^ 1);
@@ -520,7 +531,7 @@ void mxfp4_product_kernel(const ProductArgs P)
                         else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
                     }
                 constexpr int LANES = COLS / PER16, AT_ONCE = 64 / LANES;       // lanes a row, rows an instruction
-                T *C = static_cast<T *>(P.C) + (long long)(m_first + 32 * i) * P.ldc + n_first + 32 * j0;
+                T *C = C_first + 32LL * i * P.ldc + 32 * j0;
                 const int rows = P.M - m_first - 32 * i, cols = n_left - 32 * j0;
                 if (full) {
 #pragma unroll
@@ -543,6 +554,26 @@ void mxfp4_product_kernel(const ProductArgs P)
                 }
                 __builtin_amdgcn_sched_barrier(0);      // else all results leave the accumulators first, for want of registers to memory
             }
+    }
+}
+
+// C = sum of `split` partial products [M,N], one behind the other, + bias, always in that order.  Bound by reading them, or by its own
+// launch: 17 us for 7 parts of 1536 x 1536 (66 MB, 3.9 TB/s), 4 us for 16 of 100 x 200.  grid (ceil(N / 256), rows), block 256
+template <typename T> __global__ __launch_bounds__(256) void mxfp4_join_kernel(const float *__restrict__ parts, const ProductArgs P)
+{
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n >= P.N) return;
+    const float bias = P.bias ? P.bias[n] : 0.f;
+    const size_t part = (size_t)P.M * P.N;
+    for (int m = blockIdx.y; m < P.M; m += gridDim.y) {
+        const float *p = parts + (size_t)m * P.N + n;
+        float v = p[0];
+#pragma unroll 4
+        for (int s = 1; s < P.split; ++s) v += p[s * part];
+        v += bias;
+        T *to = static_cast<T *>(P.C) + (long long)m * P.ldc + n;
+        if constexpr (sizeof(T) == 4) *to = v;
+        else *to = (bf16_t)pack_bf16(v, 0.f);
     }
 }
 
@@ -676,25 +707,62 @@ int mxfp4_matmul_prepare()
 // what they load, small ones leave fewer CUs idle: measured, large / medium / small,
 //   8192 x 8192 x 8192    264 / 302 / 459 us        4096 x 5120 x 5120    78 / 65 / 102 us       512 x 5120 x 5120   33 / 17 / 17 us
 //   4096 x 4096 x 4096     38 /  45 /  65 us        2048 x 2048 x 2048    18 / 11 /  12 us       300 x 5120 x 5120   40 / 21 / 14 us
-template <typename L> static double tile_time(int M, int N, int K)
+template <typename L> static double tile_time(int M, int N, int stages, int split)
 {
     constexpr int R = L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4;
     constexpr double start = R == 1 ? 7.0 : R == 2 ? 3.5 : 2.0, alone = R == 1 ? 1.6 : R == 2 ? 0.62 : 0.38, full = R == 1 ? 1.78 : R == 2 ? 1.09 : 0.86;
-    const long long tiles = (long long)cdiv(M, L::BM) * cdiv(N, L::BN), rounds = tiles / (256 * R), rest = (tiles - rounds * 256 * R + 255) / 256;
-    const double stages = cdiv(K, 256);
-    const double last = rest == 0 ? 0.0 : start + stages * (R == 1 ? alone : alone + (full - alone) * (double)(rest - 1) / (R > 1 ? R - 1 : 1));
-    return (double)rounds * (start + stages * full) + last;
+    const long long tiles = (long long)cdiv(M, L::BM) * cdiv(N, L::BN) * split, rounds = tiles / (256 * R), rest = (tiles - rounds * 256 * R + 255) / 256;
+    const double per = cdiv(stages, split);
+    const double last = rest == 0 ? 0.0 : start + per * (R == 1 ? alone : alone + (full - alone) * (double)(rest - 1) / (R > 1 ? R - 1 : 1));
+    return (double)rounds * (start + per * full) + last;
 }
 
-template <typename L> static int product_tiles(ProductArgs P, int out_dtype, hipStream_t st)
+// Which tiles, and in how many parts the contraction: the least time by that model, parts of four stages at least.  Adding them up is
+// a second launch and the parts' way out and back: 5 us, and 0.5 us for each MB of a part.  Measured, one part / as chosen:
+//   1536 x 1536 x 75,600   223 / 116 us  (7)        512 x 512 x 65,536    112 /  23 us (16)       64 x 5120 x 13,824    28 / 16 us (3)
+//    500 x  700 x 20,000    38 /  17 us  (5)        256 x 256 x 16,384     23 /  14 us (13)      512 x  512 x  8192     13 / 13 us (4)
+struct ProductPlan {
+    int size, split, per;           // size: 0 small, 1 medium, 2 large
+};
+
+static ProductPlan product_plan(int M, int N, int K)
+{
+    const int stages = cdiv(K, 256);
+    ProductPlan best = {0, 1, stages};
+    double least = 1e300;
+    for (int split = 1; split <= 16 && (split == 1 || stages >= 4 * split); ++split) {
+        const int per = cdiv(stages, split);
+        if (split > 1 && (cdiv(stages, per) != split || (double)split * M * N > (1 << 28))) continue;
+        const double join = split == 1 ? 0.0 : 5.0 + 0.5 * split * (double)M * N * sizeof(float) * 1e-6;
+        const double t[3] = {tile_time<Small>(M, N, stages, split), tile_time<Medium>(M, N, stages, split), tile_time<Large>(M, N, stages, split)};
+        for (int size = 0; size < 3; ++size)
+            if (t[size] + join < least * (size > best.size && split == best.split ? 1.0 : 0.999)) {
+                least = t[size] + join;
+                best = {size, split, per};
+            }
+    }
+    return best;
+}
+
+size_t mxfp4_matmul_ws_bytes(int M, int N, int K)
+{
+    if (few(M, N, K)) return 256;
+    const ProductPlan p = product_plan(M, N, K);
+    return p.split == 1 ? 256 : (size_t)p.split * M * N * sizeof(float);
+}
+
+template <typename L, typename T> static int product_tiles(ProductArgs P, hipStream_t st)
 {
     P.tiles_n = cdiv(P.N, L::BN);
-    const int tiles = cdiv(P.M, L::BM) * P.tiles_n, resident = 256 * (L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4);
-    const int grid = tiles < resident ? tiles : resident;
-    if (out_dtype == SVG2_BF16) mxfp4_product_kernel<L, bf16_t><<<grid, 64 * L::WAVES, L::LDS, st>>>(P);
-    else mxfp4_product_kernel<L, float><<<grid, 64 * L::WAVES, L::LDS, st>>>(P);
+    const int tiles = cdiv(P.M, L::BM) * P.tiles_n * P.split, resident = 256 * (L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4);
+    mxfp4_product_kernel<L, T><<<tiles < resident ? tiles : resident, 64 * L::WAVES, L::LDS, st>>>(P);
     SVG2_HIP_CHECK(hipGetLastError());
     return SVG2_OK;
+}
+
+template <typename T> static int product_sized(int size, const ProductArgs &P, hipStream_t st)
+{
+    return size == 2 ? product_tiles<Large, T>(P, st) : size == 1 ? product_tiles<Medium, T>(P, st) : product_tiles<Small, T>(P, st);
 }
 
 static int product_few(const ProductArgs &P, int out_dtype, hipStream_t st)
@@ -711,15 +779,25 @@ static int product_few(const ProductArgs &P, int out_dtype, hipStream_t st)
 }
 
 int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
-                        int out_dtype, void *C, int64_t ldc, hipStream_t st)
+                        int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st)
 {
-    const ProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
-                           static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0};
+    ProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
+                     static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0, 1, cdiv(K, 256)};
     if (few(M, N, K)) return product_few(P, out_dtype, st);
-    const double large = tile_time<Large>(M, N, K), medium = tile_time<Medium>(M, N, K), small = tile_time<Small>(M, N, K);
-    if (large <= medium && large <= small) return product_tiles<Large>(P, out_dtype, st);
-    if (medium <= small) return product_tiles<Medium>(P, out_dtype, st);
-    return product_tiles<Small>(P, out_dtype, st);
+    const ProductPlan p = product_plan(M, N, K);
+    if (p.split == 1) return out_dtype == SVG2_BF16 ? product_sized<bf16_t>(p.size, P, st) : product_sized<float>(p.size, P, st);
+    P.split = p.split;
+    P.per = p.per;
+    ProductArgs parts = P;
+    parts.bias = nullptr;
+    parts.C = ws;
+    parts.ldc = N;
+    SVG2_TRY(product_sized<float>(p.size, parts, st));
+    const dim3 grid(cdiv(N, 256), M < 4096 ? M : 4096);
+    if (out_dtype == SVG2_BF16) mxfp4_join_kernel<bf16_t><<<grid, 256, 0, st>>>(static_cast<const float *>(ws), P);
+    else mxfp4_join_kernel<float><<<grid, 256, 0, st>>>(static_cast<const float *>(ws), P);
+    SVG2_HIP_CHECK(hipGetLastError());
+    return SVG2_OK;
 }
 
 }  // namespace svg2

@@ -133,6 +133,8 @@ def _operand(R, K, seed, exps=(-6, 7)):
 PRODUCTS = [(1, 1, 1), (1, 64, 128), (1, 513, 640), (2, 96, 300), (7, 1000, 1000), (16, 130, 4224), (15, 33, 17000), (17, 255, 256),
             (33, 65, 129), (64, 512, 2048), (65, 127, 384), (128, 128, 128), (129, 257, 512), (255, 300, 1280), (256, 256, 256),
             (300, 1023, 777), (513, 640, 1000), (1000, 77, 64),
+            # few tiles and a long contraction: in parts, the last of them shorter, with 128 columns more
+            (70, 60, 20000), (130, 260, 16384), (129, 100, 33000), (300, 520, 24704),
             # more tiles of 64 x 64 than fit at once, and more than one of 128 x 128 or 256 x 256 for a workgroup; one to five stages
             (2049, 2177, 100), (2000, 2100, 513), (4129, 4225, 300), (4095, 4090, 513), (8190, 4093, 300), (4090, 8100, 1100)]
 
@@ -223,26 +225,28 @@ def test_linear_and_its_gradients(svg2):
     assert_within(dw, *ops.product(q(DY.T), q(X.T)), torch.float32, "dw")
 
 
-@pytest.mark.parametrize("M,N", [(1, 520), (130, 520), (2060, 2050)])
-def test_product_in_a_graph_beside_another(svg2, M, N):
-    """Two captured graphs, replayed with eager calls between them, then the same two products at once on two streams."""
-    K = 2176
+@pytest.mark.parametrize("M,N,K", [(1, 520, 2176), (130, 520, 2176), (2060, 2050, 2176), (100, 200, 20000)])
+def test_product_in_a_graph_beside_another(svg2, M, N, K):
+    """Two captured graphs, each with a workspace of its own (the last shape uses it), replayed with eager calls between them, then the
+    same two products at once on two streams."""
     sets = []
     for seed in (1, 2):
         _, _, a, sa = _operand(M, K, seed)
         _, _, b, sb = _operand(N, K, 10 + seed)
         ref = svg2.svg2_matmul_mxfp4(a, sa, b, sb)
-        sets.append((a, sa, b, sb, ref, torch.empty_like(ref)))
+        ws = torch.empty(svg2.load_library().svg2_matmul_mxfp4_workspace_size(M, N, K), dtype=torch.uint8, device="cuda")
+        sets.append((a, sa, b, sb, ref, torch.empty_like(ref), ws))
     graphs = []
-    for a, sa, b, sb, ref, out in sets:
+    for a, sa, b, sb, ref, out, ws in sets:
         torch.cuda.synchronize()
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
-            svg2.svg2_matmul_mxfp4(a, sa, b, sb, out=out)
+            svg2.svg2_matmul_mxfp4(a, sa, b, sb, out=out, ws=ws)
         graphs.append(g)
     for rep in range(4):
-        for (a, sa, b, sb, ref, out), g in zip(sets, graphs):
+        for (a, sa, b, sb, ref, out, ws), g in zip(sets, graphs):
             out.zero_()
+            ws.random_(0, 256)
             g.replay()
             again = svg2.svg2_matmul_mxfp4(a, sa, b, sb)
             torch.cuda.synchronize()
@@ -252,9 +256,9 @@ def test_product_in_a_graph_beside_another(svg2, M, N):
         s[5].zero_()
     torch.cuda.synchronize()
     for _ in range(5):
-        for (a, sa, b, sb, ref, out), s in zip(sets, streams):
+        for (a, sa, b, sb, ref, out, ws), s in zip(sets, streams):
             with torch.cuda.stream(s):
-                svg2.svg2_matmul_mxfp4(a, sa, b, sb, out=out)
+                svg2.svg2_matmul_mxfp4(a, sa, b, sb, out=out, ws=ws)
     torch.cuda.synchronize()
     assert all(torch.equal(s[5], s[4]) for s in sets)
 

@@ -150,16 +150,28 @@ def test_dequantize_mxfp4_refuses(lib):
 
 
 def test_matmul_mxfp4_refuses(lib):
-    ok = (1 << 20, 2 << 20, 3 << 20, 4 << 20, 128, 256, 512, None, 1, 5 << 20, 256, None)
+    ok = (1 << 20, 2 << 20, 3 << 20, 4 << 20, 128, 256, 512, None, 1, 5 << 20, 256, 256, 1 << 40, None)
     for at, v, code, word in ((0, None, 1, b"A:"), (1, None, 1, b"A:"), (2, 8, 1, b"B:"), (3, None, 1, b"B:"), (4, 0, 1, b"rows"), (5, -3, 1, b"rows"),
                               (6, 0, 1, b"columns"), (6, (1 << 24) + 1, 1, b"2^24"), (7, 2, 1, b"aligned"), (8, 9, 2, b"dtype"), (9, None, 1, b"null"),
-                              (9, (5 << 20) + 1, 1, b"aligned"), (10, 255, 1, b"ldc"), (9, 1 << 20, 1, b"alias")):
+                              (9, (5 << 20) + 1, 1, b"aligned"), (10, 255, 1, b"ldc"), (9, 1 << 20, 1, b"alias"), (11, 8, 1, b"aligned"),
+                              (12, 16, 3, b"workspace")):
         args = list(ok)
         args[at] = v
         assert lib.svg2_matmul_mxfp4(*args) == code, (at, v)
         assert word in lib.svg2_last_error(), (at, v, lib.svg2_last_error())
-    assert lib.svg2_matmul_mxfp4(1 << 20, 2 << 20, 3 << 20, 4 << 20, 1 << 21, 1 << 21, 512, None, 1, 5 << 20, 1 << 21, None) == 1
+    assert lib.svg2_matmul_mxfp4(1 << 20, 2 << 20, 3 << 20, 4 << 20, 1 << 21, 1 << 21, 512, None, 1, 5 << 20, 1 << 21, None, 0, None) == 1
     assert b"tiles" in lib.svg2_last_error()
+    # a long contraction of few tiles needs a workspace, an ordinary product none
+    size = lib.svg2_matmul_mxfp4_workspace_size
+    assert size(75600, 5120, 5120) == 256 and size(1, 15360, 5120) == 256 and size(0, 4, 4) == 256 and size(4, 4, 1 << 25) == 256
+    need = size(512, 512, 65536)
+    assert need >= 2 * 512 * 512 * 4
+    args = [1 << 20, 2 << 20, 3 << 20, 4 << 20, 512, 512, 65536, None, 1, 5 << 20, 512, None, 0, None]
+    assert lib.svg2_matmul_mxfp4(*args) == 1 and b"workspace" in lib.svg2_last_error()
+    args[11:13] = [6 << 20, need - 1]
+    assert lib.svg2_matmul_mxfp4(*args) == 3 and b"workspace" in lib.svg2_last_error()
+    args[11:13] = [5 << 20, need]
+    assert lib.svg2_matmul_mxfp4(*args) == 1 and b"alias" in lib.svg2_last_error()
 
 
 def test_bindings_refuse(lib):
