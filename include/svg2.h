@@ -367,7 +367,7 @@ int svg2_kmeans_pp_init(const void *X, int dtype, int H, int N, int d, int C,
  *   norm_weight    fp32, 16-byte aligned, or NULL: no norm
  *   pos            [B,N,n_axes] int32, batch stride pos_stride_b (0: all batches share one), dense inside
  *   freq           [d/2] fp64; both may be NULL where nothing is rotated
- *   n_axes 1..4, axis_pairs >= 0 with sum d/2; eps > 0; d 64 or 128; B*N <= 2^26
+ *   n_axes 1..4 (0 where nothing is rotated), axis_pairs >= 0 with sum d/2; eps > 0; d 64 or 128; B*N <= 2^26
  * svg2_rope_backward: with dY (strides dst_stride, of any sign: it is only read) the gradients
  *   dX[t] [B,N,H,d] with strides dx_stride (alignment as src; must not overlap an input), and
  *   dW[t] (shape of norm_weight[t], fp32; ignored where that is NULL).

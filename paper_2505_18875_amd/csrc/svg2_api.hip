@@ -104,8 +104,8 @@ static int check_rope(const svg2_rope_args *a, bool dst_written)
         SVG2_REQUIRE(multiple_of(a->norm_weight[t], 16), SVG2_INVALID_ARG, "norm_weight[%d] is not 16-byte aligned", t);
         SVG2_REQUIRE(a->eps > 0.f && a->eps < 1e30f, SVG2_INVALID_ARG, "eps = %g must be positive and finite", (double)a->eps);
     }
+    SVG2_REQUIRE(a->n_axes >= (rotated ? 1 : 0) && a->n_axes <= 4, SVG2_INVALID_ARG, "n_axes = %d must be in 1..4", a->n_axes);
     if (rotated) {
-        SVG2_REQUIRE(a->n_axes >= 1 && a->n_axes <= 4, SVG2_INVALID_ARG, "n_axes = %d must be in 1..4", a->n_axes);
         long long pairs = 0;
         for (int k = 0; k < a->n_axes; ++k) {
             SVG2_REQUIRE(a->axis_pairs[k] >= 0, SVG2_INVALID_ARG, "axis_pairs[%d] = %d is negative", k, a->axis_pairs[k]);

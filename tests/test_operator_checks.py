@@ -66,6 +66,7 @@ REFUSED = [
     (dict(n_tensors=0), 1, b"n_tensors"), (dict(n_tensors=4), 1, b"n_tensors"), (dict(dtype=5), 2, b"dtype"), (dict(d=96), 2, b"head dimension"),
     (dict(B=0), 1, b"B = 0"), (dict(N=0), 1, b"N = 0"), (dict(H=0), 1, b"H = 0"), (dict(B=1 << 14, N=1 << 13), 1, b"2^26"),
     (dict(pairing=2), 1, b"pairing"), (dict(norm_scope=-1), 1, b"norm_scope"), (dict(n_axes=0), 1, b"n_axes"), (dict(n_axes=5), 1, b"n_axes"),
+    (dict(rotate=(0, 0, 0), n_axes=5), 1, b"n_axes"), (dict(rotate=(0, 0, 0), n_axes=-1), 1, b"n_axes"),
     (dict(axis_pairs=(12, 10, 9)), 1, b"pairs"), (dict(axis_pairs=(42, -10, 0)), 1, b"negative"), (dict(pos=None), 1, b"pos and freq"),
     (dict(freq=None), 1, b"pos and freq"), (dict(src_stride=(2048, 252, 64)), 1, b"src stride"), (dict(pos_stride_b=-1), 1, b"pos_stride_b"),
     (dict(norm=(8, None, None)), 1, b"norm_weight[0]"), (dict(norm=(256, None, None), eps=0.0), 1, b"eps"),
