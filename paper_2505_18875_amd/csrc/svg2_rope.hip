@@ -13,7 +13,7 @@
 // needs an element of another's.  The angle of a lane's pairs is the same for every head, so four cosines and sines per lane and
 // token serve all of them: cheap enough to compute in place, in 64 bits up to the quarter turn (positions of 10^6 times a
 // frequency of 1 leave no fraction in 32), instead of reading a table.
-// Q, K and V of 75,600 tokens of 40 heads of 128 in bf16 (4.6 GB in and out): 881 us, 5.3 TB/s; a large copy reaches 5.0.
+// Q, K and V of 75,600 tokens of 40 heads of 128 in bf16 (4.6 GB in and out): 856 to 881 us, 5.3 to 5.4 TB/s, the rate of a large copy.
 #include <type_traits>
 
 #include "svg2_common.h"
