@@ -170,13 +170,14 @@ __device__ __forceinline__ float group_sum(float x, int width)
 }
 
 // ---- forward ---------------------------------------------------------------
-// grid (ceil(B N / (256 / G)), tensors), block 256: G lanes a token.  64, or where a token has fewer than 512 values the 8, 16 or 32
-// that hold them: one head of 64 a wavefront, 4096 tokens, took 11 us, eight of them take 5.
+// grid (ceil(B N / (256 / G)), tensors, 1), block 256: G lanes a token.  64, or where a token has fewer than 512 values the 8, 16 or 32
+// that hold them: one head of 64 a wavefront, 4096 tokens, took 11 us, eight of them take 5.  More than 2^23 workgroups go on in the
+// third dimension (see token_grid).
 template <typename T, int D, bool ADJ, int G, int CH> __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs A)
 {
     constexpr int LPH = D / 8, HPS = G / LPH;
     const int lane = threadIdx.x % G, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int token = blockIdx.x * (256 / G) + (G == 64 ? wave : (int)threadIdx.x / G), t = blockIdx.y;
+    const int token = (blockIdx.z * gridDim.x + blockIdx.x) * (256 / G) + (G == 64 ? wave : (int)threadIdx.x / G), t = blockIdx.y;
     if (token >= A.B * A.N) return;             // all lanes of a token together: the sums below stay inside them
     const int b = token / A.N, n = token - b * A.N;
     const int hl = lane / LPH, c = lane % LPH;
@@ -673,6 +674,14 @@ template <int D, typename F> static void with_lanes(int H, F f)
     else f(std::integral_constant<int, 64>());
 }
 
+// A launch takes fewer than 2^32 threads in a dimension, and 2^26 tokens of a wavefront each are that many: the workgroups behind the
+// first 2^23 go into the third dimension.  Some of the last row of them have no token: rope_kernel asks.
+static dim3 token_grid(int workgroups, int tensors)
+{
+    const int most = 1 << 23;
+    return workgroups <= most ? dim3(workgroups, tensors) : dim3(most, tensors, cdiv(workgroups, most));
+}
+
 static int forward(const svg2_rope_args *a, const RopeArgs &A, hipStream_t st)
 {
     return with_types(a, [&](auto *tp, auto dim, auto adj) -> int {
@@ -683,10 +692,10 @@ static int forward(const svg2_rope_args *a, const RopeArgs &A, hipStream_t st)
         // more than two steps of a wavefront: a workgroup a token, up to where both are bound by memory
         if (lanes > 128 && tokens <= 8192 && lanes <= 256) rope_row_kernel<T, D, ADJ, 1><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
         else if (lanes > 128 && tokens <= 8192 && lanes <= 768) rope_row_kernel<T, D, ADJ, 3><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
-        else if (lanes > 128) rope_kernel<T, D, ADJ, 64, 10><<<dim3(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
+        else if (lanes > 128) rope_kernel<T, D, ADJ, 64, 10><<<token_grid(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
         else with_lanes<D>(A.H, [&](auto g) {
             constexpr int G = decltype(g)::value;
-            rope_kernel<T, D, ADJ, G, G == 64 ? 2 : 1><<<dim3(cdiv(tokens, 256 / G), a->n_tensors), 256, 0, st>>>(A);
+            rope_kernel<T, D, ADJ, G, G == 64 ? 2 : 1><<<token_grid(cdiv(tokens, 256 / G), a->n_tensors), 256, 0, st>>>(A);
         });
         SVG2_HIP_CHECK(hipGetLastError());
         return SVG2_OK;
@@ -721,6 +730,7 @@ static RopeBwdPlan bwd_plan(const svg2_rope_args *a)
         p.P = p.blocks < 64 ? p.blocks : 64;
         if (p.P > most) p.P = most;
         p.rinv_bytes = align256(3 * (size_t)tokens * sizeof(float));
+        if (p.blocks > 1 << 22) p.blocks = 1 << 22;     // its workgroups stride over the tokens (a launch: see token_grid)
     }
     p.total = p.rinv_bytes + 3 * (size_t)p.P * p.cols * sizeof(float);
     if (p.total < 256) p.total = 256;
