@@ -357,7 +357,7 @@ int svg2_kmeans_pp_init(const void *X, int dtype, int H, int N, int d, int C,
  *                                          (p, p + d/2) (SVG2_ROPE_HALVES)
  * and y = x' otherwise (a tensor that is only moved is copied bit for bit).
  * Axis k takes the next axis_pairs[k] pairs; a token at position 0 and a pair
- * of frequency 0 are not rotated.  Angles are formed in double precision, norm
+ * of frequency 0 are not rotated: y = x' there, whatever the pair holds.  Angles are formed in double precision, norm
  * and rotation in fp32, rounded once to dtype.
  *   src, dst       [B,N,H,d] dtype each, element (b,n,h,i) at b*stride[0] + n*stride[1] + h*stride[2] + i (elements);
  *                  16-byte aligned, strides multiples of 16 bytes.  The layer's [B*H,N,d] has strides (H*N*d, d, N*d).

@@ -152,13 +152,15 @@ __device__ __forceinline__ void angles(const RopeArgs &A, int b, int n, int c, f
     for (int k = 0; k < 4; ++k) angle(A, position(A, b, n), 4 * c + k, cs[k], sn[k]);
 }
 
+// A sine of 0 is that of an angle of 0 (no other double comes that near to a multiple of pi / 2): such a pair is left as it is, since 0
+// times an infinity would make its partner NaN, and plus 0 times a negative number a negative zero positive.
 template <bool ADJ> __device__ __forceinline__ void turn(float *v, const float *cs, const float *sn, float sense)
 {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const float a = v[at<ADJ>(k, 0)], b = v[at<ADJ>(k, 1)], s = sense * sn[k];
-        v[at<ADJ>(k, 0)] = a * cs[k] - b * s;
-        v[at<ADJ>(k, 1)] = a * s + b * cs[k];
+        v[at<ADJ>(k, 0)] = s == 0.f ? a : a * cs[k] - b * s;
+        v[at<ADJ>(k, 1)] = s == 0.f ? b : a * s + b * cs[k];
     }
 }
 
