@@ -502,9 +502,13 @@ def _head_order(tensors, name, device, dtype, shape):
     return [H * s[0] if B > 1 else 0, s[1], s[0] if H > 1 else 0], ptrs
 
 
-def svg2_grid_positions(grid, *, first=(0, 0, 0), extra=0, device="cuda"):
+def svg2_grid_positions(grid, *, first=None, extra=0, device="cuda"):
     """Positions (time, height, width) of a video's tokens in raster order, int32 [T*Y*X + extra, 3], the grid starting at
-    `first`; `extra` tokens behind the video's (text) get position 0, which rotates nothing."""
+    `first` (0 on every axis); `extra` tokens behind the video's (text) get position 0, which rotates nothing.  A grid of
+    other axes (one to the rotary call's four) gives as many columns."""
+    first = (0,) * len(grid) if first is None else first
+    if len(first) < len(grid):
+        raise ValueError("first has %d axes, the grid has %d" % (len(first), len(grid)))
     axes = [torch.arange(n, dtype=torch.int32, device=device) + f for n, f in zip(grid, first)]
     video = torch.stack([a.reshape(-1) for a in torch.meshgrid(*axes, indexing="ij")], 1)
     return torch.cat([video, video.new_zeros((extra, len(axes)))]).contiguous()
