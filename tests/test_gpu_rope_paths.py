@@ -59,3 +59,62 @@ def test_what_is_not_rotated_keeps_its_bits(svg2, dtype, pairing, H):
             ref, size = ops.turn(x64, a, pairing, sense), ops.pair_norm(x64, pairing)
         bound = (12 * ops.U + 2.0 ** -51 * 20) * size
         assert_within(got[:, :, moving][None], ref[..., moving], bound[..., moving], dtype)
+
+
+# a norm over the head goes through the heads 16 (of 128) or 32 (of 64) at a time: one, two and three rounds, the last of them partial;
+# fewer tokens than wavefronts and more
+HEADS = [(torch.bfloat16, 1, 37, 40, 128), (torch.float32, 2, 19, 17, 128), (torch.float32, 1, 23, 33, 64), (torch.float32, 1, 1, 67, 64),
+         (torch.bfloat16, 1, 2111, 40, 128), (torch.float32, 3, 701, 35, 64), (torch.bfloat16, 2, 5, 32, 64), (torch.float32, 1, 11, 16, 128)]
+
+
+@pytest.mark.parametrize("pairing", ["adjacent", "halves"])
+@pytest.mark.parametrize("dtype,B,N,H,d", HEADS)
+def test_gradients_of_a_norm_over_many_heads(svg2, dtype, B, N, H, d, pairing):
+    g = torch.Generator().manual_seed(N + H)
+    qk = torch.randn((B, N, 2, H, d), generator=g).to(dtype).cuda()
+    x = [qk[:, :, i] for i in range(2)]
+    grads = [torch.randn((B * H, N, d), generator=g).to(dtype).cuda() for _ in range(2)]
+    w = [1 + 0.3 * torch.randn((d,), generator=g) for _ in range(2)]
+    pos = torch.randint(0, 97, (N, 2), generator=g, dtype=torch.int32)
+    share = (d // 2 - 11, 11)
+    freq = torch.cat([10000.0 ** (-torch.arange(n, dtype=torch.float64) / n) for n in share])
+    res = svg2.svg2_rope_backward(grads, x, pos.cuda(), freq.cuda(), axis_pairs=share, norm_weights=[t.cuda() for t in w], pairing=pairing)
+    a = ops.angles(pos.numpy()[None], freq.numpy(), share)
+    for i in range(2):
+        gi = grads[i].view(B, H, N, d).transpose(1, 2)
+        dx, bound, dw, dw_bound = ops.rope_backward(gi.double().cpu().numpy(), x[i].double().cpu().numpy(), w[i].double().numpy(), a, "head",
+                                                    1e-6, pairing)
+        assert_within(res.grads[i], dx, bound, dtype, "dx %d" % i)
+        assert_within(res.dweights[i], dw, dw_bound, torch.float32, "dw %d" % i)
+
+
+@pytest.mark.parametrize("pairing", ["adjacent", "halves"])
+@pytest.mark.parametrize("scope,H,d", [("head", 3, 64), ("token", 3, 64), ("head", 33, 64), ("token", 17, 128), ("token", 65, 128)])
+def test_gradients_are_the_slope_of_the_formula(svg2, scope, H, d, pairing):
+    """The gradients, along random directions, against central differences of the formula in 64 bits.  With steps of h = 2^-17 a difference
+    is off by a third of what doubling the step changes (its error goes with h^2), and by the rounding of its two values: 16 operations of 2^-53
+    of the sum of magnitudes, over h.  The gradients are off by their bounds and one rounding to fp32."""
+    N, eps = 7, 1e-6
+    g = torch.Generator().manual_seed(H + d)
+    x, dy, dir_x = (torch.randn((1, N, H, d), generator=g) for _ in range(3))
+    shape = (d,) if scope == "head" else (H, d)
+    w, dir_w = 1 + 0.3 * torch.randn(shape, generator=g), torch.randn(shape, generator=g)
+    pos = torch.randint(0, 50, (N, 3), generator=g, dtype=torch.int32)
+    share = (d // 2 - 20, 10, 10)
+    freq = torch.cat([10000.0 ** (-torch.arange(n, dtype=torch.float64) / n) for n in share])
+    res = svg2.svg2_rope_backward([dy.cuda()], [x.cuda()], pos.cuda(), freq.cuda(), axis_pairs=share, norm_weights=[w.cuda()], norm_scope=scope,
+                                  eps=eps, pairing=pairing)
+    a = ops.angles(pos.numpy()[None], freq.numpy(), share)
+    x, dy, dir_x, w, dir_w = (t.double().numpy() for t in (x, dy, dir_x, w, dir_w))
+
+    def slope(h):
+        y = [ops.rope(x + s * h * dir_x, w + s * h * dir_w, a, scope, eps, pairing)[0] * dy for s in (1, -1)]
+        return (y[0].sum() - y[1].sum()) / (2 * h), 16 * 2.0 ** -53 * np.abs(y[0]).sum() / h
+
+    want, rounding = slope(2.0 ** -17)
+    twice, _ = slope(2.0 ** -16)
+    _, bound, _, dw_bound = ops.rope_backward(dy, x, w, a, scope, eps, pairing)
+    dx, dw = (t.double().cpu().numpy() for t in (res.grads[0], res.dweights[0]))
+    tol = ((bound + ops.U * np.abs(dx)) * np.abs(dir_x)).sum() + ((dw_bound + ops.U * np.abs(dw)) * np.abs(dir_w)).sum()
+    got = (dx * dir_x).sum() + (dw * dir_w).sum()
+    assert abs(got - want) <= tol + rounding + abs(twice - want), (got, want, tol, rounding, twice)
