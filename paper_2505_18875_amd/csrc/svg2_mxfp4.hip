@@ -586,11 +586,28 @@ template <typename T> __global__ __launch_bounds__(256) void mxfp4_join_kernel(c
 // columns 32 (l / 16) ..: 64 neighbouring bytes of a row, two instructions a cache line.  16 rows of B a workgroup, the rows of A
 // behind the last as the last; every wavefront has FEW_PAIRS lines of its rows on their way before it uses the first.  The
 // wavefronts' sums meet in LDS and are added in order.
-// Measured, this kernel / 64 x 64 tiles, us: one row and 15,360 x 5120 weights (42 MB with their scales) 10.7 / 13.5, 5120 x 5120
-// 7.2 / 10.4, 64 x 8192 4.7 / 13.2; from some 40 MB on the tiles' loads, which do not wait for registers, win: 16 rows, 20,480 x 5120
-// 15.9 / 13.6, 20,480 x 8192 24.4 / 19.4.
+// Measured, this kernel / tiles, us: 5120 x 5120 weights and a row 7.2 / 10.4, 64 x 8192 4.7 / 13.2; the same weights again and again (the
+// last cache holds them) and, in brackets, as many sets of weights in turn as come from memory:
+//                      1 row                       4 rows                      8 rows                      16 rows
+//   15,360 x 5120      10.0 / 12.5 (12.3 / 18.4)   10.2 / 12.4 (13.1 / 18.2)   10.8 / 12.4 (13.6 / 18.2)   12.3 / 12.4 (15.9 / 18.2)
+//   20,480 x 5120      12.4 / 12.7 (15.6 / 20.3)   12.3 / 12.8 (16.3 / 20.2)   12.8 / 12.8 (17.2 / 18.8)   14.9 / 12.9 (19.8 / 18.9)
+//   20,480 x 8192      17.7 / 18.3 (20.8 / 22.6)   18.2 / 18.4 (21.9 / 21.7)   19.3 / 18.6 (24.0 / 22.0)   22.4 / 19.1 (27.9 / 22.5)
+//   32,768 x 8192      26.2 / 21.8 (29.6 / 37.0)   27.1 / 21.5 (31.4 / 34.9)   28.8 / 21.5 (35.3 / 35.0)   33.5 / 21.6 (42.0 / 35.0)
+//    4096 x 32,768     14.5 / 16.6 (17.1 / 20.7)   15.0 / 16.8 (18.4 / 20.0)   16.0 / 16.9 (18.9 / 20.1)   19.3 / 17.1 (22.7 / 20.2)
+//    4096 x 16,384      8.0 / 11.5 ( 9.4 / 13.4)    8.5 / 11.5 (10.1 / 13.3)    9.2 / 11.7 (10.6 / 13.4)   10.2 / 11.3 (12.3 / 13.6)
+//    2048 x 16,384      7.2 /  8.5 ( 8.5 / 11.6)    7.7 /  8.8 ( 9.1 / 10.9)    8.5 /  8.8 ( 9.8 / 11.0)    9.8 /  9.4 (11.7 / 11.6)
+//    1024 x 32,768     11.6 /  8.7 (13.0 / 13.0)   12.9 /  8.9 (14.5 / 13.1)   14.3 /  9.0 (16.4 / 13.2)   17.0 /  9.4 (20.4 / 13.4)
+//     512 x 65,536     21.3 / 11.1 (23.6 / 18.7)   23.8 / 11.3 (26.4 / 18.7)   26.4 / 11.5 (30.0 / 19.1)   31.7 / 11.6 (37.2 / 19.1)
+// so up to 4 rows take it to 10 * 2^24 weights, up to 16 rows to 5 * 2^24; rows longer than 2^14, which one workgroup goes through alone
+// here and several workgroups in tiles, only where 4096 of them keep the card busy.  Within the rule 5120 x 13,824 is better in tiles where the
+// cache has it: 12.1 / 10.8 (14.1 / 14.0) for one row, 16.3 / 11.6 (19.8 / 13.9) for 16.
+// What bounds it: 98 registers, so four wavefronts a SIMD, 512 of the 960 workgroups of 15,360 rows of B at a time, and half of their loads are
+// of A.  It reads its 44 MB past L2 at 4.2 TB/s where the last cache has them, at 3.5 TB/s from memory.
 constexpr int FEW_ROWS = 16, FEW_PAIRS = 4, FEW_WAVES = 16;
-static bool few(int M, int N, int K) { return M <= FEW_ROWS && (long long)N * K <= 5 << 24; }
+static bool few(int M, int N, int K)
+{
+    return M <= FEW_ROWS && (long long)N * K <= (M <= 4 ? 10 : 5) << 24 && (K <= 1 << 14 || N >= 4096);
+}
 
 template <typename T> __global__ __launch_bounds__(64 * FEW_WAVES) void mxfp4_few_kernel(const ProductArgs P)
 {

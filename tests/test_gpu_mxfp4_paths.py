@@ -82,3 +82,24 @@ def test_product_on_every_path(svg2, M, N, K):
     assert bool(got[M // 2].isnan().all()) and bool(got[:, N // 3].isnan().all())
     got[M // 2], got[:, N // 3] = ref[M // 2], ref[:, N // 3]
     assert bool((got == ref).all())
+
+
+# both sides of the borders of the kernel for few rows: 4 rows and 10 * 2^24 weights, 16 rows and 5 * 2^24, rows of 2^14 and 4096 of them
+@pytest.mark.parametrize("M,N,K", [(1, 20480, 8192), (4, 20480, 8192), (4, 20481, 8192), (3, 18431, 5376), (2, 300, 400000), (4, 400, 500000),
+                                   (4, 4096, 16512), (4, 4095, 16512), (16, 4095, 16384), (16, 97, 16512),
+                                   (5, 16384, 5120), (5, 16385, 5120), (16, 8192, 10240), (16, 8192, 10368), (17, 8192, 2048)])
+def test_product_of_few_rows_beside_its_borders(svg2, M, N, K):
+    """Rows of ones and of twos, and weights of 0 to 1.5 in halves at scale 1: sums of up to 500,096 halves of at most 6, exact in fp32."""
+    nk = -(-K // 128)
+    assert 6 * nk * 128 < 2 ** 24
+    b, sb = small_operand(N, nk, 5)
+    sb.fill_(127)
+    a = torch.full((M, nk * 64), 0x22, dtype=torch.uint8, device="cuda")
+    sa = torch.full((nk, M, 4), 127, dtype=torch.uint8, device="cuda")
+    sa[:, M // 2] = 128
+    sums = torch.zeros((N,), dtype=torch.float64, device="cuda")
+    for n0 in range(0, N, 2048):
+        sums[n0:n0 + 2048] = svg2.svg2_dequantize_mxfp4(b[n0:n0 + 2048], sb[:, n0:n0 + 2048].clone(), dtype=torch.float32).double().sum(1)
+    got = svg2.svg2_matmul_mxfp4(a, sa, b, sb, out_dtype=torch.float32)
+    for m in range(M):
+        assert bool((got[m].double() == (2 if m == M // 2 else 1) * sums).all()), m
