@@ -373,7 +373,8 @@ int svg2_kmeans_pp_init(const void *X, int dtype, int H, int N, int d, int C,
  *   dW[t] (shape of norm_weight[t], fp32; ignored where that is NULL).
  *   args as in the forward call; args->dst is ignored, args->src is read where norm_weight is given.
  * The sums over tokens are formed in a fixed order: results are the same from
- * run to run.
+ * run to run.  They are fp32 within one of 64 to 2048 shares of the tokens (by
+ * the length of a token, fewer where there are few tokens), fp64 over the shares.
  * ------------------------------------------------------------------------- */
 enum { SVG2_ROPE_ADJACENT = 0, SVG2_ROPE_HALVES = 1 };
 enum { SVG2_NORM_HEAD = 0, SVG2_NORM_TOKEN = 1 };

@@ -95,7 +95,7 @@ template <typename T, bool STREAM> __device__ __forceinline__ void load8(const Q
 
 // rows: grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a row of 128 columns, 4 lanes a block of 32.  A value is read
 // once, a lane's eight stay in registers, and a block's maximum goes round four neighbouring lanes without LDS.  Bound by HBM:
-// 75,600 x 5120 bf16 (774 MB in, 206 out) 178 to 191 us, 5.1 to 5.5 TB/s.
+// 75,600 x 5120 bf16 (774 MB in, 206 out) 180 to 192 us, 5.1 to 5.4 TB/s; 75,599 x 5119, whose rows share lines, 236.
 template <typename T, bool STREAM> __global__ __launch_bounds__(256) void mxfp4_quant_kernel(const QuantArgs A)
 {
     const int lane16 = threadIdx.x & 15, K = A.G * A.Kg, nk = (K + 127) / 128;
@@ -123,7 +123,8 @@ template <typename T, bool STREAM> __global__ __launch_bounds__(256) void mxfp4_
 // grid (ceil(K / 64) rounded up to 8, slices of the rows), block 256: tiles of 128 rows x 64 columns through LDS; four lanes a column,
 // 32 rows each.  A slice is `per` neighbouring tiles, an even number: two of them fill a cache line of codes.  Neighbouring columns go to
 // the same XCD (every eighth workgroup): where rows are not whole lines they share some.
-// Bound by HBM where X is large (75,600 x 5120 bf16: 240 us, 4.1 TB/s), by its few long steps where it is small (16,384 x 1536: 13 us).
+// Bound by HBM where X is large (75,600 x 5120 bf16: 240 us, 4.1 TB/s; 75,599 x 5119, whose rows share lines, 401), by its few long steps where
+// it is small (16,384 x 1536: 14 us; 1021 x 777 fp32: 7 us, 52 workgroups with two tiles each, one after the other).
 // In LDS a row takes 33 words in bf16 (65 in fp32), and 8 words more for each 32 rows before it, so that the 64 lanes of a wavefront,
 // 16 columns x 4 blocks, read every bank once (fp32: twice, as the 256 bytes must).
 template <typename T, bool STREAM> __global__ __launch_bounds__(256) void mxfp4_quant_t_kernel(const QuantArgs A, int per)
@@ -185,7 +186,8 @@ __device__ __forceinline__ void scale_factors(unsigned byte, float &a, float &b)
 }
 
 // grid (row groups, slices of the columns), block 256: a lane writes 16 bytes, 8 or 4 values.  Bound by the writes: 75,600 x 5120 bf16 in
-// 145 us, 5.3 TB/s of values, the codes from the last cache where they were written just before.
+// 145 us, 5.3 TB/s of values, the codes from the last cache where they were written just before.  Rows that are not whole lines: the steps of
+// 256 bytes begin inside a line, so lines are written in two pieces, 75,599 x 5119 in 312 us.
 template <typename T> constexpr int values_rows() { return 256 / (128 * (int)sizeof(T) / 16); }     // rows of a workgroup: 16 bf16, 8 fp32
 
 template <typename T, bool STREAM>
@@ -283,7 +285,8 @@ template <int I, int J> __device__ __forceinline__ void settle(f32x16 (&a)[I][J]
 // sets: the next quarter is read from LDS while the matrix instructions of this one run.  The one barrier of a stage stands before
 // its last quarter: the next stage has arrived by then, and this one's place is free as soon as its last quarter is in registers.
 // Where there are few tiles and many stages, a part of the stages is a tile of its own (split), and mxfp4_join_kernel adds them up.
-// In LDS row r has 128 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.
+// In LDS row r has 128 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.  Bank conflicts are counted
+// where results go through LDS, 1536 cycles a tile of 256 x 256 whatever the number of its stages (6.6 % of the LDS cycles at 20 stages).
 // Rows behind the last are read as the last and not stored.
 template <int WM_, int WN_, int WI_, int WJ_> struct Tile {
     static constexpr int WM = WM_, WN = WN_, WI = WI_, WJ = WJ_, WAVES = WM * WN, BM = 32 * WI * WM, BN = 32 * WJ * WN;
@@ -738,7 +741,8 @@ template <typename L> static double tile_time(int M, int N, int stages, int spli
     return (double)rounds * (start + per * full) + last;
 }
 
-// Which tiles, and in how many parts the contraction: the least time by that model, parts of four stages at least.  Adding them up is
+// Which tiles, and in how many parts the contraction: the least time by that model, parts of four stages at least, 16 parts at most (more
+// were not measured; 64 x 64 x 1,000,064 runs on 16 workgroups, 126 us, where its operands take 13 to read).  Adding them up is
 // a second launch and the parts' way out and back: 5 us, and 0.5 us for each MB of a part.  Measured, one part / as chosen:
 //   1536 x 1536 x 75,600   223 / 116 us  (7)        512 x 512 x 65,536    112 /  23 us (16)       64 x 5120 x 13,824    28 / 16 us (3)
 //    500 x  700 x 20,000    38 /  17 us  (5)        256 x 256 x 16,384     23 /  14 us (13)      512 x  512 x  8192     13 / 13 us (4)

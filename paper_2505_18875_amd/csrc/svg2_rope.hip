@@ -13,7 +13,7 @@
 // needs an element of another's.  The angle of a lane's pairs is the same for every head, so four cosines and sines per lane and
 // token serve all of them: cheap enough to compute in place, in 64 bits up to the quarter turn (positions of 10^6 times a
 // frequency of 1 leave no fraction in 32), instead of reading a table.
-// Q, K and V of 75,600 tokens of 40 heads of 128 in bf16 (4.6 GB in and out): 856 to 881 us, 5.3 to 5.4 TB/s, the rate of a large copy.
+// Q, K and V of 75,600 tokens of 40 heads of 128 in bf16 (4.6 GB in and out): 859 to 887 us, 5.2 to 5.4 TB/s, the rate of a large copy.
 #include <type_traits>
 
 #include "svg2_common.h"
@@ -318,7 +318,9 @@ template <typename T, int D, bool ADJ, int S> __global__ __launch_bounds__(256) 
 
 // ---- backward --------------------------------------------------------------
 // How the weights' gradient is summed: per lane over the tokens that pass through it, over the block's wavefronts in LDS where
-// they hold the same columns, over the blocks by rope_dw_kernel, each in a fixed order, so that it is the same from run to run.
+// they hold the same columns, over the blocks by rope_dw_kernel, each in a fixed order, so that it is the same from run to run.  The first
+// two in fp32, where a lane's additions in a row grow with the tokens (821 of them for 420,000 tokens of 40 heads of 128 under a norm over the
+// token, each off by 2^-24 of the sum at most); over the blocks in 64 bits.
 enum { DW_NONE, DW_STEP, DW_ROW, DW_LONG };
 //   DW_NONE    no norm: the forward's kernels, turning back
 //   DW_STEP    [d] weights, or [H,d] of a token that is one step of a wavefront: 8 sums per lane (rope_bwd_kernel)
@@ -691,7 +693,10 @@ static int forward(const svg2_rope_args *a, const RopeArgs &A, hipStream_t st)
         constexpr int D = decltype(dim)::value;
         constexpr bool ADJ = decltype(adj)::value;
         const int lanes = A.H * (D / 8), tokens = A.B * A.N;
-        // more than two steps of a wavefront: a workgroup a token, up to where both are bound by memory
+        // More than two steps of a wavefront: a workgroup a token, up to where both are bound by memory (figures beside rope_row_kernel).
+        // Its edges, us for Q, K and V of heads of 128: 48 heads are the most that rope_row_kernel's three steps hold, one token 3.7, 49
+        // heads by a wavefront 9.5; 40 heads are the most that rope_kernel's ten steps hold, a longer token is read twice under a norm over
+        // the token: 75,600 tokens of 40 heads 859, of 41 heads 1008 (norm per head, read once: 864 and 897).
         if (lanes > 128 && tokens <= 8192 && lanes <= 256) rope_row_kernel<T, D, ADJ, 1><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
         else if (lanes > 128 && tokens <= 8192 && lanes <= 768) rope_row_kernel<T, D, ADJ, 3><<<dim3(tokens, a->n_tensors), 256, 0, st>>>(A);
         else if (lanes > 128) rope_kernel<T, D, ADJ, 64, 10><<<token_grid(cdiv(tokens, 4), a->n_tensors), 256, 0, st>>>(A);
