@@ -103,3 +103,35 @@ def test_product_of_few_rows_beside_its_borders(svg2, M, N, K):
     got = svg2.svg2_matmul_mxfp4(a, sa, b, sb, out_dtype=torch.float32)
     for m in range(M):
         assert bool((got[m].double() == (2 if m == M // 2 else 1) * sums).all()), m
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_quantize_takes_any_view_with_contiguous_groups(svg2, dtype, transposed):
+    """Rows that are one row, a transposed matrix as groups of one column, windows that overlap, one row, one column: as their dense copies."""
+    g = torch.Generator().manual_seed(9)
+    base = torch.randn((300, 517), generator=g).to(dtype).cuda()
+    views = [base[7].expand(130, 517),                              # stride 0
+             base.t().unsqueeze(-1),                                # [517, 300, 1]: any matrix, a column a group
+             base.as_strided((90, 300), (7, 1), 3),                 # rows that overlap
+             base.as_strided((40, 11, 33), (517, 64, 1), 1),        # groups with gaps, off every alignment
+             base[:1], base[:, 3:4], base[5:6, 5:6]]
+    for v in views:
+        dense = v.contiguous().reshape(v.shape[0], -1)
+        got, ref = svg2.svg2_quantize_mxfp4(v, transposed=transposed), svg2.svg2_quantize_mxfp4(dense, transposed=transposed)
+        assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1]), (v.shape, v.stride())
+
+
+def test_an_operand_times_itself_and_two_streams(svg2):
+    """A and B may be one operand; products on two streams share operands but not workspaces."""
+    a, sa = small_operand(300, 160, 3)
+    v = svg2.svg2_dequantize_mxfp4(a, sa, dtype=torch.float32).double()
+    ref = torch.matmul(v, v.t().contiguous()).float()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = []
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            outs.append(svg2.svg2_matmul_mxfp4(a, sa, a, sa, out_dtype=torch.float32))
+    torch.cuda.synchronize()
+    assert all(bool((o == ref).all()) for o in outs)

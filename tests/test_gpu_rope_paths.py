@@ -118,3 +118,45 @@ def test_gradients_are_the_slope_of_the_formula(svg2, scope, H, d, pairing):
     tol = ((bound + ops.U * np.abs(dx)) * np.abs(dir_x)).sum() + ((dw_bound + ops.U * np.abs(dw)) * np.abs(dir_w)).sum()
     got = (dx * dir_x).sum() + (dw * dir_w).sum()
     assert abs(got - want) <= tol + rounding + abs(twice - want), (got, want, tol, rounding, twice)
+
+
+# which tensors have a norm, which are rotated; one to three of them; axes without pairs
+MIXED = [((None, "w"), (True, False)), (("w", None), (False, True)), (("w",), (False,)), ((None, None, "w"), (True, False, True)),
+         (("w", "w", "w"), (False, False, False)), ((None, None), (False, False))]
+
+
+@pytest.mark.parametrize("scope,H,d", [("head", 5, 64), ("token", 2, 128), ("token", 9, 128), ("token", 33, 128), ("token", 65, 128)])
+@pytest.mark.parametrize("normed,rotate", MIXED)
+def test_each_tensor_has_its_own_norm_and_rotation(svg2, normed, rotate, scope, H, d):
+    B, N, n = 2, 11, len(normed)
+    g = torch.Generator().manual_seed(H + n)
+    packed = torch.randn((B, N, n, H, d), generator=g).cuda()
+    x = [packed[:, :, i] for i in range(n)]
+    dy = [torch.randn((B * H, N, d), generator=g).cuda() for _ in range(n)]
+    w = [None if k is None else 1 + 0.3 * torch.randn((d,) if scope == "head" else (H, d), generator=g) for k in normed]
+    share = (0, d // 2 - 5, 0, 5)
+    pos = torch.randint(-60, 60, (B, N, 4), generator=g, dtype=torch.int32)
+    freq = 10.0 ** -torch.rand(d // 2, generator=g, dtype=torch.float64)
+    kw = dict(axis_pairs=share, rotate=rotate, norm_weights=[None if t is None else t.cuda() for t in w], norm_scope=scope, pairing="halves")
+    place = (pos.cuda(), freq.cuda()) if any(rotate) else (None, None)
+    out = svg2.svg2_rope(x, *place, **kw)
+    res = svg2.svg2_rope_backward(dy, x, *place, **kw)
+    angle = ops.angles(pos.numpy(), freq.numpy(), share)
+    for i in range(n):
+        heads = lambda t: t.view(B, H, N, d).transpose(1, 2)        # noqa: E731
+        if w[i] is None and not rotate[i]:
+            assert torch.equal(heads(out[i]), x[i]) and torch.equal(res.grads[i], heads(dy[i])) and res.dweights[i] is None
+            continue
+        x64, g64 = (t.double().cpu().numpy() for t in (x[i], heads(dy[i])))
+        w64 = None if w[i] is None else w[i].double().numpy()
+        a = angle if rotate[i] else None
+        y, bound = ops.rope(x64, w64, a, scope, 1e-6, "halves")
+        far = 2.0 ** -51 * 60                                       # an angle is one 64-bit product
+        assert_within(heads(out[i]), y, bound + far * ops.pair_norm(y, "halves"), torch.float32, "y %d" % i)
+        dx, bound, dw, dw_bound = ops.rope_backward(g64, x64, w64, a, scope, 1e-6, "halves")
+        # without a rotation the gradient's own size stands for its pair's: the bound of a rotation is the larger
+        assert_within(res.grads[i], dx, bound + far * ops.pair_norm(np.abs(dx), "halves"), torch.float32, "dx %d" % i)
+        if w64 is None:
+            assert res.dweights[i] is None
+        else:
+            assert_within(res.dweights[i], dw, dw_bound, torch.float32, "dw %d" % i)
