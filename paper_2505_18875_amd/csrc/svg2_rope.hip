@@ -152,8 +152,8 @@ __device__ __forceinline__ void angles(const RopeArgs &A, int b, int n, int c, f
     for (int k = 0; k < 4; ++k) angle(A, position(A, b, n), 4 * c + k, cs[k], sn[k]);
 }
 
-// A sine of 0 is that of an angle of 0 (no other double comes that near to a multiple of pi / 2): such a pair is left as it is, since 0
-// times an infinity would make its partner NaN, and plus 0 times a negative number a negative zero positive.
+// A sine of 0 is that of an angle of 0, or below 2^-150 (no other double comes that near to a multiple of pi / 2): such a pair is left as it
+// is, since 0 times an infinity would make its partner NaN, and 0 times a negative number, taken off, a negative zero positive.
 template <bool ADJ> __device__ __forceinline__ void turn(float *v, const float *cs, const float *sn, float sense)
 {
 #pragma unroll
