@@ -441,6 +441,83 @@ int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const 
                       void *stream);
 
 /* ---------------------------------------------------------------------------
+ * svg2_layer_norm -- the norm in front of each of a block's products.  For row n of group b (a batch entry, or a frame with a
+ * timestep of its own),
+ *   y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * s + o,   s = weight, or 1 + weight where one_plus is set (a modulation)
+ * Statistics and sums are fp32, the mean taken off before squares are summed; one rounding at the end.
+ *   x             [B,N,D] dtype, element (b,n,i) at b*x_stride[0] + n*x_stride[1] + i (elements), any strides, any address that its
+ *                 elements may have
+ *   weight, bias  fp32 [D], or [B,D] with weight_stride / bias_stride elements from a group's to the next (0: all groups share one);
+ *                 NULL: no factor, no offset
+ *   y             [B,N,D] y_dtype, strides y_stride, positive wherever the dimension is larger than 1.  y may be x with the same
+ *                 strides and type; any other overlap is undefined.
+ *   eps > 0; 1 <= D <= 16384; B*N <= 2^26
+ * svg2_layer_norm_fp8: the result as an FP8 operand of B*N rows (row b*N + n) and D columns (svg2_quantize_fp8_blocks: the same
+ * storage, scales and rounding, from the fp32 values); args->y, y_stride and y_dtype are ignored.
+ * svg2_layer_norm_backward: with dY [B,N,D] y_dtype (strides y_stride, of any sign: it is only read) the gradients
+ *   dX [B,N,D] dtype with strides dx_stride (positive as y's; may be dY with the same strides and type, no other overlap),
+ *   dW fp32 of weight, dB fp32 of the offset, dense: [D], or [B,D] where weight or bias has a stride (both have or none has, where both are
+ *                given); NULL: not wanted; weight NULL: no dW.
+ *   args as in the forward call; args->y is ignored, bias is not read.
+ * Sums over rows are formed in a fixed order, fp32 within a share of the rows and 64 bits over the shares (as many as 1024, four rows at least): results
+ * are the same from run to run.
+ * ------------------------------------------------------------------------- */
+typedef struct svg2_layer_norm_args {
+    int dtype, y_dtype;
+    int B, N, D;
+    const void *x;
+    int64_t x_stride[2];
+    const float *weight;
+    const float *bias;
+    int64_t weight_stride;
+    int64_t bias_stride;
+    int one_plus;
+    float eps;
+    void *y;
+    int64_t y_stride[2];
+} svg2_layer_norm_args;
+
+int svg2_layer_norm(const svg2_layer_norm_args *args, void *stream);
+int svg2_layer_norm_fp8(const svg2_layer_norm_args *args, void *codes, void *scales, void *stream);
+size_t svg2_layer_norm_backward_workspace_size(const svg2_layer_norm_args *args);
+int svg2_layer_norm_backward(const svg2_layer_norm_args *args, const void *dY, void *dX, const int64_t *dx_stride, float *dW, float *dB,
+                             void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * 8-bit floating point with a scale for each block of 128 -- projections between bf16 and MXFP4.  128 neighbouring values
+ * along the contracted axis share one power of two (a byte, exponent + 127, 255 = NaN); a value is OCP E4M3 (as in
+ * svg2_quantize_fp8).  The block's exponent is the smallest with max |x| <= 448 * 2^exponent, at least -127; x / 2^exponent is
+ * rounded to nearest, ties to even, and nothing saturates.  A block that holds an infinity or a NaN is all NaN.
+ * An operand of R rows and K columns is stored, with Kp = K rounded up to 128, as
+ *   codes  [R, Kp] bytes                 16-byte aligned
+ *   scales [ceil(Kp/512), R, 4] bytes    scale of columns 128b .. 128b+127 of row r at [b/4, r, b%4]; 16-byte aligned
+ * with zeros in the columns behind K and in the scales behind the last block.
+ *
+ * svg2_quantize_fp8_blocks: X [M,G,Kg] dtype as for svg2_quantize_mxfp4, M rows of K = G*Kg columns.
+ *   codes, scales       operand of M rows, K columns, or both NULL
+ *   codes_t, scales_t   operand of K rows, M columns (X^T, blocks along the rows of X: what a gradient's product contracts), or both
+ *                       NULL; one of the two at least is wanted, both come from one read of X
+ *   square != 0: 128 x 128 values share a scale, so that both operands stand for the same values (weights, whose transpose the gradient
+ *   of the input multiplies)
+ * Any strides of X, any address that its elements may have.
+ * svg2_dequantize_fp8_blocks: the values of an operand, exactly where dtype has them, into X [R,K] dtype with row stride ldx >= K.
+ *
+ * svg2_matmul_fp8_blocks: C [M,N] = A B^T + bias for operands A (M rows) and B (N rows) of K columns; out_dtype, ldc, bias,
+ * gradients, workspace and limits as for svg2_matmul_mxfp4.  A bf16 result is formed by the matrix cores' E4M3 instructions, whose sums of eight
+ * neighbouring products keep 13 bits below the largest of them (fp32 from there on: some 10^-5 of the result in all); an fp32 result
+ * from the values as bf16, fp32 sums throughout, at less than half the rate (a value below 2^-126 may count as 0 there).
+ * Rows and columns up to 2^26, M*G*Kg < 2^40 (the product: K up to 2^24, C up to 2^23 tiles of 128 x 128).
+ * ------------------------------------------------------------------------- */
+int svg2_quantize_fp8_blocks(const void *X, int dtype, int M, int G, int Kg, int64_t stride_m, int64_t stride_g, int square,
+                             void *codes, void *scales, void *codes_t, void *scales_t, void *stream);
+int svg2_dequantize_fp8_blocks(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx,
+                               void *stream);
+size_t svg2_matmul_fp8_blocks_workspace_size(int M, int N, int K);
+int svg2_matmul_fp8_blocks(const void *A, const void *A_scales, const void *B, const void *B_scales, int M, int N, int K,
+                           const float *bias, int out_dtype, void *C, int64_t ldc, void *ws, size_t ws_bytes,
+                           void *stream);
+
+/* ---------------------------------------------------------------------------
  * Timing for benchmarks (HOST-side state, one per process).
  * svg2_profile_enable(1): every later svg2_forward* call records HIP events
  * around its stages on the caller's stream (events are created on first use;

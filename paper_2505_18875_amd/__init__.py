@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     svg2_quantize_fp8, svg2_sparse_attn_fp8, svg2_forward_fp8,
     svg2_grid_positions, svg2_rope_frequencies, svg2_rope, svg2_rope_backward,
     svg2_quantize_mxfp4, svg2_dequantize_mxfp4, svg2_matmul_mxfp4,
+    svg2_layer_norm, svg2_layer_norm_fp8, svg2_layer_norm_backward,
+    svg2_quantize_fp8_blocks, svg2_dequantize_fp8_blocks, svg2_matmul_fp8_blocks,
 )

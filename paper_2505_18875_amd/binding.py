@@ -39,6 +39,8 @@ EXPORTS = (
     "svg2_kmeans_pp_init_workspace_size", "svg2_kmeans_pp_init",
     "svg2_rope", "svg2_rope_backward_workspace_size", "svg2_rope_backward",
     "svg2_quantize_mxfp4", "svg2_dequantize_mxfp4", "svg2_matmul_mxfp4_workspace_size", "svg2_matmul_mxfp4",
+    "svg2_layer_norm", "svg2_layer_norm_fp8", "svg2_layer_norm_backward_workspace_size", "svg2_layer_norm_backward",
+    "svg2_quantize_fp8_blocks", "svg2_dequantize_fp8_blocks", "svg2_matmul_fp8_blocks_workspace_size", "svg2_matmul_fp8_blocks",
     "svg2_profile_enable", "svg2_profile_read", "svg2_profile_read_kernels",
 )
 STAGES = ("kmeans", "permute", "select", "attn_plan", "attn")
@@ -66,7 +68,11 @@ NORM_SCOPES = ("head", "token")
 _ROPE_ARGS = struct.Struct("@6i3P3P3i3P3q3qPqPi4iiif0q")
 
 
-_P3, _I3 = ctypes.c_void_p * 3, ctypes.c_int64 * 3
+# svg2_layer_norm_args, likewise
+_NORM_ARGS = struct.Struct("@5iPqqPPqqifPqq")
+
+
+_P3, _I3, _I2 = ctypes.c_void_p * 3, ctypes.c_int64 * 3, ctypes.c_int64 * 2
 
 _lib = None
 
@@ -119,6 +125,14 @@ def load_library() -> ctypes.CDLL:
         lib.svg2_dequantize_mxfp4.argtypes = [vp, vp, i, i, i, vp, i64, vp]
         lib.svg2_matmul_mxfp4_workspace_size.argtypes = [i, i, i]
         lib.svg2_matmul_mxfp4.argtypes = [vp, vp, vp, vp, i, i, i, vp, i, vp, i64, vp, sz, vp]
+        lib.svg2_layer_norm.argtypes = [vp, vp]
+        lib.svg2_layer_norm_fp8.argtypes = [vp, vp, vp, vp]
+        lib.svg2_layer_norm_backward_workspace_size.argtypes = [vp]
+        lib.svg2_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.svg2_quantize_fp8_blocks.argtypes = [vp, i, i, i, i, i64, i64, i, vp, vp, vp, vp, vp]
+        lib.svg2_dequantize_fp8_blocks.argtypes = lib.svg2_dequantize_mxfp4.argtypes
+        lib.svg2_matmul_fp8_blocks_workspace_size.argtypes = [i, i, i]
+        lib.svg2_matmul_fp8_blocks.argtypes = lib.svg2_matmul_mxfp4.argtypes
         lib.svg2_profile_enable.argtypes = [i]
         lib.svg2_profile_read.argtypes = [vp, vp]
         lib.svg2_profile_read_kernels.argtypes = [vp, vp]
@@ -696,6 +710,176 @@ def svg2_matmul_mxfp4(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bf
     with _on(dev):
         _check(lib.svg2_matmul_mxfp4(a, sa, b, sb, M, N, Kp, _dense(bias, "bias", dev, torch.float32, (N,)), _dtype_code(C), ptr, ld,
                                      _dev(ws), 0 if ws is None else ws.numel(), _raw_stream(dev)))
+    return C
+
+
+def _norm_args(x, weight, bias, eps, one_plus, y_dtype, y, y_stride, dev):
+    """svg2_layer_norm_args of x [N,D] or [B,N,D], with every check that needs the tensors; groups, rows and columns."""
+    shape = x.shape
+    if len(shape) == 3:
+        B, N, D = shape
+        xs = _outer_strides(shape, x.stride())
+    elif len(shape) == 2:
+        (N, D), B = shape, 1
+        xs = [0, *_outer_strides(shape, x.stride())]
+    else:
+        raise ValueError("x must be [N,D] or [B,N,D], got %s" % list(shape))
+    w, ws = _per_group(weight, "weight", dev, B, D)
+    b, bs = _per_group(bias, "bias", dev, B, D)
+    return _NORM_ARGS.pack(_dtype_code(x), y_dtype, B, N, D, x.data_ptr(), *xs, w, b, ws, bs, 1 if one_plus else 0, eps, y,
+                           *y_stride), B, N, D
+
+
+def _per_group(t, name, dev, B, D):
+    """Address and group stride of fp32 [D], or [B,D] of any row stride; 0, 0 for None."""
+    if t is None:
+        return 0, 0
+    shape = t.shape
+    if (shape != (D,) and shape != (B, D)) or t.dtype is not torch.float32 or t.device != dev:
+        _refuse(t, name, dev, torch.float32, (B, D) if len(shape) == 2 else (D,))
+    stride = t.stride()
+    if stride[-1] != 1 and D > 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+    return t.data_ptr(), stride[0] if len(shape) == 2 and B > 1 else 0
+
+
+def _norm_out(t, name, dev, dtype, shape):
+    """Address and (group, row) strides of a [N,D] or [B,N,D] result or gradient."""
+    if t.shape != shape or t.device != dev or (dtype is not None and t.dtype is not dtype):
+        _refuse(t, name, dev, t.dtype if dtype is None else dtype, shape)
+    outer = _outer_strides(shape, t.stride())
+    return t.data_ptr(), outer if len(shape) == 3 else [0, *outer]
+
+
+def svg2_layer_norm(x, weight=None, bias=None, *, eps=1e-6, one_plus=False, out_dtype=None, out=None):
+    """(x - mean) / sqrt(variance + eps) * s + bias over the last dimension, s = weight, or 1 + weight with one_plus.
+
+    x: [N,D] or [B,N,D], any strides; weight, bias: fp32 [D] for all rows, [B,D] for each group (rows of a wider table of
+    modulations), or None.  The result has x's type, or out_dtype, or goes to `out` (any strides; x itself)."""
+    lib = load_library()
+    dev, shape = _gpu(x, "x"), x.shape
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype if out_dtype is None else out_dtype, device=dev)
+    y, ys = _norm_out(out, "out", dev, out_dtype, shape)
+    a = _norm_args(x, weight, bias, eps, one_plus, _dtype_code(out), y, ys, dev)[0]
+    with _on(dev):
+        _check(lib.svg2_layer_norm(a, _raw_stream(dev)))
+    return out
+
+
+def svg2_layer_norm_fp8(x, weight=None, bias=None, *, eps=1e-6, one_plus=False):
+    """svg2_layer_norm's result as an operand of svg2_matmul_fp8_blocks (codes, scales), row b*N + n of x [B,N,D]."""
+    lib = load_library()
+    dev = _gpu(x, "x")
+    a, B, N, D = _norm_args(x, weight, bias, eps, one_plus, 0, 0, (0, 0), dev)
+    codes, scales = _fp8_blocks_empty(B * N, D, dev)
+    with _on(dev):
+        _check(lib.svg2_layer_norm_fp8(a, codes.data_ptr(), scales.data_ptr(), _raw_stream(dev)))
+    return codes, scales
+
+
+def svg2_layer_norm_backward(grad, x, weight=None, bias=None, *, eps=1e-6, one_plus=False, out=None, ws=None):
+    """Gradients of svg2_layer_norm: grad (x's shape, any strides) and the forward call's arguments -> grad of x (dense, or
+    `out`), dweight and dbias (fp32 [D] or [B,D], None where the argument is None)."""
+    lib = load_library()
+    dev, shape = _gpu(x, "x"), x.shape
+    out = torch.empty(shape, dtype=x.dtype, device=dev) if out is None else out
+    g, gs = _norm_out(grad, "grad", dev, None, shape)
+    dx, ds = _norm_out(out, "out", dev, x.dtype, shape)
+    a, B, N, D = _norm_args(x, weight, bias, eps, one_plus, _dtype_code(grad), 0, gs, dev)
+    for t in (weight, bias):
+        if t is not None and B > 1 and t.dim() == 2 and t.stride(0) == 0:
+            raise ValueError("weight and bias of a group each must be rows of their own: expanded rows are shared ones, [D]")
+    dw, db = [None if t is None else torch.empty(t.shape, dtype=torch.float32, device=dev) for t in (weight, bias)]
+    with _on(dev):
+        if ws is None:
+            need = lib.svg2_layer_norm_backward_workspace_size(a)
+            if need > 256:              # at 256 the call uses none
+                ws = _workspace(need, dev)
+        _check(lib.svg2_layer_norm_backward(a, g, dx, _I2(*ds), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+                                            _dev(ws), 0 if ws is None else ws.numel(), _raw_stream(dev)))
+    return SimpleNamespace(grad=out, dweight=dw, dbias=db)
+
+
+def _fp8_blocks_empty(R, K, device):
+    nk = -(-K // 128)
+    codes = torch.empty((R, nk * 128), dtype=torch.uint8, device=device)
+    return codes, codes.new_empty((-(-nk // 4), R, 4))
+
+
+def _fp8_blocks_operand(codes, scales, name, device):
+    """Checks an operand's two tensors; rows and padded columns."""
+    shape = codes.shape
+    if len(shape) != 2 or shape[1] % 128:
+        raise ValueError("%s: codes must be [R, Kp] with Kp a multiple of 128, got %s" % (name, list(shape)))
+    R, Kp = shape
+    return R, Kp, _dense(codes, name, device, torch.uint8, shape), _dense(scales, name, device, torch.uint8, (-(-Kp // 512), R, 4))
+
+
+def svg2_quantize_fp8_blocks(X, *, transposed=False, square=False):
+    """X [M,K], or [M,G,Kg] for K = G*Kg columns in groups of any stride (the layer's O as O.transpose(0, 1)) -> E4M3 operand
+    with a power of two for each block of 128 columns: codes [M,Kp], scales [ceil(Kp/512),M,4] uint8.  transposed: of X^T, [K
+    rows, M columns]; transposed="both": ((codes, scales), (codes, scales)) of X and of X^T from one read.  square: one scale for
+    128 x 128 values."""
+    lib = load_library()
+    dev, shape = _gpu(X, "X"), X.shape
+    strides = _outer_strides(shape, X.stride())
+    if len(shape) == 2:
+        (M, K), G, (sm,), sg = shape, 1, strides, 0
+        Kg = K
+    elif len(shape) == 3:
+        (M, G, Kg), (sm, sg) = shape, strides
+        K = G * Kg
+    else:
+        raise ValueError("X must be [M,K] or [M,G,Kg]")
+    if transposed not in (False, True, "both"):
+        raise ValueError("transposed must be False, True or \"both\"")
+    codes, scales = (None, None) if transposed is True else _fp8_blocks_empty(M, K, dev)
+    codes_t, scales_t = _fp8_blocks_empty(K, M, dev) if transposed else (None, None)
+    with _on(dev):
+        _check(lib.svg2_quantize_fp8_blocks(X.data_ptr(), _dtype_code(X), M, G, Kg, sm, sg, 1 if square else 0,
+                                            *[None if t is None else t.data_ptr() for t in (codes, scales, codes_t, scales_t)],
+                                            _raw_stream(dev)))
+    return (codes, scales) if not transposed else (codes_t, scales_t) if transposed is True else ((codes, scales), (codes_t, scales_t))
+
+
+def svg2_dequantize_fp8_blocks(codes, scales, K=None, *, dtype=torch.bfloat16, out=None):
+    """The values of such an operand, [R,K] (K: all padded columns where None)."""
+    lib = load_library()
+    dev = _gpu(codes, "codes")
+    R, Kp, c, s = _fp8_blocks_operand(codes, scales, "operand", dev)
+    K = Kp if K is None else K
+    if not Kp - 128 < K <= Kp:
+        raise ValueError("K = %d does not belong to %d padded columns" % (K, Kp))
+    out = torch.empty((R, K), dtype=dtype, device=dev) if out is None else out
+    ptr, ld = _rows(out, "out", dev, (R, K))
+    with _on(dev):
+        _check(lib.svg2_dequantize_fp8_blocks(c, s, R, K, _dtype_code(out), ptr, ld, _raw_stream(dev)))
+    return out
+
+
+@functools.lru_cache(maxsize=4096)
+def _fp8_blocks_workspace_size(M, N, K):
+    return load_library().svg2_matmul_fp8_blocks_workspace_size(M, N, K)
+
+
+def svg2_matmul_fp8_blocks(A, A_scales, B, B_scales, *, bias=None, out_dtype=torch.bfloat16, out=None, ws=None):
+    """C [M,N] = A B^T + bias of two such operands (M and N rows of the same columns); bias fp32 [N]."""
+    lib = load_library()
+    dev = _gpu(A, "A")
+    M, Kp, a, sa = _fp8_blocks_operand(A, A_scales, "A", dev)
+    N, Kb, b, sb = _fp8_blocks_operand(B, B_scales, "B", dev)
+    if Kb != Kp:
+        raise ValueError("A has %d padded columns, B has %d" % (Kp, Kb))
+    C = torch.empty((M, N), dtype=out_dtype, device=dev) if out is None else out
+    ptr, ld = _rows(C, "out", dev, (M, N))
+    if ws is None:
+        need = _fp8_blocks_workspace_size(M, N, Kp)
+        if need > 256:                  # at 256 the product uses none
+            ws = _workspace(need, dev)
+    with _on(dev):
+        _check(lib.svg2_matmul_fp8_blocks(a, sa, b, sb, M, N, Kp, _dense(bias, "bias", dev, torch.float32, (N,)), _dtype_code(C), ptr,
+                                          ld, _dev(ws), 0 if ws is None else ws.numel(), _raw_stream(dev)))
     return C
 
 

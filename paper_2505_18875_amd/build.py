@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsvg2_hip.so")
 TEST_LIB = os.path.join(HERE, "libsvg2_hip_test.so")
 SOURCES = ["svg2_api.hip", "svg2_permute.hip", "svg2_select.hip", "svg2_kmeans.hip", "svg2_attn.hip", "svg2_fp8.hip",
-           "svg2_diag.hip", "svg2_rope.hip", "svg2_mxfp4.hip"]
+           "svg2_diag.hip", "svg2_rope.hip", "svg2_mxfp4.hip", "svg2_norm.hip", "svg2_fp8_blocks.hip"]
 TEST_HOOKS = ["svg2_diag.hip"]              # sources with entry points for the tests
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

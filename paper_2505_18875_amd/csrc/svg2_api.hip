@@ -119,8 +119,8 @@ static int check_rope(const svg2_rope_args *a, bool dst_written)
     return SVG2_OK;
 }
 
-// rows, columns and buffers of a microscaled operand
-static int check_mxfp4(const char *name, const void *codes, const void *scales, long long R, long long K)
+// rows, columns and buffers of a quantised operand
+static int check_operand(const char *name, const void *codes, const void *scales, long long R, long long K)
 {
     SVG2_REQUIRE(R >= 1 && K >= 1 && R <= 67108864 && K <= 67108864, SVG2_INVALID_ARG,
                  "%s: %lld rows and %lld columns must be in 1..2^26", name, R, K);
@@ -134,6 +134,29 @@ static int check_dtype(int dtype)
     SVG2_REQUIRE(dtype == SVG2_F32 || dtype == SVG2_BF16, SVG2_UNSUPPORTED, "dtype %d is not SVG2_F32 or SVG2_BF16", dtype);
     return SVG2_OK;
 }
+
+// strides of a [B,N,D] tensor that svg2_layer_norm* writes
+static int check_norm_strides(const svg2_layer_norm_args *a, const char *name, const int64_t *stride)
+{
+    const int sizes[2] = {a->B, a->N};
+    for (int k = 0; k < 2; ++k)
+        SVG2_REQUIRE(sizes[k] == 1 || stride[k] > 0, SVG2_INVALID_ARG, "%s stride %d = %lld must be positive", name, k, (long long)stride[k]);
+    return SVG2_OK;
+}
+
+static int check_norm(const svg2_layer_norm_args *a)
+{
+    SVG2_REQUIRE(a != nullptr, SVG2_INVALID_ARG, "args is null");
+    SVG2_TRY(check_dtype(a->dtype));
+    SVG2_REQUIRE(a->B >= 1 && a->N >= 1 && (double)a->B * a->N <= 67108864.0, SVG2_INVALID_ARG,
+                 "B = %d and N = %d must be positive and B * N = %g at most 2^26", a->B, a->N, (double)a->B * a->N);
+    SVG2_REQUIRE(a->D >= 1 && a->D <= 16384, SVG2_INVALID_ARG, "D = %d must be in 1..16384", a->D);
+    SVG2_REQUIRE(a->eps > 0.f && a->eps < 1e30f, SVG2_INVALID_ARG, "eps = %g must be positive and finite", (double)a->eps);
+    SVG2_REQUIRE(multiple_of(a->weight, 4) && multiple_of(a->bias, 4), SVG2_INVALID_ARG, "weight or bias is not aligned to its elements");
+    return SVG2_OK;
+}
+
+static bool aligned_to(const void *p, int dtype) { return multiple_of(p, dtype == SVG2_BF16 ? 2 : 4); }
 
 // (kernel, device) pairs whose dynamic-LDS limit has been raised, with the size it was raised to
 struct LdsAttr {
@@ -694,7 +717,7 @@ int svg2_quantize_mxfp4(const void *X, int dtype, int M, int G, int Kg, int64_t 
     SVG2_TRY(check_dtype(dtype));
     SVG2_REQUIRE(G >= 1 && Kg >= 1, SVG2_INVALID_ARG, "G = %d and Kg = %d must be positive", G, Kg);
     const long long K = (long long)G * Kg;
-    SVG2_TRY(check_mxfp4("result", codes, scales, transposed ? K : M, transposed ? M : K));
+    SVG2_TRY(check_operand("result", codes, scales, transposed ? K : M, transposed ? M : K));
     SVG2_REQUIRE(X != nullptr, SVG2_INVALID_ARG, "X is null");
     SVG2_REQUIRE(multiple_of(X, dtype == SVG2_BF16 ? 2 : 4), SVG2_INVALID_ARG, "X is not aligned to its elements");
     SVG2_REQUIRE(X != codes && X != scales && codes != scales, SVG2_INVALID_ARG, "codes and scales must not alias X or each other");
@@ -706,7 +729,7 @@ int svg2_dequantize_mxfp4(const void *codes, const void *scales, int R, int K, i
 {
     clear_error();
     SVG2_TRY(check_dtype(dtype));
-    SVG2_TRY(check_mxfp4("operand", codes, scales, R, K));
+    SVG2_TRY(check_operand("operand", codes, scales, R, K));
     SVG2_REQUIRE(X != nullptr, SVG2_INVALID_ARG, "X is null");
     SVG2_REQUIRE(multiple_of(X, dtype == SVG2_BF16 ? 2 : 4), SVG2_INVALID_ARG, "X is not aligned to its elements");
     SVG2_REQUIRE(ldx >= K, SVG2_INVALID_ARG, "ldx = %lld is less than K = %d", (long long)ldx, K);
@@ -722,6 +745,21 @@ static int check_product_size(int M, int N, int K)
     return SVG2_OK;
 }
 
+static int check_product(const void *A, const void *A_scales, const void *B, const void *B_scales, int M, int N, int K, const float *bias,
+                         int out_dtype, const void *C, int64_t ldc)
+{
+    SVG2_TRY(check_dtype(out_dtype));
+    SVG2_TRY(check_operand("A", A, A_scales, M, K));
+    SVG2_TRY(check_operand("B", B, B_scales, N, K));
+    SVG2_TRY(check_product_size(M, N, K));
+    SVG2_REQUIRE(C != nullptr, SVG2_INVALID_ARG, "C is null");
+    SVG2_REQUIRE(multiple_of(C, out_dtype == SVG2_BF16 ? 2 : 4) && multiple_of(bias, 4), SVG2_INVALID_ARG,
+                 "C or bias is not aligned to its elements");
+    SVG2_REQUIRE(ldc >= N, SVG2_INVALID_ARG, "ldc = %lld is less than N = %d", (long long)ldc, N);
+    SVG2_REQUIRE(C != A && C != A_scales && C != B && C != B_scales && C != bias, SVG2_INVALID_ARG, "C must not alias an input");
+    return SVG2_OK;
+}
+
 size_t svg2_matmul_mxfp4_workspace_size(int M, int N, int K)
 {
     if (M < 1 || N < 1 || K < 1 || M > 67108864 || N > 67108864 || check_product_size(M, N, K) != SVG2_OK) return 256;
@@ -732,20 +770,123 @@ int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const 
                       const float *bias, int out_dtype, void *C, int64_t ldc, void *ws, size_t ws_bytes, void *stream)
 {
     clear_error();
-    SVG2_TRY(check_dtype(out_dtype));
-    SVG2_TRY(check_mxfp4("A", A, A_scales, M, K));
-    SVG2_TRY(check_mxfp4("B", B, B_scales, N, K));
-    SVG2_TRY(check_product_size(M, N, K));
-    SVG2_REQUIRE(C != nullptr, SVG2_INVALID_ARG, "C is null");
-    SVG2_REQUIRE(multiple_of(C, out_dtype == SVG2_BF16 ? 2 : 4) && multiple_of(bias, 4), SVG2_INVALID_ARG,
-                 "C or bias is not aligned to its elements");
-    SVG2_REQUIRE(ldc >= N, SVG2_INVALID_ARG, "ldc = %lld is less than N = %d", (long long)ldc, N);
-    SVG2_REQUIRE(C != A && C != A_scales && C != B && C != B_scales && C != bias, SVG2_INVALID_ARG, "C must not alias an input");
+    SVG2_TRY(check_product(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc));
     const size_t need = mxfp4_matmul_ws_bytes(M, N, K);         // 256: none is used
     if (need > 256 || ws) SVG2_TRY(check_ws(ws, ws_bytes, need));
     SVG2_REQUIRE(need == 256 || (ws != A && ws != B && ws != C), SVG2_INVALID_ARG, "the workspace must not alias an operand");
     SVG2_TRY(mxfp4_matmul_prepare());
     return mxfp4_matmul_launch(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc, ws, static_cast<hipStream_t>(stream));
+}
+
+int svg2_layer_norm(const svg2_layer_norm_args *a, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_norm(a));
+    SVG2_TRY(check_dtype(a->y_dtype));
+    SVG2_TRY(check_norm_strides(a, "y", a->y_stride));
+    SVG2_REQUIRE(a->x && a->y, SVG2_INVALID_ARG, "x and y must be non-null");
+    SVG2_REQUIRE(aligned_to(a->x, a->dtype) && aligned_to(a->y, a->y_dtype), SVG2_INVALID_ARG, "x or y is not aligned to its elements");
+    SVG2_REQUIRE(a->x != a->y || (a->dtype == a->y_dtype && memcmp(a->x_stride, a->y_stride, sizeof(a->x_stride)) == 0), SVG2_INVALID_ARG,
+                 "y is x with other strides or of another type");
+    SVG2_REQUIRE(a->y != a->weight && a->y != a->bias, SVG2_INVALID_ARG, "y must not alias weight or bias");
+    return layer_norm_launch(a, static_cast<hipStream_t>(stream));
+}
+
+int svg2_layer_norm_fp8(const svg2_layer_norm_args *a, void *codes, void *scales, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_norm(a));
+    SVG2_REQUIRE(a->x != nullptr, SVG2_INVALID_ARG, "x is null");
+    SVG2_REQUIRE(aligned_to(a->x, a->dtype), SVG2_INVALID_ARG, "x is not aligned to its elements");
+    SVG2_TRY(check_operand("result", codes, scales, (long long)a->B * a->N, a->D));
+    SVG2_REQUIRE(codes != scales && codes != a->x && scales != a->x && codes != a->weight && scales != a->weight && codes != a->bias &&
+                     scales != a->bias, SVG2_INVALID_ARG, "codes and scales must not alias an input or each other");
+    return layer_norm_fp8_launch(a, codes, scales, static_cast<hipStream_t>(stream));
+}
+
+size_t svg2_layer_norm_backward_workspace_size(const svg2_layer_norm_args *a)
+{
+    if (check_norm(a) != SVG2_OK) return 256;
+    return layer_norm_bwd_ws_bytes(a);
+}
+
+int svg2_layer_norm_backward(const svg2_layer_norm_args *a, const void *dY, void *dX, const int64_t *dx_stride, float *dW, float *dB,
+                             void *ws, size_t ws_bytes, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_norm(a));
+    SVG2_TRY(check_dtype(a->y_dtype));
+    SVG2_REQUIRE(a->x && dY && dX && dx_stride, SVG2_INVALID_ARG, "x, dY, dX and dx_stride must be non-null");
+    SVG2_TRY(check_norm_strides(a, "dX", dx_stride));
+    SVG2_REQUIRE(aligned_to(a->x, a->dtype) && aligned_to(dY, a->y_dtype) && aligned_to(dX, a->dtype), SVG2_INVALID_ARG,
+                 "x, dY or dX is not aligned to its elements");
+    SVG2_REQUIRE(multiple_of(dW, 4) && multiple_of(dB, 4), SVG2_INVALID_ARG, "dW or dB is not aligned to its elements");
+    SVG2_REQUIRE(!dW || a->weight, SVG2_INVALID_ARG, "dW is given, weight is null");
+    SVG2_REQUIRE(a->B == 1 || !a->weight || !a->bias || (a->weight_stride == 0) == (a->bias_stride == 0), SVG2_INVALID_ARG,
+                 "weight_stride = %lld and bias_stride = %lld: gradients need both shared or both of a group", (long long)a->weight_stride,
+                 (long long)a->bias_stride);
+    SVG2_REQUIRE(dX != a->x, SVG2_INVALID_ARG, "dX must not alias x");
+    SVG2_REQUIRE(dX != dY || (a->dtype == a->y_dtype && memcmp(dx_stride, a->y_stride, sizeof(a->y_stride)) == 0), SVG2_INVALID_ARG,
+                 "dX is dY with other strides or of another type");
+    for (const float *p : {dW, dB})
+        SVG2_REQUIRE(!p || (p != a->x && p != dY && p != dX && p != a->weight && p != a->bias), SVG2_INVALID_ARG,
+                     "dW and dB must not alias another tensor");
+    SVG2_REQUIRE(!dW || dW != dB, SVG2_INVALID_ARG, "dW must not alias dB");
+    const size_t need = layer_norm_bwd_ws_bytes(a);             // 256: none is used
+    if (need > 256 || ws) SVG2_TRY(check_ws(ws, ws_bytes, need));
+    SVG2_REQUIRE(need == 256 || (ws != dW && ws != dB && ws != dX && ws != dY && ws != a->x), SVG2_INVALID_ARG, "the workspace must not alias a tensor");
+    return layer_norm_bwd_launch(a, dY, dX, dx_stride, dW, dB, ws, static_cast<hipStream_t>(stream));
+}
+
+int svg2_quantize_fp8_blocks(const void *X, int dtype, int M, int G, int Kg, int64_t stride_m, int64_t stride_g, int square, void *codes,
+                             void *scales, void *codes_t, void *scales_t, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_dtype(dtype));
+    SVG2_REQUIRE(G >= 1 && Kg >= 1, SVG2_INVALID_ARG, "G = %d and Kg = %d must be positive", G, Kg);
+    const long long K = (long long)G * Kg;
+    SVG2_REQUIRE(codes || scales || codes_t || scales_t, SVG2_INVALID_ARG, "no result is wanted: codes, scales, codes_t and scales_t are null");
+    if (codes || scales) SVG2_TRY(check_operand("result", codes, scales, M, K));
+    if (codes_t || scales_t) SVG2_TRY(check_operand("transposed result", codes_t, scales_t, K, M));
+    SVG2_REQUIRE((double)M * (double)K < 1099511627776.0, SVG2_INVALID_ARG, "M*G*Kg is 2^40 or more");
+    SVG2_REQUIRE(X != nullptr, SVG2_INVALID_ARG, "X is null");
+    SVG2_REQUIRE(aligned_to(X, dtype), SVG2_INVALID_ARG, "X is not aligned to its elements");
+    const void *out[4] = {codes, scales, codes_t, scales_t};
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j <= i; ++j)
+            SVG2_REQUIRE(!out[i] || (out[i] != X && (i == j || out[i] != out[j])), SVG2_INVALID_ARG, "codes and scales must not alias X or each other");
+    return fp8_blocks_quant_launch(X, dtype, M, G, Kg, stride_m, stride_g, square != 0, codes, scales, codes_t, scales_t,
+                                   static_cast<hipStream_t>(stream));
+}
+
+int svg2_dequantize_fp8_blocks(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_dtype(dtype));
+    SVG2_TRY(check_operand("operand", codes, scales, R, K));
+    SVG2_REQUIRE(X != nullptr, SVG2_INVALID_ARG, "X is null");
+    SVG2_REQUIRE(aligned_to(X, dtype), SVG2_INVALID_ARG, "X is not aligned to its elements");
+    SVG2_REQUIRE(ldx >= K, SVG2_INVALID_ARG, "ldx = %lld is less than K = %d", (long long)ldx, K);
+    SVG2_REQUIRE(X != codes && X != scales, SVG2_INVALID_ARG, "X must not alias an input");
+    return fp8_blocks_values_launch(codes, scales, R, K, dtype, X, ldx, static_cast<hipStream_t>(stream));
+}
+
+size_t svg2_matmul_fp8_blocks_workspace_size(int M, int N, int K)
+{
+    if (M < 1 || N < 1 || K < 1 || M > 67108864 || N > 67108864 || check_product_size(M, N, K) != SVG2_OK) return 256;
+    return fp8_blocks_matmul_ws_bytes(M, N, K);
+}
+
+int svg2_matmul_fp8_blocks(const void *A, const void *A_scales, const void *B, const void *B_scales, int M, int N, int K,
+                           const float *bias, int out_dtype, void *C, int64_t ldc, void *ws, size_t ws_bytes, void *stream)
+{
+    clear_error();
+    SVG2_TRY(check_product(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc));
+    const size_t need = fp8_blocks_matmul_ws_bytes(M, N, K);    // 256: none is used
+    if (need > 256 || ws) SVG2_TRY(check_ws(ws, ws_bytes, need));
+    SVG2_REQUIRE(need == 256 || (ws != A && ws != B && ws != C), SVG2_INVALID_ARG, "the workspace must not alias an operand");
+    SVG2_TRY(fp8_blocks_matmul_prepare());
+    return fp8_blocks_matmul_launch(A, A_scales, B, B_scales, M, N, K, bias, out_dtype, C, ldc, ws, static_cast<hipStream_t>(stream));
 }
 
 int svg2_profile_enable(int level)

@@ -214,4 +214,20 @@ size_t mxfp4_matmul_ws_bytes(int M, int N, int K);
 int mxfp4_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
                         int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st);
 
+// layer norm, its result as an FP8 operand, its gradients (svg2_norm.hip)
+int layer_norm_launch(const svg2_layer_norm_args *a, hipStream_t st);
+int layer_norm_fp8_launch(const svg2_layer_norm_args *a, void *codes, void *scales, hipStream_t st);
+size_t layer_norm_bwd_ws_bytes(const svg2_layer_norm_args *a);
+int layer_norm_bwd_launch(const svg2_layer_norm_args *a, const void *dY, void *dX, const int64_t *dx_stride, float *dW, float *dB,
+                          void *ws, hipStream_t st);
+
+// E4M3 operands with a scale for each block of 128 (svg2_fp8_blocks.hip)
+int fp8_blocks_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t sm, int64_t sg, bool square, void *codes, void *scales,
+                            void *codes_t, void *scales_t, hipStream_t st);
+int fp8_blocks_values_launch(const void *codes, const void *scales, int R, int K, int dtype, void *X, int64_t ldx, hipStream_t st);
+int fp8_blocks_matmul_prepare();
+size_t fp8_blocks_matmul_ws_bytes(int M, int N, int K);
+int fp8_blocks_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
+                             int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st);
+
 }  // namespace svg2

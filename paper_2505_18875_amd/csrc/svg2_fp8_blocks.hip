@@ -1,0 +1,638 @@
+// 8-bit floating point (E4M3) operands with a scale for each block of 128: quantisation, the values back, and the product
+// C = A B^T + bias.  Storage and scales: svg2_fp8_blocks.h.
+//
+// The scales are powers of two, so that the matrix cores multiply by them (v_mfma_scale_*) and a product needs no instruction of its own
+// for them; what a power of two costs against any number is at most one of E4M3's 15 binades, no bit of a normal number.
+#include <type_traits>
+
+#include "svg2_fp8_blocks.h"
+
+namespace svg2 {
+
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// f(0), f(1), .. with each number known at compile time
+template <int FROM, int TO, typename F> __device__ __forceinline__ void static_for(F f)
+{
+    if constexpr (FROM < TO) {
+        f(std::integral_constant<int, FROM>());
+        static_for<FROM + 1, TO>(f);
+    }
+}
+
+struct BlockQuantArgs {
+    const void *X;
+    long long sm, sg;               // strides of rows and of groups of columns
+    int M, G, Kg;                   // X is [M, G, Kg]; K = G Kg columns
+    uint8_t *codes, *scales;        // operand of M rows and K columns
+    uint8_t *codes_t, *scales_t;    // operand of K rows and M columns
+};
+
+template <typename T> __device__ __forceinline__ const T *element(const BlockQuantArgs &A, long long m, int k)
+{
+    const int g = A.G == 1 ? 0 : k / A.Kg;
+    return static_cast<const T *>(A.X) + m * A.sm + g * A.sg + (k - g * A.Kg);
+}
+
+// eight neighbouring columns: one load where they are all there and in one group, whatever their address
+template <typename T, bool STREAM> __device__ __forceinline__ void load_columns(const BlockQuantArgs &A, long long m, int k, int K, float *v)
+{
+    if (k + 8 <= K && (A.G == 1 || k % A.Kg + 8 <= A.Kg)) load8<T, STREAM>(element<T>(A, m, k), v);
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k + i < K ? to_f32(*element<T>(A, m, k + i)) : 0.f;
+}
+
+// rows: grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block of 128 columns, whose eight values each stay in
+// registers; the block's maximum goes round the 16 lanes without LDS.
+template <typename T, bool STREAM> __global__ __launch_bounds__(256) void fp8_blocks_rows_kernel(const BlockQuantArgs A)
+{
+    const int lane16 = threadIdx.x & 15, K = A.G * A.Kg, nk = (K + 127) / 128, all = (nk + 3) & ~3;
+    const long long m = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (m >= A.M) return;                       // whole groups of 16 lanes
+    for (int kc = blockIdx.y; kc < all; kc += gridDim.y) {
+        unsigned byte = 0;
+        if (kc < nk) {
+            float v[8], inv;
+            load_columns<T, STREAM>(A, m, kc * 128 + lane16 * 8, K, v);
+            unsigned top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, mag(v[i]));
+            byte = e4m3_block_scale(max16(top), inv);
+            *reinterpret_cast<uint2 *>(A.codes + m * (nk * 128LL) + kc * 128 + lane16 * 8) = e4m3_codes8(v, inv);
+        }
+        if (lane16 == 0) A.scales[((long long)(kc >> 2) * A.M + m) * 4 + (kc & 3)] = (uint8_t)byte;
+    }
+}
+
+// tiles of 128 x 128 for the transposed operand, for both from one read, and for square blocks.
+// grid: tiles, those of one row of tiles neighbours; block 256: a thread holds 8 rows x 8 columns.  The maximum of a row goes round 16 lanes, that of a
+// column over the wavefront's four groups of rows and, through LDS, the four wavefronts.  The codes of eight rows of a column are eight
+// bytes: they go through LDS, column by column, and leave as lines of 128 bytes.
+template <typename T, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bounds__(256) void fp8_blocks_tile_kernel(const BlockQuantArgs A)
+{
+    __shared__ unsigned s_top[4][128];
+    __shared__ __attribute__((aligned(16))) uint8_t s_codes[128 * 144];         // a column's 128 codes and 16 bytes: 8-byte stores spread over the banks
+    const int K = A.G * A.Kg, nk = (K + 127) / 128, nm = (A.M + 127) / 128;
+    for (long long tile = blockIdx.x; tile < (long long)nm * nk; tile += gridDim.x) {
+        const int kc = (int)(tile % nk), mc = (int)(tile / nk);
+        const int lane16 = threadIdx.x & 15, rows8 = threadIdx.x >> 4, wave = threadIdx.x >> 6;
+        const long long m0 = (long long)mc * 128 + rows8 * 8;
+        const int k0 = kc * 128 + lane16 * 8;
+        float v[8][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (m0 + i < A.M) load_columns<T, false>(A, m0 + i, k0, K, v[i]);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+        }
+        unsigned row_top[8], col_top[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row_top[i] = col_top[i] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                row_top[i] = max(row_top[i], mag(v[i][e]));
+                col_top[e] = max(col_top[e], mag(v[i][e]));
+            }
+        if (SQUARE || COLS) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                col_top[e] = max(col_top[e], (unsigned)__shfl_xor((int)col_top[e], 16));
+                col_top[e] = max(col_top[e], (unsigned)__shfl_xor((int)col_top[e], 32));
+                if ((threadIdx.x & 63) < 16) s_top[wave][lane16 * 8 + e] = col_top[e];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = lane16 * 8 + e;
+                col_top[e] = max(max(s_top[0][k], s_top[1][k]), max(s_top[2][k], s_top[3][k]));
+            }
+        }
+        if (SQUARE) {
+            unsigned all = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) all = max(all, col_top[e]);
+            all = max16(all);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) row_top[e] = col_top[e] = all;
+        }
+        if (ROWS) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float inv;
+                const unsigned byte = e4m3_block_scale(SQUARE ? row_top[i] : max16(row_top[i]), inv);
+                const uint2 c = e4m3_codes8(v[i], inv);
+                if (m0 + i < A.M) {
+                    *reinterpret_cast<uint2 *>(A.codes + (m0 + i) * (nk * 128LL) + kc * 128 + lane16 * 8) = c;
+                    uint8_t *s = A.scales + ((long long)(kc >> 2) * A.M + m0 + i) * 4;
+                    if (lane16 == 0) s[kc & 3] = (uint8_t)byte;
+                    if (kc == nk - 1 && lane16 > (kc & 3) && lane16 < 4) s[lane16] = 0;
+                }
+            }
+        }
+        if (COLS) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float inv, x[8];
+                const unsigned byte = e4m3_block_scale(col_top[e], inv);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = v[i][e];
+                *reinterpret_cast<uint2 *>(s_codes + (lane16 * 8 + e) * 144 + rows8 * 8) = e4m3_codes8(x, inv);
+                const long long r = k0 + e;
+                if (r < K && rows8 < 4) {
+                    uint8_t *s = A.scales_t + ((long long)(mc >> 2) * K + r) * 4;
+                    if (rows8 == (mc & 3)) s[rows8] = (uint8_t)byte;
+                    else if (mc == nm - 1 && rows8 > (mc & 3)) s[rows8] = 0;
+                }
+            }
+            __syncthreads();
+            for (int p = threadIdx.x; p < 128 * 8; p += 256) {
+                const long long r = (long long)kc * 128 + (p >> 3);
+                if (r < K)
+                    *reinterpret_cast<u32x4 *>(A.codes_t + r * (nm * 128LL) + mc * 128 + (p & 7) * 16) =
+                        *reinterpret_cast<const u32x4 *>(s_codes + (p >> 3) * 144 + (p & 7) * 16);
+            }
+        }
+        if (COLS || SQUARE) __syncthreads();    // s_top and s_codes have been read
+    }
+}
+
+// ---- the values back -------------------------------------------------------
+// 2^(byte - 127) in two factors, neither of which leaves the normal range; byte 255 is NaN
+__device__ __forceinline__ void scale_factors(unsigned byte, float &a, float &b)
+{
+    const unsigned half = byte >> 1;
+    a = byte == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float((half + 64) << 23);       // 2^(half - 63)
+    b = __uint_as_float((byte - half + 63) << 23);                                             // 2^(byte - half - 64)
+}
+
+// grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block, eight codes each
+template <typename T, bool STREAM>
+__global__ __launch_bounds__(256) void fp8_blocks_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
+                                                                int M, int K, T *__restrict__ X, long long ldx)
+{
+    const int lane16 = threadIdx.x & 15, nk = (K + 127) / 128;
+    const long long m = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (m >= M) return;
+    for (int kc = blockIdx.y; kc < nk; kc += gridDim.y) {
+        const uint2 c = *reinterpret_cast<const uint2 *>(codes + m * (nk * 128LL) + kc * 128 + lane16 * 8);
+        float a, b, v[8];
+        scale_factors(scales[((long long)(kc >> 2) * M + m) * 4 + (kc & 3)], a, b);
+        const f32x2 p[4] = {__builtin_amdgcn_cvt_pk_f32_fp8((int)c.x, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)c.x, true),
+                            __builtin_amdgcn_cvt_pk_f32_fp8((int)c.y, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)c.y, true)};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[i >> 1][i & 1] * a * b;
+        const int k = kc * 128 + lane16 * 8;
+        T *x = X + m * ldx + k;
+        if (k + 8 <= K) store8<T, STREAM>(x, v);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + i < K) store_one(x + i, v[i]);
+    }
+}
+
+// ---- the product -----------------------------------------------------------
+struct BlockProductArgs {
+    const uint8_t *A, *B, *SA, *SB; // codes [M, Kp], [N, Kp]; scales [ceil(Kp/512), M, 4], [ceil(Kp/512), N, 4]
+    int M, N, nk;                   // nk = Kp / 128
+    const float *bias;
+    void *C;
+    long long ldc;
+    int tiles_n;
+    int split, per;                 // the contraction in `split` parts of `per` stages, each with a C of its own, one behind the other
+};
+
+// 4 bytes per lane into LDS (see load_to_lds_16)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_to_lds_4(const char *base, unsigned byte_off, const unsigned char *dst)
+{
+    const unsigned lds_addr = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(const lds_u8 *)dst);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+                 :
+                 : "v"(byte_off), "s"(base), "s"(lds_addr)
+                 : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+// Wait states between the last matrix instructions and the vector instructions that read their results, more than either the compiler
+// or the hardware asks for.  The results are operands of the statement, all of them of one: it stands behind every instruction that writes
+// them and before every one that reads them, which an s_nop by itself does not.
+template <int I, int J> __device__ __forceinline__ void settle(f32x16 (&a)[I][J])
+{
+    static_assert(I * J == 8 || I * J == 4 || I * J == 1, "");
+    if constexpr (I * J == 8)
+        asm volatile("s_nop 15\n\ts_nop 15" : "+v"(a[0][0]), "+v"(a[0][1]), "+v"(a[1][0]), "+v"(a[1][1]), "+v"(a[2][0]), "+v"(a[2][1]),
+                     "+v"(a[3][0]), "+v"(a[3][1]));
+    else if constexpr (I * J == 4) asm volatile("s_nop 15\n\ts_nop 15" : "+v"(a[0][0]), "+v"(a[0][1]), "+v"(a[1][0]), "+v"(a[1][1]));
+    else asm volatile("s_nop 15\n\ts_nop 15" : "+v"(a[0][0]));
+}
+
+// How exact the matrix cores are on E4M3 (measured; the same for every instruction that takes it): products of eight neighbouring columns
+// are added with 13 bits below the power of two of the largest of them, what is below is cut off; sums of such groups have fp32's 24
+// bits.  That is 1.4e-5 of a sum of 64 Gaussian products (rms) against 5e-9 for the same numbers as bf16, 2^-9 of the size that a bf16
+// result is rounded by.  So a bf16 result is formed by them (2.5 x the rate), and an fp32 result (EXACT) on the values as bf16, which has them all.
+struct Converted { bf16x8 q[4]; };                      // 32 values
+
+__device__ __forceinline__ Converted convert(const i32x8 &f, unsigned byte)
+{
+    Converted c;
+    const float scale = __uint_as_float(byte << 23);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)f[w], scale, false);
+        const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)f[w], scale, true);
+        c.q[w >> 1][4 * (w & 1)] = lo[0];
+        c.q[w >> 1][4 * (w & 1) + 1] = lo[1];
+        c.q[w >> 1][4 * (w & 1) + 2] = hi[0];
+        c.q[w >> 1][4 * (w & 1) + 3] = hi[1];
+    }
+    return c;
+}
+
+// The tiled product.  v_mfma_scale_f32_32x32x64_f8f6f4 on E4M3 operands: lane l gives 32 values of row l % 32 and their scale; which 32 of the
+// 64 columns is the same for both operands, and they all have one scale, so their order does not matter.  The rows of B go in
+// first: a lane's results are then neighbours in a row of C.
+//
+// Workgroup: WM x WN wavefronts of 32 WI x 32 WJ results, one tile of C after another.  A stage is a block, 128 columns of the tile's rows of either
+// side: a cache line of each.  Two stages are in LDS, one on its way while the other is used, straight from memory (global_load_lds).
+// A stage is used in slots, one for each of two halves of the columns and 32 rows of A: WJ products each.  The rows of A are read from LDS AHEAD
+// slots before they are used, those of B half a stage before.  The one barrier of a stage stands where its last reads have been made:
+// the next stage has arrived by then, and this one's place is free.  The scales of four stages are a word of a row; they come with the first of
+// the four, and a lane keeps those of its rows in registers.
+// Where there are few tiles and many stages, a part of the stages is a tile of its own (split), and fp8_blocks_join_kernel adds them up.
+// In LDS row r has 128 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.
+// Rows behind the last are read as the last and not stored.
+template <int WM_, int WN_, int WI_, int WJ_> struct Tile {
+    static constexpr int WM = WM_, WN = WN_, WI = WI_, WJ = WJ_, WAVES = WM * WN, BM = 32 * WI * WM, BN = 32 * WJ * WN;
+    static constexpr int STAGE = (BM + BN) * 128;
+    static constexpr int LA = BM / 8 / WAVES, LB = BN / 8 / WAVES, LOADS = LA + LB;     // loads of a wavefront and stage: 8 rows each
+    static constexpr int NS = (BM + BN) / 64 < WAVES ? 1 : (BM + BN) / 64 / WAVES;      // and of scales, every fourth stage
+    static constexpr int SLOTS = 2 * WI, AHEAD = WI == 4 ? 3 : WI, RING = AHEAD < 2 ? 2 : 4;
+    // results on their way out: 32 rows of 128 bytes (less where a wavefront has fewer) for each wavefront, in the stage that is free
+    template <typename T> static constexpr int out_cols() { return 32 * WJ * (int)sizeof(T) < 128 ? 32 * WJ : 128 / (int)sizeof(T); }
+    template <typename T> static constexpr int out_row() { return out_cols<T>() * (int)sizeof(T) + 16; }
+    static constexpr int OUT = WAVES * 32 * (128 + 16), BIAS = 2 * BN * 4;               // the bias of this tile and of the next
+    static constexpr int SCALES = 2 * (BM + BN) * 4, FRONT = BIAS + SCALES;              // a word of every row, of these four stages and the next
+    static constexpr int LDS = FRONT + STAGE + (OUT > STAGE ? OUT : STAGE);
+    static_assert(LA >= 1 && LB >= 1 && SLOTS % RING == 0, "");
+};
+
+__device__ __forceinline__ int spread(int r) { return ((r >> 1) & 7) ^ ((r & 1) << 2); }
+
+template <typename L, typename T, bool EXACT> __global__ __launch_bounds__(64 * L::WAVES, L::BM == 256 ? L::WAVES / 4 : 2)
+void fp8_blocks_product_kernel(const BlockProductArgs P)
+{
+    constexpr int WI = L::WI, WJ = L::WJ, BM = L::BM, BN = L::BN, STAGE = L::STAGE, LA = L::LA, LB = L::LB;
+    constexpr int LOADS = L::LOADS, SLOTS = L::SLOTS, AHEAD = L::AHEAD, RING = L::RING, BARRIER = SLOTS - AHEAD;
+    extern __shared__ __attribute__((aligned(256))) unsigned char s_tile[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = lane & 31, half = lane >> 5;
+    const long long row_bytes = (long long)P.nk * 128;
+
+    // Which tiles: the XCDs (every eighth workgroup) get contiguous parts of an order that goes down 4 tiles of C, then right, and
+    // their workgroups take turns, so that what an XCD works on at a time is a compact patch and shares its rows in that XCD's L2.
+    const int tiles_m = (P.M + BM - 1) / BM, tiles = tiles_m * P.tiles_n, total = tiles * P.split;
+    const int xcd = blockIdx.x & 7, part = total >> 3, rest = total & 7, first = xcd * part + min(xcd, rest);
+    const int mine = part + (xcd < rest), slots = (gridDim.x + 7 - xcd) >> 3;
+    const int ra = (wave / L::WN) * 32 * WI, rb = (wave % L::WN) * 32 * WJ;
+
+    int m0, n0, slice = 0, stages = P.per, first_stage = 0;
+    const char *ga, *gb;
+    unsigned off_a[LA], off_b[LB];                      // this lane's part of the loads: 8 rows x 128 bytes each
+    unsigned off_s[L::NS];
+    unsigned wa[WI], wb[WJ], next_a[WI], next_b[WJ];    // scales of the rows that this lane gives, this stage's in the lowest byte
+    auto set_tile = [&](int k) {
+        int t = first + k;
+        if (P.split > 1) {
+            slice = __builtin_amdgcn_readfirstlane(t / tiles);
+            t -= slice * tiles;
+            first_stage = slice * P.per;
+            stages = min(P.per, P.nk - first_stage);
+        }
+        const int group = t / (4 * P.tiles_n), in = t - group * 4 * P.tiles_n, high = min(4, tiles_m - group * 4);
+        m0 = __builtin_amdgcn_readfirstlane((group * 4 + in % high) * BM);
+        n0 = __builtin_amdgcn_readfirstlane((in / high) * BN);
+        ga = reinterpret_cast<const char *>(P.A) + m0 * row_bytes + first_stage * 128LL;
+        gb = reinterpret_cast<const char *>(P.B) + n0 * row_bytes + first_stage * 128LL;
+        int l = lane;
+        asm("" : "+v"(l));          // formed here, not kept in registers through the loop over the stages
+#pragma unroll
+        for (int i = 0; i < LA; ++i) {
+            const int r = (wave * LA + i) * 8 + (l >> 3);
+            off_a[i] = (unsigned)min(r, P.M - 1 - m0) * (unsigned)row_bytes + ((l & 7) ^ spread(r)) * 16;
+        }
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            const int r = (wave * LB + i) * 8 + (l >> 3);
+            off_b[i] = (unsigned)min(r, P.N - 1 - n0) * (unsigned)row_bytes + ((l & 7) ^ spread(r)) * 16;
+        }
+        // scales: BM + BN words, A's then B's, 64 a load (small tiles: some wavefronts load the same)
+#pragma unroll
+        for (int i = 0; i < L::NS; ++i) {
+            const int word = (wave * L::NS + i) * 64 % (BM + BN);
+            off_s[i] = 4u * (unsigned)(word < BM ? min(word + l, P.M - 1 - m0) : min(word - BM + l, P.N - 1 - n0));
+        }
+    };
+    // piece g of a stage's loads: LA of A, LB of B
+    auto load_piece = [&](int st, int g) {
+        unsigned char *to = s_tile + L::FRONT + (st & 1) * STAGE;
+        if (g < LA) load_to_lds_16(ga + st * 128LL, off_a[g], to + (wave * LA + g) * 1024);
+        else load_to_lds_16(gb + st * 128LL, off_b[g - LA], to + BM * 128 + (wave * LB + g - LA) * 1024);
+    };
+    auto load_scales = [&](int st) {                    // of stages st .. st + 3
+        const long long w = (first_stage + st) >> 2;
+#pragma unroll
+        for (int i = 0; i < L::NS; ++i) {
+            const int word = (wave * L::NS + i) * 64 % (BM + BN);
+            load_to_lds_4(reinterpret_cast<const char *>(word < BM ? P.SA + 4 * (w * P.M + m0) : P.SB + 4 * (w * P.N + n0)), off_s[i],
+                          s_tile + L::BIAS + ((st >> 2) & 1) * (BM + BN) * 4 + word * 4);
+        }
+    };
+    // a tile's first stage, its bias in front (some wavefronts may load the same part)
+    auto load_first = [&](int copy) {
+        if (P.bias)
+            load_to_lds_4(reinterpret_cast<const char *>(P.bias + n0), 4u * (unsigned)min(wave * 64 % BN + lane, P.N - 1 - n0),
+                          s_tile + copy * BN * 4 + wave * 64 % BN * 4);
+        load_scales(0);
+#pragma unroll
+        for (int g = 0; g < LOADS; ++g) load_piece(0, g);
+    };
+
+    f32x16 acc[WI][WJ];
+    const int at = row * 128 + ((half ^ spread(row)) << 4);         // piece 0 of the first half of a stage; piece p of half h: ^ (64 h + 32 p)
+    i32x8 a[RING], b[2][WJ];
+    Converted cb[EXACT ? WJ : 1];
+    auto read = [&](int st, int h, int rows) {
+        const unsigned char *s = s_tile + L::FRONT + (st & 1) * STAGE + rows * 128;
+        const uint4 x = *reinterpret_cast<const uint4 *>(s + (at ^ (64 * h))), y = *reinterpret_cast<const uint4 *>(s + (at ^ (64 * h + 32)));
+        return i32x8{(int)x.x, (int)x.y, (int)x.z, (int)x.w, (int)y.x, (int)y.y, (int)y.z, (int)y.w};
+    };
+    auto read_scales = [&](int st, unsigned *xa, unsigned *xb) {
+        const unsigned *s = reinterpret_cast<const unsigned *>(s_tile + L::BIAS) + ((st >> 2) & 1) * (BM + BN) + row;
+#pragma unroll
+        for (int i = 0; i < WI; ++i) xa[i] = s[ra + 32 * i];
+#pragma unroll
+        for (int j = 0; j < WJ; ++j) xb[j] = s[BM + rb + 32 * j];
+    };
+    // slot e: the reads that fall into it (from the next stage where there is one: `next`), then its products
+    auto slot = [&](int st, auto slot_number, auto next) {
+        constexpr int e = decltype(slot_number)::value, h = e / WI, i = e % WI, to = e + AHEAD;
+        constexpr bool more = decltype(next)::value;
+        if (to < SLOTS) a[to % RING] = read(st, to / WI, ra + 32 * (to % WI));
+        else if (more) a[to % RING] = read(st + 1, 0, ra + 32 * (to - SLOTS));
+        // B of the second half in the first slots, of the next stage's first half behind the barrier
+#pragma unroll
+        for (int j = 0; j < WJ; ++j) {
+            if (h == 0 && j * WI / WJ == i) b[1][j] = read(st, 1, BM + rb + 32 * j);
+            if (more && e >= BARRIER && min(j, AHEAD - 1) == e - BARRIER) b[0][j] = read(st + 1, 0, BM + rb + 32 * j);
+        }
+        if constexpr (EXACT) {
+            if (i == 0)
+#pragma unroll
+                for (int j = 0; j < WJ; ++j) cb[j] = convert(b[h][j], wb[j] & 255u);
+            const Converted ca = convert(a[e % RING], wa[i] & 255u);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int j = 0; j < WJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[j].q[q], ca.q[q], acc[i][j], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < WJ; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[h][j], a[e % RING], acc[i][j], 0, 0, 0, (int)wb[j], 0, (int)wa[i]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // One stage: a straight line of products, of which there are three (in branches the accumulators would be left in different registers,
+    // to be copied where the branches meet).  load: there is a stage behind the next.
+    auto stage = [&](int st, auto next, auto load) {
+        constexpr bool more = decltype(next)::value;
+        static_for<0, BARRIER>([&](auto e) { slot(st, e, next); });
+        // the next stage has arrived for every wavefront, and every wavefront has the last of this one in registers
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (decltype(load)::value) {
+            if (((st + 2) & 3) == 0) load_scales(st + 2);
+#pragma unroll
+            for (int g = 0; g < LOADS; ++g) load_piece(st + 2, g);
+        }
+        if (more) {
+            if (((st + 1) & 3) == 0) read_scales(st + 1, next_a, next_b);
+            else {
+#pragma unroll
+                for (int i = 0; i < WI; ++i) next_a[i] = wa[i] >> 8;
+#pragma unroll
+                for (int j = 0; j < WJ; ++j) next_b[j] = wb[j] >> 8;
+            }
+        }
+        static_for<BARRIER, SLOTS>([&](auto e) { slot(st, e, next); });
+        if (more) {
+#pragma unroll
+            for (int i = 0; i < WI; ++i) wa[i] = next_a[i];
+#pragma unroll
+            for (int j = 0; j < WJ; ++j) wb[j] = next_b[j];
+        }
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+
+    constexpr int STORES = WI * WJ * 32 * 32 * (int)sizeof(T) / 1024;       // of a wavefront and tile, if nothing of it is cut off
+    bool after = false;                                 // that many were issued behind the loads of this tile's first stage
+    int k = blockIdx.x >> 3, copy = 0;
+    if (k >= mine) return;
+    set_tile(k);
+    load_first(copy);
+    for (; k < mine; k += slots, copy ^= 1) {
+#pragma unroll
+        for (int i = 0; i < WI; ++i)
+#pragma unroll
+            for (int j = 0; j < WJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        // loads and stores come back in the order in which they were issued: the last tile's stores may still be on their way
+        if (after) wait_loads<(STORES < 63 ? STORES : 63)>();
+        else wait_loads<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read_scales(0, wa, wb);
+#pragma unroll
+        for (int j = 0; j < WJ; ++j) b[0][j] = read(0, 0, BM + rb + 32 * j);
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) a[e % RING] = read(0, e / WI, ra + 32 * (e % WI));
+        if (stages > 1)
+#pragma unroll
+            for (int g = 0; g < LOADS; ++g) load_piece(1, g);
+        int st = 0;
+        for (; st + 2 < stages; ++st) stage(st, Yes(), Yes());
+        if (st + 1 < stages) stage(st++, Yes(), No());
+        stage(st, No(), No());
+        settle(acc);
+
+        const int m_first = m0 + ra, n_first = n0 + rb, n_left = P.N - n_first;
+        const bool full = m0 + BM <= P.M && n0 + BN <= P.N;
+        T *C_first = static_cast<T *>(P.C) + ((long long)slice * P.M + m_first) * P.ldc + n_first;
+        if (k + slots < mine) {                                     // the next tile's first stage comes while this one goes out
+            set_tile(k + slots);
+            load_first(copy ^ 1);
+        }
+        after = full;
+
+        // Results: lane holds row m_first + 32 i + l % 32 of C, columns n_first + 32 j + 8 q + 4 (l / 32) .. + 3 in registers 4 q ..
+        // 4 q + 3.  Stored from there, an instruction would write 32 pieces of 16 bytes; 32 rows of 128 bytes at a time go through LDS
+        // instead (the second stage's place, a part of its own for each wavefront).
+        constexpr int COLS = L::template out_cols<T>(), ROW = L::template out_row<T>(), PER16 = 16 / (int)sizeof(T), JS = COLS / 32;
+        int l = lane;
+        asm("" : "+v"(l));
+        unsigned char *s = s_tile + L::FRONT + STAGE + wave * 32 * ROW;
+        const float *bias = reinterpret_cast<const float *>(s_tile) + copy * BN + rb;
+#pragma unroll
+        for (int i = 0; i < WI; ++i)
+#pragma unroll
+            for (int j0 = 0; j0 < WJ; j0 += JS) {
+#pragma unroll
+                for (int j = j0; j < j0 + JS; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int n = 32 * j + 8 * q + 4 * (l >> 5);
+                        float v[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
+                        if (P.bias) {
+                            const float4 add = *reinterpret_cast<const float4 *>(bias + n);
+                            v[0] += add.x; v[1] += add.y; v[2] += add.z; v[3] += add.w;
+                        }
+                        unsigned char *to = s + (l & 31) * ROW + (n - 32 * j0) * (int)sizeof(T);
+                        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(to) = make_float4(v[0], v[1], v[2], v[3]);
+                        else *reinterpret_cast<uint2 *>(to) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                    }
+                constexpr int LANES = COLS / PER16, AT_ONCE = 64 / LANES;       // lanes a row, rows an instruction
+                T *C = C_first + 32LL * i * P.ldc + 32 * j0;
+                const int rows = P.M - m_first - 32 * i, cols = n_left - 32 * j0;
+                if (full) {
+#pragma unroll
+                    for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
+                        const int r = r0 + l / LANES, c = l % LANES;
+                        const u32x4 v = *reinterpret_cast<const u32x4 *>(s + r * ROW + c * 16);
+                        u32x4_any *to = reinterpret_cast<u32x4_any *>(C + (long long)r * P.ldc + c * PER16);
+                        if (BM == 256) __builtin_nontemporal_store(v, to);      // past the operands in L2
+                        else *to = v;
+                    }
+                } else {
+                    const int c = l % LANES * PER16;
+                    for (int r = l / LANES; r < 32 && r < rows; r += AT_ONCE) {
+                        const unsigned char *from = s + r * ROW + c * (int)sizeof(T);
+                        T *to = C + (long long)r * P.ldc + c;
+                        if (c + PER16 <= cols) *reinterpret_cast<u32x4_any *>(to) = *reinterpret_cast<const u32x4 *>(from);
+                        else
+                            for (int e = 0; e < PER16 && c + e < cols; ++e) to[e] = reinterpret_cast<const T *>(from)[e];
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);      // else all results leave the accumulators first, for want of registers to memory
+            }
+    }
+}
+
+// ---- launchers -------------------------------------------------------------
+// slices of a loop so that there are some 2048 workgroups, where the loop has that many steps
+static int slices(long long blocks, int steps)
+{
+    const long long want = (2048 + blocks - 1) / blocks;
+    return (int)(want < 1 ? 1 : want > steps ? steps : want);
+}
+
+template <typename F> static int with_type(int dtype, F f)
+{
+    if (dtype == SVG2_BF16) f((bf16_t *)0);
+    else f((float *)0);
+    SVG2_HIP_CHECK(hipGetLastError());
+    return SVG2_OK;
+}
+
+int fp8_blocks_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t sm, int64_t sg, bool square, void *codes, void *scales,
+                            void *codes_t, void *scales_t, hipStream_t st)
+{
+    const BlockQuantArgs A = {X, sm, sg, M, G, Kg, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales),
+                              static_cast<uint8_t *>(codes_t), static_cast<uint8_t *>(scales_t)};
+    const int K = G * Kg;
+    return with_type(dtype, [&](auto *tp) {
+        using T = std::remove_pointer_t<decltype(tp)>;
+        if (!codes_t && !square) {
+            const int bx = cdiv(M, 16);
+            fp8_blocks_rows_kernel<T, false><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(A);
+            return;
+        }
+        const long long all = (long long)cdiv(M, 128) * cdiv(K, 128);
+        const int tiles = (int)(all < 1 << 20 ? all : 1 << 20);
+        if (square) {
+            if (!codes_t) fp8_blocks_tile_kernel<T, true, false, true><<<tiles, 256, 0, st>>>(A);
+            else if (!codes) fp8_blocks_tile_kernel<T, false, true, true><<<tiles, 256, 0, st>>>(A);
+            else fp8_blocks_tile_kernel<T, true, true, true><<<tiles, 256, 0, st>>>(A);
+        } else if (codes) fp8_blocks_tile_kernel<T, true, true, false><<<tiles, 256, 0, st>>>(A);
+        else fp8_blocks_tile_kernel<T, false, true, false><<<tiles, 256, 0, st>>>(A);
+    });
+}
+
+int fp8_blocks_values_launch(const void *codes, const void *scales, int M, int K, int dtype, void *X, int64_t ldx, hipStream_t st)
+{
+    return with_type(dtype, [&](auto *tp) {
+        using T = std::remove_pointer_t<decltype(tp)>;
+        const int bx = cdiv(M, 16);
+        fp8_blocks_values_kernel<T, false><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(
+            static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), M, K, static_cast<T *>(X), ldx);
+    });
+}
+
+using Large = Tile<2, 4, 4, 2>;
+using Medium = Tile<2, 2, 2, 2>;
+using Small = Tile<2, 2, 1, 1>;
+
+template <typename L> static int prepare_tiles()
+{
+    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&fp8_blocks_product_kernel<L, bf16_t, false>), L::LDS));
+    SVG2_TRY(set_dynamic_lds(reinterpret_cast<const void *>(&fp8_blocks_product_kernel<L, float, false>), L::LDS));
+    return set_dynamic_lds(reinterpret_cast<const void *>(&fp8_blocks_product_kernel<L, float, true>), L::LDS);
+}
+
+int fp8_blocks_matmul_prepare()
+{
+    SVG2_TRY(prepare_tiles<Large>());
+    SVG2_TRY(prepare_tiles<Medium>());
+    return prepare_tiles<Small>();
+}
+
+size_t fp8_blocks_matmul_ws_bytes(int, int, int) { return 256; }
+
+template <typename L, typename T, bool EXACT> static int product_tiles(BlockProductArgs P, hipStream_t st)
+{
+    P.tiles_n = cdiv(P.N, L::BN);
+    const int tiles = cdiv(P.M, L::BM) * P.tiles_n * P.split, resident = 256 * (L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4);
+    fp8_blocks_product_kernel<L, T, EXACT><<<tiles < resident ? tiles : resident, 64 * L::WAVES, L::LDS, st>>>(P);
+    SVG2_HIP_CHECK(hipGetLastError());
+    return SVG2_OK;
+}
+
+template <typename T, bool EXACT> static int product_sized(int size, const BlockProductArgs &P, hipStream_t st)
+{
+    return size == 2 ? product_tiles<Large, T, EXACT>(P, st) : size == 1 ? product_tiles<Medium, T, EXACT>(P, st) : product_tiles<Small, T, EXACT>(P, st);
+}
+
+int fp8_blocks_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
+                             int out_dtype, void *C, int64_t ldc, void *, hipStream_t st)
+{
+    BlockProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
+                          static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0, 1, cdiv(K, 128)};
+    const int size = cdiv(M, 256) * cdiv(N, 256) >= 200 ? 2 : cdiv(M, 128) * cdiv(N, 128) >= 300 ? 1 : 0;
+    return out_dtype == SVG2_BF16 ? product_sized<bf16_t, false>(size, P, st) : product_sized<float, true>(size, P, st);
+}
+
+}  // namespace svg2
