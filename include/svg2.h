@@ -459,8 +459,8 @@ int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const 
  *   dW fp32 of weight, dB fp32 of the offset, dense: [D], or [B,D] where weight or bias has a stride (both have or none has, where both are
  *                given); NULL: not wanted; weight NULL: no dW.
  *   args as in the forward call; args->y is ignored, bias is not read.
- * Sums over rows are formed in a fixed order, fp32 within a share of the rows and 64 bits over the shares (as many as 1024, four rows at least): results
- * are the same from run to run.
+ * Sums over rows are formed in a fixed order, fp32 within a share of the rows and 64 bits over the shares (320 to 5120 of them by the length of a row,
+ * fewer where there are few rows: two rows at least each): results are the same from run to run.
  * ------------------------------------------------------------------------- */
 typedef struct svg2_layer_norm_args {
     int dtype, y_dtype;

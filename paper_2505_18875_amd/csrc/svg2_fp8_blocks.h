@@ -82,18 +82,18 @@ __device__ __forceinline__ unsigned e4m3_block_scale(unsigned amax_bits, float &
     return byte;
 }
 
-// eight values times inv -> eight codes, to nearest even (in a block of scale 255: zeros)
+// eight values times inv -> eight codes, to nearest even (in a block of scale 255, whose inv is 0: zeros)
 __device__ __forceinline__ uint2 e4m3_codes8(const float *v, float inv)
 {
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = inv == 0.f ? 0.f : v[i] * inv;
+    for (int i = 0; i < 8; ++i) x[i] = v[i] * inv;
     int a = 0, b = 0;
     a = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], a, false);
     a = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], a, true);
     b = __builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], b, false);
     b = __builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], b, true);
-    return make_uint2((unsigned)a, (unsigned)b);
+    return inv == 0.f ? make_uint2(0u, 0u) : make_uint2((unsigned)a, (unsigned)b);
 }
 
 // largest of 16 neighbouring lanes' values, in all of them

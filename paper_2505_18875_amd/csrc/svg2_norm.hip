@@ -29,31 +29,84 @@ struct NormArgs {
 // Rows whose sums leave fp32's range (an infinity and a NaN among them) are taken again times this: squares of the largest numbers, 16384 of
 // them, then stay below 2^126, and those of a row that needs it stay above 2^-30, so that eps is nothing beside them.
 constexpr float SHRINK = 0x1p-72f;
+constexpr int WAVES = 16;           // most of a workgroup
 
 __device__ __forceinline__ bool finite(float x) { return mag(x) < 0x7F800000u; }
 
-// sum over the LANES threads of a row: 16 or 32 neighbouring lanes, a wavefront, or (LANES > 64) a workgroup, through s
-template <int LANES> __device__ __forceinline__ float row_sum(float x, float *s)
+// x / y by inv, 1 / y rounded: times inv alone, the mean of a constant row would not be that constant
+__device__ __forceinline__ float quotient(float x, float y, float inv)
 {
-#pragma unroll
-    for (int o = (LANES < 64 ? LANES : 64) >> 1; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    if constexpr (LANES > 64) {
-        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
-        __syncthreads();
-        x = 0.f;
-#pragma unroll
-        for (int k = 0; k < LANES / 64; ++k) x += s[k];
+    const float q = x * inv;
+    return fmaf(fmaf(-q, y, x), inv, q);
+}
+
+// sum over 16, 32 or 64 neighbouring lanes, in all of them: no trip through LDS, which takes __shfl_xor some hundred cycles a step
+template <int LANES> __device__ __forceinline__ float lane_sum(float x)
+{
+    auto dpp = [](float v, auto control) {
+        return __uint_as_float((unsigned)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), decltype(control)::value, 0xF, 0xF, true));
+    };
+    x += dpp(x, std::integral_constant<int, 0xB1>());           // quad_perm [1,0,3,2]
+    x += dpp(x, std::integral_constant<int, 0x4E>());           // quad_perm [2,3,0,1]
+    x += dpp(x, std::integral_constant<int, 0x124>());          // row_ror:4
+    x += dpp(x, std::integral_constant<int, 0x128>());          // row_ror:8
+    if constexpr (LANES >= 32) {                                // odd rows of 16 against even ones
+        const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    }
+    if constexpr (LANES == 64) {                                // the upper half against the lower
+        const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
     }
     return x;
 }
 
-// eight columns from k on; 0 behind D
-template <typename T> __device__ __forceinline__ void load_row8(const T *row, int k, int D, float *v)
+// Eight neighbouring columns as they are in memory.
+template <typename T> struct Raw { u32x4 q[sizeof(T) / 2]; };
+
+// columns k .. k + 7 of a row, zeros behind D
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *row, int k, int D)
 {
-    if (k + 8 <= D) load8<T>(row + k, v);
+    Raw<T> r;
+    if (k + 8 <= D) {
+        const u32x4_any *p = reinterpret_cast<const u32x4_any *>(row + k);
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(T) / 2; ++i) r.q[i] = p[i];
+    } else {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = k + i < D ? row[k + i] : (T)0;
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(T) / 2; ++i)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (sizeof(T) == 4) r.q[i][w] = __float_as_uint(e[4 * i + w]);
+                else r.q[i][w] = e[2 * w] | (unsigned)e[2 * w + 1] << 16;
+            }
+    }
+    return r;
+}
+
+template <typename T> __device__ __forceinline__ void decode(const Raw<T> &r, float *v)
+{
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 2; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (sizeof(T) == 4) v[4 * i + w] = __uint_as_float(r.q[i][w]);
+            else {
+                v[2 * w] = __uint_as_float(r.q[i][w] << 16);
+                v[2 * w + 1] = __uint_as_float(r.q[i][w] & 0xFFFF0000u);
+            }
+        }
+}
+
+__device__ __forceinline__ void load_weight8(const float *row, int k, int D, float *v)
+{
+    if (k + 8 <= D) load8<float>(row + k, v);
     else
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k + i < D ? to_f32(row[k + i]) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = k + i < D ? row[k + i] : 0.f;
 }
 
 template <typename T> __device__ __forceinline__ void store_row8(T *row, int k, int D, const float *v)
@@ -65,84 +118,162 @@ template <typename T> __device__ __forceinline__ void store_row8(T *row, int k, 
             if (k + i < D) store_one(row + k + i, v[i]);
 }
 
-// grid: workgroups stride over the rows; block 256, or LANES where a row takes more: LANES threads a row, CH steps of 8 columns a thread
-template <typename TX, typename TY, bool FP8, int LANES, int CH>
-__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_kernel(const NormArgs A)
+// One round over the wavefronts of a workgroup for a row's mean and sum of squares.  Each wavefront sums its columns' squares about its own mean;
+// of all of them together,
+//   mean = sum(n_k mean_k) / D,   squares = sum(squares_k + n_k (mean_k - mean)^2),   sum g (x - mean) = sum(gx_k + (mean_k - mean) g_k)
+// which cancels nothing, as sums of x and x^2 would.  Two copies in turn: one is written again only behind a barrier that every thread reaches
+// after it has read it.
+struct Wave { float mean, squares, g, gx; };
+
+// columns of wavefront k, CH steps of 8 T columns a row
+template <int CH> __device__ __forceinline__ float wave_columns(int k, int T, int D)
 {
-    constexpr int BLOCK = LANES < 256 ? 256 : LANES, ROWS = BLOCK / LANES;
-    __shared__ float s_sum[4][LANES > 64 ? LANES / 64 : 1];
-    const int t = threadIdx.x % LANES, D = A.D, nk = (D + 127) / 128;
-    const long long rows = (long long)A.B * A.N;
-    const float count = (float)D;               // sums are divided by it: times 1 / D, the mean of a constant row would not be that constant
-    for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / LANES; row < rows; row += (long long)gridDim.x * ROWS) {
-        const int b = (int)(row / A.N);
-        const long long n = row - (long long)b * A.N;
-        const TX *x = static_cast<const TX *>(A.x) + b * A.xs[0] + n * A.xs[1];
-        float v[CH][8], sum = 0.f, sq = 0.f;
+    int n = 0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) n += min(max(D - (c * T + 64 * k) * 8, 0), 512);
+    return (float)n;
+}
+
+// mean, squares, g and gx of a row from those of this wavefront.  Every 16 lanes take one wavefront's each.
+template <bool GRADIENT> __device__ __forceinline__ void join_waves(Wave &x, Wave *s, int waves, float count, float D, float inv_d)
+{
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    const int k = threadIdx.x & 15;
+    Wave w = {0.f, 0.f, 0.f, 0.f};
+    if (k < waves) w = s[k];
+    x.mean = quotient(lane_sum<16>(count * w.mean), D, inv_d);
+    const float d = k < waves ? w.mean - x.mean : 0.f;
+    x.squares = lane_sum<16>(fmaf(count * d, d, w.squares));
+    if (GRADIENT) {
+        x.g = lane_sum<16>(w.g);
+        x.gx = lane_sum<16>(fmaf(d, w.g, w.gx));
+    }
+}
+
+// v - mean (0 where there is no column), and the sum of its squares
+template <int CH> __device__ __forceinline__ float deviations(float (&v)[CH][8], float mean, int t, int T, int D, bool ragged)
+{
+    float squares = 0.f;
+    auto each = [&](auto by_column) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            load_row8(x, (c * LANES + t) * 8, D, v[c]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += v[c][i];
-        }
-        float eps = A.eps;
-        sum = row_sum<LANES>(sum, s_sum[0]);
-        if (!finite(sum)) {                                     // the same for the whole row, here and below
-            sum = eps = 0.f;
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum += v[c][i] *= SHRINK;
-            sum = row_sum<LANES>(sum, s_sum[1]);
-        }
-        const float mean = sum / count;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
+            float m = (c * T + t) * 8 < D ? mean : 0.f;
+            asm("" : "+v"(m));      // once for the eight: the compiler would choose between v and v - mean eight times
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                v[c][i] = (c * LANES + t) * 8 + i < D ? v[c][i] - mean : 0.f;
-                sq = fmaf(v[c][i], v[c][i], sq);
+                v[c][i] -= !decltype(by_column)::value || (c * T + t) * 8 + i < D ? m : 0.f;
+                squares = fmaf(v[c][i], v[c][i], squares);
             }
-        sq = row_sum<LANES>(sq, s_sum[2]);
-        if (!finite(sq)) {
-            sq = eps = 0.f;
+        }
+    };
+    if (ragged) each(std::true_type());
+    else each(std::false_type());
+    return squares;
+}
+
+// LANES threads a row, CH steps of 8 columns a thread: 16, 32 or 64 lanes of a block of 256, or (0) a workgroup of up to 1024.  Each row's place (slot) goes
+// through neighbouring rows and keeps their factors and offsets in registers: from the caches they would be twice to four times the
+// bytes of the rows themselves.  The next row is on its way while this one is used.
+template <typename TX, typename TY, bool FP8, int LANES, int CH>
+__global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX) == 2 ? 5 : 4) : 2) void layer_norm_kernel(const NormArgs A)
+{
+    __shared__ Wave s_wave[2][LANES ? 1 : WAVES];
+    constexpr int PLACES = 256 / (LANES ? LANES : 256);
+    const int T = LANES ? LANES : (int)blockDim.x, t = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, D = A.D, nk = (D + 127) / 128;
+    const long long rows = (long long)A.B * A.N, places = (long long)gridDim.x * PLACES;
+    const long long place = (long long)blockIdx.x * PLACES + (PLACES > 1 ? threadIdx.x / (256 / PLACES) : 0);
+    const long long from = rows * place / places, to = rows * (place + 1) / places;
+    const bool ragged = D & 7;                                  // a thread's eight columns are all there or none, but for these lengths
+    const float count = (float)D, inv_count = 1.f / count, own = LANES ? count : wave_columns<CH>(threadIdx.x >> 6, T, D);
+    const float inv_own = own > 0.f ? 1.f / own : 0.f;
+    const float other = LANES ? 0.f : wave_columns<CH>(threadIdx.x & 15, T, D);         // of the wavefront that this lane joins
+    float f[CH][8], o[CH][8];
+    int group = -1, copy = 0;
+    Raw<TX> next[CH];
+    int b = (int)(from / A.N), n = (int)(from - (long long)b * A.N);
+    auto load = [&]() {
+        const TX *x = static_cast<const TX *>(A.x) + b * A.xs[0] + n * A.xs[1];
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < CH; ++c) next[c] = load_raw(x, (c * T + t) * 8, D);
+    };
+    if (from < to) load();
+    for (long long row = from; row < to; ++row) {
+        const int rb = b, rn = n;
+        float v[CH][8];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) decode<TX>(next[c], v[c]);
+        if (++n == A.N) {
+            n = 0;
+            ++b;
+        }
+        if (row + 1 < to) load();
+        if (rb != group) {
+            group = rb;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int k = (c * T + t) * 8;
+                if (A.w) load_weight8(A.w + rb * A.ws, k, D, f[c]);
+                if (A.b) load_weight8(A.b + rb * A.bs, k, D, o[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    v[c][i] *= SHRINK;
-                    sq = fmaf(v[c][i], v[c][i], sq);
+                    f[c][i] = k + i >= D ? 0.f : A.w ? f[c][i] + A.one : 1.f;
+                    o[c][i] = A.b ? o[c][i] : 0.f;
                 }
-            sq = row_sum<LANES>(sq, s_sum[3]);
+            }
         }
-        const float r = 1.f / sqrtf(sq / count + eps);
-        const float *w = A.w ? A.w + b * A.ws : nullptr, *bias = A.b ? A.b + b * A.bs : nullptr;
+        // v becomes the deviation from the wavefront's own mean, which is `delta` off the row's
+        Wave w;
+        float eps = A.eps, delta;
+        for (bool again = false;; again = true) {               // twice where the sums are not finite: the same for the whole row
+            float sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += v[c][i];
+            const float mean = w.mean = quotient(lane_sum<LANES ? LANES : 64>(sum), own, inv_own);
+            w.squares = deviations<CH>(v, mean, t, T, D, ragged);
+            w.squares = lane_sum<LANES ? LANES : 64>(w.squares);
+            if constexpr (!LANES) {
+                join_waves<false>(w, s_wave[copy], T >> 6, other, count, inv_count);
+                copy ^= 1;
+            }
+            delta = w.mean - mean;
+            if (again || finite(w.squares)) break;
+            eps = 0.f;
+            const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                decode<TX>(load_raw(x, (c * T + t) * 8, D), v[c]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] *= SHRINK;
+            }
+        }
+        const float r = rsqrtf(fmaf(w.squares, inv_count, eps)), shift = -delta * r;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int k = (c * LANES + t) * 8;
-            float f[8], o[8];
-            if (w && k < D) load_row8(w, k, D, f);
-            if (bias && k < D) load_row8(bias, k, D, o);
+            const int k = (c * T + t) * 8;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[c][i] *= r;
-                if (w) v[c][i] *= k + i < D ? f[i] + A.one : 0.f;
-                if (bias) v[c][i] += k + i < D ? o[i] : 0.f;
-            }
+            for (int i = 0; i < 8; ++i) v[c][i] = fmaf(fmaf(v[c][i], r, shift), f[c][i], o[c][i]);
             if constexpr (!FP8) {
-                if (k < D) store_row8(static_cast<TY *>(A.y) + b * A.ys[0] + n * A.ys[1], k, D, v[c]);
+                if (k < D) store_row8(static_cast<TY *>(A.y) + rb * A.ys[0] + rn * A.ys[1], k, D, v[c]);
             } else {                                            // 16 lanes a block of 128 columns
                 unsigned top = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) top = max(top, mag(v[c][i]));
                 float inv;
                 const int kc = k >> 7;
-                const unsigned byte = e4m3_block_scale(max16(top), inv);
+                unsigned byte = e4m3_block_scale(max16(top), inv);
                 if (kc < nk) *reinterpret_cast<uint2 *>(A.codes + row * (nk * 128LL) + k) = e4m3_codes8(v[c], inv);
-                if ((t & 15) == 0) {
-                    uint8_t *s = A.scales + ((long long)(kc >> 2) * rows + row) * 4;
-                    if (kc < ((nk + 3) & ~3)) s[kc & 3] = kc < nk ? (uint8_t)byte : 0;
-                    if (LANES < 64 && t == 0)                   // the lanes of a short row do not reach the end of its word
+                else byte = 0;
+                uint8_t *s = A.scales + ((long long)(kc >> 2) * rows + row) * 4;
+                if constexpr (LANES == 0 || LANES == 64) {      // a wavefront's step is a word of scales
+                    const unsigned word = (unsigned)__builtin_amdgcn_readlane((int)byte, 0) | (unsigned)__builtin_amdgcn_readlane((int)byte, 16) << 8 |
+                                          (unsigned)__builtin_amdgcn_readlane((int)byte, 32) << 16 | (unsigned)__builtin_amdgcn_readlane((int)byte, 48) << 24;
+                    if ((t & 63) == 0 && kc < nk) *reinterpret_cast<unsigned *>(s) = word;
+                } else if ((t & 15) == 0) {
+                    s[kc & 3] = (uint8_t)byte;
+                    if (t == 0)                                 // the lanes of a short row do not reach the end of its word
                         for (int z = LANES / 16; z < 4; ++z) s[z] = 0;
                 }
             }
@@ -150,119 +281,133 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void layer_norm_kernel(c
     }
 }
 
-// grid: workgroups stride over the shares, P of each group's rows; block T: a multiple of 64 threads with CH steps of 8 columns each hold
-// a row, their columns' factors and sums
-template <typename TX, typename TY, int CH> __global__ __launch_bounds__(1024) void layer_norm_bwd_kernel(const NormArgs A)
+// grid: workgroups stride over the shares, P of each group's rows.  LANES threads a row, CH steps of 8 columns a thread: 16 or 32 lanes of a block
+// of 64, or (0) the block, a multiple of 64 threads.  A thread keeps its columns' factors and sums; the next row is on its way while this
+// one is used.
+template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bounds__(LANES ? 64 : 512) void layer_norm_bwd_kernel(const NormArgs A)
 {
-    __shared__ float s_sum[4][2][16];
-    const int t = threadIdx.x, T = blockDim.x, waves = T >> 6, wave = t >> 6, D = A.D;
+    constexpr int AT_ONCE = LANES ? 64 / (LANES ? LANES : 64) : 1, SUM = LANES ? LANES : 64;     // rows; lanes of a sum
+    __shared__ Wave s_wave[2][WAVES];
+    const int T = LANES ? LANES : (int)blockDim.x, t = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, D = A.D;
     const int groups = A.per_group ? A.B : 1;
     const long long rows = A.per_group ? A.N : (long long)A.B * A.N, shares = (long long)groups * A.P;
-    const float count = (float)D;
-    // sums over the workgroup of two values at once; `copy`: another one each time, until a barrier later
-    auto sums = [&](float &a, float &b, int copy) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            a += __shfl_xor(a, o);
-            b += __shfl_xor(b, o);
-        }
-        if ((t & 63) == 0) {
-            s_sum[copy][0][wave] = a;
-            s_sum[copy][1][wave] = b;
-        }
-        __syncthreads();
-        a = b = 0.f;
-        for (int k = 0; k < waves; ++k) {
-            a += s_sum[copy][0][k];
-            b += s_sum[copy][1][k];
-        }
-    };
+    const bool ragged = D & 7;
+    const float count = (float)D, inv_count = 1.f / count, own = LANES ? count : wave_columns<CH>(t >> 6, T, D), other = LANES ? 0.f : wave_columns<CH>(t & 15, T, D);
+    const float inv_own = own > 0.f ? 1.f / own : 0.f;
+    int copy = 0;
     for (long long share = blockIdx.x; share < shares; share += gridDim.x) {
         const int group = (int)(share / A.P), part = (int)(share - (long long)group * A.P);
         float acc_w[CH][8], acc_b[CH][8], f[CH][8];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            if (A.w) load_row8(A.w + group * A.ws, (c * T + t) * 8, D, f[c]);
+            if (A.w) load_weight8(A.w + group * A.ws, (c * T + t) * 8, D, f[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 acc_w[c][i] = acc_b[c][i] = 0.f;
                 f[c][i] = A.w ? f[c][i] + A.one : 1.f;
             }
         }
-        const long long from = rows * part / A.P, to = rows * (part + 1) / A.P;
-        for (long long row = from; row < to; ++row) {
-            const long long b = A.per_group ? group : row / A.N, n = A.per_group ? row : row - b * A.N;
+        const long long from = rows * part / A.P + (LANES ? threadIdx.x / SUM : 0), to = rows * (part + 1) / A.P;
+        int b = A.per_group ? group : (int)(from / A.N), n = A.per_group ? (int)from : (int)(from - (long long)b * A.N);
+        Raw<TX> next_x[CH];
+        Raw<TY> next_g[CH];
+        auto load = [&]() {
             const TX *x = static_cast<const TX *>(A.x) + b * A.xs[0] + n * A.xs[1];
             const TY *dy = static_cast<const TY *>(A.dy) + b * A.ys[0] + n * A.ys[1];
-            float vx[CH][8], vg[CH][8], sx = 0.f, sg = 0.f;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const int k = (c * T + t) * 8;
-                load_row8(x, k, D, vx[c]);
-                load_row8(dy, k, D, vg[c]);
+                next_x[c] = load_raw(x, (c * T + t) * 8, D);
+                next_g[c] = load_raw(dy, (c * T + t) * 8, D);
             }
+        };
+        if (from < to) load();
+        for (long long row = from; row < to; row += AT_ONCE) {
+            const int rb = b, rn = n;
+            float vx[CH][8], vg[CH][8], gf[CH][8], sg = 0.f;
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+            for (int c = 0; c < CH; ++c) {
+                decode<TX>(next_x[c], vx[c]);
+                decode<TY>(next_g[c], vg[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    sx += vx[c][i];
+                    gf[c][i] = vg[c][i] * f[c][i];
+                    sg += gf[c][i];
                     acc_b[c][i] += vg[c][i];
-                    sg = fmaf(vg[c][i], f[c][i], sg);
                 }
-            sums(sx, sg, 0);
-            float eps = A.eps, scale = 1.f;                     // of vx
-            if (!finite(sx)) {
-                float none = sx = eps = 0.f;
+            }
+            sg = lane_sum<SUM>(sg);
+            n += AT_ONCE;
+            if (!A.per_group)
+                while (n >= A.N) {
+                    n -= A.N;
+                    ++b;
+                }
+            if (row + AT_ONCE < to) load();
+            // vx becomes the deviation from the wavefront's own mean, which is `delta` off the row's
+            Wave w;
+            float eps = A.eps, scale = 1.f, delta;              // scale: of vx
+            for (bool again = false;; again = true) {           // twice where the sums are not finite: the same for the whole row
+                float sum = 0.f;
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum += vx[c][i];
+                const float mean = w.mean = quotient(lane_sum<SUM>(sum), own, inv_own);
+                w.g = sg;
+                w.squares = lane_sum<SUM>(deviations<CH>(vx, mean, t, T, D, ragged));
+                w.gx = 0.f;
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w.gx = fmaf(gf[c][i], vx[c][i], w.gx);
+                w.gx = lane_sum<SUM>(w.gx);
+                if (!LANES && T > 64) {
+                    join_waves<true>(w, s_wave[copy], T >> 6, other, count, inv_count);
+                    copy ^= 1;
+                }
+                delta = w.mean - mean;
+                if (again || finite(w.squares)) break;
+                eps = 0.f;
                 scale = SHRINK;
+                const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
 #pragma unroll
-                for (int c = 0; c < CH; ++c)
+                for (int c = 0; c < CH; ++c) {
+                    decode<TX>(load_raw(x, (c * T + t) * 8, D), vx[c]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sx += vx[c][i] *= SHRINK;
-                sums(sx, none, 1);
-            }
-            const float mean = sx / count, mean_g = sg / count;
-            float sxx = 0.f, sgx = 0.f;
-#pragma unroll
-            for (int c = 0; c < CH; ++c)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    vx[c][i] = (c * T + t) * 8 + i < D ? vx[c][i] - mean : 0.f;
-                    sxx = fmaf(vx[c][i], vx[c][i], sxx);
-                    sgx = fmaf(vg[c][i] * f[c][i], vx[c][i], sgx);
+                    for (int i = 0; i < 8; ++i) vx[c][i] *= SHRINK;
                 }
-            sums(sxx, sgx, 2);
-            if (!finite(sxx)) {
-                sxx = sgx = eps = 0.f;
-                scale *= SHRINK;
-#pragma unroll
-                for (int c = 0; c < CH; ++c)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        vx[c][i] *= SHRINK;
-                        sxx = fmaf(vx[c][i], vx[c][i], sxx);
-                        sgx = fmaf(vg[c][i] * f[c][i], vx[c][i], sgx);
-                    }
-                sums(sxx, sgx, 3);
             }
-            const float r = 1.f / sqrtf(sxx / count + eps), mean_gn = sgx * r / count;
-            TX *dx = static_cast<TX *>(A.dx) + b * A.ds[0] + n * A.ds[1];
+            const float r = rsqrtf(fmaf(w.squares, inv_count, eps)), rs = r * scale, shift = -delta * r;
+            const float by_n = -(w.gx * r * inv_count) * rs, by_1 = -(w.g * inv_count) * rs;
+            TX *dx = static_cast<TX *>(A.dx) + rb * A.ds[0] + rn * A.ds[1];
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float xn = vx[c][i] * r;
+                    const float xn = fmaf(vx[c][i], r, shift);
                     acc_w[c][i] = fmaf(vg[c][i], xn, acc_w[c][i]);
-                    v[i] = r * scale * (vg[c][i] * f[c][i] - mean_g - xn * mean_gn);
+                    v[i] = fmaf(xn, by_n, fmaf(gf[c][i], rs, by_1));
                 }
                 const int k = (c * T + t) * 8;
                 if (k < D) store_row8(dx, k, D, v);
             }
         }
+        if constexpr (LANES) {                                  // the rows that the wavefront had at once
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int other_rows = SUM; other_rows < 64; other_rows <<= 1) {
+                        acc_w[c][i] += __shfl_xor(acc_w[c][i], other_rows);
+                        acc_b[c][i] += __shfl_xor(acc_b[c][i], other_rows);
+                    }
+        }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int k = (c * T + t) * 8;
-            if (k >= D) continue;
+            if (k >= D || (LANES && (int)threadIdx.x >= LANES)) continue;
             if (A.dw) store_row8(A.dw + share * D, k, D, acc_w[c]);
             if (A.db) store_row8(A.db + share * D, k, D, acc_b[c]);
         }
@@ -323,16 +468,21 @@ static NormArgs norm_args(const svg2_layer_norm_args *a)
 template <typename TX, typename TY, bool FP8> static void norm_forward(const NormArgs &A, hipStream_t st)
 {
     const long long rows = (long long)A.B * A.N;
-    auto grid = [&](int per) { return (int)((rows + per - 1) / per < (1 << 20) ? (rows + per - 1) / per : 1 << 20); };
+    // Workgroups of `per` places: some rows each, so that factors and offsets are read seldom, but enough of them for the whole card and
+    // for places that are through early to be followed by others.  75,600 x 5120 bf16, rows a place: 37 336 us, 18 312, 9 292, 5 288; 16,384 x
+    // 5120: 8 71, 4 67, 2 77.  FP8 results leave fewer bytes to hide that reading behind: 75,600 x 5120, 16 rows 302, 8 312, 4 336.
+    constexpr int each = FP8 ? 16 : 4;
+    auto grid = [&](int per) {
+        const long long one = (rows + per - 1) / per, some = (rows + each * per - 1) / (each * per);
+        return (int)(one < 2048 ? one : some < 2048 ? 2048 : some);
+    };
+    const int steps = cdiv(A.D, 512);
     if (A.D <= 128) layer_norm_kernel<TX, TY, FP8, 16, 1><<<grid(16), 256, 0, st>>>(A);
     else if (A.D <= 256) layer_norm_kernel<TX, TY, FP8, 32, 1><<<grid(8), 256, 0, st>>>(A);
     else if (A.D <= 512) layer_norm_kernel<TX, TY, FP8, 64, 1><<<grid(4), 256, 0, st>>>(A);
     else if (A.D <= 1024) layer_norm_kernel<TX, TY, FP8, 64, 2><<<grid(4), 256, 0, st>>>(A);
-    else if (A.D <= 2048) layer_norm_kernel<TX, TY, FP8, 256, 1><<<grid(1), 256, 0, st>>>(A);
-    else if (A.D <= 4096) layer_norm_kernel<TX, TY, FP8, 256, 2><<<grid(1), 256, 0, st>>>(A);
-    else if (A.D <= 6144) layer_norm_kernel<TX, TY, FP8, 256, 3><<<grid(1), 256, 0, st>>>(A);
-    else if (A.D <= 8192) layer_norm_kernel<TX, TY, FP8, 1024, 1><<<grid(1), 1024, 0, st>>>(A);
-    else layer_norm_kernel<TX, TY, FP8, 1024, 2><<<grid(1), 1024, 0, st>>>(A);
+    else if (A.D <= 8192) layer_norm_kernel<TX, TY, FP8, 0, 2><<<grid(1), cdiv(steps, 2) * 64, 0, st>>>(A);
+    else layer_norm_kernel<TX, TY, FP8, 0, 4><<<grid(1), cdiv(steps, 4) * 64, 0, st>>>(A);
 }
 
 int layer_norm_launch(const svg2_layer_norm_args *a, hipStream_t st)
@@ -364,19 +514,32 @@ static bool per_group(const svg2_layer_norm_args *a)
     return a->B > 1 && ((a->weight && a->weight_stride) || (a->bias && a->bias_stride));
 }
 
-static int norm_parts(const svg2_layer_norm_args *a)
+struct NormBwdPlan {
+    bool own;                       // groups have sums of their own
+    int lanes, ch, threads, P;      // threads of a row (0: all), their steps of 8 columns, threads; parts of a group's rows
+};
+
+// Steps of a thread, us for 387M bf16 values: rows of 776 columns one 631, two 651; 1280 846 / 761; 1536 570 / 550; 5120 662 / 482.
+// Parts: 2560 wavefronts of two steps or 5120 of one are what the card holds at once, two rows each at least.
+static NormBwdPlan norm_bwd_plan(const svg2_layer_norm_args *a)
 {
-    const bool own = per_group(a);
-    const long long rows = own ? a->N : (long long)a->B * a->N;
-    long long parts = own ? (1024 + a->B - 1) / a->B : 1024;
-    if (parts > (rows + 3) / 4) parts = (rows + 3) / 4;
-    return (int)parts;
+    NormBwdPlan p;
+    p.own = per_group(a);
+    p.lanes = a->D <= 128 ? 16 : a->D <= 256 ? 32 : 0;
+    p.ch = a->D <= 1024 ? 1 : a->D <= 8192 ? 2 : 4;
+    p.threads = cdiv(cdiv(a->D, 512), p.ch) * 64;
+    const long long rows = p.own ? a->N : (long long)a->B * a->N, groups = p.own ? a->B : 1;
+    const long long shares = (p.ch == 1 ? 5120 : 2560) / (p.threads / 64), each = p.lanes ? 2 * (64 / p.lanes) : 2;
+    long long parts = (shares + groups - 1) / groups;
+    if (parts > (rows + each - 1) / each) parts = (rows + each - 1) / each;
+    p.P = (int)parts;
+    return p;
 }
 
 size_t layer_norm_bwd_ws_bytes(const svg2_layer_norm_args *a)
 {
-    const int P = norm_parts(a);
-    return P == 1 ? 256 : 2 * align256((size_t)(per_group(a) ? a->B : 1) * P * a->D * sizeof(float));
+    const NormBwdPlan p = norm_bwd_plan(a);
+    return p.P == 1 ? 256 : 2 * align256((size_t)(p.own ? a->B : 1) * p.P * a->D * sizeof(float));
 }
 
 int layer_norm_bwd_launch(const svg2_layer_norm_args *a, const void *dY, void *dX, const int64_t *dx_stride, float *dW, float *dB,
@@ -387,8 +550,9 @@ int layer_norm_bwd_launch(const svg2_layer_norm_args *a, const void *dY, void *d
     A.dx = dX;
     A.ds[0] = dx_stride[0];
     A.ds[1] = dx_stride[1];
-    A.per_group = per_group(a);
-    A.P = norm_parts(a);
+    const NormBwdPlan p = norm_bwd_plan(a);
+    A.per_group = p.own;
+    A.P = p.P;
     const int groups = A.per_group ? A.B : 1;
     if (A.P == 1) {
         A.dw = dW;
@@ -399,12 +563,14 @@ int layer_norm_bwd_launch(const svg2_layer_norm_args *a, const void *dY, void *d
     }
     const long long shares = (long long)groups * A.P;
     const int blocks = (int)(shares < 1 << 20 ? shares : 1 << 20);
-    const int steps = cdiv(A.D, 512), threads = A.D <= 512 ? 64 : cdiv(steps, 2) * 64;
     auto launch = [&](auto *tx, auto *ty) {
         using TX = std::remove_pointer_t<decltype(tx)>;
         using TY = std::remove_pointer_t<decltype(ty)>;
-        if (A.D <= 512) layer_norm_bwd_kernel<TX, TY, 1><<<blocks, threads, 0, st>>>(A);
-        else layer_norm_bwd_kernel<TX, TY, 2><<<blocks, threads, 0, st>>>(A);
+        if (p.lanes == 16) layer_norm_bwd_kernel<TX, TY, 16, 1><<<blocks, 64, 0, st>>>(A);
+        else if (p.lanes == 32) layer_norm_bwd_kernel<TX, TY, 32, 1><<<blocks, 64, 0, st>>>(A);
+        else if (p.ch == 1) layer_norm_bwd_kernel<TX, TY, 0, 1><<<blocks, p.threads, 0, st>>>(A);
+        else if (p.ch == 2) layer_norm_bwd_kernel<TX, TY, 0, 2><<<blocks, p.threads, 0, st>>>(A);
+        else layer_norm_bwd_kernel<TX, TY, 0, 4><<<blocks, p.threads, 0, st>>>(A);
     };
     const bool x16 = a->dtype == SVG2_BF16, y16 = a->y_dtype == SVG2_BF16;
     if (x16 && y16) launch((bf16_t *)0, (bf16_t *)0);
