@@ -11,9 +11,7 @@
 namespace svg2 {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));     // 16 bytes at any element's address: one load or store all the same
-typedef u32x2 u32x2_any __attribute__((aligned(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -33,42 +31,74 @@ __device__ __forceinline__ void store_one(bf16_t *p, float v) { *p = (bf16_t)pac
 // |x| as bits: they order like the magnitudes, NaN above infinity
 __device__ __forceinline__ unsigned mag(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
-// eight neighbouring elements from any address; STREAM: past the caches
-template <typename T, bool STREAM = false> __device__ __forceinline__ void load8(const T *from, float *v)
+// Eight neighbouring columns as they are in memory.
+template <typename T> struct Raw { u32x4 q[sizeof(T) / 2]; };
+
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *from)
 {
     const u32x4_any *p = reinterpret_cast<const u32x4_any *>(from);
-    const u32x4 a = STREAM ? __builtin_nontemporal_load(p) : *p;
-    if constexpr (sizeof(T) == 4) {
-        const u32x4 b = STREAM ? __builtin_nontemporal_load(p + 1) : p[1];
-        const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    Raw<T> r;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-    } else {
-        const unsigned w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
-    }
+    for (unsigned i = 0; i < sizeof(T) / 2; ++i) r.q[i] = p[i];
+    return r;
 }
 
-template <typename T, bool STREAM = false> __device__ __forceinline__ void store8(T *to, const float *v)
+// f(0) .. f(7)
+template <typename T, typename F> __device__ __forceinline__ Raw<T> raw_of(F f)
+{
+    T e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = f(i);
+    Raw<T> r;
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 2; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if constexpr (sizeof(T) == 4) r.q[i][w] = __float_as_uint(e[4 * i + w]);
+            else r.q[i][w] = e[2 * w] | (unsigned)e[2 * w + 1] << 16;
+        }
+    return r;
+}
+
+// columns k .. k + 7 of a row, zeros behind D
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *row, int k, int D)
+{
+    if (k + 8 <= D) return load_raw<T>(row + k);
+    return raw_of<T>([&](int i) { return k + i < D ? row[k + i] : (T)0; });
+}
+
+// value i of the eight
+template <typename T> __device__ __forceinline__ float value(const Raw<T> &r, int i)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(r.q[i >> 2][i & 3]);
+    else return __uint_as_float(i & 1 ? r.q[0][i >> 1] & 0xFFFF0000u : r.q[0][i >> 1] << 16);
+}
+
+template <typename T> __device__ __forceinline__ void decode(const Raw<T> &r, float *v)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = value<T>(r, i);
+}
+
+// eight neighbouring elements from and to any address
+template <typename T> __device__ __forceinline__ void load8(const T *from, float *v) { decode<T>(load_raw<T>(from), v); }
+
+template <typename T> __device__ __forceinline__ void store8(T *to, const float *v)
 {
     u32x4_any *p = reinterpret_cast<u32x4_any *>(to);
-    u32x4 a, b;
     if constexpr (sizeof(T) == 4) {
-        a = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-        b = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
-    } else {
-        a = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    }
-    if (STREAM) __builtin_nontemporal_store(a, p);
-    else *p = a;
-    if constexpr (sizeof(T) == 4) {
-        if (STREAM) __builtin_nontemporal_store(b, p + 1);
-        else p[1] = b;
-    }
+        p[0] = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        p[1] = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+    } else *p = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+}
+
+// bits of the largest magnitude of eight values
+__device__ __forceinline__ unsigned largest8(const float *v)
+{
+    unsigned top = mag(v[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = max(top, mag(v[i]));
+    return top;
 }
 
 // the scale byte of a block whose largest magnitude has these fp32 bits, and the factor 2^-exponent for its values.  A mantissa above

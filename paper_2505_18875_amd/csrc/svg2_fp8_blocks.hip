@@ -37,18 +37,16 @@ template <typename T> __device__ __forceinline__ const T *element(const BlockQua
     return static_cast<const T *>(A.X) + m * A.sm + g * A.sg + (k - g * A.Kg);
 }
 
-// eight neighbouring columns: one load where they are all there and in one group, whatever their address
-template <typename T, bool STREAM> __device__ __forceinline__ void load_columns(const BlockQuantArgs &A, long long m, int k, int K, float *v)
+// eight neighbouring columns: one load where they are all there and in one group, whatever their address; zeros behind K
+template <typename T> __device__ __forceinline__ Raw<T> load_columns(const BlockQuantArgs &A, long long m, int k, int K)
 {
-    if (k + 8 <= K && (A.G == 1 || k % A.Kg + 8 <= A.Kg)) load8<T, STREAM>(element<T>(A, m, k), v);
-    else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k + i < K ? to_f32(*element<T>(A, m, k + i)) : 0.f;
+    if (k + 8 <= K && (A.G == 1 || k % A.Kg + 8 <= A.Kg)) return load_raw<T>(element<T>(A, m, k));
+    return raw_of<T>([&](int i) { return k + i < K ? *element<T>(A, m, k + i) : (T)0; });
 }
 
 // rows: grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block of 128 columns, whose eight values each stay in
 // registers; the block's maximum goes round the 16 lanes without LDS.
-template <typename T, bool STREAM> __global__ __launch_bounds__(256) void fp8_blocks_rows_kernel(const BlockQuantArgs A)
+template <typename T> __global__ __launch_bounds__(256) void fp8_blocks_rows_kernel(const BlockQuantArgs A)
 {
     const int lane16 = threadIdx.x & 15, K = A.G * A.Kg, nk = (K + 127) / 128, all = (nk + 3) & ~3;
     const long long m = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
@@ -57,11 +55,8 @@ template <typename T, bool STREAM> __global__ __launch_bounds__(256) void fp8_bl
         unsigned byte = 0;
         if (kc < nk) {
             float v[8], inv;
-            load_columns<T, STREAM>(A, m, kc * 128 + lane16 * 8, K, v);
-            unsigned top = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, mag(v[i]));
-            byte = e4m3_block_scale(max16(top), inv);
+            decode<T>(load_columns<T>(A, m, kc * 128 + lane16 * 8, K), v);
+            byte = e4m3_block_scale(max16(largest8(v)), inv);
             *reinterpret_cast<uint2 *>(A.codes + m * (nk * 128LL) + kc * 128 + lane16 * 8) = e4m3_codes8(v, inv);
         }
         if (lane16 == 0) A.scales[((long long)(kc >> 2) * A.M + m) * 4 + (kc & 3)] = (uint8_t)byte;
@@ -69,50 +64,61 @@ template <typename T, bool STREAM> __global__ __launch_bounds__(256) void fp8_bl
 }
 
 // tiles of 128 x 128 for the transposed operand, for both from one read, and for square blocks.
-// grid: tiles, those of one row of tiles neighbours; block 256: a thread holds 8 rows x 8 columns.  The maximum of a row goes round 16 lanes, that of a
-// column over the wavefront's four groups of rows and, through LDS, the four wavefronts.  The codes of eight rows of a column are eight
-// bytes: they go through LDS, column by column, and leave as lines of 128 bytes.
+// grid: workgroups stride over the tiles, those of one row of tiles neighbours; block 256: a thread holds 8 rows x 8 columns, as they are in
+// memory.  The maximum of a row goes round 16 lanes, that of a column over the wavefront's four groups of rows and, through LDS, the four
+// wavefronts.  The codes of eight rows of a column are eight bytes: they go through LDS, column by column, and leave as lines of 128 bytes.
 template <typename T, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bounds__(256) void fp8_blocks_tile_kernel(const BlockQuantArgs A)
 {
     __shared__ unsigned s_top[4][128];
-    __shared__ __attribute__((aligned(16))) uint8_t s_codes[128 * 144];         // a column's 128 codes and 16 bytes: 8-byte stores spread over the banks
+    __shared__ __attribute__((aligned(16))) uint8_t s_codes[COLS ? 128 * 144 : 16];     // a column's 128 codes and 16 bytes: stores of 8 bytes spread over the banks
     const int K = A.G * A.Kg, nk = (K + 127) / 128, nm = (A.M + 127) / 128;
+    const int lane16 = threadIdx.x & 15, rows8 = threadIdx.x >> 4, wave = threadIdx.x >> 6;
     for (long long tile = blockIdx.x; tile < (long long)nm * nk; tile += gridDim.x) {
-        const int kc = (int)(tile % nk), mc = (int)(tile / nk);
-        const int lane16 = threadIdx.x & 15, rows8 = threadIdx.x >> 4, wave = threadIdx.x >> 6;
+        const int kc = (int)(tile % nk), mc = (int)(tile / nk), k0 = kc * 128 + lane16 * 8;
         const long long m0 = (long long)mc * 128 + rows8 * 8;
-        const int k0 = kc * 128 + lane16 * 8;
-        float v[8][8];
+        Raw<T> x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (m0 + i < A.M) load_columns<T, false>(A, m0 + i, k0, K, v[i]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+            if (m0 + i < A.M) x[i] = load_columns<T>(A, m0 + i, k0, K);
+            else x[i] = raw_of<T>([](int) { return (T)0; });
         }
-        unsigned row_top[8], col_top[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) row_top[i] = col_top[i] = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                row_top[i] = max(row_top[i], mag(v[i][e]));
-                col_top[e] = max(col_top[e], mag(v[i][e]));
+        auto row_result = [&](int i, const float *v, unsigned top) {
+            float inv;
+            const unsigned byte = e4m3_block_scale(top, inv);
+            const uint2 c = e4m3_codes8(v, inv);
+            if (m0 + i < A.M) {
+                *reinterpret_cast<uint2 *>(A.codes + (m0 + i) * (nk * 128LL) + kc * 128 + lane16 * 8) = c;
+                uint8_t *s = A.scales + ((long long)(kc >> 2) * A.M + m0 + i) * 4;
+                if (lane16 == 0) s[kc & 3] = (uint8_t)byte;
+                if (kc == nk - 1 && lane16 > (kc & 3) && lane16 < 4) s[lane16] = 0;
             }
-        if (SQUARE || COLS) {
+        };
+        unsigned col_top[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                col_top[e] = max(col_top[e], (unsigned)__shfl_xor((int)col_top[e], 16));
-                col_top[e] = max(col_top[e], (unsigned)__shfl_xor((int)col_top[e], 32));
-                if ((threadIdx.x & 63) < 16) s_top[wave][lane16 * 8 + e] = col_top[e];
-            }
-            __syncthreads();
+        for (int e = 0; e < 8; ++e) col_top[e] = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int k = lane16 * 8 + e;
-                col_top[e] = max(max(s_top[0][k], s_top[1][k]), max(s_top[2][k], s_top[3][k]));
-            }
+        for (int i = 0; i < 8; ++i) {
+            float v[8];
+            decode<T>(x[i], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) col_top[e] = max(col_top[e], mag(v[e]));
+            if (ROWS && !SQUARE) row_result(i, v, max16(largest8(v)));
+            // one row after another, and its values formed again below: kept, the 64 of them and what they become take 213 registers
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (unsigned w = 0; w < sizeof(T) / 2; ++w) asm volatile("" : "+v"(x[i].q[w]));
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            col_top[e] = max(col_top[e], (unsigned)__shfl_xor((int)col_top[e], 16));
+            col_top[e] = max(col_top[e], (unsigned)__shfl_xor((int)col_top[e], 32));
+            if ((threadIdx.x & 63) < 16) s_top[wave][lane16 * 8 + e] = col_top[e];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int k = lane16 * 8 + e;
+            col_top[e] = max(max(s_top[0][k], s_top[1][k]), max(s_top[2][k], s_top[3][k]));
         }
         if (SQUARE) {
             unsigned all = 0;
@@ -120,36 +126,31 @@ template <typename T, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bou
             for (int e = 0; e < 8; ++e) all = max(all, col_top[e]);
             all = max16(all);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) row_top[e] = col_top[e] = all;
-        }
-        if (ROWS) {
+            for (int e = 0; e < 8; ++e) col_top[e] = all;
+            if (ROWS)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float inv;
-                const unsigned byte = e4m3_block_scale(SQUARE ? row_top[i] : max16(row_top[i]), inv);
-                const uint2 c = e4m3_codes8(v[i], inv);
-                if (m0 + i < A.M) {
-                    *reinterpret_cast<uint2 *>(A.codes + (m0 + i) * (nk * 128LL) + kc * 128 + lane16 * 8) = c;
-                    uint8_t *s = A.scales + ((long long)(kc >> 2) * A.M + m0 + i) * 4;
-                    if (lane16 == 0) s[kc & 3] = (uint8_t)byte;
-                    if (kc == nk - 1 && lane16 > (kc & 3) && lane16 < 4) s[lane16] = 0;
+                for (int i = 0; i < 8; ++i) {
+                    float v[8];
+                    decode<T>(x[i], v);
+                    row_result(i, v, all);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-            }
         }
         if (COLS) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float inv, x[8];
+                float inv, v[8];
                 const unsigned byte = e4m3_block_scale(col_top[e], inv);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = v[i][e];
-                *reinterpret_cast<uint2 *>(s_codes + (lane16 * 8 + e) * 144 + rows8 * 8) = e4m3_codes8(x, inv);
+                for (int i = 0; i < 8; ++i) v[i] = value<T>(x[i], e);
+                *reinterpret_cast<uint2 *>(s_codes + (lane16 * 8 + e) * 144 + rows8 * 8) = e4m3_codes8(v, inv);
                 const long long r = k0 + e;
                 if (r < K && rows8 < 4) {
                     uint8_t *s = A.scales_t + ((long long)(mc >> 2) * K + r) * 4;
                     if (rows8 == (mc & 3)) s[rows8] = (uint8_t)byte;
                     else if (mc == nm - 1 && rows8 > (mc & 3)) s[rows8] = 0;
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
             __syncthreads();
             for (int p = threadIdx.x; p < 128 * 8; p += 256) {
@@ -159,7 +160,7 @@ template <typename T, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bou
                         *reinterpret_cast<const u32x4 *>(s_codes + (p >> 3) * 144 + (p & 7) * 16);
             }
         }
-        if (COLS || SQUARE) __syncthreads();    // s_top and s_codes have been read
+        __syncthreads();                        // s_top and s_codes have been read
     }
 }
 
@@ -173,7 +174,7 @@ __device__ __forceinline__ void scale_factors(unsigned byte, float &a, float &b)
 }
 
 // grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block, eight codes each
-template <typename T, bool STREAM>
+template <typename T>
 __global__ __launch_bounds__(256) void fp8_blocks_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                 int M, int K, T *__restrict__ X, long long ldx)
 {
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(256) void fp8_blocks_values_kernel(const uint8_t *_
         for (int i = 0; i < 8; ++i) v[i] = p[i >> 1][i & 1] * a * b;
         const int k = kc * 128 + lane16 * 8;
         T *x = X + m * ldx + k;
-        if (k + 8 <= K) store8<T, STREAM>(x, v);
+        if (k + 8 <= K) store8<T>(x, v);
         else
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -542,6 +543,88 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
     }
 }
 
+// C = sum of `split` partial products [M,N], one behind the other, + bias, always in that order; a thread takes four columns where N is a multiple
+// of four.  grid (ceil(N / (256 * PER)), rows), block 256
+template <typename T, int PER> __global__ __launch_bounds__(256) void fp8_blocks_join_kernel(const float *__restrict__ parts, const BlockProductArgs P)
+{
+    typedef float vec __attribute__((ext_vector_type(PER)));
+    const int n = (blockIdx.x * 256 + threadIdx.x) * PER;
+    if (n >= P.N) return;
+    vec bias;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) bias[e] = P.bias ? P.bias[n + e] : 0.f;
+    const size_t part = (size_t)P.M * P.N;
+    for (int m = blockIdx.y; m < P.M; m += gridDim.y) {
+        const float *p = parts + (size_t)m * P.N + n;
+        vec v = *reinterpret_cast<const vec *>(p);
+#pragma unroll 4
+        for (int s = 1; s < P.split; ++s) v += *reinterpret_cast<const vec *>(p + s * part);
+        v += bias;
+        T *to = static_cast<T *>(P.C) + (long long)m * P.ldc + n;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) store_one(to + e, v[e]);
+    }
+}
+
+// Few rows (M up to 16): the rows of B are read once, and how fast they come is what counts, so nothing goes through LDS and the
+// contraction is split over the wavefronts of a workgroup.  16 rows of B a workgroup, the rows of A behind the last as the last; a lane gives 32
+// neighbouring bytes of row l % 16, four lanes the block of 128.  Every wavefront has FEW_BLOCKS blocks of its rows on their way before it
+// uses the first (four 15.6 us at 15,360 x 5120 weights, eight, whose registers go to memory, 116).  The wavefronts' sums meet in LDS and are
+// added in order.
+// Measured, this kernel / tiles, us; the same weights again and again (the last cache holds them) and, in brackets, as many sets of weights in
+// turn as come from memory:
+//                     1 row                       8 rows                      16 rows
+//   15,360 x 5120     15.1 / 18.5 (17.0 / 21.3)   18.7 / 19.1 (21.0 / 22.5)   21.9 / 20.2 (25.0 / 23.6)
+//    5120 x 5120       8.1 / 11.3 ( 8.6 / 11.4)   10.2 / 11.1 (10.4 / 10.8)   11.8 / 11.2 (12.0 / 10.9)
+//   20,480 x 8192     29.8 / 29.6 (33.3 / 35.7)   35.5 / 30.1 (40.0 / 36.7)   41.6 / 30.8 (46.5 / 37.4)
+//    4096 x 16,384    15.9 / 15.6 (17.9 / 18.9)   17.9 / 15.4 (19.4 / 19.3)   19.6 / 15.8 (20.8 / 19.2)
+//    2048 x 16,384    12.0 / 11.2 (13.2 / 13.1)   15.2 / 11.2 (16.0 / 13.5)   17.8 / 11.3 (18.6 / 13.4)
+// so up to 4 rows take it to 10 * 2^24 weights, up to 8 rows to 5 * 2^24, of rows up to 8192 long.
+constexpr int FEW_BLOCKS = 2, FEW_WAVES = 16;
+
+template <typename T, bool EXACT> __global__ __launch_bounds__(64 * FEW_WAVES) void fp8_blocks_few_kernel(const BlockProductArgs P)
+{
+    __shared__ __attribute__((aligned(16))) float s_sum[FEW_WAVES * 256];          // [wavefront][row of A][row of B]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int r = lane & 15, g = lane >> 4, n0 = blockIdx.x * 16;
+    const int n = min(n0 + r, P.N - 1), m = min(r, P.M - 1);
+    const uint8_t *b = P.B + (long long)n * P.nk * 128 + g * 32, *a = P.A + (long long)m * P.nk * 128 + g * 32;
+    const uint8_t *sb = P.SB + n * 4LL, *sa = P.SA + m * 4LL;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    const i32x8 none = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int k0 = wave; k0 < P.nk; k0 += waves * FEW_BLOCKS) {
+        i32x8 vb[FEW_BLOCKS], va[FEW_BLOCKS];
+        unsigned xb[FEW_BLOCKS], xa[FEW_BLOCKS];
+#pragma unroll
+        for (int u = 0; u < FEW_BLOCKS; ++u) {
+            const int kc = k0 + u * waves;
+            const bool there = kc < P.nk;                           // zeros behind the end: they add nothing
+            vb[u] = there ? *reinterpret_cast<const i32x8 *>(b + kc * 128LL) : none;
+            xb[u] = there ? sb[(long long)(kc >> 2) * P.N * 4 + (kc & 3)] : 0u;
+            va[u] = there ? *reinterpret_cast<const i32x8 *>(a + kc * 128LL) : none;
+            xa[u] = there ? sa[(long long)(kc >> 2) * P.M * 4 + (kc & 3)] : 0u;
+        }
+#pragma unroll
+        for (int u = 0; u < FEW_BLOCKS; ++u) {
+            if constexpr (EXACT) {
+                const Converted cb = convert(vb[u], xb[u]), ca = convert(va[u], xa[u]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cb.q[q], ca.q[q], acc, 0, 0, 0);
+            } else acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vb[u], va[u], acc, 0, 0, 0, (int)xb[u], 0, (int)xa[u]);
+        }
+    }
+    asm volatile("s_nop 15\n\ts_nop 15" : "+v"(acc));              // (see settle)
+    // lane holds row l % 16 of A, rows 4 (l / 16) .. + 3 of B
+    *reinterpret_cast<float4 *>(s_sum + (wave * 16 + r) * 16 + 4 * g) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    __syncthreads();
+    const int i = threadIdx.x, row = i >> 4, col = n0 + (i & 15);
+    if (i >= 256 || row >= P.M || col >= P.N) return;
+    float v = 0.f;
+    for (int k = 0; k < waves; ++k) v += s_sum[k * 256 + i];
+    if (P.bias) v += P.bias[col];
+    store_one(static_cast<T *>(P.C) + (long long)row * P.ldc + col, v);
+}
+
 // ---- launchers -------------------------------------------------------------
 // slices of a loop so that there are some 2048 workgroups, where the loop has that many steps
 static int slices(long long blocks, int steps)
@@ -568,7 +651,7 @@ int fp8_blocks_quant_launch(const void *X, int dtype, int M, int G, int Kg, int6
         using T = std::remove_pointer_t<decltype(tp)>;
         if (!codes_t && !square) {
             const int bx = cdiv(M, 16);
-            fp8_blocks_rows_kernel<T, false><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(A);
+            fp8_blocks_rows_kernel<T><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(A);
             return;
         }
         const long long all = (long long)cdiv(M, 128) * cdiv(K, 128);
@@ -587,7 +670,7 @@ int fp8_blocks_values_launch(const void *codes, const void *scales, int M, int K
     return with_type(dtype, [&](auto *tp) {
         using T = std::remove_pointer_t<decltype(tp)>;
         const int bx = cdiv(M, 16);
-        fp8_blocks_values_kernel<T, false><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(
+        fp8_blocks_values_kernel<T><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(
             static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), M, K, static_cast<T *>(X), ldx);
     });
 }
@@ -610,7 +693,68 @@ int fp8_blocks_matmul_prepare()
     return prepare_tiles<Small>();
 }
 
-size_t fp8_blocks_matmul_ws_bytes(int, int, int) { return 256; }
+static bool few(int M, int N, int K)
+{
+    return M <= 8 && K <= 8192 && (long long)N * K <= (M <= 4 ? 10LL : 5LL) << 24;
+}
+
+// Microseconds that the product takes with these tiles, by what was measured: `start` a tile, and for each stage
+// alone with one workgroup a CU up to full with as many as fit (Large 1, Medium 2, Small 4).  Large tiles do most with
+// what they load, small ones leave fewer CUs idle: measured, large / medium / small, bf16 results and (fp32)
+//   8192 x 8192 x 8192  451 / 520 / 836 us (799 / 888 / 1250)     4096 x 4096 x 4096  58 / 62 / 103 us (103 / 113 / 153)
+//   4096 x 5120 x 5120  120 / 104 / 169 us (210 / 170 / 237)      2048 x 2048 x 2048  25 / 14 /  16 us (40 / 21 / 22)
+//    512 x 5120 x 5120   56 /  29 /  25 us (93 / 37 / 36)          300 x 5120 x 5120  55 / 27 /  22 us (93 / 37 / 26)
+template <typename L> static double tile_time(int M, int N, int stages, int split, bool exact)
+{
+    constexpr int R = L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4;
+    const double start = R == 1 ? 6.0 : R == 2 ? 3.0 : 2.0;
+    const double alone = exact ? (R == 1 ? 2.7 : R == 2 ? 0.83 : 0.43) : (R == 1 ? 1.45 : R == 2 ? 0.63 : 0.40);
+    const double full = exact ? (R == 1 ? 3.05 : R == 2 ? 1.65 : 1.13) : (R == 1 ? 1.66 : R == 2 ? 0.98 : 0.75);
+    const long long tiles = (long long)cdiv(M, L::BM) * cdiv(N, L::BN) * split, rounds = tiles / (256 * R), rest = (tiles - rounds * 256 * R + 255) / 256;
+    const double per = cdiv(stages, split);
+    const double last = rest == 0 ? 0.0 : start + per * (R == 1 ? alone : alone + (full - alone) * (double)(rest - 1) / (R > 1 ? R - 1 : 1));
+    return (double)rounds * (start + per * full) + last;
+}
+
+// Which tiles, and in how many parts the contraction: the least time by that model; parts of whole words of scales (four stages), 16 parts at
+// most.  Adding them up is a second launch and the parts' way out and back: 2.5 us, and 0.2 us for each MB of a part.  Measured, one part / as
+// chosen, fp32 results (bf16):
+//   1536 x 1536 x 16,384  102 / 82 us (64 / 57)     1536 x 1536 x 75,600  470 / 291 us (297 / 186)     512 x 512 x 16,384  58 / 21 us (57 / 16)
+struct BlockProductPlan {
+    int size, split, per;           // size: 0 small, 1 medium, 2 large
+};
+
+static BlockProductPlan product_plan(int M, int N, int K, bool exact)
+{
+    const int stages = cdiv(K, 128);
+    BlockProductPlan best = {0, 1, stages};
+    double least = 1e300;
+    for (int split = 1; split <= 16 && (split == 1 || stages >= 8 * split); ++split) {
+        const int per = split == 1 ? stages : cdiv(cdiv(stages, split), 4) * 4;
+        if (split > 1 && (cdiv(stages, per) != split || (double)split * M * N > (1 << 28))) continue;
+        const double join = split == 1 ? 0.0 : 2.5 + 0.2 * split * (double)M * N * sizeof(float) * 1e-6;
+        const double t[3] = {tile_time<Small>(M, N, stages, split, exact), tile_time<Medium>(M, N, stages, split, exact),
+                             tile_time<Large>(M, N, stages, split, exact)};
+        for (int size = 0; size < 3; ++size)
+            if (t[size] + join < least * (size > best.size && split == best.split ? 1.0 : 0.999)) {
+                least = t[size] + join;
+                best = {size, split, per};
+            }
+    }
+    return best;
+}
+
+size_t fp8_blocks_matmul_ws_bytes(int M, int N, int K)
+{
+    if (few(M, N, K)) return 256;
+    size_t most = 256;              // of either type of result
+    for (bool exact : {false, true}) {
+        const BlockProductPlan p = product_plan(M, N, K, exact);
+        const size_t need = p.split == 1 ? 256 : (size_t)p.split * M * N * sizeof(float);
+        if (need > most) most = need;
+    }
+    return most;
+}
 
 template <typename L, typename T, bool EXACT> static int product_tiles(BlockProductArgs P, hipStream_t st)
 {
@@ -626,13 +770,46 @@ template <typename T, bool EXACT> static int product_sized(int size, const Block
     return size == 2 ? product_tiles<Large, T, EXACT>(P, st) : size == 1 ? product_tiles<Medium, T, EXACT>(P, st) : product_tiles<Small, T, EXACT>(P, st);
 }
 
+static int product_few(const BlockProductArgs &P, int out_dtype, hipStream_t st)
+{
+    // 4 wavefronts, 8 or 16: enough of them for the whole card, not more than there are blocks in a row.  Fewer to a workgroup leave others on the CU
+    // when some are through: 15,360 x 5120, 16 wavefronts 18.7 us, 8 15.1
+    const int blocks = cdiv(P.N, 16);
+    int waves = 4;
+    while (waves < FEW_WAVES && waves < P.nk && (long long)blocks * waves < 8192) waves *= 2;
+    if (out_dtype == SVG2_BF16) fp8_blocks_few_kernel<bf16_t, false><<<blocks, 64 * waves, 0, st>>>(P);
+    else fp8_blocks_few_kernel<float, true><<<blocks, 64 * waves, 0, st>>>(P);
+    SVG2_HIP_CHECK(hipGetLastError());
+    return SVG2_OK;
+}
+
 int fp8_blocks_matmul_launch(const void *A, const void *SA, const void *B, const void *SB, int M, int N, int K, const float *bias,
-                             int out_dtype, void *C, int64_t ldc, void *, hipStream_t st)
+                             int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st)
 {
     BlockProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
                           static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0, 1, cdiv(K, 128)};
-    const int size = cdiv(M, 256) * cdiv(N, 256) >= 200 ? 2 : cdiv(M, 128) * cdiv(N, 128) >= 300 ? 1 : 0;
-    return out_dtype == SVG2_BF16 ? product_sized<bf16_t, false>(size, P, st) : product_sized<float, true>(size, P, st);
+    if (few(M, N, K)) return product_few(P, out_dtype, st);
+    const BlockProductPlan p = product_plan(M, N, K, out_dtype == SVG2_F32);
+    if (p.split == 1) return out_dtype == SVG2_BF16 ? product_sized<bf16_t, false>(p.size, P, st) : product_sized<float, true>(p.size, P, st);
+    P.split = p.split;
+    P.per = p.per;
+    BlockProductArgs parts = P;
+    parts.bias = nullptr;
+    parts.C = ws;
+    parts.ldc = N;
+    SVG2_TRY(out_dtype == SVG2_BF16 ? (product_sized<float, false>(p.size, parts, st)) : (product_sized<float, true>(p.size, parts, st)));
+    const int wide = N % 4 == 0 ? 4 : 1;
+    const dim3 grid(cdiv(N, 256 * wide), M < 4096 ? M : 4096);
+    const float *from = static_cast<const float *>(ws);
+    if (out_dtype == SVG2_BF16) {
+        if (wide == 4) fp8_blocks_join_kernel<bf16_t, 4><<<grid, 256, 0, st>>>(from, P);
+        else fp8_blocks_join_kernel<bf16_t, 1><<<grid, 256, 0, st>>>(from, P);
+    } else {
+        if (wide == 4) fp8_blocks_join_kernel<float, 4><<<grid, 256, 0, st>>>(from, P);
+        else fp8_blocks_join_kernel<float, 1><<<grid, 256, 0, st>>>(from, P);
+    }
+    SVG2_HIP_CHECK(hipGetLastError());
+    return SVG2_OK;
 }
 
 }  // namespace svg2

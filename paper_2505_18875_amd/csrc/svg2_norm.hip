@@ -61,46 +61,6 @@ template <int LANES> __device__ __forceinline__ float lane_sum(float x)
     return x;
 }
 
-// Eight neighbouring columns as they are in memory.
-template <typename T> struct Raw { u32x4 q[sizeof(T) / 2]; };
-
-// columns k .. k + 7 of a row, zeros behind D
-template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *row, int k, int D)
-{
-    Raw<T> r;
-    if (k + 8 <= D) {
-        const u32x4_any *p = reinterpret_cast<const u32x4_any *>(row + k);
-#pragma unroll
-        for (unsigned i = 0; i < sizeof(T) / 2; ++i) r.q[i] = p[i];
-    } else {
-        T e[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = k + i < D ? row[k + i] : (T)0;
-#pragma unroll
-        for (unsigned i = 0; i < sizeof(T) / 2; ++i)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                if constexpr (sizeof(T) == 4) r.q[i][w] = __float_as_uint(e[4 * i + w]);
-                else r.q[i][w] = e[2 * w] | (unsigned)e[2 * w + 1] << 16;
-            }
-    }
-    return r;
-}
-
-template <typename T> __device__ __forceinline__ void decode(const Raw<T> &r, float *v)
-{
-#pragma unroll
-    for (unsigned i = 0; i < sizeof(T) / 2; ++i)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if constexpr (sizeof(T) == 4) v[4 * i + w] = __uint_as_float(r.q[i][w]);
-            else {
-                v[2 * w] = __uint_as_float(r.q[i][w] << 16);
-                v[2 * w + 1] = __uint_as_float(r.q[i][w] & 0xFFFF0000u);
-            }
-        }
-}
-
 __device__ __forceinline__ void load_weight8(const float *row, int k, int D, float *v)
 {
     if (k + 8 <= D) load8<float>(row + k, v);
@@ -258,12 +218,9 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
             if constexpr (!FP8) {
                 if (k < D) store_row8(static_cast<TY *>(A.y) + rb * A.ys[0] + rn * A.ys[1], k, D, v[c]);
             } else {                                            // 16 lanes a block of 128 columns
-                unsigned top = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = max(top, mag(v[c][i]));
                 float inv;
                 const int kc = k >> 7;
-                unsigned byte = e4m3_block_scale(max16(top), inv);
+                unsigned byte = e4m3_block_scale(max16(largest8(v[c])), inv);
                 if (kc < nk) *reinterpret_cast<uint2 *>(A.codes + row * (nk * 128LL) + k) = e4m3_codes8(v[c], inv);
                 else byte = 0;
                 uint8_t *s = A.scales + ((long long)(kc >> 2) * rows + row) * 4;
