@@ -203,6 +203,7 @@ __global__ __launch_bounds__(256) void fp8_blocks_values_kernel(const uint8_t *_
 struct BlockProductArgs {
     const uint8_t *A, *B, *SA, *SB; // codes [M, Kp], [N, Kp]; scales [ceil(Kp/512), M, 4], [ceil(Kp/512), N, 4]
     int M, N, nk;                   // nk = Kp / 128
+    int rows_a;                     // of A's scales: M, or more where these are some rows of a larger product
     const float *bias;
     void *C;
     long long ldc;
@@ -355,7 +356,7 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
 #pragma unroll
         for (int i = 0; i < L::NS; ++i) {
             const int word = (wave * L::NS + i) * 64 % (BM + BN);
-            load_to_lds_4(reinterpret_cast<const char *>(word < BM ? P.SA + 4 * (w * P.M + m0) : P.SB + 4 * (w * P.N + n0)), off_s[i],
+            load_to_lds_4(reinterpret_cast<const char *>(word < BM ? P.SA + 4 * (w * P.rows_a + m0) : P.SB + 4 * (w * P.N + n0)), off_s[i],
                           s_tile + L::BIAS + ((st >> 2) & 1) * (BM + BN) * 4 + word * 4);
         }
     };
@@ -385,8 +386,17 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
 #pragma unroll
         for (int j = 0; j < WJ; ++j) xb[j] = s[BM + rb + 32 * j];
     };
-    // slot e: the reads that fall into it (from the next stage where there is one: `next`), then its products
-    auto slot = [&](int st, auto slot_number, auto next) {
+    auto take_scales = [&](int st) {
+        const int shift = 8 * (st & 3);
+#pragma unroll
+        for (int i = 0; i < WI; ++i) wa[i] = next_a[i] >> shift;
+#pragma unroll
+        for (int j = 0; j < WJ; ++j) wb[j] = next_b[j] >> shift;
+    };
+    // Slot e: the reads that fall into it (from the next stage where there is one: `next`), its products, and its share of the loads of the stage
+    // behind that (`load`).  In one piece behind the barrier, the 64 loads of a workgroup keep its wavefronts from the matrix cores for as long
+    // as the memory pipe takes to accept them, some 17 cycles each: 8192 x 8192 x 8192 423 us, behind a product each 400.
+    auto slot = [&](int st, auto slot_number, auto next, auto load) {
         constexpr int e = decltype(slot_number)::value, h = e / WI, i = e % WI, to = e + AHEAD;
         constexpr bool more = decltype(next)::value;
         if (to < SLOTS) a[to % RING] = read(st, to / WI, ra + 32 * (to % WI));
@@ -397,6 +407,15 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
             if (h == 0 && j * WI / WJ == i) b[1][j] = read(st, 1, BM + rb + 32 * j);
             if (more && e >= BARRIER && min(j, AHEAD - 1) == e - BARRIER) b[0][j] = read(st + 1, 0, BM + rb + 32 * j);
         }
+        auto loads = [&](int j) {
+            constexpr int PLACES = AHEAD * WJ;
+            if (decltype(load)::value && e >= BARRIER) {
+                if (e == BARRIER && j == 0) load_scales(st + 2);
+#pragma unroll
+                for (int g = 0; g < LOADS; ++g)
+                    if (g * PLACES / LOADS == (e - BARRIER) * WJ + j) load_piece(st + 2, g);
+            }
+        };
         if constexpr (EXACT) {
             if (i == 0)
 #pragma unroll
@@ -406,10 +425,16 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
             for (int q = 0; q < 4; ++q)
 #pragma unroll
                 for (int j = 0; j < WJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cb[j].q[q], ca.q[q], acc[i][j], 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < WJ; ++j) loads(j);
         } else {
 #pragma unroll
-            for (int j = 0; j < WJ; ++j)
+            for (int j = 0; j < WJ; ++j) {
                 acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b[h][j], a[e % RING], acc[i][j], 0, 0, 0, (int)wb[j], 0, (int)wa[i]);
+                __builtin_amdgcn_sched_barrier(0);
+                loads(j);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -417,32 +442,14 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
     // to be copied where the branches meet).  load: there is a stage behind the next.
     auto stage = [&](int st, auto next, auto load) {
         constexpr bool more = decltype(next)::value;
-        static_for<0, BARRIER>([&](auto e) { slot(st, e, next); });
+        static_for<0, BARRIER>([&](auto e) { slot(st, e, next, load); });
         // the next stage has arrived for every wavefront, and every wavefront has the last of this one in registers
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (decltype(load)::value) {
-            if (((st + 2) & 3) == 0) load_scales(st + 2);
-#pragma unroll
-            for (int g = 0; g < LOADS; ++g) load_piece(st + 2, g);
-        }
-        if (more) {
-            if (((st + 1) & 3) == 0) read_scales(st + 1, next_a, next_b);
-            else {
-#pragma unroll
-                for (int i = 0; i < WI; ++i) next_a[i] = wa[i] >> 8;
-#pragma unroll
-                for (int j = 0; j < WJ; ++j) next_b[j] = wb[j] >> 8;
-            }
-        }
-        static_for<BARRIER, SLOTS>([&](auto e) { slot(st, e, next); });
-        if (more) {
-#pragma unroll
-            for (int i = 0; i < WI; ++i) wa[i] = next_a[i];
-#pragma unroll
-            for (int j = 0; j < WJ; ++j) wb[j] = next_b[j];
-        }
+        if (more) read_scales(st + 1, next_a, next_b);
+        static_for<BARRIER, SLOTS>([&](auto e) { slot(st, e, next, load); });
+        if (more) take_scales(st + 1);
     };
     using Yes = std::true_type;
     using No = std::false_type;
@@ -465,7 +472,8 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
         else wait_loads<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        read_scales(0, wa, wb);
+        read_scales(0, next_a, next_b);
+        take_scales(0);
 #pragma unroll
         for (int j = 0; j < WJ; ++j) b[0][j] = read(0, 0, BM + rb + 32 * j);
 #pragma unroll
@@ -602,7 +610,7 @@ template <typename T, bool EXACT> __global__ __launch_bounds__(64 * FEW_WAVES) v
             vb[u] = there ? *reinterpret_cast<const i32x8 *>(b + kc * 128LL) : none;
             xb[u] = there ? sb[(long long)(kc >> 2) * P.N * 4 + (kc & 3)] : 0u;
             va[u] = there ? *reinterpret_cast<const i32x8 *>(a + kc * 128LL) : none;
-            xa[u] = there ? sa[(long long)(kc >> 2) * P.M * 4 + (kc & 3)] : 0u;
+            xa[u] = there ? sa[(long long)(kc >> 2) * P.rows_a * 4 + (kc & 3)] : 0u;
         }
 #pragma unroll
         for (int u = 0; u < FEW_BLOCKS; ++u) {
@@ -744,6 +752,22 @@ static BlockProductPlan product_plan(int M, int N, int K, bool exact)
     return best;
 }
 
+// Large tiles go out 256 at a time: rows of tiles that do not fill a last round are better done by smaller tiles that do, in a launch of their own
+// (75,600 x 5120 x 5120 is 23 rounds and 32 tiles).  How many rows stay with the large ones, and which take the rest.
+struct BlockProductRest {
+    int large, size;
+};
+
+static BlockProductRest product_rest(int M, int N, int stages, bool exact)
+{
+    const int tiles_n = cdiv(N, 256), tiles = cdiv(M, 256) * tiles_n, rounds = tiles / 256, keep = rounds * 256 / tiles_n * 256;
+    if (tiles % 256 == 0 || keep < 256 || keep >= M) return {M, 0};
+    const double whole = tile_time<Large>(M, N, stages, 1, exact), most = tile_time<Large>(keep, N, stages, 1, exact) + 2.0;
+    const double small = tile_time<Small>(M - keep, N, stages, 1, exact), medium = tile_time<Medium>(M - keep, N, stages, 1, exact);
+    if (most + (small < medium ? small : medium) > 0.99 * whole) return {M, 0};
+    return {keep, small < medium ? 0 : 1};
+}
+
 size_t fp8_blocks_matmul_ws_bytes(int M, int N, int K)
 {
     if (few(M, N, K)) return 256;
@@ -787,10 +811,23 @@ int fp8_blocks_matmul_launch(const void *A, const void *SA, const void *B, const
                              int out_dtype, void *C, int64_t ldc, void *ws, hipStream_t st)
 {
     BlockProductArgs P = {static_cast<const uint8_t *>(A), static_cast<const uint8_t *>(B), static_cast<const uint8_t *>(SA),
-                          static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), bias, C, ldc, 0, 1, cdiv(K, 128)};
+                          static_cast<const uint8_t *>(SB), M, N, cdiv(K, 128), M, bias, C, ldc, 0, 1, cdiv(K, 128)};
     if (few(M, N, K)) return product_few(P, out_dtype, st);
-    const BlockProductPlan p = product_plan(M, N, K, out_dtype == SVG2_F32);
-    if (p.split == 1) return out_dtype == SVG2_BF16 ? product_sized<bf16_t, false>(p.size, P, st) : product_sized<float, true>(p.size, P, st);
+    const bool exact = out_dtype == SVG2_F32;
+    const BlockProductPlan p = product_plan(M, N, K, exact);
+    if (p.split == 1) {
+        auto rows = [&](int from, int count, int size) {
+            BlockProductArgs part = P;
+            part.M = count;
+            part.A += (size_t)from * P.nk * 128;
+            part.SA += 4 * (size_t)from;
+            part.C = static_cast<char *>(C) + (size_t)from * ldc * (exact ? 4 : 2);
+            return exact ? product_sized<float, true>(size, part, st) : product_sized<bf16_t, false>(size, part, st);
+        };
+        const BlockProductRest r = p.size == 2 ? product_rest(M, N, P.nk, exact) : BlockProductRest{M, 0};
+        SVG2_TRY(rows(0, r.large, p.size));
+        return r.large == M ? SVG2_OK : rows(r.large, M - r.large, r.size);
+    }
     P.split = p.split;
     P.per = p.per;
     BlockProductArgs parts = P;
