@@ -34,12 +34,13 @@ __device__ __forceinline__ unsigned mag(float x) { return __float_as_uint(x) & 0
 // Eight neighbouring columns as they are in memory.
 template <typename T> struct Raw { u32x4 q[sizeof(T) / 2]; };
 
-template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *from)
+// STREAM, here and below: past the caches
+template <typename T, bool STREAM = false> __device__ __forceinline__ Raw<T> load_raw(const T *from)
 {
     const u32x4_any *p = reinterpret_cast<const u32x4_any *>(from);
     Raw<T> r;
 #pragma unroll
-    for (unsigned i = 0; i < sizeof(T) / 2; ++i) r.q[i] = p[i];
+    for (unsigned i = 0; i < sizeof(T) / 2; ++i) r.q[i] = STREAM ? __builtin_nontemporal_load(p + i) : p[i];
     return r;
 }
 
@@ -83,13 +84,17 @@ template <typename T> __device__ __forceinline__ void decode(const Raw<T> &r, fl
 // eight neighbouring elements from and to any address
 template <typename T> __device__ __forceinline__ void load8(const T *from, float *v) { decode<T>(load_raw<T>(from), v); }
 
-template <typename T> __device__ __forceinline__ void store8(T *to, const float *v)
+template <typename T, bool STREAM = false> __device__ __forceinline__ void store8(T *to, const float *v)
 {
     u32x4_any *p = reinterpret_cast<u32x4_any *>(to);
+    auto store = [](const u32x4 &x, u32x4_any *at) {
+        if (STREAM) __builtin_nontemporal_store(x, at);
+        else *at = x;
+    };
     if constexpr (sizeof(T) == 4) {
-        p[0] = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-        p[1] = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
-    } else *p = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        store(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, p);
+        store(u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])}, p + 1);
+    } else store(u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])}, p);
 }
 
 // bits of the largest magnitude of eight values

@@ -38,15 +38,15 @@ template <typename T> __device__ __forceinline__ const T *element(const BlockQua
 }
 
 // eight neighbouring columns: one load where they are all there and in one group, whatever their address; zeros behind K
-template <typename T> __device__ __forceinline__ Raw<T> load_columns(const BlockQuantArgs &A, long long m, int k, int K)
+template <typename T, bool STREAM> __device__ __forceinline__ Raw<T> load_columns(const BlockQuantArgs &A, long long m, int k, int K)
 {
-    if (k + 8 <= K && (A.G == 1 || k % A.Kg + 8 <= A.Kg)) return load_raw<T>(element<T>(A, m, k));
+    if (k + 8 <= K && (A.G == 1 || k % A.Kg + 8 <= A.Kg)) return load_raw<T, STREAM>(element<T>(A, m, k));
     return raw_of<T>([&](int i) { return k + i < K ? *element<T>(A, m, k + i) : (T)0; });
 }
 
 // rows: grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block of 128 columns, whose eight values each stay in
 // registers; the block's maximum goes round the 16 lanes without LDS.
-template <typename T> __global__ __launch_bounds__(256) void fp8_blocks_rows_kernel(const BlockQuantArgs A)
+template <typename T, bool STREAM> __global__ __launch_bounds__(256) void fp8_blocks_rows_kernel(const BlockQuantArgs A)
 {
     const int lane16 = threadIdx.x & 15, K = A.G * A.Kg, nk = (K + 127) / 128, all = (nk + 3) & ~3;
     const long long m = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
@@ -55,7 +55,7 @@ template <typename T> __global__ __launch_bounds__(256) void fp8_blocks_rows_ker
         unsigned byte = 0;
         if (kc < nk) {
             float v[8], inv;
-            decode<T>(load_columns<T>(A, m, kc * 128 + lane16 * 8, K), v);
+            decode<T>(load_columns<T, STREAM>(A, m, kc * 128 + lane16 * 8, K), v);
             byte = e4m3_block_scale(max16(largest8(v)), inv);
             *reinterpret_cast<uint2 *>(A.codes + m * (nk * 128LL) + kc * 128 + lane16 * 8) = e4m3_codes8(v, inv);
         }
@@ -67,7 +67,7 @@ template <typename T> __global__ __launch_bounds__(256) void fp8_blocks_rows_ker
 // grid: workgroups stride over the tiles, those of one row of tiles neighbours; block 256: a thread holds 8 rows x 8 columns, as they are in
 // memory.  The maximum of a row goes round 16 lanes, that of a column over the wavefront's four groups of rows and, through LDS, the four
 // wavefronts.  The codes of eight rows of a column are eight bytes: they go through LDS, column by column, and leave as lines of 128 bytes.
-template <typename T, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bounds__(256) void fp8_blocks_tile_kernel(const BlockQuantArgs A)
+template <typename T, bool STREAM, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bounds__(256) void fp8_blocks_tile_kernel(const BlockQuantArgs A)
 {
     __shared__ unsigned s_top[4][128];
     __shared__ __attribute__((aligned(16))) uint8_t s_codes[COLS ? 128 * 144 : 16];     // a column's 128 codes and 16 bytes: stores of 8 bytes spread over the banks
@@ -79,7 +79,7 @@ template <typename T, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bou
         Raw<T> x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (m0 + i < A.M) x[i] = load_columns<T>(A, m0 + i, k0, K);
+            if (m0 + i < A.M) x[i] = load_columns<T, STREAM>(A, m0 + i, k0, K);
             else x[i] = raw_of<T>([](int) { return (T)0; });
         }
         auto row_result = [&](int i, const float *v, unsigned top) {
@@ -174,7 +174,7 @@ __device__ __forceinline__ void scale_factors(unsigned byte, float &a, float &b)
 }
 
 // grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block, eight codes each
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void fp8_blocks_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                 int M, int K, T *__restrict__ X, long long ldx)
 {
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) void fp8_blocks_values_kernel(const uint8_t *_
         for (int i = 0; i < 8; ++i) v[i] = p[i >> 1][i & 1] * a * b;
         const int k = kc * 128 + lane16 * 8;
         T *x = X + m * ldx + k;
-        if (k + 8 <= K) store8<T>(x, v);
+        if (k + 8 <= K) store8<T, STREAM>(x, v);
         else
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -641,10 +641,20 @@ static int slices(long long blocks, int steps)
     return (int)(want < 1 ? 1 : want > steps ? steps : want);
 }
 
-template <typename F> static int with_type(int dtype, F f)
+// Values of 64 MB and more whose rows are whole lines are written past the caches, which the codes, half their size, then keep: 16,384 x 5120
+// bf16 quantised both ways and both back 197 -> 167 us, 15,360 x 5120 in squares 188 -> 133.  Smaller ones are better left there for
+// whoever reads them next; rows that share lines too.  An X of 64 to 256 MB, the size of the last cache, is read past them as well: both ways 73 ->
+// 67 us; a larger one is not there to begin with (75,600 x 5120 both ways 301 us, past the caches 308).
+static bool streamed(const void *X, double elements, int64_t ld, int es)
 {
-    if (dtype == SVG2_BF16) f((bf16_t *)0);
-    else f((float *)0);
+    return elements * es >= 67108864.0 && (reinterpret_cast<uintptr_t>(X) & 127) == 0 && ld * es % 128 == 0;
+}
+
+// f(type, STREAM) with both known at compile time
+template <typename F> static int with_types(int dtype, bool stream, F f)
+{
+    if (dtype == SVG2_BF16) stream ? f((bf16_t *)0, std::true_type()) : f((bf16_t *)0, std::false_type());
+    else stream ? f((float *)0, std::true_type()) : f((float *)0, std::false_type());
     SVG2_HIP_CHECK(hipGetLastError());
     return SVG2_OK;
 }
@@ -654,31 +664,33 @@ int fp8_blocks_quant_launch(const void *X, int dtype, int M, int G, int Kg, int6
 {
     const BlockQuantArgs A = {X, sm, sg, M, G, Kg, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales),
                               static_cast<uint8_t *>(codes_t), static_cast<uint8_t *>(scales_t)};
-    const int K = G * Kg;
-    return with_type(dtype, [&](auto *tp) {
+    const int K = G * Kg, es = dtype == SVG2_BF16 ? 2 : 4;
+    const bool lines = G == 1 || (sg * es % 128 == 0 && Kg * es % 128 == 0);
+    return with_types(dtype, lines && streamed(X, (double)M * K, sm, es) && (double)M * K * es < 268435456.0, [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
+        constexpr bool S = decltype(stream)::value;
         if (!codes_t && !square) {
             const int bx = cdiv(M, 16);
-            fp8_blocks_rows_kernel<T><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(A);
+            fp8_blocks_rows_kernel<T, S><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(A);
             return;
         }
         const long long all = (long long)cdiv(M, 128) * cdiv(K, 128);
         const int tiles = (int)(all < 1 << 20 ? all : 1 << 20);
         if (square) {
-            if (!codes_t) fp8_blocks_tile_kernel<T, true, false, true><<<tiles, 256, 0, st>>>(A);
-            else if (!codes) fp8_blocks_tile_kernel<T, false, true, true><<<tiles, 256, 0, st>>>(A);
-            else fp8_blocks_tile_kernel<T, true, true, true><<<tiles, 256, 0, st>>>(A);
-        } else if (codes) fp8_blocks_tile_kernel<T, true, true, false><<<tiles, 256, 0, st>>>(A);
-        else fp8_blocks_tile_kernel<T, false, true, false><<<tiles, 256, 0, st>>>(A);
+            if (!codes_t) fp8_blocks_tile_kernel<T, S, true, false, true><<<tiles, 256, 0, st>>>(A);
+            else if (!codes) fp8_blocks_tile_kernel<T, S, false, true, true><<<tiles, 256, 0, st>>>(A);
+            else fp8_blocks_tile_kernel<T, S, true, true, true><<<tiles, 256, 0, st>>>(A);
+        } else if (codes) fp8_blocks_tile_kernel<T, S, true, true, false><<<tiles, 256, 0, st>>>(A);
+        else fp8_blocks_tile_kernel<T, S, false, true, false><<<tiles, 256, 0, st>>>(A);
     });
 }
 
 int fp8_blocks_values_launch(const void *codes, const void *scales, int M, int K, int dtype, void *X, int64_t ldx, hipStream_t st)
 {
-    return with_type(dtype, [&](auto *tp) {
+    return with_types(dtype, streamed(X, (double)M * K, ldx, dtype == SVG2_BF16 ? 2 : 4), [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
         const int bx = cdiv(M, 16);
-        fp8_blocks_values_kernel<T><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(
+        fp8_blocks_values_kernel<T, decltype(stream)::value><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(
             static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), M, K, static_cast<T *>(X), ldx);
     });
 }
