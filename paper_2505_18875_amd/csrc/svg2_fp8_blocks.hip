@@ -740,44 +740,40 @@ template <typename L> static double tile_time(int M, int N, int stages, int spli
 // most.  Adding them up is a second launch and the parts' way out and back: 2.5 us, and 0.2 us for each MB of a part.  Measured, one part / as
 // chosen, fp32 results (bf16):
 //   1536 x 1536 x 16,384  102 / 82 us (64 / 57)     1536 x 1536 x 75,600  470 / 291 us (297 / 186)     512 x 512 x 16,384  58 / 21 us (57 / 16)
+// Large tiles go out 256 at a time: the last rows of C, whose tiles would not fill a last round, may be a launch of smaller ones that do
+// (75,600 x 5120 x 5120 is 23 rounds and 32 tiles: 1600 us, the 336 last rows by themselves 1560).
 struct BlockProductPlan {
     int size, split, per;           // size: 0 small, 1 medium, 2 large
+    int rest, rest_size;            // of the rows of C, the last ones that other tiles take
 };
 
 static BlockProductPlan product_plan(int M, int N, int K, bool exact)
 {
     const int stages = cdiv(K, 128);
-    BlockProductPlan best = {0, 1, stages};
+    BlockProductPlan best = {0, 1, stages, 0, 0};
     double least = 1e300;
+    auto offer = [&](double time, const BlockProductPlan &plan) {
+        if (time < least * 0.999) {
+            least = time;
+            best = plan;
+        }
+    };
     for (int split = 1; split <= 16 && (split == 1 || stages >= 8 * split); ++split) {
         const int per = split == 1 ? stages : cdiv(cdiv(stages, split), 4) * 4;
         if (split > 1 && (cdiv(stages, per) != split || (double)split * M * N > (1 << 28))) continue;
         const double join = split == 1 ? 0.0 : 2.5 + 0.2 * split * (double)M * N * sizeof(float) * 1e-6;
-        const double t[3] = {tile_time<Small>(M, N, stages, split, exact), tile_time<Medium>(M, N, stages, split, exact),
-                             tile_time<Large>(M, N, stages, split, exact)};
-        for (int size = 0; size < 3; ++size)
-            if (t[size] + join < least * (size > best.size && split == best.split ? 1.0 : 0.999)) {
-                least = t[size] + join;
-                best = {size, split, per};
-            }
+        offer(join + tile_time<Small>(M, N, stages, split, exact), {0, split, per, 0, 0});
+        offer(join + tile_time<Medium>(M, N, stages, split, exact), {1, split, per, 0, 0});
+        offer(join + tile_time<Large>(M, N, stages, split, exact), {2, split, per, 0, 0});
+    }
+    const long long tiles_n = cdiv(N, 256), keep = cdiv(M, 256) * tiles_n / 256 * 256 / tiles_n * 256;      // rows that fill whole rounds
+    if (keep >= 256 && keep < M) {
+        const int rest = M - (int)keep;
+        const double large = tile_time<Large>((int)keep, N, stages, 1, exact) + 2.0;        // and a launch
+        offer(large + tile_time<Small>(rest, N, stages, 1, exact), {2, 1, stages, rest, 0});
+        offer(large + tile_time<Medium>(rest, N, stages, 1, exact), {2, 1, stages, rest, 1});
     }
     return best;
-}
-
-// Large tiles go out 256 at a time: rows of tiles that do not fill a last round are better done by smaller tiles that do, in a launch of their own
-// (75,600 x 5120 x 5120 is 23 rounds and 32 tiles).  How many rows stay with the large ones, and which take the rest.
-struct BlockProductRest {
-    int large, size;
-};
-
-static BlockProductRest product_rest(int M, int N, int stages, bool exact)
-{
-    const int tiles_n = cdiv(N, 256), tiles = cdiv(M, 256) * tiles_n, rounds = tiles / 256, keep = rounds * 256 / tiles_n * 256;
-    if (tiles % 256 == 0 || keep < 256 || keep >= M) return {M, 0};
-    const double whole = tile_time<Large>(M, N, stages, 1, exact), most = tile_time<Large>(keep, N, stages, 1, exact) + 2.0;
-    const double small = tile_time<Small>(M - keep, N, stages, 1, exact), medium = tile_time<Medium>(M - keep, N, stages, 1, exact);
-    if (most + (small < medium ? small : medium) > 0.99 * whole) return {M, 0};
-    return {keep, small < medium ? 0 : 1};
 }
 
 size_t fp8_blocks_matmul_ws_bytes(int M, int N, int K)
@@ -836,9 +832,8 @@ int fp8_blocks_matmul_launch(const void *A, const void *SA, const void *B, const
             part.C = static_cast<char *>(C) + (size_t)from * ldc * (exact ? 4 : 2);
             return exact ? product_sized<float, true>(size, part, st) : product_sized<bf16_t, false>(size, part, st);
         };
-        const BlockProductRest r = p.size == 2 ? product_rest(M, N, P.nk, exact) : BlockProductRest{M, 0};
-        SVG2_TRY(rows(0, r.large, p.size));
-        return r.large == M ? SVG2_OK : rows(r.large, M - r.large, r.size);
+        SVG2_TRY(rows(0, M - p.rest, p.size));
+        return p.rest ? rows(M - p.rest, p.rest, p.rest_size) : SVG2_OK;
     }
     P.split = p.split;
     P.per = p.per;
