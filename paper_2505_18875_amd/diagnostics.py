@@ -13,10 +13,11 @@ figures; every number comes from the library's kernels through the C ABI):
              0.99: per-step layer time, density and attention recall      (Section 4.3, centroid cache)
   block      the attention block of a video transformer around the layer, from hidden states to hidden states:
              projection to Q, K, V, RMS norm + rotary positions + head order, svg2_forward, projection of O; with
-             the projections on MXFP4 operands and in bf16, time by stage, and output error of both against fp32
-             projections                                               (Section 5.1, "Models")
+             the projections on MXFP4 operands, on FP8 operands (a scale for each block of 128) and in bf16, time by
+             stage, and output error of each against fp32 projections; --norm: a modulated layer norm in front
+                                                                       (Section 5.1, "Models")
 
-Usage: python -m paper_2505_18875_amd.diagnostics {recall,clusters,seeding,fp8,sequence,block} [--workload wan_like] [--heads 8]
+Usage: python -m paper_2505_18875_amd.diagnostics {recall,clusters,seeding,fp8,sequence,block} [--workload wan_like] [--heads 8] [--norm]
 """
 from __future__ import annotations
 
@@ -299,13 +300,29 @@ def block(args):
     side = 2 * (d // 6)                         # height and width get a third of a head each, rounded down to pairs
     pairs = ((d - 2 * side) // 2, side // 2, side // 2)
     pos, freq = svg2.svg2_grid_positions(w.grid), svg2.svg2_rope_frequencies(pairs)
-    q_qkv, q_out = svg2.svg2_quantize_mxfp4(w_qkv), svg2.svg2_quantize_mxfp4(w_out)
+    quantised = {"mxfp4": [svg2.svg2_quantize_mxfp4(t) for t in (w_qkv, w_out)],
+                 "fp8": [svg2.svg2_quantize_fp8_blocks(t, square=True) for t in (w_qkv, w_out)]}
+    # the norm in front of the projection, modulated by a timestep
+    scale, shift = [0.3 * torch.randn((1, D), generator=g, device="cuda") for _ in range(2)]
     cent = {}
 
-    def project(kind, x, weight, quantised, bias):
-        """x [N,D] or O in head order [H,N,d] -> [N, rows of weight]"""
+    def norm(kind):
+        """What the projection takes: the hidden states, or their modulated norm, as an FP8 operand for the fp8 projection."""
+        if not args.norm:
+            return hidden
+        call = svg2.svg2_layer_norm_fp8 if kind == "fp8" else svg2.svg2_layer_norm
+        y = call(hidden[None], scale, shift, one_plus=True)
+        return y if kind == "fp8" else y[0]
+
+    def project(kind, x, which, bias):
+        """x [N,D], an FP8 operand, or O in head order [H,N,d] -> [N, rows of the weight]"""
+        weight = (w_qkv, w_out)[which]
+        if kind == "fp8":
+            a = x if isinstance(x, tuple) else svg2.svg2_quantize_fp8_blocks(x.transpose(0, 1) if x.dim() == 3 else x)
+            return svg2.svg2_matmul_fp8_blocks(*a, *quantised[kind][which], bias=bias)
         if kind == "mxfp4":
-            return svg2.svg2_matmul_mxfp4(*svg2.svg2_quantize_mxfp4(x.transpose(0, 1) if x.dim() == 3 else x), *quantised, bias=bias)
+            return svg2.svg2_matmul_mxfp4(*svg2.svg2_quantize_mxfp4(x.transpose(0, 1) if x.dim() == 3 else x), *quantised[kind][which],
+                                          bias=bias)
         x = x.transpose(0, 1).reshape(N, D) if x.dim() == 3 else x
         if kind == "fp32":
             return (x.float() @ weight.float().t() + bias).to(bf16)
@@ -327,17 +344,20 @@ def block(args):
 
     ref = {}
     print("Attention block of %d tokens and %d channels (%d heads of %d): %s" % (N, D, H, d, w.name))
-    print("\n| projections | to Q, K, V ms | norm + rotary + head order ms | svg2_forward ms | of O ms | block ms | "
-          "rel. rms err of Q, K, V | of O | of the block |\n|---|---|---|---|---|---|---|---|---|")
-    for kind in ("fp32", "bf16", "mxfp4"):
-        t1, qkv = _timed(lambda: project(kind, hidden, w_qkv, q_qkv, b_qkv))
+    print("\n| projections%s | to Q, K, V ms | norm + rotary + head order ms | svg2_forward ms | of O ms | block ms | "
+          "rel. rms err of Q, K, V | of O | of the block |\n|---|---|---|---|---|---|---|---|---|%s" %
+          ((" | layer norm ms", "---|") if args.norm else ("", "")))
+    for kind in ("fp32", "bf16", "fp8", "mxfp4"):
+        t0, x = _timed(lambda: norm(kind))
+        t1, qkv = _timed(lambda: project(kind, x, 0, b_qkv))
         t2, (q, k, v) = _timed(lambda: rope(qkv))
         t3, O = _timed(lambda: layer(q, k, v))
-        t4, out = _timed(lambda: project(kind, O, w_out, q_out, b_out))
+        t4, out = _timed(lambda: project(kind, O, 1, b_out))
         if kind == "fp32":
             ref = dict(qkv=qkv, O=O, out=out)
-        print("| %s | %.3f | %.3f | %.3f | %.3f | %.3f | %.4f | %.4f | %.4f |" %
-              (kind, t1, t2, t3, t4, t1 + t2 + t3 + t4, rel(qkv, ref["qkv"]), rel(O, ref["O"]), rel(out, ref["out"])))
+        t0 = t0 if args.norm else 0.0
+        print("| %s%s | %.3f | %.3f | %.3f | %.3f | %.3f | %.4f | %.4f | %.4f |" %
+              (kind, " | %.3f" % t0 if args.norm else "", t1, t2, t3, t4, t0 + t1 + t2 + t3 + t4, rel(qkv, ref["qkv"]), rel(O, ref["O"]), rel(out, ref["out"])))
 
 
 def main():
@@ -345,6 +365,7 @@ def main():
     ap.add_argument("what", choices=("recall", "clusters", "seeding", "fp8", "sequence", "block"))
     ap.add_argument("--workload", default="wan_like", choices=sorted(wl.WORKLOADS))
     ap.add_argument("--heads", type=int, default=8)
+    ap.add_argument("--norm", action="store_true", help="block: a modulated layer norm in front of the first projection")
     args = ap.parse_args()
     import torch
     import paper_2505_18875_amd as svg2
