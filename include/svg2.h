@@ -456,9 +456,10 @@ int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const 
  * storage, scales and rounding, from the fp32 values); args->y, y_stride and y_dtype are ignored.
  * svg2_layer_norm_backward: with dY [B,N,D] y_dtype (strides y_stride, of any sign: it is only read) the gradients
  *   dX [B,N,D] dtype with strides dx_stride (positive as y's; may be dY with the same strides and type, no other overlap),
- *   dW fp32 of weight, dB fp32 of the offset, dense: [D], or [B,D] where weight or bias has a stride (both have or none has, where both are
- *                given); NULL: not wanted; weight NULL: no dW.
- *   args as in the forward call; args->y is ignored, bias is not read.
+ *   dW, dB       fp32 of weight and bias, dense: [D], or [B,D] where they have a stride (both or none); NULL: not wanted, and where weight or
+ *                bias is NULL
+ *   args as in the forward call; args->y is ignored, bias is not read.  Where svg2_layer_norm_backward_workspace_size returns 256 no workspace is
+ *   used and ws may be NULL.
  * Sums over rows are formed in a fixed order, fp32 within a share of the rows and 64 bits over the shares (320 to 5120 of them by the length of a row,
  * fewer where there are few rows: two rows at least each): results are the same from run to run.
  * ------------------------------------------------------------------------- */

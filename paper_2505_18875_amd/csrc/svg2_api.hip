@@ -821,7 +821,7 @@ int svg2_layer_norm_backward(const svg2_layer_norm_args *a, const void *dY, void
     SVG2_REQUIRE(aligned_to(a->x, a->dtype) && aligned_to(dY, a->y_dtype) && aligned_to(dX, a->dtype), SVG2_INVALID_ARG,
                  "x, dY or dX is not aligned to its elements");
     SVG2_REQUIRE(multiple_of(dW, 4) && multiple_of(dB, 4), SVG2_INVALID_ARG, "dW or dB is not aligned to its elements");
-    SVG2_REQUIRE(!dW || a->weight, SVG2_INVALID_ARG, "dW is given, weight is null");
+    SVG2_REQUIRE((!dW || a->weight) && (!dB || a->bias), SVG2_INVALID_ARG, "dW is given, weight is null; or dB, bias");
     SVG2_REQUIRE(a->B == 1 || !a->weight || !a->bias || (a->weight_stride == 0) == (a->bias_stride == 0), SVG2_INVALID_ARG,
                  "weight_stride = %lld and bias_stride = %lld: gradients need both shared or both of a group", (long long)a->weight_stride,
                  (long long)a->bias_stride);

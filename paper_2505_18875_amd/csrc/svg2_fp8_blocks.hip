@@ -45,7 +45,7 @@ template <typename T, bool STREAM> __device__ __forceinline__ Raw<T> load_column
 }
 
 // rows: grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block of 128 columns, whose eight values each stay in
-// registers; the block's maximum goes round the 16 lanes without LDS.
+// registers; the block's maximum goes round the 16 lanes without LDS.  Bound by HBM: 16,384 x 5120 bf16 46 us, 5.4 TB/s, 75,600 x 5120 235, 4.9.
 template <typename T, bool STREAM> __global__ __launch_bounds__(256) void fp8_blocks_rows_kernel(const BlockQuantArgs A)
 {
     const int lane16 = threadIdx.x & 15, K = A.G * A.Kg, nk = (K + 127) / 128, all = (nk + 3) & ~3;
@@ -67,6 +67,8 @@ template <typename T, bool STREAM> __global__ __launch_bounds__(256) void fp8_bl
 // grid: workgroups stride over the tiles, those of one row of tiles neighbours; block 256: a thread holds 8 rows x 8 columns, as they are in
 // memory.  The maximum of a row goes round 16 lanes, that of a column over the wavefront's four groups of rows and, through LDS, the four
 // wavefronts.  The codes of eight rows of a column are eight bytes: they go through LDS, column by column, and leave as lines of 128 bytes.
+// Bound by HBM: 16,384 x 5120 bf16 both ways 67 us, 5.0 TB/s (rows and transposed in calls of their own 94), transposed 48, in squares both ways 61;
+// small ones by their few workgroups (16,384 x 1536 both ways 25 us, 1536 of them), rows that share lines by those (75,599 x 5119 both ways 417).
 template <typename T, bool STREAM, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bounds__(256) void fp8_blocks_tile_kernel(const BlockQuantArgs A)
 {
     __shared__ unsigned s_top[4][128];
@@ -173,7 +175,8 @@ __device__ __forceinline__ void scale_factors(unsigned byte, float &a, float &b)
     b = __uint_as_float((byte - half + 63) << 23);                                             // 2^(byte - half - 64)
 }
 
-// grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block, eight codes each
+// grid (ceil(M / 16), slices of the columns), block 256: 16 lanes a block, eight codes each.  Bound by the writes: 16,384 x 5120 bf16 39 us, the codes
+// from the last cache; 75,600 x 5120 237, 4.9 TB/s
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void fp8_blocks_values_kernel(const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                                 int M, int K, T *__restrict__ X, long long ldx)
@@ -274,6 +277,13 @@ __device__ __forceinline__ Converted convert(const i32x8 &f, unsigned byte)
 // Where there are few tiles and many stages, a part of the stages is a tile of its own (split), and fp8_blocks_join_kernel adds them up.
 // In LDS row r has 128 bytes, its 16-byte piece c at c ^ spread(r): eight neighbouring rows then take every bank once.
 // Rows behind the last are read as the last and not stored.
+// What bounds it is the power: a loop of nothing but this instruction on operands in registers does 3.7 PFLOP/s (operands of zeros 5.0), its clock
+// at 1.8 GHz of 2.4.  8192 x 8192 x 8192, 400 us, 2.75 PFLOP/s: the matrix pipes are busy 70 % of the cycles, at 1.8 GHz too, since operands on
+// their way through LDS take power as well; 75,600 x 5120 x 5120, 1560 us, 2.54 PFLOP/s, 69 %: a tile's results take some 5 us beyond its 40
+// stages.  fp32 results: 16,384 x 5120 x 5120 600 us, 1.43 PFLOP/s, busy 77 % at 1.69 GHz.
+// Four stages in LDS for small tiles, three on their way, change nothing (1021 x 1537 x 1000 6.9 us either way).
+// Steps, 8192 x 8192 x 8192: tiles through LDS, two stages 415; loads behind a product each 423 -- the compiler had moved every product of a stage
+// behind its barrier, for want of a straight line: the branch around the scales of every fourth stage; loaded every stage, with no branch 400.
 template <int WM_, int WN_, int WI_, int WJ_> struct Tile {
     static constexpr int WM = WM_, WN = WN_, WI = WI_, WJ = WJ_, WAVES = WM * WN, BM = 32 * WI * WM, BN = 32 * WJ * WN;
     static constexpr int STAGE = (BM + BN) * 128;
@@ -460,6 +470,14 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
     if (k >= mine) return;
     set_tile(k);
     load_first(copy);
+    // the second stage of the first tile comes with the first; later tiles' second stages have to wait for the results that leave through their place
+    auto load_second = [&]() {
+        if (stages > 1)
+#pragma unroll
+            for (int g = 0; g < LOADS; ++g) load_piece(1, g);
+    };
+    load_second();
+    bool second = true;
     for (; k < mine; k += slots, copy ^= 1) {
 #pragma unroll
         for (int i = 0; i < WI; ++i)
@@ -469,6 +487,7 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
         // loads and stores come back in the order in which they were issued: the last tile's stores may still be on their way
         if (after) wait_loads<(STORES < 63 ? STORES : 63)>();
+        else if (second && stages > 1) wait_loads<LOADS>();
         else wait_loads<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -478,9 +497,8 @@ void fp8_blocks_product_kernel(const BlockProductArgs P)
         for (int j = 0; j < WJ; ++j) b[0][j] = read(0, 0, BM + rb + 32 * j);
 #pragma unroll
         for (int e = 0; e < AHEAD; ++e) a[e % RING] = read(0, e / WI, ra + 32 * (e % WI));
-        if (stages > 1)
-#pragma unroll
-            for (int g = 0; g < LOADS; ++g) load_piece(1, g);
+        if (!second) load_second();
+        second = false;
         int st = 0;
         for (; st + 2 < stages; ++st) stage(st, Yes(), Yes());
         if (st + 1 < stages) stage(st++, Yes(), No());

@@ -5,8 +5,11 @@
 // backward, with g = dy s:
 //   dx = r (g - mean(g) - n mean(g n)),   dw = sum of dy n,   db = sum of dy   over the rows that share them
 //
-// Every element is read once and written once, some ten operations each: HBM bounds it.  A row stays in registers between its sums and its
-// result, the mean is taken off before squares are summed.
+// Every element is read once and written once, some ten operations each: HBM bounds it, where the sums keep out of the way.  A row stays in
+// registers between its sums and its result; the mean is taken off before squares are summed.
+// 75,600 x 5120 bf16 (1.55 GB in and out) 288 us, 5.4 TB/s, the rate of a large copy; the same as an FP8 operand (1.16 GB) 303 us: there the
+// instructions bound it, some 17 an element of which 6 are loads' conversions, sums and reductions over a row that one round of barriers takes.
+// Gradients of 16,384 x 5120 bf16 (0.50 GB) 110 us and 6 to add up the weights', 4.6 TB/s, of 75,600 x 5120 485 us, 4.8 TB/s.
 #include <type_traits>
 
 #include "svg2_fp8_blocks.h"
@@ -132,9 +135,9 @@ template <int CH> __device__ __forceinline__ float deviations(float (&v)[CH][8],
     return squares;
 }
 
-// LANES threads a row, CH steps of 8 columns a thread: 16, 32 or 64 lanes of a block of 256, or (0) a workgroup of up to 1024.  Each row's place (slot) goes
-// through neighbouring rows and keeps their factors and offsets in registers: from the caches they would be twice to four times the
-// bytes of the rows themselves.  The next row is on its way while this one is used.
+// LANES threads a row, CH steps of 8 columns a thread: 16, 32 or 64 lanes of a block of 256, or (0) a workgroup of up to 512.  A place, the threads
+// of a row, goes through neighbouring rows and keeps their factors and offsets in registers: from the caches, they are twice to four times the
+// bytes of the rows themselves (75,600 x 5120 bf16 that way 474 us).  The next row is on its way while this one is used.
 template <typename TX, typename TY, bool FP8, int LANES, int CH>
 __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX) == 2 ? 5 : 4) : 2) void layer_norm_kernel(const NormArgs A)
 {
@@ -371,7 +374,8 @@ template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bound
     }
 }
 
-// grid (ceil(D / 64), groups by strides, 2), block 1024: dw and db = sum of the P partial sums, 64 bits; 16 wavefronts take every 16th
+// grid (ceil(D / 32), groups by strides, 2), block 1024: dw and db = sum of the P partial sums, 64 bits, always in the same order; 32 threads a column
+// take every 32nd.  Bound by its launch and the partial sums (21 MB of 16,384 x 5120: 6 us).
 struct NormJoin {
     const float *parts[2];
     float *out[2];
@@ -380,22 +384,23 @@ struct NormJoin {
 
 __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const NormJoin J)
 {
-    __shared__ double s[16][64];
-    const int j = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + j, z = blockIdx.z;
+    __shared__ double s[32][32];
+    const int j = threadIdx.x & 31, share = threadIdx.x >> 5, i = blockIdx.x * 32 + j, z = blockIdx.z;
     if (!J.out[z]) return;
     for (int g = blockIdx.y; g < J.groups; g += gridDim.y) {
         double sum = 0.0;
         if (i < J.D) {
-            const float *p = J.parts[z] + ((size_t)g * J.P + wave) * J.D + i;
+            const float *p = J.parts[z] + ((size_t)g * J.P + share) * J.D + i;
 #pragma unroll 8
-            for (int k = wave; k < J.P; k += 16, p += 16 * (size_t)J.D) sum += *p;
+            for (int k = share; k < J.P; k += 32, p += 32 * (size_t)J.D) sum += *p;
         }
-        s[wave][j] = sum;
+        s[share][j] = sum;
         __syncthreads();
-        if (wave == 0 && i < J.D) {
-            for (int k = 1; k < 16; ++k) sum += s[k][j];
-            J.out[z][(size_t)g * J.D + i] = (float)sum;
+        for (int half = 16; half > 0; half >>= 1) {
+            if (share < half) s[share][j] += s[share + half][j];
+            __syncthreads();
         }
+        if (share == 0 && i < J.D) J.out[z][(size_t)g * J.D + i] = (float)s[0][j];
         __syncthreads();
     }
 }
@@ -496,7 +501,7 @@ static NormBwdPlan norm_bwd_plan(const svg2_layer_norm_args *a)
 size_t layer_norm_bwd_ws_bytes(const svg2_layer_norm_args *a)
 {
     const NormBwdPlan p = norm_bwd_plan(a);
-    return p.P == 1 ? 256 : 2 * align256((size_t)(p.own ? a->B : 1) * p.P * a->D * sizeof(float));
+    return p.P == 1 || (!a->weight && !a->bias) ? 256 : 2 * align256((size_t)(p.own ? a->B : 1) * p.P * a->D * sizeof(float));
 }
 
 int layer_norm_bwd_launch(const svg2_layer_norm_args *a, const void *dY, void *dX, const int64_t *dx_stride, float *dW, float *dB,
@@ -537,7 +542,7 @@ int layer_norm_bwd_launch(const svg2_layer_norm_args *a, const void *dY, void *d
     SVG2_HIP_CHECK(hipGetLastError());
     if (A.P > 1 && (dW || dB)) {
         const NormJoin J = {{A.dw, A.db}, {dW, dB}, A.D, A.P, groups};
-        layer_norm_join_kernel<<<dim3(cdiv(A.D, 64), groups < 1024 ? groups : 1024, 2), 1024, 0, st>>>(J);
+        layer_norm_join_kernel<<<dim3(cdiv(A.D, 32), groups < 1024 ? groups : 1024, 2), 1024, 0, st>>>(J);
         SVG2_HIP_CHECK(hipGetLastError());
     }
     return SVG2_OK;

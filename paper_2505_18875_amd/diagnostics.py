@@ -285,7 +285,7 @@ def block(args):
     w = wl.WORKLOADS[args.workload]
     if w.dtype != "bf16":
         raise SystemExit("the block runs in bf16")
-    H, d, N, bf16 = args.heads, w.d, w.N, torch.bfloat16
+    H, d, N, bf16, normed = args.heads, w.d, w.N, torch.bfloat16, getattr(args, "norm", False)
     D = H * d
     # hidden states with the workload's components: centre of the token's component plus unit noise; random weights, so that a
     # projected channel has the hidden states' variance
@@ -308,7 +308,7 @@ def block(args):
 
     def norm(kind):
         """What the projection takes: the hidden states, or their modulated norm, as an FP8 operand for the fp8 projection."""
-        if not args.norm:
+        if not normed:
             return hidden
         call = svg2.svg2_layer_norm_fp8 if kind == "fp8" else svg2.svg2_layer_norm
         y = call(hidden[None], scale, shift, one_plus=True)
@@ -346,7 +346,7 @@ def block(args):
     print("Attention block of %d tokens and %d channels (%d heads of %d): %s" % (N, D, H, d, w.name))
     print("\n| projections%s | to Q, K, V ms | norm + rotary + head order ms | svg2_forward ms | of O ms | block ms | "
           "rel. rms err of Q, K, V | of O | of the block |\n|---|---|---|---|---|---|---|---|---|%s" %
-          ((" | layer norm ms", "---|") if args.norm else ("", "")))
+          ((" | layer norm ms", "---|") if normed else ("", "")))
     for kind in ("fp32", "bf16", "fp8", "mxfp4"):
         t0, x = _timed(lambda: norm(kind))
         t1, qkv = _timed(lambda: project(kind, x, 0, b_qkv))
@@ -355,9 +355,9 @@ def block(args):
         t4, out = _timed(lambda: project(kind, O, 1, b_out))
         if kind == "fp32":
             ref = dict(qkv=qkv, O=O, out=out)
-        t0 = t0 if args.norm else 0.0
+        t0 = t0 if normed else 0.0
         print("| %s%s | %.3f | %.3f | %.3f | %.3f | %.3f | %.4f | %.4f | %.4f |" %
-              (kind, " | %.3f" % t0 if args.norm else "", t1, t2, t3, t4, t0 + t1 + t2 + t3 + t4, rel(qkv, ref["qkv"]), rel(O, ref["O"]), rel(out, ref["out"])))
+              (kind, " | %.3f" % t0 if normed else "", t1, t2, t3, t4, t0 + t1 + t2 + t3 + t4, rel(qkv, ref["qkv"]), rel(O, ref["O"]), rel(out, ref["out"])))
 
 
 def main():

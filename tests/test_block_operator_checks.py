@@ -85,7 +85,7 @@ def _backward(lib, a, dY=7 << 20, dX=8 << 20, stride=(800, 100), dW=9 << 20, dB=
     return lib.svg2_layer_norm_backward(ctypes.addressof(a), dY, dX, (ctypes.c_int64 * 2)(*stride) if stride else None, dW, dB, ws, ws_bytes, None)
 
 
-@pytest.mark.parametrize("change,code,word", REFUSED + [(dict(y_dtype=2), 2, b"dtype"), (dict(weight=None), 1, b"weight is null"),
+@pytest.mark.parametrize("change,code,word", REFUSED + [(dict(y_dtype=2), 2, b"dtype"), (dict(weight=None), 1, b"weight is null"), (dict(bias=None), 1, b"bias"),
                                                         (dict(weight_stride=0), 1, b"both"), (dict(bias_stride=0), 1, b"both")])
 def test_layer_norm_backward_refuses(lib, change, code, word):
     a = _args(**change)
@@ -113,6 +113,7 @@ def test_layer_norm_backward_workspace_sizes(lib):
         return lib.svg2_layer_norm_backward_workspace_size(ctypes.addressof(a))
     assert size(B=1, N=1) == 256 and size(B=1000, N=3) == 256 and size(D=0) == 256
     shared = dict(weight_stride=0, bias_stride=0)
+    assert size(B=1, N=75600, weight=None, bias=None) == 256    # nothing to add up
     assert size(B=1000, N=3, **shared) > 256                    # 3000 rows that share one sum
     assert 2 * 2 * 100 * 4 < size(B=1, N=75600, D=100) < 1 << 23
     assert size(B=2, N=1 << 24, D=16384) < 1 << 28              # stays bounded

@@ -180,3 +180,12 @@ def test_an_operand_times_itself_and_one_tensor_twice(svg2):
     assert_within(res.dweight, dw[0], dw_bound[0], F32)
     assert_within(res.dbias, db[0], db_bound[0], F32)
     assert HALF_STEP[BF16] == 2.0 ** -8 and np.isfinite(dx).all()
+
+
+@pytest.mark.parametrize("normed", [False, True])
+def test_the_block_diagnostic_has_them(svg2, capsys, normed):
+    from types import SimpleNamespace
+    from paper_2505_18875_amd import diagnostics
+    diagnostics.block(SimpleNamespace(workload="small", heads=2, norm=normed))
+    rows = [l for l in capsys.readouterr().out.splitlines() if l.startswith(("| fp32", "| bf16", "| fp8", "| mxfp4"))]
+    assert len(rows) == 4 and all("nan" not in r and r.count("|") == (11 if normed else 10) for r in rows)
