@@ -436,7 +436,7 @@ template <typename TX, typename TY, bool FP8> static void norm_forward(const Nor
     constexpr int each = FP8 ? 16 : 4;
     auto grid = [&](int per) {
         const long long one = (rows + per - 1) / per, some = (rows + each * per - 1) / (each * per);
-        return (int)(one < 2048 ? one : some < 2048 ? 2048 : some);
+        return (int)(one < 2048 ? one : some < 2048 ? 2048 : some < 1 << 22 ? some : 1 << 22);       // a launch has fewer than 2^32 threads
     };
     const int steps = cdiv(A.D, 512);
     if (A.D <= 128) layer_norm_kernel<TX, TY, FP8, 16, 1><<<grid(16), 256, 0, st>>>(A);
