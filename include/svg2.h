@@ -460,8 +460,8 @@ int svg2_matmul_mxfp4(const void *A, const void *A_scales, const void *B, const 
  *                bias is NULL
  *   args as in the forward call; args->y is ignored, bias is not read.  Where svg2_layer_norm_backward_workspace_size returns 256 no workspace is
  *   used and ws may be NULL.
- * Sums over rows are formed in a fixed order, fp32 within a share of the rows and 64 bits over the shares (320 to 5120 of them by the length of a row,
- * fewer where there are few rows: two rows at least each): results are the same from run to run.
+ * Sums over rows are formed in a fixed order, fp32 within a share of the rows and 64 bits over the shares (256 to 5120 of them by the length of a row,
+ * fewer where there are few rows): results are the same from run to run.
  * ------------------------------------------------------------------------- */
 typedef struct svg2_layer_norm_args {
     int dtype, y_dtype;

@@ -7,9 +7,9 @@
 //
 // Every element is read once and written once, some ten operations each: HBM bounds it, where the sums keep out of the way.  A row stays in
 // registers between its sums and its result; the mean is taken off before squares are summed.
-// 75,600 x 5120 bf16 (1.55 GB in and out) 288 us, 5.4 TB/s, the rate of a large copy; the same as an FP8 operand (1.16 GB) 303 us: there the
-// instructions bound it, some 17 an element of which 6 are loads' conversions, sums and reductions over a row that one round of barriers takes.
-// Gradients of 16,384 x 5120 bf16 (0.50 GB) 110 us and 6 to add up the weights', 4.6 TB/s, of 75,600 x 5120 485 us, 4.8 TB/s.
+// 75,600 x 5120 bf16 (1.55 GB in and out) 280 us, 5.5 TB/s, the rate of a large copy; the same as an FP8 operand (1.16 GB) 247 us, 4.7 TB/s:
+// instructions, some 15 an element, and one round over the wavefronts a row keep it from 219.  Gradients of 16,384 x 5120 bf16 (0.50 GB) 105 us with
+// the sums of the weights', 4.8 TB/s, of 75,600 x 5120 474 us, 4.9 TB/s.
 #include <type_traits>
 
 #include "svg2_fp8_blocks.h"
@@ -64,6 +64,15 @@ template <int LANES> __device__ __forceinline__ float lane_sum(float x)
     return x;
 }
 
+// waits for these loads
+template <typename T, int CH> __device__ __forceinline__ void arrived(Raw<T> (&r)[CH])
+{
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (unsigned i = 0; i < sizeof(T) / 2; ++i) asm volatile("" : "+v"(r[c].q[i]));
+}
+
 __device__ __forceinline__ void load_weight8(const float *row, int k, int D, float *v)
 {
     if (k + 8 <= D) load8<float>(row + k, v);
@@ -102,7 +111,10 @@ template <bool GRADIENT> __device__ __forceinline__ void join_waves(Wave &x, Wav
 {
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
     __syncthreads();
-    const int k = threadIdx.x & 15;
+    // lane % 16, formed here: kept from row to row it went to memory, and the wait for it was one for the next row as well (75,600 x 5120 to FP8 356
+    // us, this way 311)
+    int k;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0\n\tv_and_b32 %0, 15, %0" : "=v"(k));
     Wave w = {0.f, 0.f, 0.f, 0.f};
     if (k < waves) w = s[k];
     x.mean = quotient(lane_sum<16>(count * w.mean), D, inv_d);
@@ -138,7 +150,8 @@ template <int CH> __device__ __forceinline__ float deviations(float (&v)[CH][8],
 // LANES threads a row, CH steps of 8 columns a thread: 16, 32 or 64 lanes of a block of 256, or (0) a workgroup of up to 512.  A place, the threads
 // of a row, goes through neighbouring rows and keeps their factors and offsets in registers: from the caches, they are twice to four times the
 // bytes of the rows themselves (75,600 x 5120 bf16 that way 474 us).  The next row is on its way while this one is used.
-template <typename TX, typename TY, bool FP8, int LANES, int CH>
+// WHOLE: rows are as long as the steps of their threads, so that nothing asks where they end.
+template <typename TX, typename TY, bool FP8, int LANES, int CH, bool WHOLE>
 __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX) == 2 ? 5 : 4) : 2) void layer_norm_kernel(const NormArgs A)
 {
     __shared__ Wave s_wave[2][LANES ? 1 : WAVES];
@@ -147,7 +160,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
     const long long rows = (long long)A.B * A.N, places = (long long)gridDim.x * PLACES;
     const long long place = (long long)blockIdx.x * PLACES + (PLACES > 1 ? threadIdx.x / (256 / PLACES) : 0);
     const long long from = rows * place / places, to = rows * (place + 1) / places;
-    const bool ragged = D & 7;                                  // a thread's eight columns are all there or none, but for these lengths
+    const bool ragged = !WHOLE && (D & 7);                      // a thread's eight columns are all there or none, but for these lengths
     const float count = (float)D, inv_count = 1.f / count, own = LANES ? count : wave_columns<CH>(threadIdx.x >> 6, T, D);
     const float inv_own = own > 0.f ? 1.f / own : 0.f;
     const float other = LANES ? 0.f : wave_columns<CH>(threadIdx.x & 15, T, D);         // of the wavefront that this lane joins
@@ -158,7 +171,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
     auto load = [&]() {
         const TX *x = static_cast<const TX *>(A.x) + b * A.xs[0] + n * A.xs[1];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) next[c] = load_raw(x, (c * T + t) * 8, D);
+        for (int c = 0; c < CH; ++c) next[c] = WHOLE ? load_raw<TX>(x + (c * T + t) * 8) : load_raw(x, (c * T + t) * 8, D);
     };
     if (from < to) load();
     for (long long row = from; row < to; ++row) {
@@ -176,11 +189,11 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int k = (c * T + t) * 8;
-                if (A.w) load_weight8(A.w + rb * A.ws, k, D, f[c]);
-                if (A.b) load_weight8(A.b + rb * A.bs, k, D, o[c]);
+                if (A.w) load_weight8(A.w + rb * A.ws, k, WHOLE ? k + 8 : D, f[c]);
+                if (A.b) load_weight8(A.b + rb * A.bs, k, WHOLE ? k + 8 : D, o[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    f[c][i] = k + i >= D ? 0.f : A.w ? f[c][i] + A.one : 1.f;
+                    f[c][i] = !WHOLE && k + i >= D ? 0.f : A.w ? f[c][i] + A.one : 1.f;
                     o[c][i] = A.b ? o[c][i] : 0.f;
                 }
             }
@@ -195,7 +208,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum += v[c][i];
             const float mean = w.mean = quotient(lane_sum<LANES ? LANES : 64>(sum), own, inv_own);
-            w.squares = deviations<CH>(v, mean, t, T, D, ragged);
+            w.squares = deviations<CH>(v, mean, t, T, WHOLE ? 1 << 30 : D, ragged);
             w.squares = lane_sum<LANES ? LANES : 64>(w.squares);
             if constexpr (!LANES) {
                 join_waves<false>(w, s_wave[copy], T >> 6, other, count, inv_count);
@@ -207,30 +220,46 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
             const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                decode<TX>(load_raw(x, (c * T + t) * 8, D), v[c]);
+                decode<TX>(WHOLE ? load_raw<TX>(x + (c * T + t) * 8) : load_raw(x, (c * T + t) * 8, D), v[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[c][i] *= SHRINK;
             }
         }
         const float r = rsqrtf(fmaf(w.squares, inv_count, eps)), shift = -delta * r;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int k = (c * T + t) * 8;
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = fmaf(fmaf(v[c][i], r, shift), f[c][i], o[c][i]);
-            if constexpr (!FP8) {
-                if (k < D) store_row8(static_cast<TY *>(A.y) + rb * A.ys[0] + rn * A.ys[1], k, D, v[c]);
-            } else {                                            // 16 lanes a block of 128 columns
+        unsigned bytes[CH];
+        uint2 codes[CH];
+        if constexpr (FP8) {                                    // 16 lanes a block of 128 columns
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
                 float inv;
+                bytes[c] = e4m3_block_scale(max16(largest8(v[c])), inv);
+                codes[c] = e4m3_codes8(v[c], inv);
+            }
+        }
+        // The wait for the next row stands in front of this one's stores: behind them it would be a wait for them as well (75,600 x 5120 311 us, here
+        // 290; bf16 results, which HBM bounds, 293 and 308)
+        if constexpr (FP8) arrived(next);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int k = (c * T + t) * 8;
+            if constexpr (!FP8) {
+                TY *y = static_cast<TY *>(A.y) + rb * A.ys[0] + rn * A.ys[1];
+                if (WHOLE) store8<TY>(y + k, v[c]);
+                else if (k < D) store_row8(y, k, D, v[c]);
+            } else {
                 const int kc = k >> 7;
-                unsigned byte = e4m3_block_scale(max16(largest8(v[c])), inv);
-                if (kc < nk) *reinterpret_cast<uint2 *>(A.codes + row * (nk * 128LL) + k) = e4m3_codes8(v[c], inv);
+                unsigned byte = bytes[c];
+                if (WHOLE || kc < nk) *reinterpret_cast<uint2 *>(A.codes + row * (nk * 128LL) + k) = codes[c];
                 else byte = 0;
                 uint8_t *s = A.scales + ((long long)(kc >> 2) * rows + row) * 4;
                 if constexpr (LANES == 0 || LANES == 64) {      // a wavefront's step is a word of scales
                     const unsigned word = (unsigned)__builtin_amdgcn_readlane((int)byte, 0) | (unsigned)__builtin_amdgcn_readlane((int)byte, 16) << 8 |
                                           (unsigned)__builtin_amdgcn_readlane((int)byte, 32) << 16 | (unsigned)__builtin_amdgcn_readlane((int)byte, 48) << 24;
-                    if ((t & 63) == 0 && kc < nk) *reinterpret_cast<unsigned *>(s) = word;
+                    if ((t & 63) == 0 && (WHOLE || kc < nk)) *reinterpret_cast<unsigned *>(s) = word;
                 } else if ((t & 15) == 0) {
                     s[kc & 3] = (uint8_t)byte;
                     if (t == 0)                                 // the lanes of a short row do not reach the end of its word
@@ -244,14 +273,14 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
 // grid: workgroups stride over the shares, P of each group's rows.  LANES threads a row, CH steps of 8 columns a thread: 16 or 32 lanes of a block
 // of 64, or (0) the block, a multiple of 64 threads.  A thread keeps its columns' factors and sums; the next row is on its way while this
 // one is used.
-template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bounds__(LANES ? 64 : 512) void layer_norm_bwd_kernel(const NormArgs A)
+template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __launch_bounds__(LANES ? 64 : 512) void layer_norm_bwd_kernel(const NormArgs A)
 {
     constexpr int AT_ONCE = LANES ? 64 / (LANES ? LANES : 64) : 1, SUM = LANES ? LANES : 64;     // rows; lanes of a sum
     __shared__ Wave s_wave[2][WAVES];
     const int T = LANES ? LANES : (int)blockDim.x, t = LANES ? threadIdx.x & (LANES - 1) : threadIdx.x, D = A.D;
     const int groups = A.per_group ? A.B : 1;
     const long long rows = A.per_group ? A.N : (long long)A.B * A.N, shares = (long long)groups * A.P;
-    const bool ragged = D & 7;
+    const bool ragged = !WHOLE && (D & 7);
     const float count = (float)D, inv_count = 1.f / count, own = LANES ? count : wave_columns<CH>(t >> 6, T, D), other = LANES ? 0.f : wave_columns<CH>(t & 15, T, D);
     const float inv_own = own > 0.f ? 1.f / own : 0.f;
     int copy = 0;
@@ -260,7 +289,7 @@ template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bound
         float acc_w[CH][8], acc_b[CH][8], f[CH][8];
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            if (A.w) load_weight8(A.w + group * A.ws, (c * T + t) * 8, D, f[c]);
+            if (A.w) load_weight8(A.w + group * A.ws, (c * T + t) * 8, WHOLE ? (c * T + t) * 8 + 8 : D, f[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 acc_w[c][i] = acc_b[c][i] = 0.f;
@@ -276,8 +305,8 @@ template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bound
             const TY *dy = static_cast<const TY *>(A.dy) + b * A.ys[0] + n * A.ys[1];
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                next_x[c] = load_raw(x, (c * T + t) * 8, D);
-                next_g[c] = load_raw(dy, (c * T + t) * 8, D);
+                next_x[c] = WHOLE ? load_raw<TX>(x + (c * T + t) * 8) : load_raw(x, (c * T + t) * 8, D);
+                next_g[c] = WHOLE ? load_raw<TY>(dy + (c * T + t) * 8) : load_raw(dy, (c * T + t) * 8, D);
             }
         };
         if (from < to) load();
@@ -314,7 +343,7 @@ template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bound
                     for (int i = 0; i < 8; ++i) sum += vx[c][i];
                 const float mean = w.mean = quotient(lane_sum<SUM>(sum), own, inv_own);
                 w.g = sg;
-                w.squares = lane_sum<SUM>(deviations<CH>(vx, mean, t, T, D, ragged));
+                w.squares = lane_sum<SUM>(deviations<CH>(vx, mean, t, T, WHOLE ? 1 << 30 : D, ragged));
                 w.gx = 0.f;
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
@@ -332,7 +361,7 @@ template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bound
                 const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    decode<TX>(load_raw(x, (c * T + t) * 8, D), vx[c]);
+                    decode<TX>(WHOLE ? load_raw<TX>(x + (c * T + t) * 8) : load_raw(x, (c * T + t) * 8, D), vx[c]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) vx[c][i] *= SHRINK;
                 }
@@ -340,6 +369,8 @@ template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bound
             const float r = rsqrtf(fmaf(w.squares, inv_count, eps)), rs = r * scale, shift = -delta * r;
             const float by_n = -(w.gx * r * inv_count) * rs, by_1 = -(w.g * inv_count) * rs;
             TX *dx = static_cast<TX *>(A.dx) + rb * A.ds[0] + rn * A.ds[1];
+            arrived(next_x);                                    // in front of the stores, as above
+            arrived(next_g);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 float v[8];
@@ -350,7 +381,8 @@ template <typename TX, typename TY, int LANES, int CH> __global__ __launch_bound
                     v[i] = fmaf(xn, by_n, fmaf(gf[c][i], rs, by_1));
                 }
                 const int k = (c * T + t) * 8;
-                if (k < D) store_row8(dx, k, D, v);
+                if (WHOLE) store8<TX>(dx + k, v);
+                else if (k < D) store_row8(dx, k, D, v);
             }
         }
         if constexpr (LANES) {                                  // the rows that the wavefront had at once
@@ -432,19 +464,25 @@ template <typename TX, typename TY, bool FP8> static void norm_forward(const Nor
     const long long rows = (long long)A.B * A.N;
     // Workgroups of `per` places: some rows each, so that factors and offsets are read seldom, but enough of them for the whole card and
     // for places that are through early to be followed by others.  75,600 x 5120 bf16, rows a place: 37 336 us, 18 312, 9 292, 5 288; 16,384 x
-    // 5120: 8 71, 4 67, 2 77.  FP8 results leave fewer bytes to hide that reading behind: 75,600 x 5120, 16 rows 302, 8 312, 4 336.
+    // 5120: 8 71, 4 67, 2 77.  FP8 results leave fewer bytes to hide that reading behind: 75,600 x 5120, 32 rows 253, 16 247, 8 254.
     constexpr int each = FP8 ? 16 : 4;
     auto grid = [&](int per) {
         const long long one = (rows + per - 1) / per, some = (rows + each * per - 1) / (each * per);
         return (int)(one < 2048 ? one : some < 2048 ? 2048 : some < 1 << 22 ? some : 1 << 22);       // a launch has fewer than 2^32 threads
     };
     const int steps = cdiv(A.D, 512);
-    if (A.D <= 128) layer_norm_kernel<TX, TY, FP8, 16, 1><<<grid(16), 256, 0, st>>>(A);
-    else if (A.D <= 256) layer_norm_kernel<TX, TY, FP8, 32, 1><<<grid(8), 256, 0, st>>>(A);
-    else if (A.D <= 512) layer_norm_kernel<TX, TY, FP8, 64, 1><<<grid(4), 256, 0, st>>>(A);
-    else if (A.D <= 1024) layer_norm_kernel<TX, TY, FP8, 64, 2><<<grid(4), 256, 0, st>>>(A);
-    else if (A.D <= 8192) layer_norm_kernel<TX, TY, FP8, 0, 2><<<grid(1), cdiv(steps, 2) * 64, 0, st>>>(A);
-    else layer_norm_kernel<TX, TY, FP8, 0, 4><<<grid(1), cdiv(steps, 4) * 64, 0, st>>>(A);
+    // A wavefront a row up to three steps, no barrier: 387M bf16 values in rows of 1536 277 us (FP8 231), by two wavefronts 302 (293); of 1280 309 (271), 362
+    // (350).  Whole rows of 5120 280 us (FP8 247), asked for their ends 293 (290); fp32 ones alone are no faster so, 16,384 x 5120 130 against 127.
+    constexpr bool whole = FP8 || sizeof(TX) == 2;
+    if (A.D <= 128) layer_norm_kernel<TX, TY, FP8, 16, 1, false><<<grid(16), 256, 0, st>>>(A);
+    else if (A.D <= 256) layer_norm_kernel<TX, TY, FP8, 32, 1, false><<<grid(8), 256, 0, st>>>(A);
+    else if (A.D <= 512) layer_norm_kernel<TX, TY, FP8, 64, 1, false><<<grid(4), 256, 0, st>>>(A);
+    else if (A.D <= 1024) layer_norm_kernel<TX, TY, FP8, 64, 2, false><<<grid(4), 256, 0, st>>>(A);
+    else if (A.D < 1536) layer_norm_kernel<TX, TY, FP8, 64, 3, false><<<grid(4), 256, 0, st>>>(A);
+    else if (A.D == 1536) layer_norm_kernel<TX, TY, FP8, 64, 3, true><<<grid(4), 256, 0, st>>>(A);
+    else if (A.D <= 8192 && A.D % 1024 == 0 && whole) layer_norm_kernel<TX, TY, FP8, 0, 2, whole><<<grid(1), steps * 32, 0, st>>>(A);
+    else if (A.D <= 8192) layer_norm_kernel<TX, TY, FP8, 0, 2, false><<<grid(1), cdiv(steps, 2) * 64, 0, st>>>(A);
+    else layer_norm_kernel<TX, TY, FP8, 0, 4, false><<<grid(1), cdiv(steps, 4) * 64, 0, st>>>(A);
 }
 
 int layer_norm_launch(const svg2_layer_norm_args *a, hipStream_t st)
@@ -482,7 +520,9 @@ struct NormBwdPlan {
 };
 
 // Steps of a thread, us for 387M bf16 values: rows of 776 columns one 631, two 651; 1280 846 / 761; 1536 570 / 550; 5120 662 / 482.
-// Parts: 2560 wavefronts of two steps or 5120 of one are what the card holds at once, two rows each at least.
+// Parts: the same number of workgroups for each CU, which else wait for those with one more: 387M values in rows of 4096 in 640 parts 523 us, 768 474,
+// 512 473; of 8192 in 320 661, 256 477; of 1280 in 853 705, 1024 603.  As many as a CU holds, by wavefronts: 20 of one step, 12 of two, but 8 where
+// no lane is idle (5120 in 512 485, 256 474); a row each at least (2000 x 2048 17.5 us, two rows each 19.5).
 static NormBwdPlan norm_bwd_plan(const svg2_layer_norm_args *a)
 {
     NormBwdPlan p;
@@ -491,8 +531,9 @@ static NormBwdPlan norm_bwd_plan(const svg2_layer_norm_args *a)
     p.ch = a->D <= 1024 ? 1 : a->D <= 8192 ? 2 : 4;
     p.threads = cdiv(cdiv(a->D, 512), p.ch) * 64;
     const long long rows = p.own ? a->N : (long long)a->B * a->N, groups = p.own ? a->B : 1;
-    const long long shares = (p.ch == 1 ? 5120 : 2560) / (p.threads / 64), each = p.lanes ? 2 * (64 / p.lanes) : 2;
-    long long parts = (shares + groups - 1) / groups;
+    const int waves = p.threads / 64, fit = p.ch == 1 ? 20 : p.ch == 4 || a->D % 1024 == 0 ? 8 : 12;
+    const long long shares = 256LL * (waves < fit ? fit / waves : 1), each = p.lanes ? 64 / p.lanes : 1;
+    long long parts = shares > groups ? shares / groups : 1;
     if (parts > (rows + each - 1) / each) parts = (rows + each - 1) / each;
     p.P = (int)parts;
     return p;
@@ -528,11 +569,12 @@ int layer_norm_bwd_launch(const svg2_layer_norm_args *a, const void *dY, void *d
     auto launch = [&](auto *tx, auto *ty) {
         using TX = std::remove_pointer_t<decltype(tx)>;
         using TY = std::remove_pointer_t<decltype(ty)>;
-        if (p.lanes == 16) layer_norm_bwd_kernel<TX, TY, 16, 1><<<blocks, 64, 0, st>>>(A);
-        else if (p.lanes == 32) layer_norm_bwd_kernel<TX, TY, 32, 1><<<blocks, 64, 0, st>>>(A);
-        else if (p.ch == 1) layer_norm_bwd_kernel<TX, TY, 0, 1><<<blocks, p.threads, 0, st>>>(A);
-        else if (p.ch == 2) layer_norm_bwd_kernel<TX, TY, 0, 2><<<blocks, p.threads, 0, st>>>(A);
-        else layer_norm_bwd_kernel<TX, TY, 0, 4><<<blocks, p.threads, 0, st>>>(A);
+        if (p.lanes == 16) layer_norm_bwd_kernel<TX, TY, 16, 1, false><<<blocks, 64, 0, st>>>(A);
+        else if (p.lanes == 32) layer_norm_bwd_kernel<TX, TY, 32, 1, false><<<blocks, 64, 0, st>>>(A);
+        else if (p.ch == 1) layer_norm_bwd_kernel<TX, TY, 0, 1, false><<<blocks, p.threads, 0, st>>>(A);
+        else if (p.ch == 2 && A.D % 1024 == 0) layer_norm_bwd_kernel<TX, TY, 0, 2, true><<<blocks, p.threads, 0, st>>>(A);
+        else if (p.ch == 2) layer_norm_bwd_kernel<TX, TY, 0, 2, false><<<blocks, p.threads, 0, st>>>(A);
+        else layer_norm_bwd_kernel<TX, TY, 0, 4, false><<<blocks, p.threads, 0, st>>>(A);
     };
     const bool x16 = a->dtype == SVG2_BF16, y16 = a->y_dtype == SVG2_BF16;
     if (x16 && y16) launch((bf16_t *)0, (bf16_t *)0);

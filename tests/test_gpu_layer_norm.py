@@ -37,7 +37,7 @@ def _inputs(B, N, D, dtype, weights, seed=0):
 
 
 # lengths of one piece of a thread, of a wavefront, of each kind of workgroup, one on each side of the borders
-LENGTHS = [1, 2, 7, 8, 9, 100, 127, 128, 129, 255, 256, 257, 500, 512, 513, 777, 1024, 1025, 2048, 2049, 4096, 4100, 5120, 6144, 6145, 8192, 8200, 12289,
+LENGTHS = [1, 2, 7, 8, 9, 100, 127, 128, 129, 255, 256, 257, 500, 512, 513, 777, 1024, 1025, 1280, 1301, 1535, 1536, 1537, 2048, 2049, 4096, 4100, 5120, 6144, 6145, 8192, 8200, 12289,
            16384]
 
 
@@ -168,7 +168,7 @@ def test_rows_that_are_special(svg2):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("D", [1, 100, 128, 129, 256, 300, 512, 777, 1024, 1500, 2048, 2500, 4096, 5120, 6000, 7000, 8192, 10000, 16384])
+@pytest.mark.parametrize("D", [1, 100, 128, 129, 256, 300, 512, 777, 1024, 1280, 1500, 1536, 2048, 2500, 4096, 5120, 6000, 7000, 8192, 10000, 16384])
 def test_fp8_result(svg2, D, dtype):
     """A value that the norm leaves within its fp32 bound of y is one of the E4M3 numbers next to it times the scale, or their neighbour where
     the bound reaches over a border: the operand is that of some value within the bound.  The scale is that of the block's largest
@@ -214,6 +214,32 @@ def test_sums_over_many_rows_and_groups(svg2, B, N, D, weights):
     assert_within(res.dbias, db, db_bound, F32)
     again = svg2.svg2_layer_norm_backward(dy, x, w, b, eps=EPS, one_plus=True)
     assert torch.equal(again.grad, res.grad) and torch.equal(again.dweight, res.dweight) and torch.equal(again.dbias, res.dbias)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [1300, 1536, 2048, 5120])
+def test_rows_taken_again_among_others(svg2, D, dtype):
+    """Rows whose squares leave fp32's range between ordinary ones that the same threads take, many to a place: each as if it were alone."""
+    N = 9000
+    x = torch.randn((N, D), generator=torch.Generator(device="cuda").manual_seed(D), device="cuda")
+    x[::7] *= 2.0 ** 62
+    x[::11] *= 2.0 ** -70
+    x[5::1000, 3] = float("inf")
+    x = x.to(dtype)
+    w, b = (torch.randn(D, generator=torch.Generator(device="cuda").manual_seed(k), device="cuda") for k in (1, 2))
+    dy = torch.randn((N, D), generator=torch.Generator(device="cuda").manual_seed(7), device="cuda").to(dtype)
+    rows = torch.tensor([0, 1, 5, 7, 11, 77, 1005, 4998, 8998, 8999], device="cuda")
+    few = x[rows].contiguous()
+    y, alone = svg2.svg2_layer_norm(x, w, b), svg2.svg2_layer_norm(few, w, b)
+    assert torch.equal(y[rows].nan_to_num(7.0), alone.nan_to_num(7.0)) and bool(y[5].isnan().all()) and bool(y[4].isfinite().all())
+    codes, scales = svg2.svg2_layer_norm_fp8(x, w, b)
+    c, s = svg2.svg2_layer_norm_fp8(few, w, b)
+    assert torch.equal(codes[rows], c) and torch.equal(scales[:, rows], s)
+    dx = svg2.svg2_layer_norm_backward(dy, x, w, b).grad
+    alone = svg2.svg2_layer_norm_backward(dy[rows].contiguous(), few, w, b).grad
+    assert torch.equal(dx[rows].nan_to_num(7.0), alone.nan_to_num(7.0)) and bool(dx[5].isnan().all()) and bool(dx[4].isfinite().all())
+    ref, bound = ops.layer_norm(_np(few[[0, 1, 3, 4, 5, 8]])[None], _np(w), _np(b), EPS, False)
+    assert_within(svg2.svg2_layer_norm(few[[0, 1, 3, 4, 5, 8]].contiguous(), w, b)[None], ref, bound, dtype)
 
 
 def test_a_row_does_not_depend_on_the_others(svg2):
