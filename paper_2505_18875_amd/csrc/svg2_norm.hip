@@ -73,6 +73,31 @@ template <typename T, int CH> __device__ __forceinline__ void arrived(Raw<T> (&r
         for (unsigned i = 0; i < sizeof(T) / 2; ++i) asm volatile("" : "+v"(r[c].q[i]));
 }
 
+// Columns k .. k + 7 of a row of D, in two steps, so that nothing waits where it is loaded: threads at and behind the end of the row load its last eight
+// columns, and what is not theirs is moved out when it is used.  (With a branch for each column that is there, the last wavefront had no next row on
+// its way: gradients of 16,384 x 5112 bf16 199 us, of 5120 108, now 126 and 104.)  Rows of fewer than eight: column by column.
+template <typename T, bool WHOLE, int LANES> __device__ __forceinline__ Raw<T> load_columns(const T *row, int k, int D)
+{
+    if (WHOLE) return load_raw<T>(row + k);
+    if (LANES == 16 && D < 8) return load_raw(row, k, D);
+    return load_raw<T>(row + min(k, D - 8));
+}
+
+// end: the wavefront reaches the end of the row
+template <typename T, bool WHOLE, int LANES> __device__ __forceinline__ void use_columns(const Raw<T> &r, int k, int D, bool end, float *v)
+{
+    decode<T>(r, v);
+    if (WHOLE || !end || (LANES == 16 && D < 8)) return;
+    const int s = k - min(k, D - 8);                            // 8 and more: none is there
+    if (D & 7)
+#pragma unroll
+        for (int by = 4; by; by >>= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = !(s & by) ? v[i] : i + by < 8 ? v[i + by] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = s < 8 ? v[i] : 0.f;
+}
+
 __device__ __forceinline__ void load_weight8(const float *row, int k, int D, float *v)
 {
     if (k + 8 <= D) load8<float>(row + k, v);
@@ -150,9 +175,10 @@ template <int CH> __device__ __forceinline__ float deviations(float (&v)[CH][8],
 // LANES threads a row, CH steps of 8 columns a thread: 16, 32 or 64 lanes of a block of 256, or (0) a workgroup of up to 512.  A place, the threads
 // of a row, goes through neighbouring rows and keeps their factors and offsets in registers: from the caches, they are twice to four times the
 // bytes of the rows themselves (75,600 x 5120 bf16 that way 474 us).  The next row is on its way while this one is used.
-// WHOLE: rows are as long as the steps of their threads, so that nothing asks where they end.
+// WHOLE: rows are as long as the steps of their threads, so that nothing asks where they end.  Wavefronts a SIMD: four at least, five where they fit
+// without going to memory (31,299 x 1855 to FP8 with five 45 us, four 42).
 template <typename TX, typename TY, bool FP8, int LANES, int CH, bool WHOLE>
-__global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX) == 2 ? 5 : 4) : 2) void layer_norm_kernel(const NormArgs A)
+__global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX) == 2 && (WHOLE || !FP8) ? 5 : 4) : 2) void layer_norm_kernel(const NormArgs A)
 {
     __shared__ Wave s_wave[2][LANES ? 1 : WAVES];
     constexpr int PLACES = 256 / (LANES ? LANES : 256);
@@ -164,6 +190,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
     const float count = (float)D, inv_count = 1.f / count, own = LANES ? count : wave_columns<CH>(threadIdx.x >> 6, T, D);
     const float inv_own = own > 0.f ? 1.f / own : 0.f;
     const float other = LANES ? 0.f : wave_columns<CH>(threadIdx.x & 15, T, D);         // of the wavefront that this lane joins
+    const int last = LANES ? LANES : (__builtin_amdgcn_readfirstlane(threadIdx.x) & ~63) + 64;
     float f[CH][8], o[CH][8];
     int group = -1, copy = 0;
     Raw<TX> next[CH];
@@ -171,14 +198,14 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
     auto load = [&]() {
         const TX *x = static_cast<const TX *>(A.x) + b * A.xs[0] + n * A.xs[1];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) next[c] = WHOLE ? load_raw<TX>(x + (c * T + t) * 8) : load_raw(x, (c * T + t) * 8, D);
+        for (int c = 0; c < CH; ++c) next[c] = load_columns<TX, WHOLE, LANES>(x, (c * T + t) * 8, D);
     };
     if (from < to) load();
     for (long long row = from; row < to; ++row) {
         const int rb = b, rn = n;
         float v[CH][8];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) decode<TX>(next[c], v[c]);
+        for (int c = 0; c < CH; ++c) use_columns<TX, WHOLE, LANES>(next[c], (c * T + t) * 8, D, (c * T + last) * 8 > D, v[c]);
         if (++n == A.N) {
             n = 0;
             ++b;
@@ -220,7 +247,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
             const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                decode<TX>(WHOLE ? load_raw<TX>(x + (c * T + t) * 8) : load_raw(x, (c * T + t) * 8, D), v[c]);
+                use_columns<TX, WHOLE, LANES>(load_columns<TX, WHOLE, LANES>(x, (c * T + t) * 8, D), (c * T + t) * 8, D, true, v[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[c][i] *= SHRINK;
             }
@@ -272,8 +299,8 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
 
 // grid: workgroups stride over the shares, P of each group's rows.  LANES threads a row, CH steps of 8 columns a thread: 16 or 32 lanes of a block
 // of 64, or (0) the block, a multiple of 64 threads.  A thread keeps its columns' factors and sums; the next row is on its way while this
-// one is used.
-template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __launch_bounds__(LANES ? 64 : 512) void layer_norm_bwd_kernel(const NormArgs A)
+// one is used.  Three wavefronts a SIMD at least: 31,299 x 1855 fp32 160 us, with two 174.
+template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __launch_bounds__(LANES ? 64 : 512, CH == 2 ? 3 : 1) void layer_norm_bwd_kernel(const NormArgs A)
 {
     constexpr int AT_ONCE = LANES ? 64 / (LANES ? LANES : 64) : 1, SUM = LANES ? LANES : 64;     // rows; lanes of a sum
     __shared__ Wave s_wave[2][WAVES];
@@ -283,6 +310,7 @@ template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __
     const bool ragged = !WHOLE && (D & 7);
     const float count = (float)D, inv_count = 1.f / count, own = LANES ? count : wave_columns<CH>(t >> 6, T, D), other = LANES ? 0.f : wave_columns<CH>(t & 15, T, D);
     const float inv_own = own > 0.f ? 1.f / own : 0.f;
+    const int last = LANES ? LANES : (__builtin_amdgcn_readfirstlane(threadIdx.x) & ~63) + 64;
     int copy = 0;
     for (long long share = blockIdx.x; share < shares; share += gridDim.x) {
         const int group = (int)(share / A.P), part = (int)(share - (long long)group * A.P);
@@ -305,8 +333,8 @@ template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __
             const TY *dy = static_cast<const TY *>(A.dy) + b * A.ys[0] + n * A.ys[1];
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                next_x[c] = WHOLE ? load_raw<TX>(x + (c * T + t) * 8) : load_raw(x, (c * T + t) * 8, D);
-                next_g[c] = WHOLE ? load_raw<TY>(dy + (c * T + t) * 8) : load_raw(dy, (c * T + t) * 8, D);
+                next_x[c] = load_columns<TX, WHOLE, LANES>(x, (c * T + t) * 8, D);
+                next_g[c] = load_columns<TY, WHOLE, LANES>(dy, (c * T + t) * 8, D);
             }
         };
         if (from < to) load();
@@ -315,8 +343,9 @@ template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __
             float vx[CH][8], vg[CH][8], gf[CH][8], sg = 0.f;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                decode<TX>(next_x[c], vx[c]);
-                decode<TY>(next_g[c], vg[c]);
+                const bool end = (c * T + last) * 8 > D;
+                use_columns<TX, WHOLE, LANES>(next_x[c], (c * T + t) * 8, D, end, vx[c]);
+                use_columns<TY, WHOLE, LANES>(next_g[c], (c * T + t) * 8, D, end, vg[c]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     gf[c][i] = vg[c][i] * f[c][i];
@@ -361,7 +390,7 @@ template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __
                 const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    decode<TX>(WHOLE ? load_raw<TX>(x + (c * T + t) * 8) : load_raw(x, (c * T + t) * 8, D), vx[c]);
+                    use_columns<TX, WHOLE, LANES>(load_columns<TX, WHOLE, LANES>(x, (c * T + t) * 8, D), (c * T + t) * 8, D, true, vx[c]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) vx[c][i] *= SHRINK;
                 }
