@@ -29,6 +29,7 @@ struct BlockQuantArgs {
     int M, G, Kg;                   // X is [M, G, Kg]; K = G Kg columns
     uint8_t *codes, *scales;        // operand of M rows and K columns
     uint8_t *codes_t, *scales_t;    // operand of K rows and M columns
+    int per_xcd;                    // tiles that follow each other on one XCD; 0: every eighth
 };
 
 template <typename T> __device__ __forceinline__ const T *element(const BlockQuantArgs &A, long long m, int k)
@@ -64,18 +65,22 @@ template <typename T, bool STREAM> __global__ __launch_bounds__(256) void fp8_bl
 }
 
 // tiles of 128 x 128 for the transposed operand, for both from one read, and for square blocks.
-// grid: workgroups stride over the tiles, those of one row of tiles neighbours; block 256: a thread holds 8 rows x 8 columns, as they are in
+// grid: workgroups stride over the tiles, those of one row of tiles neighbours, on one XCD where they share lines; block 256: a thread holds 8 rows x 8 columns, as they are in
 // memory.  The maximum of a row goes round 16 lanes, that of a column over the wavefront's four groups of rows and, through LDS, the four
 // wavefronts.  The codes of eight rows of a column are eight bytes: they go through LDS, column by column, and leave as lines of 128 bytes.
 // Bound by HBM: 16,384 x 5120 bf16 both ways 67 us, 5.0 TB/s (rows and transposed in calls of their own 94), transposed 48, in squares both ways 61;
-// small ones by their few workgroups (16,384 x 1536 both ways 25 us, 1536 of them), rows that share lines by those (75,599 x 5119 both ways 417).
+// small ones by their few workgroups (16,384 x 1536 both ways 25 us, 1536 of them).  Rows that are not whole lines (75,599 x 5119 both ways 356 us,
+// 31,299 x 2047 65) have neighbouring tiles read the same ones, twice from memory if those go to the next XCD each (415, 107).
 template <typename T, bool STREAM, bool ROWS, bool COLS, bool SQUARE> __global__ __launch_bounds__(256) void fp8_blocks_tile_kernel(const BlockQuantArgs A)
 {
     __shared__ unsigned s_top[4][128];
     __shared__ __attribute__((aligned(16))) uint8_t s_codes[COLS ? 128 * 144 : 16];     // a column's 128 codes and 16 bytes: stores of 8 bytes spread over the banks
     const int K = A.G * A.Kg, nk = (K + 127) / 128, nm = (A.M + 127) / 128;
     const int lane16 = threadIdx.x & 15, rows8 = threadIdx.x >> 4, wave = threadIdx.x >> 6;
-    for (long long tile = blockIdx.x; tile < (long long)nm * nk; tile += gridDim.x) {
+    const long long all = (long long)nm * nk, turns = A.per_xcd ? 8LL * A.per_xcd : all;
+    for (long long turn = blockIdx.x; turn < turns; turn += gridDim.x) {
+        const long long tile = A.per_xcd ? (turn & 7) * A.per_xcd + (turn >> 3) : turn;
+        if (tile >= all) continue;
         const int kc = (int)(tile % nk), mc = (int)(tile / nk), k0 = kc * 128 + lane16 * 8;
         const long long m0 = (long long)mc * 128 + rows8 * 8;
         Raw<T> x[8];
@@ -680,10 +685,12 @@ template <typename F> static int with_types(int dtype, bool stream, F f)
 int fp8_blocks_quant_launch(const void *X, int dtype, int M, int G, int Kg, int64_t sm, int64_t sg, bool square, void *codes, void *scales,
                             void *codes_t, void *scales_t, hipStream_t st)
 {
-    const BlockQuantArgs A = {X, sm, sg, M, G, Kg, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales),
-                              static_cast<uint8_t *>(codes_t), static_cast<uint8_t *>(scales_t)};
     const int K = G * Kg, es = dtype == SVG2_BF16 ? 2 : 4;
     const bool lines = G == 1 || (sg * es % 128 == 0 && Kg * es % 128 == 0);
+    const long long all = (long long)cdiv(M, 128) * cdiv(K, 128);
+    const bool shared = !lines || sm * es % 128 != 0 || (reinterpret_cast<uintptr_t>(X) & 127) != 0;
+    const BlockQuantArgs A = {X, sm, sg, M, G, Kg, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales),
+                              static_cast<uint8_t *>(codes_t), static_cast<uint8_t *>(scales_t), shared ? (int)((all + 7) / 8) : 0};
     return with_types(dtype, lines && streamed(X, (double)M * K, sm, es) && (double)M * K * es < 268435456.0, [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
         constexpr bool S = decltype(stream)::value;
@@ -692,8 +699,8 @@ int fp8_blocks_quant_launch(const void *X, int dtype, int M, int G, int Kg, int6
             fp8_blocks_rows_kernel<T, S><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(A);
             return;
         }
-        const long long all = (long long)cdiv(M, 128) * cdiv(K, 128);
-        const int tiles = (int)(all < 1 << 20 ? all : 1 << 20);
+        const long long turns = A.per_xcd ? 8LL * A.per_xcd : all;
+        const int tiles = (int)(turns < 1 << 20 ? turns : 1 << 20);
         if (square) {
             if (!codes_t) fp8_blocks_tile_kernel<T, S, true, false, true><<<tiles, 256, 0, st>>>(A);
             else if (!codes) fp8_blocks_tile_kernel<T, S, false, true, true><<<tiles, 256, 0, st>>>(A);
