@@ -751,6 +751,13 @@ def _norm_out(t, name, dev, dtype, shape):
     return t.data_ptr(), outer if len(shape) == 3 else [0, *outer]
 
 
+def _dense_like(x, dtype):
+    """A dense tensor of x's shape, its address and (group, row) strides; one of fewer than two dimensions is refused with x."""
+    t = torch.empty_like(x) if dtype is x.dtype and x.is_contiguous() else torch.empty(x.shape, dtype=dtype, device=x.device)
+    stride = t.stride()
+    return t, t.data_ptr(), stride[:2] if len(stride) == 3 else (0, *stride[:1])
+
+
 def svg2_layer_norm(x, weight=None, bias=None, *, eps=1e-6, one_plus=False, out_dtype=None, out=None):
     """(x - mean) / sqrt(variance + eps) * s + bias over the last dimension, s = weight, or 1 + weight with one_plus.
 
@@ -759,8 +766,9 @@ def svg2_layer_norm(x, weight=None, bias=None, *, eps=1e-6, one_plus=False, out_
     lib = load_library()
     dev, shape = _gpu(x, "x"), x.shape
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype if out_dtype is None else out_dtype, device=dev)
-    y, ys = _norm_out(out, "out", dev, out_dtype, shape)
+        out, y, ys = _dense_like(x, x.dtype if out_dtype is None else out_dtype)
+    else:
+        y, ys = _norm_out(out, "out", dev, out_dtype, shape)
     a = _norm_args(x, weight, bias, eps, one_plus, _dtype_code(out), y, ys, dev)[0]
     with _on(dev):
         _check(lib.svg2_layer_norm(a, _raw_stream(dev)))
@@ -783,14 +791,17 @@ def svg2_layer_norm_backward(grad, x, weight=None, bias=None, *, eps=1e-6, one_p
     `out`), dweight and dbias (fp32 [D] or [B,D], None where the argument is None)."""
     lib = load_library()
     dev, shape = _gpu(x, "x"), x.shape
-    out = torch.empty(shape, dtype=x.dtype, device=dev) if out is None else out
     g, gs = _norm_out(grad, "grad", dev, None, shape)
-    dx, ds = _norm_out(out, "out", dev, x.dtype, shape)
+    if out is None:
+        out, dx, ds = _dense_like(x, x.dtype)
+    else:
+        dx, ds = _norm_out(out, "out", dev, x.dtype, shape)
     a, B, N, D = _norm_args(x, weight, bias, eps, one_plus, _dtype_code(grad), 0, gs, dev)
     for t in (weight, bias):
         if t is not None and B > 1 and t.dim() == 2 and t.stride(0) == 0:
             raise ValueError("weight and bias of a group each must be rows of their own: expanded rows are shared ones, [D]")
-    dw, db = [None if t is None else torch.empty(t.shape, dtype=torch.float32, device=dev) for t in (weight, bias)]
+    dw, db = [None if t is None else torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=torch.float32, device=dev)
+              for t in (weight, bias)]
     with _on(dev):
         if ws is None:
             need = lib.svg2_layer_norm_backward_workspace_size(a)
