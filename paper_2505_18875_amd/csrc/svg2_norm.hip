@@ -551,7 +551,8 @@ struct NormBwdPlan {
 // Steps of a thread, us for 387M bf16 values: rows of 776 columns one 631, two 651; 1280 846 / 761; 1536 570 / 550; 5120 662 / 482.
 // Parts: the same number of workgroups for each CU, which else wait for those with one more: 387M values in rows of 4096 in 640 parts 523 us, 768 474,
 // 512 473; of 8192 in 320 661, 256 477; of 1280 in 853 705, 1024 603.  As many as a CU holds, by wavefronts: 20 of one step, 12 of two, but 8 where
-// no lane is idle (5120 in 512 485, 256 474); a row each at least (2000 x 2048 17.5 us, two rows each 19.5).
+// no lane is idle (5120 in 512 485, 256 474).  Where there are not half again as many rows, two rows each: more would be more to add up (999 x 777
+// in 999 parts 9.3 + 6.4 us, in 500 7.8 + 5.2).
 static NormBwdPlan norm_bwd_plan(const svg2_layer_norm_args *a)
 {
     NormBwdPlan p;
@@ -561,10 +562,9 @@ static NormBwdPlan norm_bwd_plan(const svg2_layer_norm_args *a)
     p.threads = cdiv(cdiv(a->D, 512), p.ch) * 64;
     const long long rows = p.own ? a->N : (long long)a->B * a->N, groups = p.own ? a->B : 1;
     const int waves = p.threads / 64, fit = p.ch == 1 ? 20 : p.ch == 4 || a->D % 1024 == 0 ? 8 : 12;
-    const long long shares = 256LL * (waves < fit ? fit / waves : 1), each = p.lanes ? 64 / p.lanes : 1;
-    long long parts = shares > groups ? shares / groups : 1;
-    if (parts > (rows + each - 1) / each) parts = (rows + each - 1) / each;
-    p.P = (int)parts;
+    const long long shares = 256LL * (waves < fit ? fit / waves : 1), at_once = p.lanes ? 64 / p.lanes : 1, turns = (rows + at_once - 1) / at_once;
+    const long long parts = shares > groups ? shares / groups : 1;
+    p.P = (int)(2 * turns >= 3 * parts ? parts : (turns + 1) / 2);
     return p;
 }
 
