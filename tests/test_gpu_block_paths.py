@@ -157,3 +157,18 @@ def test_a_group_for_every_row(svg2, B):
     assert_within(res.grad, dx, bound, F32)
     assert_within(res.dweight, dw, dw_bound, F32)
     assert np.array_equal(up(res.dbias), db)
+
+
+@pytest.mark.parametrize("M,K", [(1031, 1543), (129, 2047), (5000, 130), (1, 1025)])
+@pytest.mark.parametrize("square", [False, True])
+def test_tiles_of_rows_that_share_lines(svg2, M, K, square):
+    """Rows that are not whole lines of memory have their tiles in another order: the same operands, both ways, as from rows that are."""
+    x = torch.randn((M, K), generator=torch.Generator(device="cuda").manual_seed(M + K), device="cuda").bfloat16()
+    lines = torch.zeros((M, -(-K // 64) * 64), dtype=x.dtype, device="cuda")[:, :K]
+    lines.copy_(x)
+    assert lines.stride(0) * 2 % 128 == 0 and x.stride(0) * 2 % 128 != 0
+    for transposed in (True, "both"):
+        got, want = (svg2.svg2_quantize_fp8_blocks(t, transposed=transposed, square=square) for t in (x, lines))
+        for g, w in zip(got, want):
+            for a, b in zip(g, w) if transposed == "both" else ((g, w),):
+                assert torch.equal(a, b)

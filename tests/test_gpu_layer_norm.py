@@ -242,6 +242,26 @@ def test_rows_taken_again_among_others(svg2, D, dtype):
     assert_within(svg2.svg2_layer_norm(few[[0, 1, 3, 4, 5, 8]].contiguous(), w, b)[None], ref, bound, dtype)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [5, 9, 127, 255, 510, 1021, 1301, 2047, 5119, 9001])
+def test_in_place_with_rows_taken_again(svg2, D, dtype):
+    """The end of a row is loaded with columns of the thread in front, and a row that is taken again is read twice: neither may see results that are
+    written over x, or over dy."""
+    x = torch.randn((700, D), generator=torch.Generator(device="cuda").manual_seed(D), device="cuda")
+    x[::3] *= 2.0 ** 62
+    x = x.to(dtype)
+    w, b, dy = (torch.randn(s, generator=torch.Generator(device="cuda").manual_seed(k), device="cuda") for k, s in ((1, D), (2, D), (3, (700, D))))
+    dy = dy.to(dtype)
+    want = svg2.svg2_layer_norm_backward(dy, x, w, b)
+    again = dy.clone()
+    got = svg2.svg2_layer_norm_backward(again, x, w, b, out=again)
+    assert torch.equal(again, want.grad) and torch.equal(got.dweight, want.dweight) and torch.equal(got.dbias, want.dbias)
+    y = svg2.svg2_layer_norm(x, w, b)
+    assert bool(y.isfinite().all())
+    svg2.svg2_layer_norm(x, w, b, out=x)
+    assert torch.equal(x, y)
+
+
 def test_a_row_does_not_depend_on_the_others(svg2):
     x, w, b = _inputs(1, 300, 1000, BF16, "shared")
     y = svg2.svg2_layer_norm(x[0], w, b)
