@@ -43,16 +43,20 @@ __device__ __forceinline__ float quotient(float x, float y, float inv)
     return fmaf(fmaf(-q, y, x), inv, q);
 }
 
-// sum over 16, 32 or 64 neighbouring lanes, in all of them: no trip through LDS, which takes __shfl_xor some hundred cycles a step
+// sum over 16, 32 or 64 neighbouring lanes, in all of them: no trip through LDS, which takes __shfl_xor some hundred cycles a step.  The same bits in
+// every lane, since each step adds what two halves have, either way round: a row's lanes decide by it together whether they go on, to barriers too.
+// (Rotated by 4 before 8, half of the lanes would add their neighbours' quads in another order; a product, unless it is rounded first, would be fused
+// with the first addition, each lane's own with its neighbour's rounded one.)
 template <int LANES> __device__ __forceinline__ float lane_sum(float x)
 {
     auto dpp = [](float v, auto control) {
         return __uint_as_float((unsigned)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), decltype(control)::value, 0xF, 0xF, true));
     };
+    asm("" : "+v"(x));
     x += dpp(x, std::integral_constant<int, 0xB1>());           // quad_perm [1,0,3,2]
     x += dpp(x, std::integral_constant<int, 0x4E>());           // quad_perm [2,3,0,1]
-    x += dpp(x, std::integral_constant<int, 0x124>());          // row_ror:4
     x += dpp(x, std::integral_constant<int, 0x128>());          // row_ror:8
+    x += dpp(x, std::integral_constant<int, 0x124>());          // row_ror:4
     if constexpr (LANES >= 32) {                                // odd rows of 16 against even ones
         const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
         x = __uint_as_float(y[0]) + __uint_as_float(y[1]);
