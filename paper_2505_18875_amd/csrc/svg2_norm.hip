@@ -30,7 +30,8 @@ struct NormArgs {
 };
 
 // Rows whose sums leave fp32's range (an infinity and a NaN among them) are taken again times this: squares of the largest numbers, 16384 of
-// them, then stay below 2^126, and those of a row that needs it stay above 2^-30, so that eps is nothing beside them.
+// them, then stay below 2^126.  Either their squares were too many, which are then above 2^-30, eps nothing beside them; or their sum was, of numbers
+// above 2^113, two of which differ by 2^16 then, if any do.  If none do, the row has no variance, as one of zeros.
 constexpr float SHRINK = 0x1p-72f;
 constexpr int WAVES = 16;           // most of a workgroup
 
@@ -102,6 +103,34 @@ template <typename T, bool WHOLE, int LANES> __device__ __forceinline__ void use
     for (int i = 0; i < 8; ++i) v[i] = s < 8 ? v[i] : 0.f;
 }
 
+// Gradients of a row that is taken again: the row times SHRINK; or, with true, zeros for a row of one finite number, whose sum need not be a multiple
+// of it in fp32.
+template <typename TX, int LANES, int CH, bool WHOLE> __device__ __forceinline__ bool take_again(const TX *row, float (&v)[CH][8], int t, int T, int D)
+{
+    asm volatile("" : "+v"(t), "+s"(D));        // what is formed of them is formed here, not kept in registers through all rows
+    const float first = to_f32(row[0]);
+    int others = finite(first) && first != 0.f ? 0 : 1;                // columns that differ from the first
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int k = (c * T + t) * 8;
+        use_columns<TX, WHOLE, LANES>(load_columns<TX, WHOLE, LANES>(row, k, D), k, D, true, v[c]);
+        others += WHOLE ? 8 : min(max(D - k, 0), 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) others -= v[c][i] == first;         // (places behind the end have 0)
+    }
+    bool same = others == 0;
+    if constexpr (LANES) {                                      // of the row's lanes; others may be past their last row
+        const unsigned long long other = __ballot(!same) >> (threadIdx.x & 63 & ~(LANES - 1));
+        same = (other & (~0ULL >> (64 - LANES))) == 0;
+    } else same = __syncthreads_and(same);
+    const float by = same ? 0.f : SHRINK;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c][i] *= by;
+    return same;
+}
+
 __device__ __forceinline__ void load_weight8(const float *row, int k, int D, float *v)
 {
     if (k + 8 <= D) load8<float>(row + k, v);
@@ -155,6 +184,25 @@ template <bool GRADIENT> __device__ __forceinline__ void join_waves(Wave &x, Wav
     }
 }
 
+// sum of f(column) over the row, in all its threads, each taking its own columns one after another
+template <int LANES, int CH, typename F> __device__ __forceinline__ float row_sum(Wave (*s)[LANES ? 1 : WAVES], int &copy, int t, int T, int D, F f)
+{
+    float sum = 0.f;
+#pragma nounroll
+    for (int c = 0; c < CH; ++c)
+#pragma nounroll
+        for (int k = (c * T + t) * 8, i = 0; i < 8 && k < D; ++i, ++k) sum += f(k);
+    sum = lane_sum<LANES ? LANES : 64>(sum);
+    if constexpr (!LANES) {
+        if ((threadIdx.x & 63) == 0) s[copy][threadIdx.x >> 6].mean = sum;
+        __syncthreads();
+        const int k = threadIdx.x & 15;
+        sum = lane_sum<16>(k < T >> 6 ? s[copy][k].mean : 0.f);
+        copy ^= 1;
+    }
+    return sum;
+}
+
 // v - mean (0 where there is no column), and the sum of its squares
 template <int CH> __device__ __forceinline__ float deviations(float (&v)[CH][8], float mean, int t, int T, int D, bool ragged)
 {
@@ -180,9 +228,9 @@ template <int CH> __device__ __forceinline__ float deviations(float (&v)[CH][8],
 // of a row, goes through neighbouring rows and keeps their factors and offsets in registers: from the caches, they are twice to four times the
 // bytes of the rows themselves (75,600 x 5120 bf16 that way 474 us).  The next row is on its way while this one is used.
 // WHOLE: rows are as long as the steps of their threads, so that nothing asks where they end.  Wavefronts a SIMD: four at least, five where they fit
-// without going to memory (31,299 x 1855 to FP8 with five 45 us, four 42).
+// without going to memory (31,299 x 1855 to FP8 with five 45 us, four 42); eight for rows of up to 512 (75,600 x 512 to FP8 with seven 25 us).
 template <typename TX, typename TY, bool FP8, int LANES, int CH, bool WHOLE>
-__global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX) == 2 && (WHOLE || !FP8) ? 5 : 4) : 2) void layer_norm_kernel(const NormArgs A)
+__global__ __launch_bounds__(LANES ? 256 : 512, LANES ? (LANES == 64 && CH == 1 && sizeof(TX) == 2 ? 8 : 1) : CH == 2 ? (sizeof(TX) == 2 && (WHOLE || !FP8) ? 5 : 4) : 2) void layer_norm_kernel(const NormArgs A)
 {
     __shared__ Wave s_wave[2][LANES ? 1 : WAVES];
     constexpr int PLACES = 256 / (LANES ? LANES : 256);
@@ -197,12 +245,36 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
     const int last = LANES ? LANES : (__builtin_amdgcn_readfirstlane(threadIdx.x) & ~63) + 64;
     float f[CH][8], o[CH][8];
     int group = -1, copy = 0;
+    unsigned left_out = 0;                                      // a bit for each row of this place that is taken again
     Raw<TX> next[CH];
     int b = (int)(from / A.N), n = (int)(from - (long long)b * A.N);
     auto load = [&]() {
         const TX *x = static_cast<const TX *>(A.x) + b * A.xs[0] + n * A.xs[1];
 #pragma unroll
         for (int c = 0; c < CH; ++c) next[c] = load_columns<TX, WHOLE, LANES>(x, (c * T + t) * 8, D);
+    };
+    // eight columns of a result
+    auto put = [&](long long row, int rb, int rn, int c, const float *v, unsigned byte, const uint2 &codes) {
+        const int k = (c * T + t) * 8;
+        if constexpr (!FP8) {
+            TY *y = static_cast<TY *>(A.y) + rb * A.ys[0] + rn * A.ys[1];
+            if (WHOLE) store8<TY>(y + k, v);
+            else if (k < D) store_row8(y, k, D, v);
+        } else {
+            const int kc = k >> 7;
+            if (WHOLE || kc < nk) *reinterpret_cast<uint2 *>(A.codes + row * (nk * 128LL) + k) = codes;
+            else byte = 0;
+            uint8_t *s = A.scales + ((long long)(kc >> 2) * rows + row) * 4;
+            if constexpr (LANES == 0 || LANES == 64) {          // a wavefront's step is a word of scales
+                const unsigned word = (unsigned)__builtin_amdgcn_readlane((int)byte, 0) | (unsigned)__builtin_amdgcn_readlane((int)byte, 16) << 8 |
+                                      (unsigned)__builtin_amdgcn_readlane((int)byte, 32) << 16 | (unsigned)__builtin_amdgcn_readlane((int)byte, 48) << 24;
+                if ((t & 63) == 0 && (WHOLE || kc < nk)) *reinterpret_cast<unsigned *>(s) = word;
+            } else if ((t & 15) == 0) {
+                s[kc & 3] = (uint8_t)byte;
+                if (t == 0)                                     // the lanes of a short row do not reach the end of its word
+                    for (int z = LANES / 16; z < 4; ++z) s[z] = 0;
+            }
+        }
     };
     if (from < to) load();
     for (long long row = from; row < to; ++row) {
@@ -231,38 +303,29 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
         }
         // v becomes the deviation from the wavefront's own mean, which is `delta` off the row's
         Wave w;
-        float eps = A.eps, delta;
-        for (bool again = false;; again = true) {               // twice where the sums are not finite: the same for the whole row
-            float sum = 0.f;
+        float sum = 0.f;
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += v[c][i];
-            const float mean = w.mean = quotient(lane_sum<LANES ? LANES : 64>(sum), own, inv_own);
-            w.squares = deviations<CH>(v, mean, t, T, WHOLE ? 1 << 30 : D, ragged);
-            w.squares = lane_sum<LANES ? LANES : 64>(w.squares);
-            if constexpr (!LANES) {
-                join_waves<false>(w, s_wave[copy], T >> 6, other, count, inv_count);
-                copy ^= 1;
-            }
-            delta = w.mean - mean;
-            if (again || finite(w.squares)) break;
-            eps = 0.f;
-            const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                use_columns<TX, WHOLE, LANES>(load_columns<TX, WHOLE, LANES>(x, (c * T + t) * 8, D), (c * T + t) * 8, D, true, v[c]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[c][i] *= SHRINK;
-            }
+            for (int i = 0; i < 8; ++i) sum += v[c][i];
+        const float mean = w.mean = quotient(lane_sum<LANES ? LANES : 64>(sum), own, inv_own);
+        w.squares = deviations<CH>(v, mean, t, T, WHOLE ? 1 << 30 : D, ragged);
+        w.squares = lane_sum<LANES ? LANES : 64>(w.squares);
+        if constexpr (!LANES) {
+            join_waves<false>(w, s_wave[copy], T >> 6, other, count, inv_count);
+            copy ^= 1;
         }
-        const float r = rsqrtf(fmaf(w.squares, inv_count, eps)), shift = -delta * r;
+        const float delta = w.mean - mean;
+        bool fine = finite(w.squares);                          // the same for the whole row
+        if (LANES == 64) fine = __builtin_amdgcn_readfirstlane(fine);
+        if (!fine) left_out |= 1u << (row - from);
+        const float r = rsqrtf(fmaf(w.squares, inv_count, A.eps)), shift = -delta * r;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[c][i] = fmaf(fmaf(v[c][i], r, shift), f[c][i], o[c][i]);
-        unsigned bytes[CH];
-        uint2 codes[CH];
+        unsigned bytes[CH] = {};
+        uint2 codes[CH] = {};
         if constexpr (FP8) {                                    // 16 lanes a block of 128 columns
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
@@ -275,36 +338,44 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? 1 : CH == 2 ? (sizeof(TX
         // 290; bf16 results, which HBM bounds, 293 and 308)
         if constexpr (FP8) arrived(next);
 #pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (fine) put(row, rb, rn, c, v[c], bytes[c], codes[c]);
+    }
+    // Rows taken again: straight from memory, in as many steps as they need, behind the loop, where they take no registers from the others (in the loop
+    // 600,000 x 64 bf16 38.7 -> 42 us, 75,600 x 512 to FP8 23.3 -> 27).  The mean of numbers that are all the same is off by a few units in the last
+    // place, since their sum need not be a multiple of them in fp32; what is left of each of them is the same too, and the sum of that is exact, so
+    // that taking its mean off as well leaves zeros.
+    for (; left_out; left_out &= left_out - 1) {
+        const long long row = from + __builtin_ctz(left_out);
+        const int rb = (int)(row / A.N), rn = (int)(row - (long long)rb * A.N);
+        const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
+        float mean = 0.f, rest = 0.f;
+        auto d = [&](int k) { return to_f32(x[k]) * SHRINK - mean - rest; };
+        mean = quotient(row_sum<LANES, CH>(s_wave, copy, t, T, D, d), count, inv_count);
+        rest = quotient(row_sum<LANES, CH>(s_wave, copy, t, T, D, d), count, inv_count);
+        const float squares = row_sum<LANES, CH>(s_wave, copy, t, T, D, [&](int k) { return d(k) * d(k); });
+        const float r = rsqrtf(fmaf(squares, inv_count, 0x1p-126f));    // any eps but 0: r times the zeros of a row of one number is 0
+#pragma nounroll
         for (int c = 0; c < CH; ++c) {
-            const int k = (c * T + t) * 8;
-            if constexpr (!FP8) {
-                TY *y = static_cast<TY *>(A.y) + rb * A.ys[0] + rn * A.ys[1];
-                if (WHOLE) store8<TY>(y + k, v[c]);
-                else if (k < D) store_row8(y, k, D, v[c]);
-            } else {
-                const int kc = k >> 7;
-                unsigned byte = bytes[c];
-                if (WHOLE || kc < nk) *reinterpret_cast<uint2 *>(A.codes + row * (nk * 128LL) + k) = codes[c];
-                else byte = 0;
-                uint8_t *s = A.scales + ((long long)(kc >> 2) * rows + row) * 4;
-                if constexpr (LANES == 0 || LANES == 64) {      // a wavefront's step is a word of scales
-                    const unsigned word = (unsigned)__builtin_amdgcn_readlane((int)byte, 0) | (unsigned)__builtin_amdgcn_readlane((int)byte, 16) << 8 |
-                                          (unsigned)__builtin_amdgcn_readlane((int)byte, 32) << 16 | (unsigned)__builtin_amdgcn_readlane((int)byte, 48) << 24;
-                    if ((t & 63) == 0 && (WHOLE || kc < nk)) *reinterpret_cast<unsigned *>(s) = word;
-                } else if ((t & 15) == 0) {
-                    s[kc & 3] = (uint8_t)byte;
-                    if (t == 0)                                 // the lanes of a short row do not reach the end of its word
-                        for (int z = LANES / 16; z < 4; ++z) s[z] = 0;
-                }
+            float u[8], inv;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int k = (c * T + t) * 8 + i;
+                u[i] = 0.f;
+                if (k < D) u[i] = fmaf(d(k) * r, A.w ? A.w[rb * A.ws + k] + A.one : 1.f, A.b ? A.b[rb * A.bs + k] : 0.f);
             }
+            const unsigned byte = FP8 ? e4m3_block_scale(max16(largest8(u)), inv) : 0;
+            put(row, rb, rn, c, u, byte, FP8 ? e4m3_codes8(u, inv) : uint2());
         }
     }
 }
 
 // grid: workgroups stride over the shares, P of each group's rows.  LANES threads a row, CH steps of 8 columns a thread: 16 or 32 lanes of a block
 // of 64, or (0) the block, a multiple of 64 threads.  A thread keeps its columns' factors and sums; the next row is on its way while this
-// one is used.  Three wavefronts a SIMD at least: 31,299 x 1855 fp32 160 us, with two 174.
-template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __launch_bounds__(LANES ? 64 : 512, CH == 2 ? 3 : 1) void layer_norm_bwd_kernel(const NormArgs A)
+// one is used.  Wavefronts a SIMD: three at least (31,299 x 1855 fp32 160 us, with two 174), five of one step where a side is bf16 (181,440 x 777 bf16
+// 200 us, with four 241).
+template <typename TX, typename TY, int LANES, int CH, bool WHOLE>
+__global__ __launch_bounds__(LANES ? 64 : 512, CH == 2 ? 3 : !LANES && CH == 1 && sizeof(TX) + sizeof(TY) < 8 ? 5 : 1) void layer_norm_bwd_kernel(const NormArgs A)
 {
     constexpr int AT_ONCE = LANES ? 64 / (LANES ? LANES : 64) : 1, SUM = LANES ? LANES : 64;     // rows; lanes of a sum
     __shared__ Wave s_wave[2][WAVES];
@@ -389,15 +460,9 @@ template <typename TX, typename TY, int LANES, int CH, bool WHOLE> __global__ __
                 }
                 delta = w.mean - mean;
                 if (again || finite(w.squares)) break;
-                eps = 0.f;
-                scale = SHRINK;
-                const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
-#pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    use_columns<TX, WHOLE, LANES>(load_columns<TX, WHOLE, LANES>(x, (c * T + t) * 8, D), (c * T + t) * 8, D, true, vx[c]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) vx[c][i] *= SHRINK;
-                }
+                const bool zeros = take_again<TX, LANES, CH, WHOLE>(static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1], vx, t, T, D);
+                eps = zeros ? A.eps : 0.f;
+                scale = zeros ? 1.f : SHRINK;
             }
             const float r = rsqrtf(fmaf(w.squares, inv_count, eps)), rs = r * scale, shift = -delta * r;
             const float by_n = -(w.gx * r * inv_count) * rs, by_1 = -(w.g * inv_count) * rs;
@@ -501,7 +566,8 @@ template <typename TX, typename TY, bool FP8> static void norm_forward(const Nor
     constexpr int each = FP8 ? 16 : 4;
     auto grid = [&](int per) {
         const long long one = (rows + per - 1) / per, some = (rows + each * per - 1) / (each * per);
-        return (int)(one < 2048 ? one : some < 2048 ? 2048 : some < 1 << 22 ? some : 1 << 22);       // a launch has fewer than 2^32 threads
+        // a launch has fewer than 2^32 threads; a place has 16 rows at most, of 2^26 (the kernel keeps a bit for each)
+        return (int)(one < 2048 ? one : some < 2048 ? 2048 : some < 1 << 22 ? some : 1 << 22);
     };
     const int steps = cdiv(A.D, 512);
     // A wavefront a row up to three steps, no barrier: 387M bf16 values in rows of 1536 277 us (FP8 231), by two wavefronts 302 (293); of 1280 309 (271), 362

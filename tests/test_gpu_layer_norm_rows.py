@@ -74,3 +74,75 @@ def test_squares_that_just_reach_the_largest_number(svg2, D):
     *_, dw, dw_bound, db, db_bound = ops.layer_norm_backward(_np(dy)[None], _np(x)[None], _np(w), EPS, False)
     assert_within(res.dweight[None], dw, dw_bound, F32)
     assert_within(res.dbias[None], db, db_bound, F32)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [1, 5, 64, *LENGTHS])
+def test_constant_rows_of_large_numbers(svg2, D, dtype):
+    """Finite rows of one number have no variance, also where their sum is past fp32 or off by a rounding that is: as rows of zeros, forward, to FP8
+    and in every gradient, the sums over all rows among them."""
+    N, large = 120, [1e35, -1e35, 2.0 ** 123, -2.0 ** 123, torch.finfo(dtype).max, torch.finfo(dtype).min, 3e30, -1.1e37]
+    r = np.random.default_rng(D)
+    x = torch.from_numpy(r.standard_normal((N, D))).to(dtype)
+    rows = torch.arange(len(large)) * 13 + 2
+    x[rows] = 0.0
+    zeros = x.cuda()
+    x[rows] = torch.tensor(large, dtype=torch.float64).to(dtype)[:, None]
+    x = x.cuda()
+    w, b = (torch.from_numpy(r.standard_normal(D)).float().cuda() for _ in range(2))
+    dy = torch.from_numpy(r.standard_normal((N, D))).to(dtype).cuda()
+    y = svg2.svg2_layer_norm(x, w, b, eps=EPS, out_dtype=F32)
+    assert bool((y[rows] == b).all())
+    assert torch.equal(y, svg2.svg2_layer_norm(zeros, w, b, eps=EPS, out_dtype=F32))
+    for got, want in zip(svg2.svg2_layer_norm_fp8(x, w, b, eps=EPS), svg2.svg2_layer_norm_fp8(zeros, w, b, eps=EPS)):
+        assert torch.equal(got, want)
+    res = svg2.svg2_layer_norm_backward(dy, x, w, b, eps=EPS)
+    dx, bound, dw, dw_bound, db, db_bound = ops.layer_norm_backward(_np(dy)[None], _np(zeros)[None], _np(w), EPS, False)
+    assert_within(res.grad[None], dx, bound, dtype)
+    assert_within(res.dweight[None], dw, dw_bound, F32)
+    assert_within(res.dbias[None], db, db_bound, F32)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, *LENGTHS])
+def test_rows_that_are_nearly_constant_or_not_finite(svg2, D, dtype):
+    """One number next to the others', first, last or between: finite, and the others of a row alike.  Rows of infinities or NaN: NaN."""
+    top = torch.tensor(2.0 ** 123, dtype=dtype)
+    near = (top.double() * (1 - torch.finfo(dtype).eps / 2)).to(dtype)
+    assert near != top
+    x = top.repeat(6, D)
+    at = [0, D - 1, D // 2]
+    for row, k in enumerate(at):
+        x[row, k] = near
+    for row, v in enumerate((float("inf"), -float("inf"), float("nan"))):
+        x[3 + row] = v
+    x = x.cuda()
+    dy = torch.from_numpy(np.random.default_rng(D).standard_normal((6, D))).to(dtype).cuda()
+    y = svg2.svg2_layer_norm(x, eps=EPS, out_dtype=F32)
+    codes, scales = svg2.svg2_layer_norm_fp8(x, eps=EPS)
+    dx = svg2.svg2_layer_norm_backward(dy, x, eps=EPS).grad
+    nk = -(-D // 128)
+    flat = scales.transpose(0, 1).reshape(6, -1)[:, :nk]
+    assert bool(y[:3].isfinite().all()) and bool((flat[:3] < 255).all()) and bool(dx[:3].isfinite().all())
+    for row, k in enumerate(at):
+        assert bool((y[row, k] < y[row, [j for j in range(D) if j != k]]).all())
+    assert bool(y[3:].isnan().all()) and bool((flat[3:] == 255).all()) and bool((codes[3:] == 0).all()) and bool(dx[3:].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, *LENGTHS])
+def test_rows_of_zeros_but_for_large_numbers_at_an_end(svg2, D, dtype):
+    """As many large columns as may stand behind the last whole eight, at either end: taken again, but not rows of one number."""
+    x = torch.zeros((14, D), dtype=dtype)
+    for n in range(1, 8):
+        x[n - 1, D - n:], x[6 + n, :n] = 2.0 ** 100, -2.0 ** 100
+    x = x.cuda()
+    r = np.random.default_rng(D)
+    w, b = (torch.from_numpy(r.standard_normal(D)).float().cuda() for _ in range(2))
+    dy = torch.from_numpy(r.standard_normal(x.shape)).to(dtype).cuda()
+    y, bound = ops.layer_norm(_np(x)[None], _np(w), _np(b), EPS, False)
+    assert_within(svg2.svg2_layer_norm(x, w, b, eps=EPS, out_dtype=F32)[None], y, bound, F32)
+    res = svg2.svg2_layer_norm_backward(dy, x, w, b, eps=EPS)
+    dx, bound, dw, dw_bound, db, db_bound = ops.layer_norm_backward(_np(dy)[None], _np(x)[None], _np(w), EPS, False)
+    assert_within(res.grad[None], dx, bound, dtype)
+    assert_within(res.dweight[None], dw, dw_bound, F32)
