@@ -30,8 +30,8 @@ struct NormArgs {
 };
 
 // Rows whose sums leave fp32's range (an infinity and a NaN among them) are taken again times this: squares of the largest numbers, 16384 of
-// them, then stay below 2^126.  Either their squares were too many, which are then above 2^-30, eps nothing beside them; or their sum was, of numbers
-// above 2^113, two of which differ by 2^16 then, if any do.  If none do, the row has no variance, as one of zeros.
+// them, then stay below 2^126.  Either their squares were too many, which are then above 2^-30; or their sum was, of numbers above 2^113, two of which
+// differ by 2^16 then, if any do.  If none do, the row has no variance, as one of zeros.  An eps of up to 1e30 may still count beside the first.
 constexpr float SHRINK = 0x1p-72f;
 constexpr int WAVES = 16;           // most of a workgroup
 
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? (LANES == 64 && CH == 1 
         mean = quotient(row_sum<LANES, CH>(s_wave, copy, t, T, D, d), count, inv_count);
         rest = quotient(row_sum<LANES, CH>(s_wave, copy, t, T, D, d), count, inv_count);
         const float squares = row_sum<LANES, CH>(s_wave, copy, t, T, D, [&](int k) { return d(k) * d(k); });
-        const float r = rsqrtf(fmaf(squares, inv_count, 0x1p-126f));    // any eps but 0: r times the zeros of a row of one number is 0
+        const float r = rsqrtf(fmaf(squares, inv_count, fmaxf(A.eps * SHRINK * SHRINK, 0x1p-126f)));    // not 0: of a row of one number, r times its zeros is 0
 #pragma nounroll
         for (int c = 0; c < CH; ++c) {
             float u[8], inv;
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(LANES ? 64 : 512, CH == 2 ? 3 : !LANES && CH == 1 &
                 delta = w.mean - mean;
                 if (again || finite(w.squares)) break;
                 const bool zeros = take_again<TX, LANES, CH, WHOLE>(static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1], vx, t, T, D);
-                eps = zeros ? A.eps : 0.f;
+                eps = zeros ? A.eps : A.eps * SHRINK * SHRINK;
                 scale = zeros ? 1.f : SHRINK;
             }
             const float r = rsqrtf(fmaf(w.squares, inv_count, eps)), rs = r * scale, shift = -delta * r;

@@ -146,3 +146,22 @@ def test_rows_of_zeros_but_for_large_numbers_at_an_end(svg2, D, dtype):
     dx, bound, dw, dw_bound, db, db_bound = ops.layer_norm_backward(_np(dy)[None], _np(x)[None], _np(w), EPS, False)
     assert_within(res.grad[None], dx, bound, dtype)
     assert_within(res.dweight[None], dw, dw_bound, F32)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [10000, 16384])
+def test_an_eps_that_large_rows_feel(svg2, D, dtype):
+    """The largest eps beside rows whose squares are past fp32 by little: some 2^-15 of their variance."""
+    N, eps = 12, 9e29
+    r = np.random.default_rng(D)
+    x = r.standard_normal((N, D))
+    x *= np.sqrt(float(np.finfo(np.float32).max) * r.uniform(0.8, 1.6, (N, 1)) / (x * x).sum(-1, keepdims=True))
+    x = torch.from_numpy(x).to(dtype).cuda()
+    w, b = (torch.from_numpy(r.standard_normal(D)).float().cuda() for _ in range(2))
+    dy = torch.from_numpy(r.standard_normal((N, D))).to(dtype).cuda()
+    y, bound = ops.layer_norm(_np(x)[None], _np(w), _np(b), eps, False)
+    assert_within(svg2.svg2_layer_norm(x, w, b, eps=eps, out_dtype=F32)[None], y, bound, F32)
+    res = svg2.svg2_layer_norm_backward(dy, x, w, b, eps=eps)
+    dx, bound, dw, dw_bound, db, db_bound = ops.layer_norm_backward(_np(dy)[None], _np(x)[None], _np(w), eps, False)
+    assert_within(res.grad[None], dx, bound, dtype)
+    assert_within(res.dweight[None], dw, dw_bound, F32)
