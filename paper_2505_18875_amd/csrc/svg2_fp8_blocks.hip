@@ -249,8 +249,8 @@ template <int I, int J> __device__ __forceinline__ void settle(f32x16 (&a)[I][J]
 
 // How exact the matrix cores are on E4M3 (measured; the same for every instruction that takes it): products of eight neighbouring columns
 // are added with 13 bits below the power of two of the largest of them, what is below is cut off; sums of such groups have fp32's 24
-// bits.  That is 1.4e-5 of a sum of 64 Gaussian products (rms), against 5e-9 for the same numbers as bf16, and against the 2^-9 by which a bf16
-// result is rounded.  So a bf16 result is formed by them, at twice the rate, and an fp32 result (EXACT) from the values as bf16, which has them all.
+// bits.  That is 1.4e-5 of a sum of 64 Gaussian products (rms), against 5e-9 for the same numbers as bf16, and against the 2^-8 by which a bf16
+// result may be rounded; where large products cancel it is more of the result, up to 7 * 2^-13 of the sum of each eight's largest.  So a bf16 result is formed by them, at twice the rate, and an fp32 result (EXACT) from the values as bf16, which has them all.
 struct Converted { bf16x8 q[4]; };                      // 32 values
 
 __device__ __forceinline__ Converted convert(const i32x8 &f, unsigned byte)
