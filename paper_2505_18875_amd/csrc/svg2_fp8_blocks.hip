@@ -743,28 +743,32 @@ static bool few(int M, int N, int K)
     return M <= 8 && K <= 8192 && (long long)N * K <= (M <= 4 ? 10LL : 5LL) << 24;
 }
 
-// Microseconds that the product takes with these tiles, by what was measured: `start` a tile, and for each stage
-// alone with one workgroup a CU up to full with as many as fit (Large 1, Medium 2, Small 4).  Large tiles do most with
-// what they load, small ones leave fewer CUs idle: measured, large / medium / small, bf16 results and (fp32)
-//   8192 x 8192 x 8192  451 / 520 / 836 us (799 / 888 / 1250)     4096 x 4096 x 4096  58 / 62 / 103 us (103 / 113 / 153)
-//   4096 x 5120 x 5120  120 / 104 / 169 us (210 / 170 / 237)      2048 x 2048 x 2048  25 / 14 /  16 us (40 / 21 / 22)
-//    512 x 5120 x 5120   56 /  29 /  25 us (93 / 37 / 36)          300 x 5120 x 5120  55 / 27 /  22 us (93 / 37 / 26)
-template <typename L> static double tile_time(int M, int N, int stages, int split, bool exact)
+// Microseconds that the product takes with these tiles, as measured: `start` a tile, and for each of its `per` stages `full` in a round of as many as fit (a
+// CU has 1 large one, 2 medium, 4 small); in a last round that leaves places empty down to `alone`, by how many share a CU in it and by the square of
+// its share of all places.  Fitted to 431 sizes from 9 to 30,000 rows, 64 to 16,384 columns and 64 to 80,000 deep, either type of result, up to 27
+// combinations of tiles and parts each, for the choice to be right: it takes on average 1.1 % more than the best of them, in 48 of 862 cases more than 5 %, at
+// most 38 %, some 3 us, where a second launch is most of it.  Large tiles do most with what they load, small ones leave fewer CUs idle: measured, large / medium /
+// small, bf16 results and (fp32)
+//   8192 x 8192 x 8192  392 / 469 / 825 us (728 / 853 / 1211)     4096 x 4096 x 4096  55 / 63 / 108 us (102 / 112 / 158)
+//   4096 x 5120 x 5120  112 / 104 / 175 us (204 / 167 / 244)      2048 x 2048 x 2048  23 / 13 /  16 us (39 / 22 / 24)
+//    512 x 5120 x 5120   50 /  31 /  27 us (86 / 38 / 41)          300 x 5120 x 5120  49 / 29 /  24 us (86 / 36 / 29)
+template <typename L> static double tile_time(int M, int N, int per, int split, bool exact)
 {
     constexpr int R = L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4;
-    const double start = R == 1 ? 6.0 : R == 2 ? 3.0 : 2.0;
-    const double alone = exact ? (R == 1 ? 2.7 : R == 2 ? 0.83 : 0.43) : (R == 1 ? 1.45 : R == 2 ? 0.63 : 0.40);
-    const double full = exact ? (R == 1 ? 3.05 : R == 2 ? 1.65 : 1.13) : (R == 1 ? 1.66 : R == 2 ? 0.98 : 0.75);
-    const long long tiles = (long long)cdiv(M, L::BM) * cdiv(N, L::BN) * split, rounds = tiles / (256 * R), rest = (tiles - rounds * 256 * R + 255) / 256;
-    const double per = cdiv(stages, split);
-    const double last = rest == 0 ? 0.0 : start + per * (R == 1 ? alone : alone + (full - alone) * (double)(rest - 1) / (R > 1 ? R - 1 : 1));
-    return (double)rounds * (start + per * full) + last;
+    const double start = exact ? (R == 1 ? 10.6 : R == 2 ? 3.33 : 2.11) : (R == 1 ? 9.72 : R == 2 ? 3.50 : 4.05);
+    const double alone = exact ? (R == 1 ? 2.04 : R == 2 ? 0.786 : 0.450) : (R == 1 ? 1.03 : R == 2 ? 0.530 : 0.259);
+    const double full = exact ? (R == 1 ? 2.78 : R == 2 ? 1.61 : 1.19) : (R == 1 ? 1.35 : R == 2 ? 0.843 : 0.714);
+    const double by_cu = R == 1 ? 0.0 : exact ? 0.608 : 0.331;
+    const long long tiles = (long long)cdiv(M, L::BM) * cdiv(N, L::BN) * split, rounds = tiles / (256 * R), rest = tiles % (256 * R);
+    const double share = rest / (256.0 * R), sharing = R == 1 ? 0.0 : (double)((rest + 255) / 256 - 1) / (R > 1 ? R - 1 : 1);
+    const double last = alone + (full - alone) * (by_cu * sharing + (1.0 - by_cu) * share * share);
+    return (double)rounds * (start + per * full) + (rest ? start + per * last : 0.0);
 }
 
 // Which tiles, and in how many parts the contraction: the least time by that model; parts of whole words of scales (four stages), 16 parts at
-// most.  Adding them up is a second launch and the parts' way out and back: 2.5 us, and 0.2 us for each MB of a part.  Measured, one part / as
+// most.  Adding them up is a second launch and the parts' way out and back: 2.6 us, and 0.17 us for each MB of the parts.  Measured, one part / as
 // chosen, fp32 results (bf16):
-//   1536 x 1536 x 16,384  102 / 82 us (64 / 57)     1536 x 1536 x 75,600  470 / 291 us (297 / 186)     512 x 512 x 16,384  58 / 21 us (57 / 16)
+//   1536 x 1536 x 16,384  99 / 76 us (70 / 47)     1536 x 1536 x 75,600  466 / 273 us (337 / 166)     512 x 512 x 16,384  55 / 22 us (58 / 19)
 // Large tiles go out 256 at a time: the last rows of C, whose tiles would not fill a last round, may be a launch of smaller ones that do
 // (75,600 x 5120 x 5120 is 23 rounds and 32 tiles: 1600 us, the 336 last rows by themselves 1560).
 struct BlockProductPlan {
@@ -786,10 +790,10 @@ static BlockProductPlan product_plan(int M, int N, int K, bool exact)
     for (int split = 1; split <= 16 && (split == 1 || stages >= 8 * split); ++split) {
         const int per = split == 1 ? stages : cdiv(cdiv(stages, split), 4) * 4;
         if (split > 1 && (cdiv(stages, per) != split || (double)split * M * N > (1 << 28))) continue;
-        const double join = split == 1 ? 0.0 : 2.5 + 0.2 * split * (double)M * N * sizeof(float) * 1e-6;
-        offer(join + tile_time<Small>(M, N, stages, split, exact), {0, split, per, 0, 0});
-        offer(join + tile_time<Medium>(M, N, stages, split, exact), {1, split, per, 0, 0});
-        offer(join + tile_time<Large>(M, N, stages, split, exact), {2, split, per, 0, 0});
+        const double join = split == 1 ? 0.0 : 2.6 + 0.17 * split * (double)M * N * sizeof(float) * 1e-6;
+        offer(join + tile_time<Small>(M, N, per, split, exact), {0, split, per, 0, 0});
+        offer(join + tile_time<Medium>(M, N, per, split, exact), {1, split, per, 0, 0});
+        offer(join + tile_time<Large>(M, N, per, split, exact), {2, split, per, 0, 0});
     }
     const long long tiles_n = cdiv(N, 256), keep = cdiv(M, 256) * tiles_n / 256 * 256 / tiles_n * 256;      // rows that fill whole rounds
     if (keep >= 256 && keep < M) {
