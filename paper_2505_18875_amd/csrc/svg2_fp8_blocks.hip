@@ -664,14 +664,14 @@ static int slices(long long blocks, int steps)
     return (int)(want < 1 ? 1 : want > steps ? steps : want);
 }
 
-// Values of 64 MB and more whose rows are whole lines are written past the caches, which the codes, half their size, then keep: 16,384 x 5120
-// bf16 quantised both ways and both back 197 -> 167 us, 15,360 x 5120 in squares 188 -> 133.  Smaller ones are better left there for
-// whoever reads them next; rows that share lines too.  An X of 64 to 256 MB, the size of the last cache, is read past them as well: both ways 73 ->
-// 67 us; a larger one is not there to begin with (75,600 x 5120 both ways 301 us, past the caches 308).
-static bool streamed(const void *X, double elements, int64_t ld, int es)
-{
-    return elements * es >= 67108864.0 && (reinterpret_cast<uintptr_t>(X) & 127) == 0 && ld * es % 128 == 0;
-}
+// What goes past the caches, where rows are whole lines (others share lines, which are better left there).
+// An X of 64 to 256 MB, the size of the last cache, when it is quantised: both ways 73 -> 67 us at 16,384 x 5120 bf16; a larger one is not there to begin
+// with (75,600 x 5120 both ways 301 us, past the caches 308).
+// Values that are written: bf16 from 128 MB on, fp32 from 256 MB on.  Smaller ones are better left there for whoever reads them next, larger ones leave
+// them to the codes: written past the caches / through them and quantised again, us, 5120 columns
+//   bf16  64 MB 41 / 37   96 MB 55 / 50   128 MB 74 / 73   144 MB 80 / 94   160 MB 85 / 103   240 MB 127 / 143   400 MB 275 / 282
+//   fp32  64 MB 49 / 38  128 MB 90 / 70   192 MB 132 / 108  240 MB 171 / 155  320 MB 212 / 223  800 MB 526 / 547
+static bool whole_lines(const void *X, int64_t ld, int es) { return (reinterpret_cast<uintptr_t>(X) & 127) == 0 && ld * es % 128 == 0; }
 
 // f(type, STREAM) with both known at compile time
 template <typename F> static int with_types(int dtype, bool stream, F f)
@@ -691,7 +691,8 @@ int fp8_blocks_quant_launch(const void *X, int dtype, int M, int G, int Kg, int6
     const bool shared = !lines || sm * es % 128 != 0 || (reinterpret_cast<uintptr_t>(X) & 127) != 0;
     const BlockQuantArgs A = {X, sm, sg, M, G, Kg, static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales),
                               static_cast<uint8_t *>(codes_t), static_cast<uint8_t *>(scales_t), shared ? (int)((all + 7) / 8) : 0};
-    return with_types(dtype, lines && streamed(X, (double)M * K, sm, es) && (double)M * K * es < 268435456.0, [&](auto *tp, auto stream) {
+    const double bytes = (double)M * K * es;
+    return with_types(dtype, lines && whole_lines(X, sm, es) && bytes >= 67108864.0 && bytes < 268435456.0, [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
         constexpr bool S = decltype(stream)::value;
         if (!codes_t && !square) {
@@ -712,7 +713,8 @@ int fp8_blocks_quant_launch(const void *X, int dtype, int M, int G, int Kg, int6
 
 int fp8_blocks_values_launch(const void *codes, const void *scales, int M, int K, int dtype, void *X, int64_t ldx, hipStream_t st)
 {
-    return with_types(dtype, streamed(X, (double)M * K, ldx, dtype == SVG2_BF16 ? 2 : 4), [&](auto *tp, auto stream) {
+    const int es = dtype == SVG2_BF16 ? 2 : 4;
+    return with_types(dtype, whole_lines(X, ldx, es) && (double)M * K * es >= 67108864.0 * es, [&](auto *tp, auto stream) {
         using T = std::remove_pointer_t<decltype(tp)>;
         const int bx = cdiv(M, 16);
         fp8_blocks_values_kernel<T, decltype(stream)::value><<<dim3(bx, slices(bx, cdiv(K, 128))), 256, 0, st>>>(

@@ -127,8 +127,9 @@ def test_the_sizes_take_different_ways(svg2):
     assert _chosen(5, 70, 640) == 256 and _chosen(200, 300, 640) == 256 and _chosen(130, 140, 16384) > 256
 
 
-# X just below, just above 64 MB and just below 256 MB, of whole lines, bf16 and fp32
-@pytest.mark.parametrize("dtype,M,K", [(BF16, 4095, 8192), (BF16, 4096, 8192), (BF16, 16380, 8128), (F32, 2047, 8192), (F32, 2048, 8192), (F32, 8191, 8160)])
+# X of whole lines, bf16 and fp32, on either side of the sizes from which it is read (64 to 256 MB) and its values are written (128 or 256 MB) past the caches
+@pytest.mark.parametrize("dtype,M,K", [(BF16, 4095, 8192), (BF16, 4096, 8192), (BF16, 8191, 8192), (BF16, 8192, 8192), (BF16, 16380, 8128), (F32, 2047, 8192), (F32, 2048, 8192),
+                                       (F32, 8191, 8160), (F32, 8192, 8192)])
 @pytest.mark.parametrize("square", [False, True])
 def test_quantize_past_the_caches(svg2, dtype, M, K, square):
     """The same operands as from rows that are not whole lines of memory, which stay in the caches; and the values back."""
