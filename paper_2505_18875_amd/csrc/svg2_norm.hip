@@ -184,23 +184,18 @@ template <bool GRADIENT> __device__ __forceinline__ void join_waves(Wave &x, Wav
     }
 }
 
-// sum of f(column) over the row, in all its threads, each taking its own columns one after another
-template <int LANES, int CH, typename F> __device__ __forceinline__ float row_sum(Wave (*s)[LANES ? 1 : WAVES], int &copy, int t, int T, int D, F f)
+// sum over the row, in all its threads, of a sum that each has of its columns
+template <int LANES> __device__ __forceinline__ float row_sum(float x, Wave (*s)[LANES ? 1 : WAVES], int &copy, int waves)
 {
-    float sum = 0.f;
-#pragma nounroll
-    for (int c = 0; c < CH; ++c)
-#pragma nounroll
-        for (int k = (c * T + t) * 8, i = 0; i < 8 && k < D; ++i, ++k) sum += f(k);
-    sum = lane_sum<LANES ? LANES : 64>(sum);
+    x = lane_sum<LANES ? LANES : 64>(x);
     if constexpr (!LANES) {
-        if ((threadIdx.x & 63) == 0) s[copy][threadIdx.x >> 6].mean = sum;
+        if ((threadIdx.x & 63) == 0) s[copy][threadIdx.x >> 6].mean = x;
         __syncthreads();
         const int k = threadIdx.x & 15;
-        sum = lane_sum<16>(k < T >> 6 ? s[copy][k].mean : 0.f);
+        x = lane_sum<16>(k < waves ? s[copy][k].mean : 0.f);
         copy ^= 1;
     }
-    return sum;
+    return x;
 }
 
 // v - mean (0 where there is no column), and the sum of its squares
@@ -341,31 +336,42 @@ __global__ __launch_bounds__(LANES ? 256 : 512, LANES ? (LANES == 64 && CH == 1 
         for (int c = 0; c < CH; ++c)
             if (fine) put(row, rb, rn, c, v[c], bytes[c], codes[c]);
     }
-    // Rows taken again: straight from memory, in as many steps as they need, behind the loop, where they take no registers from the others (in the loop
-    // 600,000 x 64 bf16 38.7 -> 42 us, 75,600 x 512 to FP8 23.3 -> 27).  The mean of numbers that are all the same is off by a few units in the last
-    // place, since their sum need not be a multiple of them in fp32; what is left of each of them is the same too, and the sum of that is exact, so
-    // that taking its mean off as well leaves zeros.
+    // Rows taken again, behind the loop, where they take no registers from the others (in the loop 600,000 x 64 bf16 38.7 -> 42 us, 75,600 x 512 to FP8
+    // 23.3 -> 27).  The mean of numbers that are all the same is off by a few units in the last place, since their sum need not be a multiple of them in
+    // fp32; what is left of each of them is the same too, and the sum of that is exact, so that taking its mean off as well leaves zeros.
     for (; left_out; left_out &= left_out - 1) {
         const long long row = from + __builtin_ctz(left_out);
         const int rb = (int)(row / A.N), rn = (int)(row - (long long)rb * A.N);
         const TX *x = static_cast<const TX *>(A.x) + rb * A.xs[0] + rn * A.xs[1];
-        float mean = 0.f, rest = 0.f;
-        auto d = [&](int k) { return to_f32(x[k]) * SHRINK - mean - rest; };
-        mean = quotient(row_sum<LANES, CH>(s_wave, copy, t, T, D, d), count, inv_count);
-        rest = quotient(row_sum<LANES, CH>(s_wave, copy, t, T, D, d), count, inv_count);
-        const float squares = row_sum<LANES, CH>(s_wave, copy, t, T, D, [&](int k) { return d(k) * d(k); });
-        const float r = rsqrtf(fmaf(squares, inv_count, fmaxf(A.eps * SHRINK * SHRINK, 0x1p-126f)));    // not 0: of a row of one number, r times its zeros is 0
-#pragma nounroll
-        for (int c = 0; c < CH; ++c) {
-            float u[8], inv;
+        float v[CH][8], squares = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int k = (c * T + t) * 8 + i;
-                u[i] = 0.f;
-                if (k < D) u[i] = fmaf(d(k) * r, A.w ? A.w[rb * A.ws + k] + A.one : 1.f, A.b ? A.b[rb * A.bs + k] : 0.f);
-            }
-            const unsigned byte = FP8 ? e4m3_block_scale(max16(largest8(u)), inv) : 0;
-            put(row, rb, rn, c, u, byte, FP8 ? e4m3_codes8(u, inv) : uint2());
+        for (int c = 0; c < CH; ++c) {
+            use_columns<TX, WHOLE, LANES>(load_columns<TX, WHOLE, LANES>(x, (c * T + t) * 8, D), (c * T + t) * 8, D, true, v[c]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] *= SHRINK;
+        }
+#pragma nounroll
+        for (int turn = 0; turn < 2; ++turn) {
+            float sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += v[c][i];
+            squares = deviations<CH>(v, quotient(row_sum<LANES>(sum, s_wave, copy, T >> 6), count, inv_count), t, T, WHOLE ? 1 << 30 : D, ragged);
+        }
+        squares = row_sum<LANES>(squares, s_wave, copy, T >> 6);
+        const float r = rsqrtf(fmaf(squares, inv_count, fmaxf(A.eps * SHRINK * SHRINK, 0x1p-126f)));    // not 0: of a row of one number, r times its zeros is 0
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int k = (c * T + t) * 8;
+            float f8[8], o8[8], inv;
+            if (A.w) load_weight8(A.w + rb * A.ws, k, WHOLE ? k + 8 : D, f8);
+            if (A.b) load_weight8(A.b + rb * A.bs, k, WHOLE ? k + 8 : D, o8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = !WHOLE && k + i >= D ? 0.f : fmaf(v[c][i] * r, A.w ? f8[i] + A.one : 1.f, A.b ? o8[i] : 0.f);
+            const unsigned byte = FP8 ? e4m3_block_scale(max16(largest8(v[c])), inv) : 0;
+            put(row, rb, rn, c, v[c], byte, FP8 ? e4m3_codes8(v[c], inv) : uint2());
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
