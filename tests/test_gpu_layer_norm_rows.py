@@ -165,3 +165,36 @@ def test_an_eps_that_large_rows_feel(svg2, D, dtype):
     dx, bound, dw, dw_bound, db, db_bound = ops.layer_norm_backward(_np(dy)[None], _np(x)[None], _np(w), eps, False)
     assert_within(res.grad[None], dx, bound, dtype)
     assert_within(res.dweight[None], dw, dw_bound, F32)
+
+
+@pytest.mark.parametrize("D", [5, 300, 2048, 5119, 10000])
+def test_the_smallest_eps(svg2, D):
+    """Rows without variance, by the smallest number that fp32 has and the smallest normal one."""
+    x = torch.tensor([7.0, 0.0, -3.0, 2.0 ** 123], device="cuda")[:, None].repeat(1, D)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    w, b, dy = (torch.randn(s, generator=g, device="cuda") for s in (D, D, (4, D)))
+    for eps in (2.0 ** -149, 2.0 ** -126):
+        assert bool((svg2.svg2_layer_norm(x, w, b, eps=eps) == b).all())
+        res = svg2.svg2_layer_norm_backward(dy, x, w, b, eps=eps)
+        zeros = np.zeros((1, 4, D))
+        dx, bound, dw, dw_bound, _, _ = ops.layer_norm_backward(_np(dy)[None], zeros, _np(w), eps, False)
+        assert_within(res.grad[None], dx, bound, F32)
+        assert_within(res.dweight[None], dw, dw_bound, F32)
+
+
+@pytest.mark.parametrize("D", [100, 777, 1536, 5120])
+def test_a_factor_of_all_rows_with_an_offset_of_each_group(svg2, D):
+    """Forward and to FP8, either way round; the gradients of such a pair are refused."""
+    from paper_2505_18875_amd.binding import Svg2Error
+    B, N = 3, 11
+    g = torch.Generator(device="cuda").manual_seed(D)
+    x, w, b = (torch.randn(s, generator=g, device="cuda") for s in ((B, N, D), (B, D), (B, D)))
+    for ww, bb in ((w[0].clone(), b), (w, b[0].clone())):
+        y = svg2.svg2_layer_norm(x, ww, bb, eps=EPS)
+        ref, bound = ops.layer_norm(_np(x), _np(ww), _np(bb), EPS, False)
+        assert_within(y, ref, bound, F32)
+        codes, scales = svg2.svg2_layer_norm_fp8(x, ww, bb, eps=EPS)
+        c, s = svg2.svg2_quantize_fp8_blocks(y.view(B * N, D))
+        assert torch.equal(codes, c) and torch.equal(scales, s)
+        with pytest.raises(Svg2Error, match="both"):
+            svg2.svg2_layer_norm_backward(x, x, ww, bb, eps=EPS)
