@@ -605,11 +605,11 @@ template <typename T, int PER> __global__ __launch_bounds__(256) void fp8_blocks
 // Measured, this kernel / tiles, us; the same weights again and again (the last cache holds them) and, in brackets, as many sets of weights in
 // turn as come from memory:
 //                     1 row                       8 rows                      16 rows
-//   15,360 x 5120     15.1 / 18.5 (17.0 / 21.3)   18.7 / 19.1 (21.0 / 22.5)   21.9 / 20.2 (25.0 / 23.6)
-//    5120 x 5120       8.1 / 11.3 ( 8.6 / 11.4)   10.2 / 11.1 (10.4 / 10.8)   11.8 / 11.2 (12.0 / 10.9)
-//   20,480 x 8192     29.8 / 29.6 (33.3 / 35.7)   35.5 / 30.1 (40.0 / 36.7)   41.6 / 30.8 (46.5 / 37.4)
-//    4096 x 16,384    15.9 / 15.6 (17.9 / 18.9)   17.9 / 15.4 (19.4 / 19.3)   19.6 / 15.8 (20.8 / 19.2)
-//    2048 x 16,384    12.0 / 11.2 (13.2 / 13.1)   15.2 / 11.2 (16.0 / 13.5)   17.8 / 11.3 (18.6 / 13.4)
+//   15,360 x 5120     15.1 / 18.7 (16.8 / 21.0)   18.4 / 19.2 (20.6 / 21.9)   21.7 / 19.9 (24.7 / 23.1)
+//    5120 x 5120       8.4 / 11.3 ( 9.5 / 11.7)   10.1 / 11.5 (11.1 / 12.0)   11.8 / 11.5 (13.2 / 12.1)
+//   20,480 x 8192     29.7 / 29.7 (33.2 / 35.8)   35.2 / 30.1 (40.2 / 36.4)   41.2 / 30.9 (47.1 / 37.2)
+//    4096 x 16,384    16.0 / 15.5 (17.0 / 18.8)   18.3 / 16.0 (18.5 / 19.2)   19.7 / 16.2 (20.2 / 19.4)
+//    2048 x 16,384    12.0 / 11.4 (13.3 / 13.1)   15.1 / 11.8 (16.1 / 13.5)   17.6 / 11.5 (18.5 / 13.8)
 // so up to 4 rows take it to 10 * 2^24 weights, up to 8 rows to 5 * 2^24, of rows up to 8192 long.
 constexpr int FEW_BLOCKS = 2, FEW_WAVES = 16;
 
@@ -748,8 +748,8 @@ static bool few(int M, int N, int K)
 // Microseconds that the product takes with these tiles, as measured: `start` a tile, and for each of its `per` stages `full` in a round of as many as fit (a
 // CU has 1 large one, 2 medium, 4 small); in a last round that leaves places empty down to `alone`, by how many share a CU in it and by the square of
 // its share of all places.  Fitted to 431 sizes from 9 to 30,000 rows, 64 to 16,384 columns and 64 to 80,000 deep, either type of result, up to 27
-// combinations of tiles and parts each, for the choice to be right: it takes on average 1.1 % more than the best of them, in 48 of 862 cases more than 5 %, at
-// most 38 %, some 3 us, where a second launch is most of it.  Large tiles do most with what they load, small ones leave fewer CUs idle: measured, large / medium /
+// combinations of tiles and parts each, and to 84 of 9 to 500 rows whose weights come from memory, for the choice to be right: it takes on average 1.3 % more
+// than the best of them, 2.1 % where weights come from memory.  Large tiles do most with what they load, small ones leave fewer CUs idle: measured, large / medium /
 // small, bf16 results and (fp32)
 //   8192 x 8192 x 8192  392 / 469 / 825 us (728 / 853 / 1211)     4096 x 4096 x 4096  55 / 63 / 108 us (102 / 112 / 158)
 //   4096 x 5120 x 5120  112 / 104 / 175 us (204 / 167 / 244)      2048 x 2048 x 2048  23 / 13 /  16 us (39 / 22 / 24)
@@ -757,10 +757,10 @@ static bool few(int M, int N, int K)
 template <typename L> static double tile_time(int M, int N, int per, int split, bool exact)
 {
     constexpr int R = L::BM == 256 ? 1 : L::BM == 128 ? 2 : 4;
-    const double start = exact ? (R == 1 ? 10.6 : R == 2 ? 3.33 : 2.11) : (R == 1 ? 9.72 : R == 2 ? 3.50 : 4.05);
-    const double alone = exact ? (R == 1 ? 2.04 : R == 2 ? 0.786 : 0.450) : (R == 1 ? 1.03 : R == 2 ? 0.530 : 0.259);
-    const double full = exact ? (R == 1 ? 2.78 : R == 2 ? 1.61 : 1.19) : (R == 1 ? 1.35 : R == 2 ? 0.843 : 0.714);
-    const double by_cu = R == 1 ? 0.0 : exact ? 0.608 : 0.331;
+    const double start = exact ? (R == 1 ? 10.8 : R == 2 ? 3.47 : 1.85) : (R == 1 ? 9.76 : R == 2 ? 3.87 : 3.62);
+    const double alone = exact ? (R == 1 ? 2.49 : R == 2 ? 0.863 : 0.450) : (R == 1 ? 1.01 : R == 2 ? 0.508 : 0.321);
+    const double full = exact ? (R == 1 ? 2.75 : R == 2 ? 1.64 : 1.20) : (R == 1 ? 1.36 : R == 2 ? 0.822 : 0.658);
+    const double by_cu = R == 1 ? 0.0 : exact ? 0.725 : 0.357;
     const long long tiles = (long long)cdiv(M, L::BM) * cdiv(N, L::BN) * split, rounds = tiles / (256 * R), rest = tiles % (256 * R);
     const double share = rest / (256.0 * R), sharing = R == 1 ? 0.0 : (double)((rest + 255) / 256 - 1) / (R > 1 ? R - 1 : 1);
     const double last = alone + (full - alone) * (by_cu * sharing + (1.0 - by_cu) * share * share);
@@ -768,9 +768,9 @@ template <typename L> static double tile_time(int M, int N, int per, int split, 
 }
 
 // Which tiles, and in how many parts the contraction: the least time by that model; parts of whole words of scales (four stages), 16 parts at
-// most.  Adding them up is a second launch and the parts' way out and back: 2.6 us, and 0.17 us for each MB of the parts.  Measured, one part / as
+// most.  Adding them up is a second launch and the parts' way out and back: 2.6 us, and 0.183 us for each MB of the parts.  Measured, one part / as
 // chosen, fp32 results (bf16):
-//   1536 x 1536 x 16,384  99 / 76 us (70 / 47)     1536 x 1536 x 75,600  466 / 273 us (337 / 166)     512 x 512 x 16,384  55 / 22 us (58 / 19)
+//   1536 x 1536 x 16,384  99 / 82 us (70 / 49)     1536 x 1536 x 75,600  466 / 282 us (337 / 169)     512 x 512 x 16,384  55 / 22 us (58 / 19)
 // Large tiles go out 256 at a time: the last rows of C, whose tiles would not fill a last round, may be a launch of smaller ones that do
 // (75,600 x 5120 x 5120 is 23 rounds and 32 tiles: 1600 us, the 336 last rows by themselves 1560).
 struct BlockProductPlan {
@@ -792,7 +792,7 @@ static BlockProductPlan product_plan(int M, int N, int K, bool exact)
     for (int split = 1; split <= 16 && (split == 1 || stages >= 8 * split); ++split) {
         const int per = split == 1 ? stages : cdiv(cdiv(stages, split), 4) * 4;
         if (split > 1 && (cdiv(stages, per) != split || (double)split * M * N > (1 << 28))) continue;
-        const double join = split == 1 ? 0.0 : 2.6 + 0.17 * split * (double)M * N * sizeof(float) * 1e-6;
+        const double join = split == 1 ? 0.0 : 2.6 + 0.183 * split * (double)M * N * sizeof(float) * 1e-6;
         offer(join + tile_time<Small>(M, N, per, split, exact), {0, split, per, 0, 0});
         offer(join + tile_time<Medium>(M, N, per, split, exact), {1, split, per, 0, 0});
         offer(join + tile_time<Large>(M, N, per, split, exact), {2, split, per, 0, 0});
