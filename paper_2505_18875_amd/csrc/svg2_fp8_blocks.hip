@@ -749,7 +749,7 @@ static bool few(int M, int N, int K)
 // CU has 1 large one, 2 medium, 4 small); in a last round that leaves places empty down to `alone`, by how many share a CU in it and by the square of
 // its share of all places.  Fitted to 431 sizes from 9 to 30,000 rows, 64 to 16,384 columns and 64 to 80,000 deep, either type of result, up to 27
 // combinations of tiles and parts each, and to 84 of 9 to 500 rows whose weights come from memory, for the choice to be right: it takes on average 1.3 % more
-// than the best of them, 2.1 % where weights come from memory.  Large tiles do most with what they load, small ones leave fewer CUs idle: measured, large / medium /
+// than the best of them, 2.1 % where weights come from memory (numbers of parts: 1 to 6, 8, 11 and 16 of the 16 that it weighs).  Large tiles do most with what they load, small ones leave fewer CUs idle: measured, large / medium /
 // small, bf16 results and (fp32)
 //   8192 x 8192 x 8192  392 / 469 / 825 us (728 / 853 / 1211)     4096 x 4096 x 4096  55 / 63 / 108 us (102 / 112 / 158)
 //   4096 x 5120 x 5120  112 / 104 / 175 us (204 / 167 / 244)      2048 x 2048 x 2048  23 / 13 /  16 us (39 / 22 / 24)

@@ -7,9 +7,9 @@
 //
 // Every element is read once and written once, some ten operations each: HBM bounds it, where the sums keep out of the way.  A row stays in
 // registers between its sums and its result; the mean is taken off before squares are summed.
-// 75,600 x 5120 bf16 (1.55 GB in and out) 280 us, 5.5 TB/s, the rate of a large copy; the same as an FP8 operand (1.16 GB) 247 us, 4.7 TB/s:
-// instructions, some 15 an element, and one round over the wavefronts a row keep it from 219.  Gradients of 16,384 x 5120 bf16 (0.50 GB) 105 us with
-// the sums of the weights', 4.8 TB/s, of 75,600 x 5120 474 us, 4.9 TB/s.
+// 75,600 x 5120 bf16 (1.55 GB in and out) 282 us, 5.5 TB/s, the rate of a large copy; the same as an FP8 operand (1.16 GB) 240 us, 4.8 TB/s:
+// instructions, some 15 an element, and one round over the wavefronts a row keep it from 219.  Gradients of 16,384 x 5120 bf16 (0.50 GB) 108 us with
+// the sums of the weights', 4.7 TB/s, of 75,600 x 5120 475 us, 4.9 TB/s.
 #include <type_traits>
 
 #include "svg2_fp8_blocks.h"
@@ -624,7 +624,8 @@ struct NormBwdPlan {
     int lanes, ch, threads, P;      // threads of a row (0: all), their steps of 8 columns, threads; parts of a group's rows
 };
 
-// Steps of a thread, us for 387M bf16 values: rows of 776 columns one 631, two 651; 1280 846 / 761; 1536 570 / 550; 5120 662 / 482.
+// Steps of a thread, one / two, us for 387M bf16 values: rows of 1280 columns 504 / 489, 1536 489 / 482, 2048 495 / 472, 4096 482 / 474; of fewer it depends on
+// how many there are: 776 516 / 497, 8192 rows of 776 in fp32 26.9 / 28.5, of 900 30.4 / 32.9, of 1024 29.1 / 25.1.
 // Parts: the same number of workgroups for each CU, which else wait for those with one more: 387M values in rows of 4096 in 640 parts 523 us, 768 474,
 // 512 473; of 8192 in 320 661, 256 477; of 1280 in 853 705, 1024 603.  As many as a CU holds, by wavefronts: 20 of one step, 12 of two, but 8 where
 // no lane is idle (5120 in 512 485, 256 474).  Where there are not half again as many rows, two rows each: more would be more to add up (999 x 777
